@@ -6,6 +6,10 @@ from .binding import (  # noqa: F401
     gear_workspace_bytes, gear_debug_fail_launch, gear_debug_helper_idle,
     gear_workspace_region, lib, make_config,
 )
+from .experts import (  # noqa: F401
+    ExpertWeights, GradList, NormOutput, Rows8, Weights8, gear_clip_grads, gear_expert_dgrad, gear_expert_matmul, gear_expert_wgrad,
+    gear_grad_norm, gear_matmul8, gear_rmsnorm, gear_rmsnorm_backward, gear_rows8, gear_weights8,
+)
 
 
 def config_for(wl, max_batch=None, max_nnz=None):

@@ -15,7 +15,7 @@ import torch
 
 GEAR_MAX_LAYERS = 8
 GEAR_OK, GEAR_ERR_INVALID, GEAR_ERR_RANGE, GEAR_ERR_CAPACITY, GEAR_ERR_HIP = range(5)
-GEAR_F32, GEAR_BF16 = 0, 1
+GEAR_F32, GEAR_BF16, GEAR_E4M3 = 0, 1, 2
 DTYPE_CODE = {"f32": GEAR_F32, "bf16": GEAR_BF16}
 TORCH_DTYPE = {GEAR_F32: torch.float32, GEAR_BF16: torch.bfloat16}
 
@@ -26,6 +26,10 @@ EXPORTS = (
     "gear_fill_normal", "gear_init_tables", "gear_step", "gear_step_static", "gear_step_adam", "gear_refresh_dfv", "gear_expired_ids", "gear_stamp_dfv",
     "gear_refresh_dfv_n", "gear_stamp_dfv_n",
     "gear_dense_workspace_bytes", "gear_dense_infer", "gear_dense_backward", "gear_dense_backward_n", "gear_group_ids",
+    "gear_rows8_ld", "gear_scales8_ld", "gear_rmsnorm", "gear_norm_backward_workspace_bytes", "gear_rmsnorm_backward", "gear_rows8",
+    "gear_packed_weights_bytes", "gear_weight_scales_bytes", "gear_pack_weights", "gear_expert_product",
+    "gear_expert_wgrad_workspace_bytes", "gear_expert_wgrad", "gear_grad_list_bytes", "gear_grad_list_pack",
+    "gear_grad_workspace_bytes", "gear_grad_norm", "gear_clip_grads",
     "gear_gemm", "gear_profile_create", "gear_profile_destroy", "gear_profile_count", "gear_profile_span",
     "gear_debug_fail_launch", "gear_debug_helper_idle", "gear_status_string",
 )
@@ -58,6 +62,36 @@ class gear_adam(C.Structure):
 class gear_dense_config(C.Structure):
     _fields_ = [("n_images", C.c_int64), ("raw_dim", C.c_int32), ("dfv_dim", C.c_int32), ("dfv_dtype", C.c_int32),
                 ("max_rows", C.c_int32)]
+
+
+class gear_norm_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float), ("x", C.c_void_p),
+                ("residual", C.c_void_p), ("gain", C.c_void_p), ("sum", C.c_void_p), ("y", C.c_void_p),
+                ("ld_x", C.c_int64), ("ld_residual", C.c_int64), ("ld_sum", C.c_int64), ("ld_y", C.c_int64),
+                ("q8", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class gear_norm_backward_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float), ("h", C.c_void_p),
+                ("dy", C.c_void_p), ("dsum", C.c_void_p), ("gain", C.c_void_p), ("dx", C.c_void_p), ("dgain", C.c_void_p),
+                ("ld_h", C.c_int64), ("ld_dy", C.c_int64), ("ld_dsum", C.c_int64), ("ld_dx", C.c_int64)]
+
+
+class gear_expert_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("out_dtype", C.c_int32), ("rows", C.c_int64), ("K", C.c_int32), ("N", C.c_int32),
+                ("experts", C.c_int32), ("x", C.c_void_p), ("x_scale", C.c_void_p), ("packed", C.c_void_p),
+                ("w_scale", C.c_void_p), ("off", C.c_void_p), ("out", C.c_void_p), ("ld_x", C.c_int64), ("ld_out", C.c_int64),
+                ("status", C.c_void_p)]
+
+
+class gear_expert_wgrad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int64), ("K", C.c_int32), ("N", C.c_int32), ("experts", C.c_int32),
+                ("dy", C.c_void_p), ("x", C.c_void_p), ("off", C.c_void_p), ("dw", C.c_void_p), ("ld_dy", C.c_int64),
+                ("ld_x", C.c_int64), ("status", C.c_void_p)]
+
+
+class gear_grad_tensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
 class gear_step_out(C.Structure):
@@ -130,6 +164,41 @@ def _load() -> C.CDLL:
     lib.gear_gemm.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                               C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
                               C.c_void_p]
+    lib.gear_rows8_ld.restype = C.c_int64
+    lib.gear_rows8_ld.argtypes = [C.c_int32]
+    lib.gear_scales8_ld.restype = C.c_int64
+    lib.gear_scales8_ld.argtypes = [C.c_int32]
+    lib.gear_rmsnorm.restype = C.c_int
+    lib.gear_rmsnorm.argtypes = [C.POINTER(gear_norm_args), C.c_void_p]
+    lib.gear_norm_backward_workspace_bytes.restype = C.c_size_t
+    lib.gear_norm_backward_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
+    lib.gear_rmsnorm_backward.restype = C.c_int
+    lib.gear_rmsnorm_backward.argtypes = [C.POINTER(gear_norm_backward_args), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.gear_rows8.restype = C.c_int
+    lib.gear_rows8.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.gear_packed_weights_bytes.restype = C.c_size_t
+    lib.gear_packed_weights_bytes.argtypes = [C.c_int32] * 5
+    lib.gear_weight_scales_bytes.restype = C.c_size_t
+    lib.gear_weight_scales_bytes.argtypes = [C.c_int32] * 3
+    lib.gear_pack_weights.restype = C.c_int
+    lib.gear_pack_weights.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                      C.c_void_p, C.c_void_p]
+    lib.gear_expert_product.restype = C.c_int
+    lib.gear_expert_product.argtypes = [C.POINTER(gear_expert_args), C.c_void_p]
+    lib.gear_expert_wgrad_workspace_bytes.restype = C.c_size_t
+    lib.gear_expert_wgrad_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32]
+    lib.gear_expert_wgrad.restype = C.c_int
+    lib.gear_expert_wgrad.argtypes = [C.POINTER(gear_expert_wgrad_args), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.gear_grad_list_bytes.restype = C.c_size_t
+    lib.gear_grad_list_bytes.argtypes = [C.c_int32]
+    lib.gear_grad_list_pack.restype = C.c_int
+    lib.gear_grad_list_pack.argtypes = [C.POINTER(gear_grad_tensor), C.c_int32, C.c_void_p, C.POINTER(C.c_int64)]
+    lib.gear_grad_workspace_bytes.restype = C.c_size_t
+    lib.gear_grad_workspace_bytes.argtypes = [C.c_int64]
+    lib.gear_grad_norm.restype = C.c_int
+    lib.gear_grad_norm.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+    lib.gear_clip_grads.restype = C.c_int
+    lib.gear_clip_grads.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
     lib.gear_profile_create.restype = C.c_void_p
     lib.gear_profile_create.argtypes = []
     lib.gear_profile_destroy.restype = None

@@ -1,0 +1,85 @@
+// What the products grouped by expert share: where an expert's rows are, and which tile is a workgroup's (gfx950 only).
+#pragma once
+
+#include "tn_tile.hpp"
+
+namespace gear {
+namespace {
+
+// The tile of a workgroup: rows [m0, m_end) of expert e from m0 on, column tile n_tile.  bad: off is not a CSR index.
+struct ExpertTile {
+  int e, m0, m_end, n_tile;
+  bool have, bad;
+};
+
+__device__ __forceinline__ int wave_add(int v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// whether off is a CSR index into `rows` rows; every lane of a wavefront gets the answer
+__device__ __forceinline__ bool offsets_ok(const int32_t *__restrict__ off, int experts, int rows, int lane) {
+  bool bad = off[0] != 0;
+  for (int e0 = 0; e0 < experts; e0 += kWave) {
+    const int e = min(e0 + lane, experts - 1), a = off[e], b = off[e + 1];
+    bad = bad || __any(a < 0 || b < a || b > rows);
+  }
+  return !bad;
+}
+
+// Row tiles of `edge` rows are counted expert by expert; tile number t (row tile t / n_tiles, column tile t % n_tiles) is
+// that of workgroup `block` after neighbouring tiles have been gathered on one XCD.  Every wavefront looks at all
+// offsets, 64 at a time, so that all workgroups agree on whether they are a CSR index.
+__device__ __forceinline__ ExpertTile expert_tile(const int32_t *__restrict__ off, int experts, int rows, int edge, int n_tiles,
+                                                  int block, int lane) {
+  ExpertTile r = {0, 0, 0, 0, false, false};
+  if (!off) {
+    const int total = (rows + edge - 1) / edge * n_tiles;
+    if (block >= total) return r;
+    const int t = xcd_remap(block, total);
+    r.m0 = t / n_tiles * edge, r.m_end = rows, r.n_tile = t % n_tiles, r.have = true;
+    return r;
+  }
+  int total = 0;
+  bool bad = off[0] != 0;
+  for (int e0 = 0; e0 < experts; e0 += kWave) {
+    const int e = min(e0 + lane, experts - 1), a = off[e], b = off[e + 1];
+    const bool wrong = a < 0 || b < a || b > rows;
+    bad = bad || __any(wrong);
+    total += wave_add(wrong || e0 + lane >= experts ? 0 : (b - a + edge - 1) / edge);
+  }
+  r.bad = bad;
+  total *= n_tiles;
+  if (bad || block >= total) return r;
+  const int t = xcd_remap(block, total), want = t / n_tiles;
+  int before = 0;
+  for (int e0 = 0; e0 < experts; e0 += kWave) {
+    const int e = min(e0 + lane, experts - 1), a = off[e], b = off[e + 1];
+    const int mine = e0 + lane >= experts ? 0 : (b - a + edge - 1) / edge;
+    int upto = mine;   // tiles of this and the lower lanes' experts
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int v = __shfl_up(upto, o, kWave);
+      if (lane >= o) upto += v;
+    }
+    const unsigned long long m = __ballot(before + upto > want);
+    if (m) {
+      const int at = __builtin_ctzll(m);
+      r.e = e0 + at;
+      r.m0 = __shfl(a, at, kWave) + (want - before - __shfl(upto - mine, at, kWave)) * edge;
+      r.m_end = __shfl(b, at, kWave);
+      break;
+    }
+    before += __shfl(upto, kWave - 1, kWave);
+  }
+  r.e = __builtin_amdgcn_readfirstlane(r.e);
+  r.m0 = __builtin_amdgcn_readfirstlane(r.m0);
+  r.m_end = __builtin_amdgcn_readfirstlane(r.m_end);
+  r.n_tile = t % n_tiles;
+  r.have = true;
+  return r;
+}
+
+}  // namespace
+}  // namespace gear

@@ -1,0 +1,308 @@
+// Root-mean-square norm of rows of features with the residual's addition, its output in 8 bits, and its backward pass:
+//
+//   h = x + residual,  s = (mean(h^2) + eps)^-1/2,  y = h s gain
+//   a = dy gain,  dx = s a - h s^3 mean(a h) + dsum,  dgain = sum over rows of dy h s
+//
+// (dx: y_c depends on h_c directly, s a, and on all of h through s, whose derivative by h_c is -s^3 h_c / dim.)
+// Every call is one pass over its rows: a row stays in the registers of the threads that read it, from the sum of its
+// squares to the last output, so what bounds these kernels is the memory they have to read and write.
+#include "eight.hpp"
+
+#include <cmath>
+
+namespace gear {
+namespace {
+
+// A row belongs to TPR threads with PER pieces of eight values each, piece i of thread t at columns 8 (t + TPR i): a
+// wavefront's accesses are contiguous, and 16 neighbouring threads hold a block of 128 columns.
+template <typename T, int TPR, int PER, bool NORM>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_args a) {
+  constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+  __shared__ float s_part[TPR / kWave];
+  const int t = threadIdx.x % TPR;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  if (ROWS > 1 && row >= a.rows) return;   // a whole wavefront, and no barrier below where a row is one wavefront's
+  const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
+  const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.ld_residual : nullptr;
+  float h[PER][8];
+  float sq = 0.0f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int c = 8 * (t + TPR * i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[i][j] = 0.0f;
+    if (c < a.dim) {
+      load8(x + c, h[i]);
+      if (NORM && res) {
+        float r[8];
+        load8(res + c, r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[i][j] += r[j];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sq += h[i][j] * h[i][j];
+  }
+  float s = 1.0f;
+  if constexpr (NORM) s = 1.0f / sqrtf(row_sum<TPR>(sq, s_part) / (float)a.dim + a.eps);
+  const int64_t ld8 = rows8_ld(a.dim), lds = scales8_ld(a.dim);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int c = 8 * (t + TPR * i);
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = h[i][j];
+    if constexpr (NORM) {
+      if (c < a.dim) {
+        if (a.sum) store8(static_cast<T *>(a.sum) + row * a.ld_sum + c, h[i]);
+        float g[8];
+        load8(a.gain + c, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = h[i][j] * s * g[j];
+      }
+    }
+    if (a.q8) {
+      float top = top8(y);
+#pragma unroll
+      for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+      const int e = exponent8(top);
+      const uint2 q = pack8(y, unscale8(e));
+      if (c < ld8) {
+        *reinterpret_cast<uint2 *>(a.q8 + row * ld8 + c) = q;
+        if (t % 16 == 0) a.scale[row * lds + c / kBlock8] = (uint8_t)(e + 127);
+      }
+      unpack8(q, scale8(e), y);
+    }
+    if (a.y && c < a.dim) store8(static_cast<T *>(a.y) + row * a.ld_y + c, y);
+  }
+  if (a.q8 && t < lds - ld8 / kBlock8) a.scale[row * lds + ld8 / kBlock8 + t] = 0;   // behind the last block: not used
+}
+
+// Backward pass.  A workgroup takes rows blockIdx.x * ROWS + threadIdx.x / TPR + k gridDim.x * ROWS and keeps its share of
+// dgain in registers; what its rows sum to becomes one row of `partial`, added up by k_sum_rows in a fixed order.
+template <typename T, int TPR, int PER>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm_backward(gear_norm_backward_args a, float *__restrict__ partial) {
+  constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+  __shared__ float s_part[TPR / kWave];
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  float dg[PER][8];
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dg[i][j] = 0.0f;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + sub; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
+    const T *hp = static_cast<const T *>(a.h) + row * a.ld_h, *dyp = static_cast<const T *>(a.dy) + row * a.ld_dy;
+    float h[PER][8], d[PER][8];
+    float sq = 0.0f, dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = 8 * (t + TPR * i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[i][j] = d[i][j] = 0.0f;
+      if (c < a.dim) {
+        load8(hp + c, h[i]);
+        load8(dyp + c, d[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = 8 * (t + TPR * i);
+      if (c >= a.dim) continue;
+      float g[8];
+      load8(a.gain + c, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        sq += h[i][j] * h[i][j];
+        dot += d[i][j] * g[j] * h[i][j];
+      }
+    }
+    sq = row_sum<TPR>(sq, s_part);
+    dot = row_sum<TPR>(dot, s_part);
+    const float s = 1.0f / sqrtf(sq / (float)a.dim + a.eps);
+    const float back = s * s * s * (dot / (float)a.dim);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = 8 * (t + TPR * i);
+      if (c >= a.dim) continue;
+      float g[8], dx[8];
+      load8(a.gain + c, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dx[j] = s * d[i][j] * g[j] - h[i][j] * back;
+        dg[i][j] += d[i][j] * h[i][j] * s;
+      }
+      if (a.dsum) {
+        float more[8];
+        load8(static_cast<const T *>(a.dsum) + row * a.ld_dsum + c, more);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dx[j] += more[j];
+      }
+      store8(static_cast<T *>(a.dx) + row * a.ld_dx + c, dx);
+    }
+  }
+  if (!partial) return;
+  if constexpr (ROWS > 1) {   // the wavefronts' shares, in ascending order
+    __shared__ float s_dg[(ROWS - 1) * PER * 8 * TPR];
+    if (sub > 0)
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s_dg[(((sub - 1) * PER + i) * 8 + j) * TPR + t] = dg[i][j];
+    __syncthreads();
+    if (sub > 0) return;
+    for (int w = 0; w < ROWS - 1; ++w)
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dg[i][j] += s_dg[((w * PER + i) * 8 + j) * TPR + t];
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int c = 8 * (t + TPR * i);
+    if (c < a.dim) store8(partial + (size_t)blockIdx.x * a.dim + c, dg[i]);
+  }
+}
+
+// out[c] = sum of partial[r][c], r < n: 16 columns a workgroup, 16 rows at a time, always in the same order
+__global__ void __launch_bounds__(256) k_sum_rows(const float *__restrict__ partial, int n, int dim, float *__restrict__ out) {
+  __shared__ float s[256];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
+  float v = 0.0f;
+  if (c < dim)
+    for (int r = r0; r < n; r += 16) v += partial[(size_t)r * dim + c];
+  s[threadIdx.x] = v;
+  __syncthreads();
+  if (r0 == 0 && c < dim) {
+    for (int r = 1; r < 16; ++r) v += s[r * 16 + threadIdx.x];
+    out[c] = v;
+  }
+}
+
+bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+bool row_distance(int64_t ld, int64_t width) { return ld >= width && ld % 8 == 0 && ld < (1 << 20); }
+bool matrix_ok(const void *p, int64_t ld, int64_t width) { return aligned(p, 16) && row_distance(ld, width); }
+bool shape_ok(int64_t rows, int32_t dim, int32_t dtype) {
+  return rows >= 0 && rows <= (1 << 30) && dim >= 8 && dim % 8 == 0 && dim <= GEAR_MAX_NORM_DIM &&
+         (dtype == GEAR_F32 || dtype == GEAR_BF16);
+}
+
+// Threads of a row: a wavefront up to 2048 columns, as many as hold the row in at most 32 values each beyond.
+template <typename T, bool NORM> hipError_t launch_norm(const gear_norm_args &a, hipStream_t s) {
+  const unsigned rows4 = (unsigned)((a.rows + 3) / 4), rows1 = (unsigned)a.rows;
+#define GEAR_NORM(TPR, PER)                                                                                        \
+  hipLaunchKernelGGL((k_rmsnorm<T, TPR, PER, NORM>), dim3(TPR == 64 ? rows4 : rows1), dim3(TPR < 256 ? 256 : TPR), 0, s, a)
+  if (a.dim <= 512)
+    GEAR_NORM(64, 1);
+  else if (a.dim <= 1024)
+    GEAR_NORM(64, 2);
+  else if (a.dim <= 2048)
+    GEAR_NORM(64, 4);
+  else if (a.dim <= 4096)
+    GEAR_NORM(256, 2);
+  else if (a.dim <= 8192)
+    GEAR_NORM(256, 4);
+  else if (a.dim <= 32768)
+    GEAR_NORM(1024, 4);
+  else
+    GEAR_NORM(1024, 8);
+#undef GEAR_NORM
+  return hipGetLastError();
+}
+
+// workgroups of the backward pass: rows are shared out to as many as the device holds, each leaves one row of partial sums
+constexpr int kBackBlocks = 1024;
+int back_blocks(int64_t rows, int32_t dim) {
+  const int64_t groups = dim <= 2048 ? (rows + 3) / 4 : rows;
+  return (int)(groups < kBackBlocks ? groups : kBackBlocks);
+}
+
+template <typename T> hipError_t launch_back(const gear_norm_backward_args &a, float *partial, hipStream_t s) {
+  const dim3 grid(back_blocks(a.rows, a.dim));
+#define GEAR_BACK(TPR, PER) \
+  hipLaunchKernelGGL((k_rmsnorm_backward<T, TPR, PER>), grid, dim3(TPR < 256 ? 256 : TPR), 0, s, a, partial)
+  if (a.dim <= 512)
+    GEAR_BACK(64, 1);
+  else if (a.dim <= 1024)
+    GEAR_BACK(64, 2);
+  else if (a.dim <= 2048)
+    GEAR_BACK(64, 4);
+  else if (a.dim <= 4096)
+    GEAR_BACK(256, 2);
+  else if (a.dim <= 8192)
+    GEAR_BACK(256, 4);
+  else if (a.dim <= 32768)
+    GEAR_BACK(1024, 4);
+  else
+    GEAR_BACK(1024, 8);
+#undef GEAR_BACK
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace gear
+
+using namespace gear;
+
+extern "C" int64_t gear_rows8_ld(int32_t dim) { return dim > 0 ? rows8_ld(dim) : 0; }
+extern "C" int64_t gear_scales8_ld(int32_t dim) { return dim > 0 ? scales8_ld(dim) : 0; }
+
+extern "C" gear_status gear_rmsnorm(const gear_norm_args *a, void *stream) {
+  if (!a || !shape_ok(a->rows, a->dim, a->dtype) || !(a->eps >= 0.0f) || !std::isfinite(a->eps)) return GEAR_ERR_INVALID;
+  if (a->rows == 0) return GEAR_OK;
+  if (!a->sum && !a->y && !a->q8) return GEAR_ERR_INVALID;
+  if (!a->q8 != !a->scale) return GEAR_ERR_INVALID;
+  if (!a->x || !a->gain || !aligned(a->gain, 16) || !matrix_ok(a->x, a->ld_x, a->dim)) return GEAR_ERR_INVALID;
+  if (a->residual && !matrix_ok(a->residual, a->ld_residual, a->dim)) return GEAR_ERR_INVALID;
+  if ((a->sum && !matrix_ok(a->sum, a->ld_sum, a->dim)) || (a->y && !matrix_ok(a->y, a->ld_y, a->dim))) return GEAR_ERR_INVALID;
+  if (a->sum && a->sum == a->y) return GEAR_ERR_INVALID;
+  if (!aligned(a->q8, 16) || !aligned(a->scale, 4)) return GEAR_ERR_INVALID;
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t err = a->dtype == GEAR_BF16 ? launch_norm<bf16_t, true>(*a, s) : launch_norm<float, true>(*a, s);
+  return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
+}
+
+extern "C" gear_status gear_rows8(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t dim, uint8_t *q8,
+                                  uint8_t *scale, void *stream) {
+  if (!shape_ok(rows, dim, dtype)) return GEAR_ERR_INVALID;
+  if (rows == 0) return GEAR_OK;
+  if (!x || !q8 || !scale || !matrix_ok(x, ld_x, dim) || !aligned(q8, 16) || !aligned(scale, 4)) return GEAR_ERR_INVALID;
+  gear_norm_args a = {};
+  a.rows = rows, a.dim = dim, a.dtype = dtype, a.x = x, a.ld_x = ld_x, a.q8 = q8, a.scale = scale;
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t err = dtype == GEAR_BF16 ? launch_norm<bf16_t, false>(a, s) : launch_norm<float, false>(a, s);
+  return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
+}
+
+extern "C" size_t gear_norm_backward_workspace_bytes(int64_t rows, int32_t dim) {
+  if (!shape_ok(rows, dim, GEAR_F32)) return 0;
+  const size_t bytes = (size_t)back_blocks(rows, dim) * dim * sizeof(float);
+  return bytes < 256 ? 256 : (bytes + 255) & ~(size_t)255;
+}
+
+extern "C" gear_status gear_rmsnorm_backward(const gear_norm_backward_args *a, void *workspace, size_t workspace_bytes,
+                                             void *stream) {
+  if (!a || !shape_ok(a->rows, a->dim, a->dtype) || !(a->eps >= 0.0f) || !std::isfinite(a->eps)) return GEAR_ERR_INVALID;
+  if (!aligned(a->dgain, 16)) return GEAR_ERR_INVALID;
+  hipStream_t s = (hipStream_t)stream;
+  if (a->rows == 0) {
+    if (a->dgain && launch_fill_zero(a->dgain, (size_t)a->dim * sizeof(float), s) != hipSuccess) return GEAR_ERR_HIP;
+    return GEAR_OK;
+  }
+  if (!a->h || !a->dy || !a->gain || !a->dx || !aligned(a->gain, 16)) return GEAR_ERR_INVALID;
+  if (!matrix_ok(a->h, a->ld_h, a->dim) || !matrix_ok(a->dy, a->ld_dy, a->dim) || !matrix_ok(a->dx, a->ld_dx, a->dim))
+    return GEAR_ERR_INVALID;
+  if (a->dsum && !matrix_ok(a->dsum, a->ld_dsum, a->dim)) return GEAR_ERR_INVALID;
+  float *partial = nullptr;
+  if (a->dgain) {
+    if (!workspace || !aligned(workspace, 256)) return GEAR_ERR_INVALID;
+    if (workspace_bytes < gear_norm_backward_workspace_bytes(a->rows, a->dim)) return GEAR_ERR_CAPACITY;
+    partial = static_cast<float *>(workspace);
+  }
+  const hipError_t err = a->dtype == GEAR_BF16 ? launch_back<bf16_t>(*a, partial, s) : launch_back<float>(*a, partial, s);
+  if (err != hipSuccess) return GEAR_ERR_HIP;
+  if (a->dgain) {
+    hipLaunchKernelGGL(k_sum_rows, dim3((a->dim + 15) / 16), dim3(256), 0, s, partial, back_blocks(a->rows, a->dim), a->dim, a->dgain);
+    if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
+  }
+  return GEAR_OK;
+}
