@@ -380,14 +380,15 @@ gear_status gear_rows8(const void *x, int32_t dtype, int64_t ld_x, int64_t rows,
                        void *stream);
 
 /* Weights laid out for the products.  w [experts x N x K] (src_dtype GEAR_F32 or GEAR_BF16, contiguous) is converted to
- * operand_dtype (GEAR_F32, GEAR_BF16 or GEAR_E4M3) and stored in the order in which the matrix instruction takes it.
- * transposed: laid out for products that contract over N instead (dX = dY W).  GEAR_E4M3 (not transposed): one scale
- * byte for each 128 x 128 weights, in scale [experts x ceil(N / 128) x gear_scales8_ld(K)], else NULL.
- * packed: gear_packed_weights_bytes bytes, 16-byte aligned.  (0 bytes on a bad argument.) */
+ * operand_dtype (GEAR_F32, GEAR_BF16 or GEAR_E4M3) and stored in the order in which the matrix instruction takes it: in
+ * `packed` for products that contract over K (Y = X W^T), in `packed_transposed` for those that contract over N (dX = dY W);
+ * either may be NULL.  GEAR_E4M3 (packed only): one scale byte for each 128 x 128 weights, in scale
+ * [experts x ceil(N / 128) x gear_scales8_ld(K)] (gear_weight_scales_bytes, 4-byte aligned), else NULL.  Both take
+ * gear_packed_weights_bytes bytes, 16-byte aligned.  (0 bytes on a bad argument.) */
 size_t gear_packed_weights_bytes(int32_t operand_dtype, int32_t experts, int32_t N, int32_t K, int32_t transposed);
 size_t gear_weight_scales_bytes(int32_t experts, int32_t N, int32_t K);
 gear_status gear_pack_weights(const void *w, int32_t src_dtype, int32_t operand_dtype, int32_t experts, int32_t N, int32_t K,
-                              int32_t transposed, void *packed, uint8_t *scale, void *stream);
+                              void *packed, void *packed_transposed, uint8_t *scale, void *stream);
 
 /* out[r] = x[r] W_e^T for the rows r in [off[e], off[e+1]) of every expert e: W_e [N x K] as packed above (from weights
  * [N x K], or transposed from [K x N]).  off [experts + 1] is device memory, 0 = off[0] <= off[1] <= ... <=

@@ -181,7 +181,7 @@ def _load() -> C.CDLL:
     lib.gear_weight_scales_bytes.restype = C.c_size_t
     lib.gear_weight_scales_bytes.argtypes = [C.c_int32] * 3
     lib.gear_pack_weights.restype = C.c_int
-    lib.gear_pack_weights.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+    lib.gear_pack_weights.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                                       C.c_void_p, C.c_void_p]
     lib.gear_expert_product.restype = C.c_int
     lib.gear_expert_product.argtypes = [C.POINTER(gear_expert_args), C.c_void_p]

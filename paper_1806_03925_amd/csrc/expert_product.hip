@@ -254,37 +254,52 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
                      n0 + wn * WN, a.N, lane);
 }
 
-template <typename C, bool F32> __global__ void __launch_bounds__(C::THREADS) k_expert_product(ProductArgs a) {
+template <typename C, bool F32> __global__ void __launch_bounds__(C::THREADS, 2) k_expert_product(ProductArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[C::LDS_BYTES];
   product_tile<C, F32>(a, lds);
 }
 
 // ---- weights in operand order -------------------------------------------------------------------------------------
 // packed [expert][32 outputs][k-block][unit][lane] of 16 bytes: output lane % 32, piece 2 unit + lane / 32 of the k-block;
-// zeros beyond the matrix.  A thread makes one piece.
-template <typename S, typename D, bool TRANSPOSED>
-__global__ void __launch_bounds__(256) k_pack(const S *__restrict__ w, int N, int K, int64_t pieces, uint4 *__restrict__ packed) {
+// zeros beyond the matrix.  A workgroup takes 64 x 64 weights through LDS, so that they are read once, in whole lines, for
+// both layouts, and a wavefront stores 1 KB of either.  Bound by memory.
+template <typename S, typename D>
+__global__ void __launch_bounds__(256) k_pack(const S *__restrict__ w, int N, int K, uint4 *__restrict__ packed, uint4 *__restrict__ transposed) {
   constexpr int V = 16 / (int)sizeof(D), KB = kKBlock / (int)sizeof(D);
-  const int out = TRANSPOSED ? K : N, in = TRANSPOSED ? N : K;   // the operand is out x in
-  const int nk = (in + KB - 1) / KB, n32 = (out + 31) / 32;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
-    const int lane = (int)(i & 63), unit = (int)((i >> 6) & 3);
-    const int64_t blk = i >> 8;
-    const int kb = (int)(blk % nk);
-    const int64_t strip = blk / nk;
-    const int64_t e = strip / n32;
-    const int o = (int)(strip % n32) * 32 + (lane & 31), k = kb * KB + (2 * unit + (lane >> 5)) * V;
-    float v[V];
+  constexpr int LD = 64 + 16 / (int)sizeof(D);   // rows 16 bytes apart in their banks
+  __shared__ __attribute__((aligned(16))) D tile[64 * LD];
+  const int k64 = (K + 63) / 64, n64 = (N + 63) / 64;
+  const int kt = blockIdx.x % k64, nt = blockIdx.x / k64 % n64, e = blockIdx.x / k64 / n64;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const bool in_matrix = o < out && k + j < in;
-      const int64_t at = TRANSPOSED ? (e * N + k + j) * K + o : (e * N + o) * K + k + j;
-      v[j] = in_matrix ? to_f32(w[at]) : 0.0f;
+  for (int i = 0; i < 2; ++i) {
+    const int n = (threadIdx.x >> 3) + 32 * i, k = (threadIdx.x & 7) * 8;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+    if (nt * 64 + n < N && kt * 64 + k < K) load8(w + ((int64_t)e * N + nt * 64 + n) * K + kt * 64 + k, v);
+    store8(tile + n * LD + k, v);
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 63, c = lane & 31, wave = threadIdx.x >> 6;
+  // 64 x 64 values are 2 strips of 32 outputs x (64 / KB) k-blocks x 4 units: 8 or 16 units, two or four for each wavefront
+#pragma unroll
+  for (int i = 0; i < 2 * (64 / KB); ++i) {
+    const int id = i * 4 + wave, unit = id & 3, kb = (id >> 2) % (64 / KB), strip = (id >> 2) / (64 / KB);
+    const int in = kb * KB + (2 * unit + (lane >> 5)) * V, out = strip * 32 + c;
+    if (packed && nt * 2 + strip < (N + 31) / 32 && kt * (64 / KB) + kb < (K + KB - 1) / KB) {
+      const int64_t blk = ((int64_t)e * ((N + 31) / 32) + nt * 2 + strip) * ((K + KB - 1) / KB) + kt * (64 / KB) + kb;
+      packed[blk * 256 + unit * 64 + lane] = *reinterpret_cast<const uint4 *>(tile + out * LD + in);
     }
-    if constexpr (sizeof(D) == 4)
-      packed[i] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-    else
-      packed[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[V - 4], v[V - 3]), pack_bf16(v[V - 2], v[V - 1]));
+    if (transposed && kt * 2 + strip < (K + 31) / 32 && nt * (64 / KB) + kb < (N + KB - 1) / KB) {
+      const int64_t blk = ((int64_t)e * ((K + 31) / 32) + kt * 2 + strip) * ((N + KB - 1) / KB) + nt * (64 / KB) + kb;
+      union {
+        D d[V];
+        uint4 u;
+      } p;
+#pragma unroll
+      for (int j = 0; j < V; ++j) p.d[j] = tile[(in + j) * LD + out];
+      transposed[blk * 256 + unit * 64 + lane] = p.u;
+    }
   }
 }
 
@@ -341,15 +356,10 @@ bool weights_ok(int operand_dtype, int experts, int N, int K, int transposed) {
          experts <= GEAR_MAX_EXPERTS && N >= 8 && N % 8 == 0 && K >= 8 && K % 8 == 0 && N < (1 << 20) && K < (1 << 20);
 }
 
-template <typename S, typename D> hipError_t launch_pack(const void *w, int experts, int N, int K, int transposed, void *packed,
-                                                         hipStream_t s) {
-  const int64_t pieces = packed_blocks(sizeof(D) == 2 ? GEAR_BF16 : GEAR_F32, experts, transposed ? K : N, transposed ? N : K) * 256;
-  const int64_t want = (pieces + 255) / 256;
-  const dim3 grid((unsigned)(want < 65536 ? want : 65536));
-  if (transposed)
-    hipLaunchKernelGGL((k_pack<S, D, true>), grid, dim3(256), 0, s, (const S *)w, N, K, pieces, (uint4 *)packed);
-  else
-    hipLaunchKernelGGL((k_pack<S, D, false>), grid, dim3(256), 0, s, (const S *)w, N, K, pieces, (uint4 *)packed);
+template <typename S, typename D>
+hipError_t launch_pack(const void *w, int experts, int N, int K, void *packed, void *transposed, hipStream_t s) {
+  const int64_t blocks = (int64_t)experts * ((N + 63) / 64) * ((K + 63) / 64);
+  hipLaunchKernelGGL((k_pack<S, D>), dim3((unsigned)blocks), dim3(256), 0, s, (const S *)w, N, K, (uint4 *)packed, (uint4 *)transposed);
   return hipGetLastError();
 }
 
@@ -371,7 +381,7 @@ hipError_t launch_tile(const ProductArgs &a, bool f32, hipStream_t s) {
 }
 
 template <int DT> hipError_t launch_product(const ProductArgs &a, bool f32, hipStream_t s) {
-  return launch_tile<DT, 2, 2, 2, 2>(a, f32, s);
+  return launch_tile<DT, 4, 1, 4, 2>(a, f32, s);
 }
 
 }  // namespace
@@ -390,26 +400,28 @@ extern "C" size_t gear_weight_scales_bytes(int32_t experts, int32_t N, int32_t K
 }
 
 extern "C" gear_status gear_pack_weights(const void *w, int32_t src_dtype, int32_t operand_dtype, int32_t experts, int32_t N,
-                                         int32_t K, int32_t transposed, void *packed, uint8_t *scale, void *stream) {
-  if (!weights_ok(operand_dtype, experts, N, K, transposed) || (src_dtype != GEAR_F32 && src_dtype != GEAR_BF16)) return GEAR_ERR_INVALID;
-  if (!w || !packed || ((uintptr_t)w & 15) || ((uintptr_t)packed & 15)) return GEAR_ERR_INVALID;
+                                         int32_t K, void *packed, void *packed_transposed, uint8_t *scale, void *stream) {
+  if (!weights_ok(operand_dtype, experts, N, K, packed_transposed != nullptr) || (src_dtype != GEAR_F32 && src_dtype != GEAR_BF16))
+    return GEAR_ERR_INVALID;
+  if (!w || (!packed && !packed_transposed) || ((uintptr_t)w & 15) || ((uintptr_t)packed & 15) || ((uintptr_t)packed_transposed & 15))
+    return GEAR_ERR_INVALID;
   if ((operand_dtype == GEAR_E4M3) != (scale != nullptr) || ((uintptr_t)scale & 3)) return GEAR_ERR_INVALID;
+  if ((int64_t)experts * ((N + 63) / 64) * ((K + 63) / 64) > (1 << 23)) return GEAR_ERR_INVALID;   // blocks are counted in 32 bits
   hipStream_t s = (hipStream_t)stream;
   hipError_t err;
   if (operand_dtype == GEAR_E4M3) {
-    const int64_t blocks = (int64_t)experts * ((N + kBlock8 - 1) / kBlock8) * ((K + kBlock8 - 1) / kBlock8);
-    if (blocks > INT32_MAX) return GEAR_ERR_INVALID;
+    const unsigned blocks = (unsigned)experts * ((N + kBlock8 - 1) / kBlock8) * ((K + kBlock8 - 1) / kBlock8);
     if (src_dtype == GEAR_BF16)
-      hipLaunchKernelGGL(k_pack8<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, s, (const bf16_t *)w, N, K, (unsigned char *)packed, scale);
+      hipLaunchKernelGGL(k_pack8<bf16_t>, dim3(blocks), dim3(256), 0, s, (const bf16_t *)w, N, K, (unsigned char *)packed, scale);
     else
-      hipLaunchKernelGGL(k_pack8<float>, dim3((unsigned)blocks), dim3(256), 0, s, (const float *)w, N, K, (unsigned char *)packed, scale);
+      hipLaunchKernelGGL(k_pack8<float>, dim3(blocks), dim3(256), 0, s, (const float *)w, N, K, (unsigned char *)packed, scale);
     err = hipGetLastError();
   } else if (operand_dtype == GEAR_BF16) {
-    err = src_dtype == GEAR_BF16 ? launch_pack<bf16_t, bf16_t>(w, experts, N, K, transposed, packed, s)
-                                 : launch_pack<float, bf16_t>(w, experts, N, K, transposed, packed, s);
+    err = src_dtype == GEAR_BF16 ? launch_pack<bf16_t, bf16_t>(w, experts, N, K, packed, packed_transposed, s)
+                                 : launch_pack<float, bf16_t>(w, experts, N, K, packed, packed_transposed, s);
   } else {
-    err = src_dtype == GEAR_BF16 ? launch_pack<bf16_t, float>(w, experts, N, K, transposed, packed, s)
-                                 : launch_pack<float, float>(w, experts, N, K, transposed, packed, s);
+    err = src_dtype == GEAR_BF16 ? launch_pack<bf16_t, float>(w, experts, N, K, packed, packed_transposed, s)
+                                 : launch_pack<float, float>(w, experts, N, K, packed, packed_transposed, s);
   }
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
 }

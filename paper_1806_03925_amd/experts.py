@@ -129,13 +129,10 @@ def _weights(w: torch.Tensor, where: str) -> Tuple[int, int, int]:
     return (1, *w.shape) if w.dim() == 2 else tuple(w.shape)
 
 
-def _pack(w: torch.Tensor, operand: int, experts: int, n: int, k: int, transposed: bool, packed, scale, where: str):
-    if packed is None:
-        size = lib.gear_packed_weights_bytes(operand, experts, n, k, int(transposed))
-        _need(size > 0, where, f"weights of {experts} x {n} x {k} have no packed form")
-        packed = torch.empty(size, dtype=torch.uint8, device=w.device)
-    _check(lib.gear_pack_weights(_ptr(w), _CODE[w.dtype], operand, experts, n, k, int(transposed), _ptr(packed), _ptr(scale), _stream()), where)
-    return packed
+def _packed_room(operand: int, experts: int, n: int, k: int, transposed: bool, device, where: str) -> torch.Tensor:
+    size = lib.gear_packed_weights_bytes(operand, experts, n, k, int(transposed))
+    _need(size > 0, where, f"weights of {experts} x {n} x {k} have no packed form")
+    return torch.empty(size, dtype=torch.uint8, device=device)
 
 
 class Weights8(NamedTuple):
@@ -153,7 +150,9 @@ def gear_weights8(w: torch.Tensor) -> Weights8:
     size = lib.gear_weight_scales_bytes(experts, n, k)
     _need(size > 0, "gear_weights8", f"weights of {experts} x {n} x {k} have no packed form")
     scale = torch.empty(size, dtype=torch.uint8, device=w.device)
-    return Weights8(_pack(w, GEAR_E4M3, experts, n, k, False, None, scale, "gear_weights8"), scale, experts, n, k)
+    packed = _packed_room(GEAR_E4M3, experts, n, k, False, w.device, "gear_weights8")
+    _check(lib.gear_pack_weights(_ptr(w), _CODE[w.dtype], GEAR_E4M3, experts, n, k, _ptr(packed), None, _ptr(scale), _stream()), "gear_weights8")
+    return Weights8(packed, scale, experts, n, k)
 
 
 class ExpertWeights:
@@ -164,16 +163,15 @@ class ExpertWeights:
         self.experts, self.N, self.K = _weights(w, "ExpertWeights")
         self.dtype = operand or w.dtype
         _need(self.dtype in _CODE, "ExpertWeights", "operand has to be float32 or bfloat16")
-        self.forward = self.transposed = None
-        self.backward = backward
+        self.forward = _packed_room(_CODE[self.dtype], self.experts, self.N, self.K, False, w.device, "ExpertWeights")
+        self.transposed = _packed_room(_CODE[self.dtype], self.experts, self.N, self.K, True, w.device, "ExpertWeights") if backward else None
         self.update(w)
 
     def update(self, w: torch.Tensor) -> None:
         e, n, k = _weights(w, "ExpertWeights.update")
         _need((e, n, k) == (self.experts, self.N, self.K), "ExpertWeights.update", "w has another shape than before")
-        self.forward = _pack(w, _CODE[self.dtype], e, n, k, False, self.forward, None, "ExpertWeights")
-        if self.backward:
-            self.transposed = _pack(w, _CODE[self.dtype], e, n, k, True, self.transposed, None, "ExpertWeights")
+        _check(lib.gear_pack_weights(_ptr(w), _CODE[w.dtype], _CODE[self.dtype], e, n, k, _ptr(self.forward), _ptr(self.transposed), None,
+                                     _stream()), "ExpertWeights.update")
 
 
 def _offsets(off: Optional[torch.Tensor], experts: int, status: Optional[torch.Tensor], device, where: str):
