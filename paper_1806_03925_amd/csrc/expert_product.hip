@@ -37,9 +37,10 @@ struct ProductArgs {
   int32_t *status;
 };
 
-// Tile shape: WAVES_M x WAVES_N wavefronts, each 32 WTM rows x 64 columns; STAGES k-blocks of x in LDS
-template <int DT_, int WTM_, int WAVES_M_, int WAVES_N_, int STAGES_> struct ProductTile {
-  static constexpr int DT = DT_, WTM = WTM_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, STAGES = STAGES_;
+// Tile shape: WAVES_M x WAVES_N wavefronts, each 32 WTM rows x 64 columns; both operands are requested AHEAD k-blocks before
+// they are multiplied, and x has one stage more in LDS
+template <int DT_, int WTM_, int WAVES_M_, int WAVES_N_, int AHEAD_> struct ProductTile {
+  static constexpr int DT = DT_, WTM = WTM_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, AHEAD = AHEAD_, STAGES = AHEAD + 1;
   static constexpr int WAVES = WAVES_M * WAVES_N, THREADS = WAVES * kWave;
   static constexpr int BM = 32 * WTM * WAVES_M, BN = WN * WAVES_N;
   static constexpr int STAGE_BYTES = BM * kKBlock, DMA = BM / 8 / WAVES;   // copies of a wavefront per stage, eight rows each
@@ -178,7 +179,7 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   const int64_t strip = (int64_t)nk * kPackedBlock;
   const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<unsigned char *>(a.packed) + ((int64_t)t.e * n32 + first32) * strip, 0, (int)(min(2, n32 - first32) * strip), 0x00020000);
-  u32x4_v b[2][2][TN];
+  u32x4_v b[C::AHEAD][2][2][TN];   // [k-block modulo AHEAD][half][unit][column tile]
   auto load = [&](u32x4_v (&to)[2][TN], int k, int half) {
     const int at = min(k, nk - 1) * kPackedBlock + half * 2048;
 #pragma unroll
@@ -222,31 +223,43 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
 
   scales(0, 0);
 #pragma unroll
-  for (int k = 0; k < C::STAGES - 1; ++k) copy(k);
-  load(b[0], 0, 0);
-  load(b[1], 0, 1);
+  for (int k = 0; k < C::AHEAD; ++k) {
+    copy(k);
+    load(b[k][0], k, 0);
+    load(b[k][1], k, 1);
+  }
   auto block = [&](int k, auto which) {
     constexpr int W = decltype(which)::value;
     if (k >= nk) return;
-    // copies of k have landed once only what was issued after them is outstanding
-    if (k == 0) wait_vm<0>(); else wait_vm<8>();
-    block_barrier();
-    copy(k + C::STAGES - 1);
+    // what was issued after the copies of k: 8 loads, and the copies and loads of the blocks between
+    wait_vm<8 + (C::AHEAD - 1) * (C::DMA + 8)>();
+    block_barrier();   // everybody's copies of k have landed, and everybody has read what copy() now overwrites
+    copy(k + C::AHEAD);
     const uint32_t at = x_rel + (uint32_t)(k % C::STAGES) * C::STAGE_BYTES;
-    mma_half<C, W>(acc, at, b[0], sx[0], sw[0]);
-    load(b[0], k + 1, 0);
-    mma_half<C, W>(acc, at ^ 64u, b[1], sx[0], sw[0]);
-    load(b[1], k + 1, 1);
+    u32x4_v (&bk)[2][2][TN] = b[W % C::AHEAD];
+    mma_half<C, W & 3>(acc, at, bk[0], sx[0], sw[0]);
+    load(bk[0], k + C::AHEAD, 0);
+    mma_half<C, W & 3>(acc, at ^ 64u, bk[1], sx[0], sw[0]);
+    load(bk[1], k + C::AHEAD, 1);
   };
-  for (int k = 0; k < nk; k += 4) {
+  auto four = [&](int k, auto first) {
+    constexpr int F = decltype(first)::value;
     scales(1, k + 4);
-    block(k, std::integral_constant<int, 0>{});
-    block(k + 1, std::integral_constant<int, 1>{});
-    block(k + 2, std::integral_constant<int, 2>{});
-    block(k + 3, std::integral_constant<int, 3>{});
+    block(k, std::integral_constant<int, F>{});
+    block(k + 1, std::integral_constant<int, F + 1>{});
+    block(k + 2, std::integral_constant<int, F + 2>{});
+    block(k + 3, std::integral_constant<int, F + 3>{});
 #pragma unroll
     for (int i = 0; i < C::WTM; ++i) sx[0][i] = sx[1][i];
     sw[0] = sw[1];
+  };
+  // bodies of the loop: as many k-blocks as scale words and register sets both divide
+  for (int k = 0; k < nk; k += C::AHEAD == 3 ? 12 : 4) {
+    four(k, std::integral_constant<int, 0>{});
+    if constexpr (C::AHEAD == 3) {
+      four(k + 4, std::integral_constant<int, 4>{});
+      four(k + 8, std::integral_constant<int, 8>{});
+    }
   }
   wait_vm<0>();    // copies beyond the end have landed too: LDS becomes the patches
   __syncthreads();
@@ -257,6 +270,141 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
 template <typename C, bool F32> __global__ void __launch_bounds__(C::THREADS, 2) k_expert_product(ProductArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[C::LDS_BYTES];
   product_tile<C, F32>(a, lds);
+}
+
+// ---- few tiles ----------------------------------------------------------------------------------------------------
+// A tile of 32 TM rows x 32 TN columns by WAVES wavefronts that take every WAVES-th k-block each and add their results up,
+// in ascending order, through LDS.  Where there are too few tiles to fill the device a product is a walk through the
+// weights, and what counts is that all of them are on their way at once: both operands go straight into registers, AHEAD
+// k-blocks before they are multiplied, and nothing waits for anybody else before the end.
+template <int DT_, int TM_, int TN_, int WAVES_, int AHEAD_> struct SplitTile {
+  static constexpr int DT = DT_, TM = TM_, TN = TN_, WAVES = WAVES_, AHEAD = AHEAD_, THREADS = WAVES * kWave, BM = 32 * TM, BN = 32 * TN;
+};
+
+template <typename C> struct SplitBlock {   // operands of a k-block in registers
+  u32x4_v x[C::TM][4], w[C::TN][4];
+  int sx[C::TM], sw;
+};
+
+template <typename C, bool F32> __device__ __forceinline__ void split_tile(const ProductArgs &a, float *sums) {
+  constexpr int DT = C::DT, TM_ = C::TM, TN_ = C::TN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_tiles = (a.N + C::BN - 1) / C::BN;
+  const ExpertTile t = expert_tile(a.off, a.experts, a.rows, C::BM, n_tiles, blockIdx.x, lane);
+  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
+  if (!t.have) return;
+  const int m0 = t.m0, n0 = t.n_tile * C::BN, m_rows = min(C::BM, t.m_end - m0);
+  const int row_bytes = a.K * operand_bytes(DT), nk = (row_bytes + kKBlock - 1) / kKBlock;
+  const int beyond = DT == GEAR_E4M3 ? nk * kKBlock : row_bytes;
+  const int r = lane & 31, g = lane >> 5;
+  const auto x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.x) + (int64_t)m0 * a.ld_x, 0,
+                                                        (int)((m_rows - 1) * a.ld_x) + nk * kKBlock, 0x00020000);
+  int x_at[TM_];
+#pragma unroll
+  for (int i = 0; i < TM_; ++i) x_at[i] = i * 32 + r < m_rows ? (i * 32 + r) * (int)a.ld_x + g * 16 : -(1 << 30);
+  const int n32 = (a.N + 31) / 32, first32 = n0 / 32;
+  const int64_t strip = (int64_t)nk * kPackedBlock;
+  const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.packed) + ((int64_t)t.e * n32 + first32) * strip, 0,
+                                                        (int)(min(TN_, n32 - first32) * strip), 0x00020000);
+  const int64_t lds8 = scales8_ld(a.K);
+  const uint8_t *xs[TM_], *ws = nullptr;
+  if constexpr (DT == GEAR_E4M3) {
+#pragma unroll
+    for (int i = 0; i < TM_; ++i) xs[i] = a.x_scale + (int64_t)(m0 + min(i * 32 + r, m_rows - 1)) * lds8;
+    ws = a.w_scale + ((int64_t)t.e * ((a.N + kBlock8 - 1) / kBlock8) + n0 / kBlock8) * lds8;
+  }
+  f32x16_v acc[TM_][TN_];
+#pragma unroll
+  for (int i = 0; i < TM_; ++i)
+#pragma unroll
+    for (int j = 0; j < TN_; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+  auto load = [&](SplitBlock<C> &b, int k) {   // past the end: the last block once more, which is not multiplied
+    const int kk = min(k, nk - 1);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int j = 0; j < TN_; ++j)
+        b.w[j][u] = __builtin_bit_cast(u32x4_v, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc, j * (int)strip + lane * 16, kk * kPackedBlock + u * 1024, 0));
+      const bool in = kk * kKBlock + (2 * u + g) * 16 < beyond;
+#pragma unroll
+      for (int i = 0; i < TM_; ++i)
+        b.x[i][u] = __builtin_bit_cast(u32x4_v, __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, in ? x_at[i] + u * 32 : -(1 << 30), kk * kKBlock, 0));
+    }
+    if constexpr (DT == GEAR_E4M3) {
+#pragma unroll
+      for (int i = 0; i < TM_; ++i) b.sx[i] = xs[i][kk];
+      b.sw = ws[kk];
+    }
+  };
+  auto mma = [&](const SplitBlock<C> &b) {
+#pragma unroll
+    for (int i = 0; i < TM_; ++i)
+#pragma unroll
+      for (int j = 0; j < TN_; ++j) {
+        if constexpr (DT == GEAR_E4M3) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const u32x4_v &w0 = b.w[j][2 * h], &w1 = b.w[j][2 * h + 1], &x0 = b.x[i][2 * h], &x1 = b.x[i][2 * h + 1];
+            const i32x8_v w = {(int)w0.x, (int)w0.y, (int)w0.z, (int)w0.w, (int)w1.x, (int)w1.y, (int)w1.z, (int)w1.w};
+            const i32x8_v x = {(int)x0.x, (int)x0.y, (int)x0.z, (int)x0.w, (int)x1.x, (int)x1.y, (int)x1.z, (int)x1.w};
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, acc[i][j], 0, 0, 0, b.sw, 0, b.sx[i]);
+          }
+        } else if constexpr (DT == GEAR_BF16) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) MFMA_BF16_T(acc[i][j], b.x[i][u], b.w[j][u]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.w[j][u][e]), __uint_as_float(b.x[i][u][e]), acc[i][j], 0, 0, 0);
+        }
+      }
+  };
+  SplitBlock<C> b[C::AHEAD + 1];
+#pragma unroll
+  for (int p = 0; p < C::AHEAD; ++p) load(b[p], wave + p * C::WAVES);
+  for (int k = wave; k < nk; k += (C::AHEAD + 1) * C::WAVES) {
+#pragma unroll
+    for (int p = 0; p <= C::AHEAD; ++p) {
+      load(b[(p + C::AHEAD) % (C::AHEAD + 1)], k + (p + C::AHEAD) * C::WAVES);
+      if (k + p * C::WAVES < nk) mma(b[p]);
+    }
+  }
+  // [wavefront][tile][element / 4][lane] of four values each: four consecutive columns of row lane % 32
+  constexpr int PARTS = TM_ * TN_ * 4;
+#pragma unroll
+  for (int i = 0; i < TM_; ++i)
+#pragma unroll
+    for (int j = 0; j < TN_; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4 *>(sums + (((wave * TM_ + i) * TN_ + j) * 256 + q * 64 + lane) * 4) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+  __syncthreads();
+  for (int part = wave; part < PARTS; part += C::WAVES) {
+    const int q = part & 3, j = (part >> 2) % TN_, i = (part >> 2) / TN_;
+    float4 v = *reinterpret_cast<const float4 *>(sums + (part * 64 + lane) * 4);
+#pragma unroll
+    for (int w = 1; w < C::WAVES; ++w) {
+      const float4 o = *reinterpret_cast<const float4 *>(sums + ((w * PARTS + part) * 64 + lane) * 4);
+      v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+    }
+    const int m = i * 32 + r, n = n0 + j * 32 + 8 * q + 4 * g;
+    if (m < m_rows && n < a.N) {
+      if constexpr (F32)
+        *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + (m0 + m) * a.ld_out + n) = v;
+      else
+        *reinterpret_cast<uint2 *>(static_cast<bf16_t *>(a.out) + (m0 + m) * a.ld_out + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    }
+  }
+}
+
+template <typename C, bool F32> __global__ void __launch_bounds__(C::THREADS) k_expert_product_split(ProductArgs a) {
+  __shared__ __attribute__((aligned(16))) float sums[C::WAVES * C::BM * C::BN];
+  split_tile<C, F32>(a, sums);
 }
 
 // ---- weights in operand order -------------------------------------------------------------------------------------
@@ -363,9 +511,9 @@ hipError_t launch_pack(const void *w, int experts, int N, int K, void *packed, v
   return hipGetLastError();
 }
 
-template <int DT, int WTM, int WAVES_M, int WAVES_N, int STAGES>
+template <int DT, int WTM, int WAVES_M, int WAVES_N, int AHEAD>
 hipError_t launch_tile(const ProductArgs &a, bool f32, hipStream_t s) {
-  using C = ProductTile<DT, WTM, WAVES_M, WAVES_N, STAGES>;
+  using C = ProductTile<DT, WTM, WAVES_M, WAVES_N, AHEAD>;
   // as many row tiles as there can be (every expert may end inside one), one at least: it looks at the offsets
   const int64_t m_tiles = ((int64_t)a.rows + C::BM - 1) / C::BM + (a.off ? a.experts - 1 : 0);
   const dim3 grid((unsigned)(m_tiles > 0 ? m_tiles * ((a.N + C::BN - 1) / C::BN) : 1));
@@ -380,8 +528,43 @@ hipError_t launch_tile(const ProductArgs &a, bool f32, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int DT, int TM, int TN, int WAVES, int AHEAD> hipError_t launch_split(const ProductArgs &a, bool f32, hipStream_t s) {
+  using C = SplitTile<DT, TM, TN, WAVES, AHEAD>;
+  const int64_t m_tiles = ((int64_t)a.rows + C::BM - 1) / C::BM + (a.off ? a.experts - 1 : 0);
+  const dim3 grid((unsigned)(m_tiles > 0 ? m_tiles * ((a.N + C::BN - 1) / C::BN) : 1));
+  if constexpr (DT == GEAR_F32) {
+    hipLaunchKernelGGL((k_expert_product_split<C, true>), grid, dim3(C::THREADS), 0, s, a);
+  } else {
+    if (f32)
+      hipLaunchKernelGGL((k_expert_product_split<C, true>), grid, dim3(C::THREADS), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_expert_product_split<C, false>), grid, dim3(C::THREADS), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+// Which shape: the largest that still gives the device something to do, by the number of tiles (with experts, of about how
+// many: half a tile more for each).  us measured, K = N where one is given, smaller / larger shape of each border:
+//   few tiles, up to 256 of 32 x 32 (one for each CU), against 32 x 128: 256 x 1024 x 1152 bf16 6.7 / 7.3, 64 x 4096 8 bits 10.2 /
+//     15.0; above, 512 x 1024 x 1152 bf16 11.4 / 7.4.  fp32, whose products are slow, up to 1024: 512 x 2048 55 / 66, 1024 x 2048 108 / 75
+//   32 x 128 up to 512 tiles, against 64 x 256: 1024 x 2048 bf16 17.0 / 18.6, 4096 x 1024 x 1152 16.2 / 12.4; but not where its many
+//     row tiles each read weights that no L2 holds: 256 x 8192 bf16 144 / 74
+//   64 x 256 below 512 tiles, against 128 x 256: 2048 x 2048 bf16 19.9 / 28.1, 4096 x 2048 36 / 33; and a little over one round of the
+//     larger tiles (two a CU): 16384 x 1024 x 1152 by 64 experts in 8 bits 30.7 / 36.7
+//   fp32: 64 x 128 by four wavefronts up to 4096 tiles: 16384 x 1024 x 1152 by 8 experts 314 / 407, 65536 x 1024 x 576 584 / 561
+//   up to 128 columns, where wider tiles are half empty: 128 x 128: 65536 x 72 x 320 in 8 bits 7.8 / 9.4
 template <int DT> hipError_t launch_product(const ProductArgs &a, bool f32, hipStream_t s) {
-  return launch_tile<DT, 4, 1, 4, 2>(a, f32, s);
+  auto tiles = [&](int bm, int bn) { return ((int64_t)(a.rows + bm - 1) / bm + (a.off ? a.experts / 2 : 0)) * ((a.N + bn - 1) / bn); };
+  if (tiles(32, 32) <= (DT == GEAR_F32 ? 1024 : 256)) return launch_split<DT, 1, 1, 4, 2>(a, f32, s);
+  if constexpr (DT == GEAR_F32) {
+    if (tiles(64, 128) <= 4096) return launch_tile<DT, 1, 2, 2, 3>(a, f32, s);
+  } else {
+    const int64_t weights = (int64_t)a.N * a.K * operand_bytes(DT);
+    if (tiles(32, 128) <= 512 && (weights <= 8 << 20 || a.rows <= 128 * (int64_t)a.experts)) return launch_tile<DT, 1, 1, 2, 3>(a, f32, s);
+    if (a.N <= 128) return launch_tile<DT, 2, 2, 2, 2>(a, f32, s);
+    if (tiles(64, 256) < 512 || (tiles(128, 256) > 512 && tiles(128, 256) <= 640)) return launch_tile<DT, 2, 1, 4, 2>(a, f32, s);
+  }
+  return launch_tile<DT, 4, 1, 4, 1>(a, f32, s);
 }
 
 }  // namespace

@@ -28,17 +28,28 @@ __device__ __forceinline__ bool offsets_ok(const int32_t *__restrict__ off, int 
   return !bad;
 }
 
-// Row tiles of `edge` rows are counted expert by expert; tile number t (row tile t / n_tiles, column tile t % n_tiles) is
-// that of workgroup `block` after neighbouring tiles have been gathered on one XCD.  Every wavefront looks at all
-// offsets, 64 at a time, so that all workgroups agree on whether they are a CSR index.
+// Tile t of m_tiles x n_tiles: kGroupRows row tiles are walked down, column by column, before the next ones.  The 64 tiles
+// that an XCD works on at a time then read 8 strips of rows and 8 of weights through its L2, not two and 32.
+constexpr int kGroupRows = 8;
+struct TileAt {
+  int m, n;
+};
+__device__ __forceinline__ TileAt tile_at(int t, int m_tiles, int n_tiles) {
+  const int first = t / (kGroupRows * n_tiles) * kGroupRows, in = t % (kGroupRows * n_tiles), rows = min(kGroupRows, m_tiles - first);
+  return {first + in % rows, in / rows};
+}
+
+// Row tiles of `edge` rows are counted expert by expert; the workgroups' tiles are in the order of tile_at after
+// neighbouring ones have been gathered on one XCD.  Every wavefront looks at all offsets, 64 at a time, so that all
+// workgroups agree on whether they are a CSR index.
 __device__ __forceinline__ ExpertTile expert_tile(const int32_t *__restrict__ off, int experts, int rows, int edge, int n_tiles,
                                                   int block, int lane) {
   ExpertTile r = {0, 0, 0, 0, false, false};
   if (!off) {
-    const int total = (rows + edge - 1) / edge * n_tiles;
-    if (block >= total) return r;
-    const int t = xcd_remap(block, total);
-    r.m0 = t / n_tiles * edge, r.m_end = rows, r.n_tile = t % n_tiles, r.have = true;
+    const int m_tiles = (rows + edge - 1) / edge;
+    if (block >= m_tiles * n_tiles) return r;
+    const TileAt t = tile_at(xcd_remap(block, m_tiles * n_tiles), m_tiles, n_tiles);
+    r.m0 = t.m * edge, r.m_end = rows, r.n_tile = t.n, r.have = true;
     return r;
   }
   int total = 0;
@@ -50,9 +61,10 @@ __device__ __forceinline__ ExpertTile expert_tile(const int32_t *__restrict__ of
     total += wave_add(wrong || e0 + lane >= experts ? 0 : (b - a + edge - 1) / edge);
   }
   r.bad = bad;
-  total *= n_tiles;
-  if (bad || block >= total) return r;
-  const int t = xcd_remap(block, total), want = t / n_tiles;
+  total = __builtin_amdgcn_readfirstlane(total);   // the same in all lanes: what follows from it is scalar
+  if (bad || block >= total * n_tiles) return r;
+  const TileAt t = tile_at(xcd_remap(block, total * n_tiles), total, n_tiles);
+  const int want = t.m;
   int before = 0;
   for (int e0 = 0; e0 < experts; e0 += kWave) {
     const int e = min(e0 + lane, experts - 1), a = off[e], b = off[e + 1];
@@ -76,7 +88,7 @@ __device__ __forceinline__ ExpertTile expert_tile(const int32_t *__restrict__ of
   r.e = __builtin_amdgcn_readfirstlane(r.e);
   r.m0 = __builtin_amdgcn_readfirstlane(r.m0);
   r.m_end = __builtin_amdgcn_readfirstlane(r.m_end);
-  r.n_tile = t % n_tiles;
+  r.n_tile = t.n;
   r.have = true;
   return r;
 }
