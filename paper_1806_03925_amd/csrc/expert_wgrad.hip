@@ -12,21 +12,115 @@ struct WgradArgs {
   int64_t ld_dy, ld_x;   // elements
   int rows, K, N, experts;
   int32_t *status;
+  float *partial;        // [pieces of experts that are cut][N x K]
+  int cut;               // rows of a piece
 };
+
+struct WgradTile {
+  int m0, n0, first, last;
+  float *dst;
+  bool have, bad;
+};
+
+__device__ __forceinline__ int pieces_of(int rows, int cut) { return max((rows + cut - 1) / cut, 1); }   // no rows: zeros to write
+
+// partial results in front of those of expert e: the pieces of all experts before it that are cut
+__device__ __forceinline__ int partials_before(const int32_t *__restrict__ off, int e, int cut, int lane) {
+  int n = 0;
+  for (int e0 = 0; e0 < e; e0 += kWave) {
+    const int at = min(e0 + lane, e - 1), rows = off[at + 1] - off[at];
+    n += e0 + lane < e && rows > cut ? pieces_of(rows, cut) : 0;
+  }
+  return wave_add(n);
+}
+
+// The tile of workgroup `block`, and the rows it adds up: an expert's rows are cut into pieces of `cut`, and what the pieces of
+// one expert add up to is left in `partial` and summed by k_wgrad_sum (an expert of one piece needs neither).  Experts come
+// in descending order of their rows (up to 64 experts, which one look at the offsets orders; with more of them chance does),
+// so that the long tiles are not the last ones.  Workgroups are spread over the XCDs by their number modulo 8, whatever they
+// cost: kSpread neighbouring tiles, which share rows of dy and x, go to one XCD, the next ones to the next.
+constexpr int kSpread = 8;
+__device__ __forceinline__ WgradTile wgrad_tile(const WgradArgs &a, int bm, int bn, int block, int lane) {
+  WgradTile r = {0, 0, 0, 0, nullptr, false, false};
+  r.bad = a.off && !offsets_ok(a.off, a.experts, a.rows, lane);
+  if (r.bad) return r;
+  const int n_tiles = (a.N + bm - 1) / bm, k_tiles = (a.K + bn - 1) / bn;
+  const int work = (block / kXcds / kSpread * kXcds + block % kXcds) * kSpread + block / kXcds % kSpread;
+  const int want = work / (n_tiles * k_tiles), tile = work % (n_tiles * k_tiles);   // the want-th piece of all
+  int e = -1, piece = 0;
+  if (!a.off) {
+    if (want < pieces_of(a.rows, a.cut)) e = 0, piece = want;
+  } else if (a.experts <= kWave) {
+    const int rows = lane < a.experts ? a.off[lane + 1] - a.off[lane] : -1, mine = lane < a.experts ? pieces_of(rows, a.cut) : 0;
+    int before = 0;   // pieces of the experts with more rows
+    for (int j = 0; j < a.experts; ++j) {
+      const int other = __shfl(rows, j, kWave), pieces = __shfl(mine, j, kWave);
+      before += other > rows || (other == rows && j < lane) ? pieces : 0;
+    }
+    const unsigned long long m = __ballot(want >= before && want < before + mine);
+    if (m) e = __builtin_ctzll(m), piece = want - __shfl(before, e, kWave);
+  } else {
+    int before = 0;
+    for (int e0 = 0; e0 < a.experts && e < 0; e0 += kWave) {
+      const int at = min(e0 + lane, a.experts - 1), mine = e0 + lane < a.experts ? pieces_of(a.off[at + 1] - a.off[at], a.cut) : 0;
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int v = __shfl_up(upto, o, kWave);
+        if (lane >= o) upto += v;
+      }
+      const unsigned long long m = __ballot(want < before + upto);
+      if (m) {
+        const int l = __builtin_ctzll(m);
+        e = e0 + l, piece = want - before - __shfl(upto - mine, l, kWave);
+      }
+      before += __shfl(upto, kWave - 1, kWave);
+    }
+  }
+  e = __builtin_amdgcn_readfirstlane(e), piece = __builtin_amdgcn_readfirstlane(piece);
+  if (e < 0) return r;
+  const int first = a.off ? a.off[e] : 0, last = a.off ? a.off[e + 1] : a.rows;
+  r.m0 = tile / k_tiles * bm, r.n0 = tile % k_tiles * bn, r.have = true;
+  r.first = first + piece * a.cut, r.last = r.first + min(last - r.first, a.cut);
+  r.dst = a.dw + (int64_t)e * a.N * a.K;
+  if (last - first > a.cut) {
+    const int before = a.off ? __builtin_amdgcn_readfirstlane(partials_before(a.off, e, a.cut, lane)) : 0;
+    r.dst = a.partial + (int64_t)(before + piece) * a.N * a.K;
+  }
+  return r;
+}
+
+// dw of the experts that were cut: their pieces in ascending order
+__global__ void __launch_bounds__(256) k_wgrad_sum(WgradArgs a) {
+  const int lane = threadIdx.x & 63, e = blockIdx.y;
+  if (a.off && !offsets_ok(a.off, a.experts, a.rows, lane)) return;
+  const int rows = a.off ? a.off[e + 1] - a.off[e] : a.rows;
+  if (rows <= a.cut) return;
+  const int before = a.off ? __builtin_amdgcn_readfirstlane(partials_before(a.off, e, a.cut, lane)) : 0, pieces = pieces_of(rows, a.cut);
+  const int64_t vec = (int64_t)a.N * a.K / 4;
+  const float4 *p = reinterpret_cast<const float4 *>(a.partial) + before * vec;
+  float4 *o = reinterpret_cast<float4 *>(a.dw) + e * vec;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < vec; i += (int64_t)gridDim.x * 256) {
+    float4 v = p[i];
+    for (int z = 1; z < pieces; ++z) {
+      const float4 w = p[z * vec + i];
+      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    o[i] = v;
+  }
+}
+// workgroups for `tiles` tiles: whole rounds of kSpread tiles on every XCD
+inline unsigned wgrad_blocks(int64_t tiles) { return (unsigned)((tiles + kSpread * kXcds - 1) / (kSpread * kXcds) * (kSpread * kXcds)); }
 
 // Rows of both operands go global -> LDS as they are; operands are assembled from there as in tn_tile.hpp.
 template <typename C> __global__ void __launch_bounds__(C::THREADS) k_expert_wgrad(WgradArgs a) {
   using T = typename C::T;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[C::STAGES * C::STAGE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool ok = !a.off || offsets_ok(a.off, a.experts, a.rows, lane);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? GEAR_OK : GEAR_ERR_RANGE;
-  if (!ok) return;
-  const int n_tiles = (a.N + C::BM - 1) / C::BM, k_tiles = (a.K + C::BN - 1) / C::BN;
-  const int work = xcd_remap(blockIdx.x, gridDim.x);
-  const int e = work / (n_tiles * k_tiles), tile = work % (n_tiles * k_tiles);
-  const int m0 = tile / k_tiles * C::BM, n0 = tile % k_tiles * C::BN;
-  const int first = a.off ? a.off[e] : 0, last = a.off ? a.off[e + 1] : a.rows;
+  const WgradTile t = wgrad_tile(a, C::BM, C::BN, blockIdx.x, lane);
+  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
+  if (!t.have) return;
+  const int m0 = t.m0, n0 = t.n0, first = t.first, last = t.last;
 
   const int wm = wave >> 1, wn = wave & 1;
   constexpr int VEC = 16 / (int)sizeof(T);
@@ -72,15 +166,15 @@ template <typename C> __global__ void __launch_bounds__(C::THREADS) k_expert_wgr
       b_addr[i] = lds_base + C::OPERAND_BYTES + at + (uint32_t)(((wn * C::WTN + i) ^ (j >> 2)) << 6);
   }
   int stage = 0, fill = C::STAGES - 1;
-  for (int t = 0; t < nk; ++t) {
-    wait_stages<2 * C::DMA, C::STAGES - 2>(nk - 1 - t);
+  for (int k = 0; k < nk; ++k) {
+    wait_stages<2 * C::DMA, C::STAGES - 2>(nk - 1 - k);
     block_barrier();
-    if (t + C::STAGES - 1 < nk) issue(t + C::STAGES - 1, fill);
+    if (k + C::STAGES - 1 < nk) issue(k + C::STAGES - 1, fill);
     mma_stage_rows<C>(acc, a_addr, b_addr, (uint32_t)stage * C::STAGE_BYTES);
     stage = stage + 1 == C::STAGES ? 0 : stage + 1;
     fill = fill + 1 == C::STAGES ? 0 : fill + 1;
   }
-  float *dst = a.dw + (int64_t)e * a.N * a.K;
+  float *dst = t.dst;
   const int c = lane & 31, g = lane >> 5;
 #pragma unroll
   for (int i = 0; i < C::WTM; ++i)
@@ -95,44 +189,47 @@ template <typename C> __global__ void __launch_bounds__(C::THREADS) k_expert_wgr
     }
 }
 
-// ---- bf16, many tiles: 256 x 256 by four wavefronts of 128 x 128 --------------------------------------------------
-// Both operands pass LDS, so LDS bounds this product: of 32 rows a tile of 128 x 128 (four wavefronts of 64 x 64) moves 48 KB
-// through it for 256 cycles of matrix instructions, this shape 96 KB for 1024.  With one wavefront per SIMD nobody else fills
-// its waits, so operands are requested a k-step (16 rows, 512 cycles of products) ahead, also across the border of a stage.
+// ---- bf16: 128 x 256 by four wavefronts of 64 x 128 ----------------------------------------------------------------
+// Both operands pass LDS, and LDS bounds this product: of 32 rows a tile of 128 x 128 (four wavefronts of 64 x 64) moves 48 KB
+// through it for 256 cycles of matrix instructions, this one 72 KB for 512.  Two workgroups share a CU, so that one stores
+// its gradient (128 KB) while the other multiplies; and operands are requested a k-step (16 rows) ahead, also across the
+// border of a stage.
 struct WideTile {
-  static constexpr int THREADS = 256, WAVES = 4, BM = 256, BN = 256, KD = 32, STAGES = 4;
-  static constexpr int ROW = 512, OPERAND_BYTES = KD * ROW, STAGE_BYTES = 2 * OPERAND_BYTES;
-  static constexpr int DMA = KD / 2 / WAVES;   // copies of a wavefront per operand and stage, two rows each
+  static constexpr int THREADS = 256, WAVES = 4, TM = 2, TN = 4, BM = 128, BN = 256, KD = 32, STAGES = 3;
+  static constexpr int ROW_A = BM * 2, ROW_B = BN * 2, A_BYTES = KD * ROW_A, STAGE_BYTES = A_BYTES + KD * ROW_B;
+  static constexpr int DMA_A = A_BYTES / 1024 / WAVES, DMA_B = KD * ROW_B / 1024 / WAVES, DMA_ALL = DMA_A + DMA_B;   // copies of a wavefront
 };
 
 struct WideFrag {
-  u32x2_v a[4][2], b[4][2];   // [32-column tile][rows +0..3 | +4..7 of the lane's eight]
-  // even and odd column tiles: the rows' XOR by 64 (row % 4) makes neighbouring tiles trade places, not offsets
-  __device__ __forceinline__ void fetch(const uint32_t (&at_a)[4], const uint32_t (&at_b)[4]) {
+  u32x2_v a[WideTile::TM][2], b[WideTile::TN][2];   // [32-column tile][rows +0..3 | +4..7 of the lane's eight]
+  __device__ __forceinline__ void fetch(const uint32_t (&at_a)[WideTile::TM], const uint32_t (&at_b)[WideTile::TN], uint32_t so_a, uint32_t so_b) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lds_read_tr<0>(a[i][0], at_a[i]);
-      lds_read_tr<4 * WideTile::ROW>(a[i][1], at_a[i]);
-      lds_read_tr<0>(b[i][0], at_b[i]);
-      lds_read_tr<4 * WideTile::ROW>(b[i][1], at_b[i]);
+    for (int i = 0; i < WideTile::TM; ++i) {
+      lds_read_tr<0>(a[i][0], at_a[i] + so_a);
+      lds_read_tr<4 * WideTile::ROW_A>(a[i][1], at_a[i] + so_a);
+    }
+#pragma unroll
+    for (int i = 0; i < WideTile::TN; ++i) {
+      lds_read_tr<0>(b[i][0], at_b[i] + so_b);
+      lds_read_tr<4 * WideTile::ROW_B>(b[i][1], at_b[i] + so_b);
     }
   }
   __device__ __forceinline__ void wait() {
     wait_lgkm<0>();
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        landed(a[i][h]);
-        landed(b[i][h]);
-      }
+      for (int i = 0; i < WideTile::TM; ++i) landed(a[i][h]);
+#pragma unroll
+      for (int i = 0; i < WideTile::TN; ++i) landed(b[i][h]);
+    }
   }
-  __device__ __forceinline__ void mma(f32x16_v (&acc)[4][4]) {
+  __device__ __forceinline__ void mma(f32x16_v (&acc)[WideTile::TM][WideTile::TN]) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < WideTile::TM; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < WideTile::TN; ++j) {
         const u32x4_v av = {a[i][0].x, a[i][0].y, a[i][1].x, a[i][1].y};
         const u32x4_v bv = {b[j][0].x, b[j][0].y, b[j][1].x, b[j][1].y};
         MFMA_BF16(acc[i][j], av, bv);
@@ -144,121 +241,135 @@ struct WideFrag {
 __device__ __forceinline__ void wgrad_wide(const WgradArgs &a, unsigned char *lds) {
   using C = WideTile;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool ok = !a.off || offsets_ok(a.off, a.experts, a.rows, lane);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? GEAR_OK : GEAR_ERR_RANGE;
-  if (!ok) return;
-  const int n_tiles = (a.N + C::BM - 1) / C::BM, k_tiles = (a.K + C::BN - 1) / C::BN;
-  const int work = xcd_remap(blockIdx.x, gridDim.x);
-  const int e = work / (n_tiles * k_tiles), tile = work % (n_tiles * k_tiles);
-  const int m0 = tile / k_tiles * C::BM, n0 = tile % k_tiles * C::BN;
-  const int first = a.off ? a.off[e] : 0, last = a.off ? a.off[e + 1] : a.rows;
+  const WgradTile t = wgrad_tile(a, C::BM, C::BN, blockIdx.x, lane);
+  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
+  if (!t.have) return;
+  const int m0 = t.m0, n0 = t.n0, first = t.first, last = t.last;
   const int wm = wave >> 1, wn = wave & 1;
   const int nk = (last - first + C::KD - 1) / C::KD;
 
-  // A copy is two rows of 512 bytes; LDS slot lane % 32 of a row receives piece (lane % 32) ^ 4 (row % 4).  Rows beyond the
-  // expert's and columns beyond the last row's end are out of the buffer's range and become zeros.
+  // A copy is four rows of dy (256 bytes) or two of x (512); the slot of a row's 16-byte piece is XOR-ed by 4 (row % 4), so that
+  // the four rows that a transposing read touches lie in different quarters of the banks.  Rows beyond the expert's and columns
+  // beyond the last row's end are out of the buffer's range and become zeros.
   const int ld_a = (int)a.ld_dy * 2, ld_b = (int)a.ld_x * 2;
-  const int krow = lane >> 5, piece = (lane & 31) ^ (4 * (2 * (wave & 1) + krow));
-  const unsigned char *pa = static_cast<const unsigned char *>(a.dy) + (int64_t)first * ld_a + m0 * 2;
-  const unsigned char *pb = static_cast<const unsigned char *>(a.x) + (int64_t)first * ld_b + n0 * 2;
+  const int row_a = lane >> 4, piece_a = (lane & 15) ^ (4 * row_a);
+  const int row_b = lane >> 5, piece_b = (lane & 31) ^ (4 * (2 * (wave & 1) + row_b));
+  const int at_a = (4 * wave + row_a) * ld_a + piece_a * 16, at_b = (2 * wave + row_b) * ld_b + piece_b * 16;
+  unsigned char *pa = static_cast<unsigned char *>(const_cast<void *>(a.dy)) + (int64_t)first * ld_a + m0 * 2;
+  unsigned char *pb = static_cast<unsigned char *>(const_cast<void *>(a.x)) + (int64_t)first * ld_b + n0 * 2;
   const int width_a = min(C::BM, a.N - m0) * 2, width_b = min(C::BN, a.K - n0) * 2;
-  auto issue = [&](int t, int stage) {
-    const int rows = min(C::KD, last - first - t * C::KD);
-    const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(pa) + (int64_t)t * C::KD * ld_a, 0,
-                                                      (rows - 1) * ld_a + width_a, 0x00020000);
-    const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(pb) + (int64_t)t * C::KD * ld_b, 0,
-                                                      (rows - 1) * ld_b + width_b, 0x00020000);
-    unsigned char *da = lds + stage * C::STAGE_BYTES + wave * 1024, *db = da + C::OPERAND_BYTES;
+  auto issue = [&](int k, int stage) {
+    const int rows = min(C::KD, last - first - k * C::KD);
+    const auto ra = __builtin_amdgcn_make_buffer_rsrc(pa + (int64_t)k * C::KD * ld_a, 0, (rows - 1) * ld_a + width_a, 0x00020000);
+    const auto rb = __builtin_amdgcn_make_buffer_rsrc(pb + (int64_t)k * C::KD * ld_b, 0, (rows - 1) * ld_b + width_b, 0x00020000);
+    unsigned char *da = lds + stage * C::STAGE_BYTES + wave * 1024, *db = da + C::A_BYTES;
 #pragma unroll
-    for (int i = 0; i < C::DMA; ++i) {
-      const int row = (i * C::WAVES + wave) * 2 + krow;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr_t)(da + i * C::WAVES * 1024), 16, row * ld_a + piece * 16, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr_t)(db + i * C::WAVES * 1024), 16, row * ld_b + piece * 16, 0, 0, 0);
-    }
+    for (int i = 0; i < C::DMA_A; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr_t)(da + i * C::WAVES * 1024), 16, at_a + i * 4 * C::WAVES * ld_a, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < C::DMA_B; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr_t)(db + i * C::WAVES * 1024), 16, at_b + i * 2 * C::WAVES * ld_b, 0, 0, 0);
     asm volatile("" ::: "memory");
   };
 #pragma unroll
   for (int p = 0; p < C::STAGES - 1; ++p)
     if (p < nk) issue(p, p);
 
-  f32x16_v acc[4][4];
+  f32x16_v acc[C::TM][C::TN];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < C::TN; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
-  uint32_t a_rel[4], b_rel[4];
+  uint32_t a_rel[C::TM], b_rel[C::TN];
   {
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
     const int j = lane & 15, h = (lane >> 4) & 1, g = lane >> 5;
-    const uint32_t at = lds_base + (uint32_t)(8 * g + (j >> 2)) * C::ROW + 32u * h + 8u * (j & 3);
+    const uint32_t row = (uint32_t)(8 * g + (j >> 2)), in = 32u * h + 8u * (j & 3);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      a_rel[i] = at + (uint32_t)(((wm * 4 + i) ^ (j >> 2)) << 6);
-      b_rel[i] = at + C::OPERAND_BYTES + (uint32_t)(((wn * 4 + i) ^ (j >> 2)) << 6);
-    }
+    for (int i = 0; i < C::TM; ++i) a_rel[i] = lds_base + row * C::ROW_A + in + (uint32_t)(((wm * C::TM + i) ^ (j >> 2)) << 6);
+#pragma unroll
+    for (int i = 0; i < C::TN; ++i) b_rel[i] = lds_base + C::A_BYTES + row * C::ROW_B + in + (uint32_t)(((wn * C::TN + i) ^ (j >> 2)) << 6);
   }
-  WideFrag f[2];
-  auto fetch = [&](WideFrag &to, uint32_t so) {
-    uint32_t at_a[4], at_b[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) at_a[i] = a_rel[i] + so, at_b[i] = b_rel[i] + so;
-    to.fetch(at_a, at_b);
-  };
   if (nk > 0) {
-    wait_stages<2 * C::DMA, C::STAGES - 2>(nk - 1);
+    WideFrag f[2];
+    wait_stages<C::DMA_ALL, C::STAGES - 2>(nk - 1);
     block_barrier();
-    fetch(f[0], 0);
+    f[0].fetch(a_rel, b_rel, 0, 0);
     f[0].wait();
     int stage = 0, fill = C::STAGES - 1;
-    for (int t = 0; t < nk; ++t) {
+    for (int k = 0; k < nk; ++k) {
       const int next = stage + 1 == C::STAGES ? 0 : stage + 1;
-      fetch(f[1], (uint32_t)stage * C::STAGE_BYTES + 16u * C::ROW);
+      const uint32_t so = (uint32_t)stage * C::STAGE_BYTES, sn = (uint32_t)next * C::STAGE_BYTES;
+      if (k + C::STAGES - 1 < nk) issue(k + C::STAGES - 1, fill);   // everybody has read what was there: the barrier of k - 1
+      f[1].fetch(a_rel, b_rel, so + 16u * C::ROW_A, so + 16u * C::ROW_B);
       f[0].mma(acc);
       f[1].wait();
-      if (t + 1 < nk) {
-        wait_stages<2 * C::DMA, C::STAGES - 3>(nk - 2 - t);   // this wave's share of stage t + 1 has landed
-        block_barrier();                                      // everybody's has, and everybody has read stages t - 1 and t
-        if (t + C::STAGES - 1 < nk) issue(t + C::STAGES - 1, fill);
-        fetch(f[0], (uint32_t)next * C::STAGE_BYTES);
+      if (k + 1 < nk) {
+        wait_stages<C::DMA_ALL, C::STAGES - 2>(nk - 2 - k);   // this wave's share of stage k + 1 has landed
+        block_barrier();                                      // everybody's has, and everybody has read stage k
+        f[0].fetch(a_rel, b_rel, sn, sn);
       }
       f[1].mma(acc);
-      if (t + 1 < nk) f[0].wait();
+      if (k + 1 < nk) f[0].wait();
       stage = next;
       fill = fill + 1 == C::STAGES ? 0 : fill + 1;
     }
   }
-  float *dst = a.dw + (int64_t)e * a.N * a.K;
+  float *dst = t.dst;
   const int c = lane & 31, g = lane >> 5;
+  const int mw = m0 + wm * 32 * C::TM + 4 * g, nw = n0 + wn * 32 * C::TN + c;
+  const bool whole = m0 + C::BM <= a.N && n0 + C::BN <= a.K;   // no test for every store
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + (wn * 4 + j) * 32 + c;
+    for (int j = 0; j < C::TN; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) {
-        const int m = m0 + (wm * 4 + i) * 32 + 8 * (q / 4) + 4 * g + (q % 4);
-        if (m < a.N && n < a.K) __builtin_nontemporal_store(acc[i][j][q], dst + (int64_t)m * a.K + n);
+        const int m = mw + i * 32 + 8 * (q / 4) + q % 4, n = nw + j * 32;
+        if (whole || (m < a.N && n < a.K)) __builtin_nontemporal_store(acc[i][j][q], dst + (int64_t)m * a.K + n);
       }
-    }
 }
 
-__global__ void __launch_bounds__(WideTile::THREADS, 1) k_expert_wgrad_wide(WgradArgs a) {
+__global__ void __launch_bounds__(WideTile::THREADS, 2) k_expert_wgrad_wide(WgradArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[WideTile::STAGES * WideTile::STAGE_BYTES];
   wgrad_wide(a, lds);
 }
 
-template <typename C> hipError_t launch(const WgradArgs &a, hipStream_t s) {
-  const int64_t tiles = (int64_t)a.experts * ((a.N + C::BM - 1) / C::BM) * ((a.K + C::BN - 1) / C::BN);
-  hipLaunchKernelGGL(k_expert_wgrad<C>, dim3((unsigned)tiles), dim3(C::THREADS), 0, s, a);
+// Tiles of a gradient: fp32 64 x 64, bf16 128 x 256, or 128 x 128 where half of those 256 would be empty
+struct WgradShape {
+  int bm, bn;
+};
+WgradShape wgrad_shape(int dtype, int K) { return dtype == GEAR_F32 ? WgradShape{64, 64} : K <= 128 ? WgradShape{128, 128} : WgradShape{128, 256}; }
+int64_t wgrad_tiles(const WgradShape &t, int N, int K) { return (int64_t)((N + t.bm - 1) / t.bm) * ((K + t.bn - 1) / t.bn); }
+
+// Rows of a piece.  Two workgroups fit on each CU: 512 at a time.  Where all experts' tiles are fewer than two rounds of that, rows are
+// cut so that one layer gives one whole round, and experts, whose sizes the host does not know, pieces of one and a half
+// fair shares.  us, uncut / cut: 65536 x 1024 x 1152 by one expert 832 / 191, 16384 x 1024 x 1152 by 8 93 / 71.
+int wgrad_cut(int dtype, int64_t rows, int experts, int N, int K) {
+  constexpr int64_t kSlots = 512, kLeast = 512;
+  const int64_t tiles = wgrad_tiles(wgrad_shape(dtype, K), N, K), whole = rows < 1 ? 1 : rows;
+  if (experts * tiles >= 2 * kSlots) return (int)whole;
+  int64_t cut = experts == 1 ? (rows + kSlots / tiles - 1) / (kSlots / tiles > 0 ? kSlots / tiles : 1) : rows * tiles * 3 / (2 * kSlots);
+  cut = (cut + 31) / 32 * 32;
+  if (cut < kLeast) cut = kLeast;
+  return (int)(cut < whole ? cut : whole);
+}
+int64_t wgrad_partials(int64_t rows, int experts, int cut) {   // pieces of experts that are cut, at most
+  const int64_t pieces = (rows + cut - 1) / cut;
+  return pieces <= 1 ? 0 : experts == 1 ? pieces : 2 * (rows / cut);
+}
+
+template <typename C> hipError_t launch(const WgradArgs &a, unsigned blocks, hipStream_t s) {
+  hipLaunchKernelGGL(k_expert_wgrad<C>, dim3(blocks), dim3(C::THREADS), 0, s, a);
   return hipGetLastError();
 }
 
 bool wgrad_ok(int dtype, int64_t rows, int experts, int N, int K) {
   return (dtype == GEAR_F32 || dtype == GEAR_BF16) && rows >= 0 && rows <= (1 << 30) && experts >= 1 && experts <= GEAR_MAX_EXPERTS &&
          N >= 8 && N % 8 == 0 && K >= 8 && K % 8 == 0 && N < (1 << 20) && K < (1 << 20) &&
-         (int64_t)experts * ((N + 63) / 64) * ((K + 63) / 64) <= (1 << 23);   // tiles are counted in 32 bits
+         (int64_t)experts * ((N + 63) / 64) * ((K + 63) / 64) <= (1 << 23);   // tiles are counted in 32 bits (cut only below 1024)
 }
 
 }  // namespace
@@ -267,7 +378,9 @@ bool wgrad_ok(int dtype, int64_t rows, int experts, int N, int K) {
 using namespace gear;
 
 extern "C" size_t gear_expert_wgrad_workspace_bytes(int32_t dtype, int64_t rows, int32_t experts, int32_t N, int32_t K) {
-  return wgrad_ok(dtype, rows, experts, N, K) ? 256 : 0;
+  if (!wgrad_ok(dtype, rows, experts, N, K)) return 0;
+  const size_t bytes = (size_t)wgrad_partials(rows, experts, wgrad_cut(dtype, rows, experts, N, K)) * N * K * sizeof(float);
+  return bytes < 256 ? 256 : (bytes + 255) & ~(size_t)255;
 }
 
 extern "C" gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *workspace, size_t workspace_bytes, void *stream) {
@@ -280,13 +393,25 @@ extern "C" gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *
   }
   if (!workspace || ((uintptr_t)workspace & 255)) return GEAR_ERR_INVALID;
   if (workspace_bytes < gear_expert_wgrad_workspace_bytes(a->dtype, a->rows, a->experts, a->N, a->K)) return GEAR_ERR_CAPACITY;
-  const WgradArgs w = {a->dy, a->x, a->off, a->dw, a->ld_dy, a->ld_x, (int)a->rows, a->K, a->N, a->experts, a->status};
+  const int cut = wgrad_cut(a->dtype, a->rows, a->experts, a->N, a->K);
+  const WgradShape shape = wgrad_shape(a->dtype, a->K);
+  const WgradArgs w = {a->dy, a->x, a->off, a->dw, a->ld_dy, a->ld_x, (int)a->rows, a->K, a->N, a->experts, a->status,
+                       static_cast<float *>(workspace), cut};
   hipStream_t s = (hipStream_t)stream;
-  if (a->dtype == GEAR_BF16 && (int64_t)a->experts * ((a->N + 255) / 256) * ((a->K + 255) / 256) >= 128) {
-    const int64_t tiles = (int64_t)a->experts * ((a->N + 255) / 256) * ((a->K + 255) / 256);
-    hipLaunchKernelGGL(k_expert_wgrad_wide, dim3((unsigned)tiles), dim3(WideTile::THREADS), 0, s, w);
-    return hipGetLastError() == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
+  const int64_t pieces = a->off ? a->experts + a->rows / cut : (a->rows + cut - 1) / cut;
+  const unsigned blocks = wgrad_blocks((pieces > 0 ? pieces : 1) * wgrad_tiles(shape, a->N, a->K));
+  if (a->dtype == GEAR_F32) {
+    if (launch<TnTile<float, 1, 1, 4>>(w, blocks, s) != hipSuccess) return GEAR_ERR_HIP;
+  } else if (shape.bn == 128) {
+    if (launch<TnTile<bf16_t, 2, 2, 3>>(w, blocks, s) != hipSuccess) return GEAR_ERR_HIP;
+  } else {
+    hipLaunchKernelGGL(k_expert_wgrad_wide, dim3(blocks), dim3(WideTile::THREADS), 0, s, w);
+    if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
   }
-  const hipError_t err = a->dtype == GEAR_BF16 ? launch<TnTile<bf16_t, 2, 2, 3>>(w, s) : launch<TnTile<float, 1, 1, 4>>(w, s);
-  return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
+  if (wgrad_partials(a->rows, a->experts, cut) > 0) {
+    const int64_t vec = (int64_t)a->N * a->K / 4, want = (vec + 255) / 256;
+    hipLaunchKernelGGL(k_wgrad_sum, dim3((unsigned)(want < 4096 ? want : 4096), (unsigned)a->experts), dim3(256), 0, s, w);
+    if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
+  }
+  return GEAR_OK;
 }
