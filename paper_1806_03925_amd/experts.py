@@ -8,29 +8,39 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
-from .binding import (GEAR_BF16, GEAR_E4M3, GEAR_ERR_INVALID, GEAR_F32, GearError, _check, _ptr, _stream, gear_expert_args,
+from .binding import (GEAR_BF16, GEAR_E4M3, GEAR_ERR_INVALID, GEAR_F32, GearError, _check, _ptr, gear_expert_args,
                       gear_expert_wgrad_args, gear_grad_tensor, gear_norm_args, gear_norm_backward_args, lib)
 
 _CODE = {torch.float32: GEAR_F32, torch.bfloat16: GEAR_BF16}
 _BYTE = (torch.uint8, torch.float8_e4m3fn)
+_raw_stream = torch._C._cuda_getCurrentRawStream   # of current_stream(), without the object around it: these calls are short
+
+
+def _refuse(where: str, what: str) -> None:
+    raise GearError(GEAR_ERR_INVALID, f"{where}: {what}")
 
 
 def _need(ok: bool, where: str, what: str) -> None:
     if not ok:
-        raise GearError(GEAR_ERR_INVALID, f"{where}: {what}")
+        _refuse(where, what)
 
 
 def _matrix(t: torch.Tensor, where: str, name: str, dtype: Optional[torch.dtype] = None, shape=None) -> int:
     """Checks a matrix on the device and returns the distance between its rows."""
-    _need(t.is_cuda and t.dim() == 2 and (t.dtype == dtype if dtype is not None else t.dtype in _CODE), where,
-          f"{name} has to be a matrix on the GPU of {dtype or 'float32 or bfloat16'}")
-    _need(shape is None or tuple(t.shape) == tuple(shape), where, f"{name} has to be {shape}, not {tuple(t.shape)}")
-    _need(t.shape[1] <= 1 or t.stride(1) == 1, where, f"{name}'s columns have to lie next to each other")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    size = t.shape
+    if not t.is_cuda or len(size) != 2 or (t.dtype is not dtype if dtype is not None else t.dtype not in _CODE):
+        _refuse(where, f"{name} has to be a matrix on the GPU of {dtype or 'float32 or bfloat16'}")
+    if shape is not None and size != shape:
+        _refuse(where, f"{name} has to be {tuple(shape)}, not {tuple(size)}")
+    apart = t.stride()
+    if apart[1] != 1 and size[1] > 1:
+        _refuse(where, f"{name}'s columns have to lie next to each other")
+    return apart[0] if size[0] > 1 else size[1]
 
 
 def _vector(t: torch.Tensor, where: str, name: str, dtype: torch.dtype, n: int) -> None:
-    _need(t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.numel() == n, where, f"{name} has to be {n} contiguous {dtype} on the GPU")
+    if not t.is_cuda or t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(where, f"{name} has to be {n} contiguous {dtype} on the GPU")
 
 
 class Rows8(NamedTuple):
@@ -45,12 +55,11 @@ class Rows8(NamedTuple):
                      torch.empty((rows, (dim + 511) // 512 * 4), dtype=torch.uint8, device=device), dim)
 
     def check(self, where: str) -> None:
-        rows = self.q.shape[0]
-        _need(self.q.is_cuda and self.q.dtype in _BYTE and self.q.is_contiguous() and self.q.shape == (rows, lib.gear_rows8_ld(self.dim)),
-              where, "q has to be [rows x gear_rows8_ld(dim)] contiguous bytes on the GPU")
-        _need(self.scale.is_cuda and self.scale.dtype == torch.uint8 and self.scale.is_contiguous() and
-              self.scale.shape == (rows, lib.gear_scales8_ld(self.dim)), where,
-              "scale has to be [rows x gear_scales8_ld(dim)] contiguous bytes on the GPU")
+        q, scale, rows = self.q, self.scale, self.q.shape[0]
+        if not q.is_cuda or q.dtype not in _BYTE or q.shape != (rows, (self.dim + 127) // 128 * 128) or not q.is_contiguous():
+            _refuse(where, "q has to be [rows x gear_rows8_ld(dim)] contiguous bytes on the GPU")
+        if not scale.is_cuda or scale.dtype is not torch.uint8 or scale.shape != (rows, (self.dim + 511) // 512 * 4) or not scale.is_contiguous():
+            _refuse(where, "scale has to be [rows x gear_scales8_ld(dim)] contiguous bytes on the GPU")
 
 
 class NormOutput(NamedTuple):
@@ -65,27 +74,39 @@ def gear_rmsnorm(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Opti
     out: memory for the results (any of its fields may be None) instead of new tensors; sum may be residual or x itself."""
     where = "gear_rmsnorm"
     ld_x = _matrix(x, where, "x")
-    rows, dim = x.shape
+    dtype, device, shape = x.dtype, x.device, x.shape
+    rows, dim = shape
     _vector(gain, where, "gain", torch.float32, dim)
+    o_sum, o_y, r8 = out if out is not None else (None, None, None)
+    p_res = p_sum = p_y = p_q = p_scale = None
     ld_r = ld_s = ld_y = 0
-    given = out or NormOutput(None, None, None)
-    o_sum = o_y = r8 = None
     if residual is not None:
-        ld_r = _matrix(residual, where, "residual", x.dtype, x.shape)
-    if residual is not None or given.sum is not None:
-        o_sum = given.sum if given.sum is not None else torch.empty((rows, dim), dtype=x.dtype, device=x.device)
-        ld_s = _matrix(o_sum, where, "sum", x.dtype, x.shape)
-    if y:
-        o_y = given.y if given.y is not None else torch.empty((rows, dim), dtype=x.dtype, device=x.device)
-        ld_y = _matrix(o_y, where, "y", x.dtype, x.shape)
-    if q8:
-        r8 = given.rows8 if given.rows8 is not None else Rows8.empty(rows, dim, x.device)
-        if given.rows8 is not None:
+        ld_r, p_res = _matrix(residual, where, "residual", dtype, shape), residual.data_ptr()
+    if o_sum is not None:
+        ld_s, p_sum = _matrix(o_sum, where, "sum", dtype, shape), o_sum.data_ptr()
+    elif residual is not None:
+        o_sum = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
+        ld_s, p_sum = dim, o_sum.data_ptr()
+    if not y:
+        o_y = None
+    elif o_y is not None:
+        ld_y, p_y = _matrix(o_y, where, "y", dtype, shape), o_y.data_ptr()
+    else:
+        o_y = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
+        ld_y, p_y = dim, o_y.data_ptr()
+    if not q8:
+        r8 = None
+    else:
+        if r8 is None:
+            r8 = Rows8.empty(rows, dim, device)
+        else:
             r8.check(where)
             _need(r8.dim == dim and r8.q.shape[0] == rows, where, "rows8 has another shape than x")
-    a = gear_norm_args(rows, dim, _CODE[x.dtype], eps, _ptr(x), _ptr(residual), _ptr(gain), _ptr(o_sum), _ptr(o_y), ld_x, ld_r, ld_s,
-                       ld_y, _ptr(r8.q) if r8 else None, _ptr(r8.scale) if r8 else None)
-    _check(lib.gear_rmsnorm(C.byref(a), _stream()), where)
+        p_q, p_scale = r8.q.data_ptr(), r8.scale.data_ptr()
+    a = gear_norm_args(rows, dim, _CODE[dtype], eps, x.data_ptr(), p_res, gain.data_ptr(), p_sum, p_y, ld_x, ld_r, ld_s, ld_y, p_q, p_scale)
+    code = lib.gear_rmsnorm(C.byref(a), _raw_stream(device.index))
+    if code:
+        _check(code, where)
     return NormOutput(o_sum, o_y, r8)
 
 
@@ -93,20 +114,26 @@ def gear_rmsnorm_backward(h: torch.Tensor, gain: torch.Tensor, dy: torch.Tensor,
                           dx: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dx, dgain) of the norm at h, dsum (what flows into the sum itself) added to dx; dx may be dy or dsum."""
     where = "gear_rmsnorm_backward"
-    ld_h, ld_dy = _matrix(h, where, "h"), _matrix(dy, where, "dy", h.dtype, h.shape)
-    rows, dim = h.shape
+    dtype, device, shape = h.dtype, h.device, h.shape
+    ld_h, ld_dy = _matrix(h, where, "h"), _matrix(dy, where, "dy", dtype, shape)
+    rows, dim = shape
     _vector(gain, where, "gain", torch.float32, dim)
-    ld_ds = _matrix(dsum, where, "dsum", h.dtype, h.shape) if dsum is not None else 0
+    ld_ds = _matrix(dsum, where, "dsum", dtype, shape) if dsum is not None else 0
     if dx is None:
-        dx = torch.empty((rows, dim), dtype=h.dtype, device=h.device)
-    ld_dx = _matrix(dx, where, "dx", h.dtype, h.shape)
+        dx, ld_dx = torch.empty_like(h) if h.is_contiguous() else h.new_empty(shape), dim
+    else:
+        ld_dx = _matrix(dx, where, "dx", dtype, shape)
     if dgain is None:
-        dgain = torch.empty(dim, dtype=torch.float32, device=h.device)
-    _vector(dgain, where, "dgain", torch.float32, dim)
-    ws = torch.empty(lib.gear_norm_backward_workspace_bytes(rows, dim), dtype=torch.uint8, device=h.device)
-    a = gear_norm_backward_args(rows, dim, _CODE[h.dtype], eps, _ptr(h), _ptr(dy), _ptr(dsum), _ptr(gain), _ptr(dx), _ptr(dgain), ld_h,
-                                ld_dy, ld_ds, ld_dx)
-    _check(lib.gear_rmsnorm_backward(C.byref(a), _ptr(ws), ws.numel(), _stream()), where)
+        dgain = torch.empty_like(gain)
+    else:
+        _vector(dgain, where, "dgain", torch.float32, dim)
+    size = lib.gear_norm_backward_workspace_bytes(rows, dim)
+    ws = torch.empty(size, dtype=torch.uint8, device=device)
+    a = gear_norm_backward_args(rows, dim, _CODE[dtype], eps, h.data_ptr(), dy.data_ptr(), _ptr(dsum), gain.data_ptr(), dx.data_ptr(),
+                                dgain.data_ptr(), ld_h, ld_dy, ld_ds, ld_dx)
+    code = lib.gear_rmsnorm_backward(C.byref(a), ws.data_ptr(), size, _raw_stream(device.index))
+    if code:
+        _check(code, where)
     return dx, dgain
 
 
@@ -119,29 +146,24 @@ def gear_rows8(x: torch.Tensor, out: Optional[Rows8] = None) -> Rows8:
         out = Rows8.empty(rows, dim, x.device)
     out.check(where)
     _need(out.dim == dim and out.q.shape[0] == rows, where, "out has another shape than x")
-    _check(lib.gear_rows8(_ptr(x), _CODE[x.dtype], ld, rows, dim, _ptr(out.q), _ptr(out.scale), _stream()), where)
+    _check(lib.gear_rows8(_ptr(x), _CODE[x.dtype], ld, rows, dim, _ptr(out.q), _ptr(out.scale), _raw_stream(x.device.index)), where)
     return out
 
 
 def _weights(w: torch.Tensor, where: str) -> Tuple[int, int, int]:
-    _need(w.is_cuda and w.dim() in (2, 3) and w.dtype in _CODE and w.is_contiguous(), where,
-          "w has to be contiguous [experts x N x K] or [N x K] on the GPU, float32 or bfloat16")
-    return (1, *w.shape) if w.dim() == 2 else tuple(w.shape)
-
-
-def _packed_room(operand: int, experts: int, n: int, k: int, transposed: bool, device, where: str) -> torch.Tensor:
-    size = lib.gear_packed_weights_bytes(operand, experts, n, k, int(transposed))
-    _need(size > 0, where, f"weights of {experts} x {n} x {k} have no packed form")
-    return torch.empty(size, dtype=torch.uint8, device=device)
+    if not w.is_cuda or w.dim() not in (2, 3) or w.dtype not in _CODE or not w.is_contiguous():
+        _refuse(where, "w has to be contiguous [experts x N x K] or [N x K] on the GPU, float32 or bfloat16")
+    return (1, *w.shape) if len(w.shape) == 2 else tuple(w.shape)
 
 
 class Weights8(NamedTuple):
-    """Weights in 8 bits, laid out for gear_matmul8."""
+    """Weights in 8 bits, laid out for gear_matmul8; status is where its calls report unless they are given a word of their own."""
     packed: torch.Tensor
     scale: torch.Tensor
     experts: int
     N: int
     K: int
+    status: torch.Tensor
 
 
 def gear_weights8(w: torch.Tensor) -> Weights8:
@@ -150,48 +172,71 @@ def gear_weights8(w: torch.Tensor) -> Weights8:
     size = lib.gear_weight_scales_bytes(experts, n, k)
     _need(size > 0, "gear_weights8", f"weights of {experts} x {n} x {k} have no packed form")
     scale = torch.empty(size, dtype=torch.uint8, device=w.device)
-    packed = _packed_room(GEAR_E4M3, experts, n, k, False, w.device, "gear_weights8")
-    _check(lib.gear_pack_weights(_ptr(w), _CODE[w.dtype], GEAR_E4M3, experts, n, k, _ptr(packed), None, _ptr(scale), _stream()), "gear_weights8")
-    return Weights8(packed, scale, experts, n, k)
+    packed = torch.empty(lib.gear_packed_weights_bytes(GEAR_E4M3, experts, n, k, 0), dtype=torch.uint8, device=w.device)
+    _check(lib.gear_pack_weights(_ptr(w), _CODE[w.dtype], GEAR_E4M3, experts, n, k, _ptr(packed), None, _ptr(scale),
+                                 _raw_stream(w.device.index)), "gear_weights8")
+    return Weights8(packed, scale, experts, n, k, torch.zeros(1, dtype=torch.int32, device=w.device))
 
 
 class ExpertWeights:
     """Weights of every expert laid out for the forward product and (transposed) for the gradient of its input, in float32
-    or bfloat16 (`operand`, w's own type if not given).  A training program calls update() when the weights have changed."""
+    or bfloat16 (`operand`, w's own type if not given).  A training program calls update() when the weights have changed.
+    status is where the products report unless they are given a word of their own."""
 
     def __init__(self, w: torch.Tensor, operand: Optional[torch.dtype] = None, backward: bool = True):
-        self.experts, self.N, self.K = _weights(w, "ExpertWeights")
+        where = "ExpertWeights"
+        self.experts, self.N, self.K = shape = _weights(w, where)
         self.dtype = operand or w.dtype
-        _need(self.dtype in _CODE, "ExpertWeights", "operand has to be float32 or bfloat16")
-        self.forward = _packed_room(_CODE[self.dtype], self.experts, self.N, self.K, False, w.device, "ExpertWeights")
-        self.transposed = _packed_room(_CODE[self.dtype], self.experts, self.N, self.K, True, w.device, "ExpertWeights") if backward else None
-        self.update(w)
+        if self.dtype not in _CODE:
+            _refuse(where, "operand has to be float32 or bfloat16")
+        self.code = _CODE[self.dtype]
+        forward = lib.gear_packed_weights_bytes(self.code, *shape, 0)
+        size = forward + (lib.gear_packed_weights_bytes(self.code, *shape, 1) if backward else 0)
+        if forward == 0:
+            _refuse(where, f"weights of {shape} have no packed form")
+        size = (size + 15) // 16 * 16
+        self.packed = torch.empty(size + 16, dtype=torch.uint8, device=w.device)
+        self.status = self.packed[size:size + 4].view(torch.int32)
+        self.forward = self.packed.data_ptr()
+        self.transposed = self.forward + forward if backward else None
+        self._lay_out(w)
+
+    def _lay_out(self, w: torch.Tensor) -> None:
+        code = lib.gear_pack_weights(w.data_ptr(), _CODE[w.dtype], self.code, self.experts, self.N, self.K, self.forward, self.transposed, None,
+                                     _raw_stream(w.device.index))
+        if code:
+            _check(code, "ExpertWeights")
 
     def update(self, w: torch.Tensor) -> None:
-        e, n, k = _weights(w, "ExpertWeights.update")
-        _need((e, n, k) == (self.experts, self.N, self.K), "ExpertWeights.update", "w has another shape than before")
-        _check(lib.gear_pack_weights(_ptr(w), _CODE[w.dtype], _CODE[self.dtype], e, n, k, _ptr(self.forward), _ptr(self.transposed), None,
-                                     _stream()), "ExpertWeights.update")
+        if _weights(w, "ExpertWeights.update") != (self.experts, self.N, self.K):
+            _refuse("ExpertWeights.update", "w has another shape than before")
+        self._lay_out(w)
 
 
-def _offsets(off: Optional[torch.Tensor], experts: int, status: Optional[torch.Tensor], device, where: str):
+def _offsets(off: Optional[torch.Tensor], experts: int, status: Optional[torch.Tensor], where: str):
     if off is None:
-        _need(experts == 1, where, "off may only be left out where there is one expert")
+        if experts != 1:
+            _refuse(where, "off may only be left out where there is one expert")
         return status
     _vector(off, where, "off", torch.int32, experts + 1)
     if status is None:
-        status = torch.empty(1, dtype=torch.int32, device=device)
+        return torch.empty(1, dtype=torch.int32, device=off.device)
+    _vector(status, where, "status", torch.int32, 1)
     return status
 
 
 def _product(where, dtype, x, x_scale, ld_x, packed, w_scale, rows, n, k, experts, off, out, out_dtype, status) -> torch.Tensor:
-    status = _offsets(off, experts, status, x.device, where)
+    device = x.device
+    status = _offsets(off, experts, status, where)
     if out is None:
-        out = torch.empty((rows, n), dtype=out_dtype, device=x.device)
-    ld_out = _matrix(out, where, "out", None, (rows, n))
-    a = gear_expert_args(dtype, _CODE[out.dtype], rows, k, n, experts, _ptr(x), _ptr(x_scale), _ptr(packed), _ptr(w_scale), _ptr(off),
-                         _ptr(out), ld_x, ld_out, _ptr(status))
-    _check(lib.gear_expert_product(C.byref(a), _stream()), where)
+        out, ld_out = torch.empty((rows, n), dtype=out_dtype, device=device) if out_dtype is not x.dtype else x.new_empty((rows, n)), n
+    else:
+        ld_out = _matrix(out, where, "out", None, (rows, n))
+    a = gear_expert_args(dtype, _CODE[out.dtype], rows, k, n, experts, x.data_ptr(), x_scale, packed, w_scale, _ptr(off),
+                         out.data_ptr(), ld_x, ld_out, _ptr(status))
+    code = lib.gear_expert_product(C.byref(a), _raw_stream(device.index))
+    if code:
+        _check(code, where)
     return out
 
 
@@ -201,9 +246,11 @@ def gear_matmul8(rows8: Rows8, weights: Weights8, off: Optional[torch.Tensor] = 
     from off[experts] on are not written.  status [1] (int32): GEAR_ERR_RANGE if off is no such list, and nothing is written."""
     where = "gear_matmul8"
     rows8.check(where)
-    _need(rows8.dim == weights.K, where, f"rows of {rows8.dim} for weights of {weights.K}")
-    return _product(where, GEAR_E4M3, rows8.q, rows8.scale, rows8.q.shape[1], weights.packed, weights.scale, rows8.q.shape[0], weights.N,
-                    weights.K, weights.experts, off, out, out_dtype, status)
+    if rows8.dim != weights.K:
+        _refuse(where, f"rows of {rows8.dim} for weights of {weights.K}")
+    rows, ld = rows8.q.shape
+    return _product(where, GEAR_E4M3, rows8.q, rows8.scale.data_ptr(), ld, weights.packed.data_ptr(), weights.scale.data_ptr(), rows, weights.N, weights.K,
+                    weights.experts, off, out, out_dtype, weights.status if status is None else status)
 
 
 def gear_expert_matmul(x: torch.Tensor, weights: ExpertWeights, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -212,7 +259,7 @@ def gear_expert_matmul(x: torch.Tensor, weights: ExpertWeights, off: Optional[to
     where = "gear_expert_matmul"
     ld = _matrix(x, where, "x", weights.dtype, (x.shape[0], weights.K))
     return _product(where, _CODE[x.dtype], x, None, ld, weights.forward, None, x.shape[0], weights.N, weights.K, weights.experts, off, out,
-                    out_dtype or x.dtype, status)
+                    out_dtype or x.dtype, weights.status if status is None else status)
 
 
 def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -220,9 +267,10 @@ def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[to
     """dy [rows x N] times the weights of each row's expert: the gradient [rows x K] of gear_expert_matmul's x."""
     where = "gear_expert_dgrad"
     ld = _matrix(dy, where, "dy", weights.dtype, (dy.shape[0], weights.N))
-    _need(weights.transposed is not None, where, "the weights were laid out without backward")
+    if weights.transposed is None:
+        _refuse(where, "the weights were laid out without backward")
     return _product(where, _CODE[dy.dtype], dy, None, ld, weights.transposed, None, dy.shape[0], weights.K, weights.N, weights.experts, off,
-                    out, out_dtype or dy.dtype, status)
+                    out, out_dtype or dy.dtype, weights.status if status is None else status)
 
 
 def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
@@ -230,17 +278,23 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     """dy_e^T x_e for every expert: [experts x N x K] float32, zeros for one without rows."""
     where = "gear_expert_wgrad"
     ld_x = _matrix(x, where, "x")
+    device = x.device
     rows, k = x.shape
     n = dy.shape[-1]
     ld_dy = _matrix(dy, where, "dy", x.dtype, (rows, n))
     experts = 1 if off is None else off.numel() - 1
-    status = _offsets(off, experts, status, x.device, where)
+    status = _offsets(off, experts, status, where)
     if dw is None:
-        dw = torch.empty((experts, n, k), dtype=torch.float32, device=x.device)
-    _vector(dw, where, "dw", torch.float32, experts * n * k)
-    ws = torch.empty(lib.gear_expert_wgrad_workspace_bytes(_CODE[x.dtype], rows, experts, n, k), dtype=torch.uint8, device=x.device)
-    a = gear_expert_wgrad_args(_CODE[x.dtype], rows, k, n, experts, _ptr(dy), _ptr(x), _ptr(off), _ptr(dw), ld_dy, ld_x, _ptr(status))
-    _check(lib.gear_expert_wgrad(C.byref(a), _ptr(ws), ws.numel(), _stream()), where)
+        dw = torch.empty((experts, n, k), dtype=torch.float32, device=device)
+    else:
+        _vector(dw, where, "dw", torch.float32, experts * n * k)
+    dtype = _CODE[x.dtype]
+    size = lib.gear_expert_wgrad_workspace_bytes(dtype, rows, experts, n, k)
+    ws = torch.empty(size, dtype=torch.uint8, device=device)
+    a = gear_expert_wgrad_args(dtype, rows, k, n, experts, dy.data_ptr(), x.data_ptr(), _ptr(off), dw.data_ptr(), ld_dy, ld_x, _ptr(status))
+    code = lib.gear_expert_wgrad(C.byref(a), ws.data_ptr(), size, _raw_stream(device.index))
+    if code:
+        _check(code, where)
     return dw
 
 
@@ -265,21 +319,27 @@ class GradList:
         self.chunks = chunks.value
         self.list = host.to(self.grads[0].device)
         self.workspace = torch.empty(lib.gear_grad_workspace_bytes(self.chunks), dtype=torch.uint8, device=self.list.device)
+        self.plan = (self.list.data_ptr(), len(self.grads), self.chunks), (self.workspace.data_ptr(), self.workspace.numel())
+
+
+def _norm_word(norm: Optional[torch.Tensor], grads: GradList, where: str) -> torch.Tensor:
+    if norm is None:
+        return torch.empty((), dtype=torch.float32, device=grads.list.device)
+    _vector(norm, where, "norm", torch.float32, 1)
+    return norm
 
 
 def gear_grad_norm(grads: GradList, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The norm [1] of all gradients of the list together."""
-    norm = torch.empty((), dtype=torch.float32, device=grads.list.device) if norm is None else norm
-    _vector(norm, "gear_grad_norm", "norm", torch.float32, 1)
-    _check(lib.gear_grad_norm(_ptr(grads.list), len(grads.grads), grads.chunks, _ptr(grads.workspace), grads.workspace.numel(), _ptr(norm),
-                              _stream()), "gear_grad_norm")
+    norm = _norm_word(norm, grads, "gear_grad_norm")
+    what, room = grads.plan
+    _check(lib.gear_grad_norm(*what, *room, norm.data_ptr(), _raw_stream(norm.device.index)), "gear_grad_norm")
     return norm
 
 
 def gear_clip_grads(grads: GradList, max_norm: float, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scales the gradients of the list so that their norm is at most max_norm; returns the norm [1] that they had."""
-    norm = torch.empty((), dtype=torch.float32, device=grads.list.device) if norm is None else norm
-    _vector(norm, "gear_clip_grads", "norm", torch.float32, 1)
-    _check(lib.gear_clip_grads(_ptr(grads.list), len(grads.grads), grads.chunks, max_norm, _ptr(grads.workspace), grads.workspace.numel(),
-                               _ptr(norm), _stream()), "gear_clip_grads")
+    norm = _norm_word(norm, grads, "gear_clip_grads")
+    what, room = grads.plan
+    _check(lib.gear_clip_grads(*what, max_norm, *room, norm.data_ptr(), _raw_stream(norm.device.index)), "gear_clip_grads")
     return norm
