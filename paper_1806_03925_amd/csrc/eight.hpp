@@ -32,6 +32,39 @@ __device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8]) {
       make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
+// the same past the L2, for results that are larger than it and not read again soon
+__device__ __forceinline__ void stream8(float *p, const float (&v)[8]) {
+  typedef float f32x4_t __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(f32x4_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_t *>(p));
+  __builtin_nontemporal_store(f32x4_t{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_t *>(p) + 1);
+}
+__device__ __forceinline__ void stream8(bf16_t *p, const float (&v)[8]) {
+  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(u32x4_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])},
+                              reinterpret_cast<u32x4_t *>(p));
+}
+
+// eight values as they lie in memory: requested early, unpacked when they are needed
+template <typename T> struct Raw8;
+template <> struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float *p) { a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4); }
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
+};
+template <> struct Raw8<bf16_t> {
+  uint4 a;
+  __device__ __forceinline__ void load(const bf16_t *p) { a = *reinterpret_cast<const uint4 *>(p); }
+  __device__ __forceinline__ void zero() { a = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+};
+
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 
 // the largest |v| of eight, those not finite left out

@@ -5,7 +5,8 @@
 //
 // (dx: y_c depends on h_c directly, s a, and on all of h through s, whose derivative by h_c is -s^3 h_c / dim.)
 // Every call is one pass over its rows: a row stays in the registers of the threads that read it, from the sum of its
-// squares to the last output, so what bounds these kernels is the memory they have to read and write.
+// squares to the last output, so what bounds these kernels is the memory they have to read and write.  10001 x 1152 bf16 with
+// residual into sum, y and 8 bits: 20.3 us, 5.1 TB/s (22.2 with results through the L2).
 #include "eight.hpp"
 
 #include <cmath>
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_arg
     for (int j = 0; j < 8; ++j) y[j] = h[i][j];
     if constexpr (NORM) {
       if (c < a.dim) {
-        if (a.sum) store8(static_cast<T *>(a.sum) + row * a.ld_sum + c, h[i]);
+        if (a.sum) stream8(static_cast<T *>(a.sum) + row * a.ld_sum + c, h[i]);
         float g[8];
         load8(a.gain + c, g);
 #pragma unroll
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_arg
       }
       unpack8(q, scale8(e), y);
     }
-    if (a.y && c < a.dim) store8(static_cast<T *>(a.y) + row * a.ld_y + c, y);
+    if (a.y && c < a.dim) stream8(static_cast<T *>(a.y) + row * a.ld_y + c, y);
   }
   if (a.q8 && t < lds - ld8 / kBlock8) a.scale[row * lds + ld8 / kBlock8 + t] = 0;   // behind the last block: not used
 }
@@ -92,28 +93,30 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm_backward(gear
     for (int j = 0; j < 8; ++j) dg[i][j] = 0.0f;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + sub; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
     const T *hp = static_cast<const T *>(a.h) + row * a.ld_h, *dyp = static_cast<const T *>(a.dy) + row * a.ld_dy;
-    float h[PER][8], d[PER][8];
+    Raw8<T> h[PER], d[PER], more[PER];   // all of them on their way before the first sum
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = 8 * (t + TPR * i);
+      h[i].zero(), d[i].zero(), more[i].zero();
+      if (c < a.dim) {
+        h[i].load(hp + c);
+        d[i].load(dyp + c);
+        if (a.dsum) more[i].load(static_cast<const T *>(a.dsum) + row * a.ld_dsum + c);
+      }
+    }
     float sq = 0.0f, dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = 8 * (t + TPR * i);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[i][j] = d[i][j] = 0.0f;
-      if (c < a.dim) {
-        load8(hp + c, h[i]);
-        load8(dyp + c, d[i]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = 8 * (t + TPR * i);
       if (c >= a.dim) continue;
-      float g[8];
+      float g[8], hv[8], dv[8];
       load8(a.gain + c, g);
+      h[i].get(hv);
+      d[i].get(dv);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        sq += h[i][j] * h[i][j];
-        dot += d[i][j] * g[j] * h[i][j];
+        sq += hv[j] * hv[j];
+        dot += dv[j] * g[j] * hv[j];
       }
     }
     sq = row_sum<TPR>(sq, s_part);
@@ -124,20 +127,17 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm_backward(gear
     for (int i = 0; i < PER; ++i) {
       const int c = 8 * (t + TPR * i);
       if (c >= a.dim) continue;
-      float g[8], dx[8];
+      float g[8], hv[8], dv[8], dx[8];
       load8(a.gain + c, g);
+      h[i].get(hv);
+      d[i].get(dv);
+      more[i].get(dx);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        dx[j] = s * d[i][j] * g[j] - h[i][j] * back;
-        dg[i][j] += d[i][j] * h[i][j] * s;
+        dx[j] = (s * dv[j] * g[j] - hv[j] * back) + dx[j];
+        dg[i][j] += dv[j] * hv[j] * s;
       }
-      if (a.dsum) {
-        float more[8];
-        load8(static_cast<const T *>(a.dsum) + row * a.ld_dsum + c, more);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dx[j] += more[j];
-      }
-      store8(static_cast<T *>(a.dx) + row * a.ld_dx + c, dx);
+      stream8(static_cast<T *>(a.dx) + row * a.ld_dx + c, dx);
     }
   }
   if (!partial) return;
@@ -163,18 +163,33 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm_backward(gear
   }
 }
 
-// out[c] = sum of partial[r][c], r < n: 16 columns a workgroup, 16 rows at a time, always in the same order
-__global__ void __launch_bounds__(256) k_sum_rows(const float *__restrict__ partial, int n, int dim, float *__restrict__ out) {
-  __shared__ float s[256];
-  const int c = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
-  float v = 0.0f;
-  if (c < dim)
-    for (int r = r0; r < n; r += 16) v += partial[(size_t)r * dim + c];
-  s[threadIdx.x] = v;
+// out[c] = sum of partial[r][c], r < n, always in the same order.  A workgroup takes 64 columns, 16 threads of four a row, 64
+// rows at a time: few workgroups, so each has to have many rows on their way.  us for 1024 rows of 1024: 4; by 16 x 16
+// threads with one column each 20.
+__global__ void __launch_bounds__(1024) k_sum_rows(const float *__restrict__ partial, int n, int dim, float *__restrict__ out) {
+  __shared__ __attribute__((aligned(16))) float s[64][64];
+  const int c = blockIdx.x * 64 + (threadIdx.x & 15) * 4, r0 = threadIdx.x >> 4;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (c < dim) {
+#pragma unroll 4
+    for (int r = r0; r < n; r += 64) {
+      const float4 p = *reinterpret_cast<const float4 *>(partial + (size_t)r * dim + c);
+      v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+    }
+  }
+  *reinterpret_cast<float4 *>(&s[r0][(threadIdx.x & 15) * 4]) = v;
   __syncthreads();
-  if (r0 == 0 && c < dim) {
-    for (int r = 1; r < 16; ++r) v += s[r * 16 + threadIdx.x];
-    out[c] = v;
+  const int col = threadIdx.x & 63, q = threadIdx.x >> 6;
+  float sum = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) sum += s[q * 4 + r][col];
+  __syncthreads();
+  s[q][col] = sum;
+  __syncthreads();
+  if (q == 0 && blockIdx.x * 64 + col < dim) {
+#pragma unroll
+    for (int r = 1; r < 16; ++r) sum += s[r][col];
+    out[blockIdx.x * 64 + col] = sum;
   }
 }
 
@@ -209,15 +224,17 @@ template <typename T, bool NORM> hipError_t launch_norm(const gear_norm_args &a,
   return hipGetLastError();
 }
 
-// workgroups of the backward pass: rows are shared out to as many as the device holds, each leaves one row of partial sums
-constexpr int kBackBlocks = 1024;
-int back_blocks(int64_t rows, int32_t dim) {
-  const int64_t groups = dim <= 2048 ? (rows + 3) / 4 : rows;
-  return (int)(groups < kBackBlocks ? groups : kBackBlocks);
+// Workgroups of the backward pass: rows are shared out to them, each leaves one row of partial sums.  As many as are on the
+// device at once, three for each CU in bf16 and two in fp32 (registers): us of 512 / 768 / 1024 / 1536 for 65536 x 2048
+// bf16 204 / 197 / 228 / 202, 65536 x 1152 131 / 120 / 145 / 123 (5.0 TB/s), 16384 x 1024 28.8 / 28.0 / 28.2 / 31.6; fp32
+// 65536 x 2048 408 / 446 / 409 / 413 (5.3 TB/s), 10001 x 512 19.0 / 19.8 / 20.6 / 22.1.
+int back_blocks(int64_t rows, int32_t dim, int32_t dtype) {
+  const int64_t groups = dim <= 2048 ? (rows + 3) / 4 : rows, most = dtype == GEAR_BF16 ? 768 : 512;
+  return (int)(groups < most ? groups : most);
 }
 
 template <typename T> hipError_t launch_back(const gear_norm_backward_args &a, float *partial, hipStream_t s) {
-  const dim3 grid(back_blocks(a.rows, a.dim));
+  const dim3 grid(back_blocks(a.rows, a.dim, a.dtype));
 #define GEAR_BACK(TPR, PER) \
   hipLaunchKernelGGL((k_rmsnorm_backward<T, TPR, PER>), grid, dim3(TPR < 256 ? 256 : TPR), 0, s, a, partial)
   if (a.dim <= 512)
@@ -275,7 +292,7 @@ extern "C" gear_status gear_rows8(const void *x, int32_t dtype, int64_t ld_x, in
 
 extern "C" size_t gear_norm_backward_workspace_bytes(int64_t rows, int32_t dim) {
   if (!shape_ok(rows, dim, GEAR_F32)) return 0;
-  const size_t bytes = (size_t)back_blocks(rows, dim) * dim * sizeof(float);
+  const size_t bytes = (size_t)back_blocks(rows, dim, GEAR_BF16) * dim * sizeof(float);
   return bytes < 256 ? 256 : (bytes + 255) & ~(size_t)255;
 }
 
@@ -301,7 +318,7 @@ extern "C" gear_status gear_rmsnorm_backward(const gear_norm_backward_args *a, v
   const hipError_t err = a->dtype == GEAR_BF16 ? launch_back<bf16_t>(*a, partial, s) : launch_back<float>(*a, partial, s);
   if (err != hipSuccess) return GEAR_ERR_HIP;
   if (a->dgain) {
-    hipLaunchKernelGGL(k_sum_rows, dim3((a->dim + 15) / 16), dim3(256), 0, s, partial, back_blocks(a->rows, a->dim), a->dim, a->dgain);
+    hipLaunchKernelGGL(k_sum_rows, dim3((a->dim + 63) / 64), dim3(1024), 0, s, partial, back_blocks(a->rows, a->dim, a->dtype), a->dim, a->dgain);
     if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
   }
   return GEAR_OK;
