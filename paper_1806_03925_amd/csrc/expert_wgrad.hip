@@ -38,8 +38,9 @@ __device__ __forceinline__ int partials_before(const int32_t *__restrict__ off, 
 // one expert add up to is left in `partial` and summed by k_wgrad_sum (an expert of one piece needs neither).  Experts come
 // in descending order of their rows (up to 64 experts, which one look at the offsets orders; with more of them chance does),
 // so that the long tiles are not the last ones.  Workgroups are spread over the XCDs by their number modulo 8, whatever they
-// cost: kSpread neighbouring tiles, which share rows of dy and x, go to one XCD, the next ones to the next.
-constexpr int kSpread = 8;
+// cost: kSpread neighbouring tiles, which share rows of dy and x, go to one XCD, the next ones to the next.  us of 8 / 16 / 32: 65536 x
+// 1024 x 1152 of one expert 180 / 171 / 170, 65536 x 2048 x 1024 of 64 392 / 392 / 421.
+constexpr int kSpread = 16;
 __device__ __forceinline__ WgradTile wgrad_tile(const WgradArgs &a, int bm, int bn, int block, int lane) {
   WgradTile r = {0, 0, 0, 0, nullptr, false, false};
   r.bad = a.off && !offsets_ok(a.off, a.experts, a.rows, lane);

@@ -43,23 +43,41 @@ def _vector(t: torch.Tensor, where: str, name: str, dtype: torch.dtype, n: int) 
         _refuse(where, f"{name} has to be {n} contiguous {dtype} on the GPU")
 
 
-class Rows8(NamedTuple):
+class Rows8:
     """Rows in 8 bits: q [rows x gear_rows8_ld(dim)] (bytes of e4m3), scale [rows x gear_scales8_ld(dim)] (exponent + 127)."""
-    q: torch.Tensor
-    scale: torch.Tensor
-    dim: int
+    __slots__ = ("rows", "dim", "ld", "device", "_q", "_scale", "_room", "p_q", "p_scale")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, dim: int):
+        rows = q.shape[0]
+        if not q.is_cuda or q.dtype not in _BYTE or q.shape != (rows, (dim + 127) // 128 * 128) or not q.is_contiguous():
+            _refuse("Rows8", "q has to be [rows x gear_rows8_ld(dim)] contiguous bytes on the GPU")
+        if not scale.is_cuda or scale.dtype is not torch.uint8 or scale.shape != (rows, (dim + 511) // 512 * 4) or not scale.is_contiguous():
+            _refuse("Rows8", "scale has to be [rows x gear_scales8_ld(dim)] contiguous bytes on the GPU")
+        self.rows, self.dim, self.ld, self.device = rows, dim, q.shape[1], q.device
+        self._q, self._scale, self._room, self.p_q, self.p_scale = q, scale, None, q.data_ptr(), scale.data_ptr()
 
     @staticmethod
     def empty(rows: int, dim: int, device) -> "Rows8":
-        return Rows8(torch.empty((rows, (dim + 127) // 128 * 128), dtype=torch.float8_e4m3fn, device=device),
-                     torch.empty((rows, (dim + 511) // 512 * 4), dtype=torch.uint8, device=device), dim)
+        """One allocation for both; the tensors are made when somebody asks for them."""
+        r = object.__new__(Rows8)
+        r.rows, r.dim, r.ld, r.device = rows, dim, (dim + 127) // 128 * 128, device
+        r._q = r._scale = None
+        r._room = torch.empty(rows * (r.ld + (dim + 511) // 512 * 4), dtype=torch.uint8, device=device)
+        r.p_q = r._room.data_ptr()
+        r.p_scale = r.p_q + rows * r.ld
+        return r
 
-    def check(self, where: str) -> None:
-        q, scale, rows = self.q, self.scale, self.q.shape[0]
-        if not q.is_cuda or q.dtype not in _BYTE or q.shape != (rows, (self.dim + 127) // 128 * 128) or not q.is_contiguous():
-            _refuse(where, "q has to be [rows x gear_rows8_ld(dim)] contiguous bytes on the GPU")
-        if not scale.is_cuda or scale.dtype is not torch.uint8 or scale.shape != (rows, (self.dim + 511) // 512 * 4) or not scale.is_contiguous():
-            _refuse(where, "scale has to be [rows x gear_scales8_ld(dim)] contiguous bytes on the GPU")
+    @property
+    def q(self) -> torch.Tensor:
+        if self._q is None:
+            self._q = self._room[:self.rows * self.ld].view(torch.float8_e4m3fn).view(self.rows, self.ld)
+        return self._q
+
+    @property
+    def scale(self) -> torch.Tensor:
+        if self._scale is None:
+            self._scale = self._room[self.rows * self.ld:].view(self.rows, (self.dim + 511) // 512 * 4)
+        return self._scale
 
 
 class NormOutput(NamedTuple):
@@ -99,10 +117,9 @@ def gear_rmsnorm(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Opti
     else:
         if r8 is None:
             r8 = Rows8.empty(rows, dim, device)
-        else:
-            r8.check(where)
-            _need(r8.dim == dim and r8.q.shape[0] == rows, where, "rows8 has another shape than x")
-        p_q, p_scale = r8.q.data_ptr(), r8.scale.data_ptr()
+        elif r8.dim != dim or r8.rows != rows:
+            _refuse(where, "rows8 has another shape than x")
+        p_q, p_scale = r8.p_q, r8.p_scale
     a = gear_norm_args(rows, dim, _CODE[dtype], eps, x.data_ptr(), p_res, gain.data_ptr(), p_sum, p_y, ld_x, ld_r, ld_s, ld_y, p_q, p_scale)
     code = lib.gear_rmsnorm(C.byref(a), _raw_stream(device.index))
     if code:
@@ -144,9 +161,9 @@ def gear_rows8(x: torch.Tensor, out: Optional[Rows8] = None) -> Rows8:
     rows, dim = x.shape
     if out is None:
         out = Rows8.empty(rows, dim, x.device)
-    out.check(where)
-    _need(out.dim == dim and out.q.shape[0] == rows, where, "out has another shape than x")
-    _check(lib.gear_rows8(_ptr(x), _CODE[x.dtype], ld, rows, dim, _ptr(out.q), _ptr(out.scale), _raw_stream(x.device.index)), where)
+    elif out.dim != dim or out.rows != rows:
+        _refuse(where, "out has another shape than x")
+    _check(lib.gear_rows8(x.data_ptr(), _CODE[x.dtype], ld, rows, dim, out.p_q, out.p_scale, _raw_stream(x.device.index)), where)
     return out
 
 
@@ -156,32 +173,44 @@ def _weights(w: torch.Tensor, where: str) -> Tuple[int, int, int]:
     return (1, *w.shape) if len(w.shape) == 2 else tuple(w.shape)
 
 
-class Weights8(NamedTuple):
-    """Weights in 8 bits, laid out for gear_matmul8; status is where its calls report unless they are given a word of their own."""
-    packed: torch.Tensor
-    scale: torch.Tensor
-    experts: int
-    N: int
-    K: int
-    status: torch.Tensor
+class _Packed:
+    """Memory of weights laid out for the products, and behind them a word that the products report into."""
+
+    def _allocate(self, size: int, device) -> None:
+        size = (size + 255) // 256 * 256
+        self.packed = torch.empty(size + 4, dtype=torch.uint8, device=device)
+        self.address = self.packed.data_ptr()
+        self.p_status = self.address + size
+
+    @property
+    def status(self) -> torch.Tensor:
+        """What the last product that was given no word of its own reported."""
+        return self.packed[-4:].view(torch.int32)
+
+
+class Weights8(_Packed):
+    """Weights in 8 bits, laid out for gear_matmul8 (gear_weights8 makes them)."""
+
+    def __init__(self, w: torch.Tensor):
+        where = "gear_weights8"
+        self.experts, self.N, self.K = shape = _weights(w, where)
+        size, scales = lib.gear_packed_weights_bytes(GEAR_E4M3, *shape, 0), lib.gear_weight_scales_bytes(*shape)
+        if size == 0:
+            _refuse(where, f"weights of {shape} have no packed form")
+        self._allocate(size + scales, w.device)
+        self.p_scale = self.address + size
+        _check(lib.gear_pack_weights(w.data_ptr(), _CODE[w.dtype], GEAR_E4M3, *shape, self.address, None, self.p_scale,
+                                     _raw_stream(w.device.index)), where)
 
 
 def gear_weights8(w: torch.Tensor) -> Weights8:
     """w ([experts x N x K] or [N x K], float32 or bfloat16) in 8 bits, a scale for every 128 x 128 weights."""
-    experts, n, k = _weights(w, "gear_weights8")
-    size = lib.gear_weight_scales_bytes(experts, n, k)
-    _need(size > 0, "gear_weights8", f"weights of {experts} x {n} x {k} have no packed form")
-    scale = torch.empty(size, dtype=torch.uint8, device=w.device)
-    packed = torch.empty(lib.gear_packed_weights_bytes(GEAR_E4M3, experts, n, k, 0), dtype=torch.uint8, device=w.device)
-    _check(lib.gear_pack_weights(_ptr(w), _CODE[w.dtype], GEAR_E4M3, experts, n, k, _ptr(packed), None, _ptr(scale),
-                                 _raw_stream(w.device.index)), "gear_weights8")
-    return Weights8(packed, scale, experts, n, k, torch.zeros(1, dtype=torch.int32, device=w.device))
+    return Weights8(w)
 
 
-class ExpertWeights:
+class ExpertWeights(_Packed):
     """Weights of every expert laid out for the forward product and (transposed) for the gradient of its input, in float32
-    or bfloat16 (`operand`, w's own type if not given).  A training program calls update() when the weights have changed.
-    status is where the products report unless they are given a word of their own."""
+    or bfloat16 (`operand`, w's own type if not given).  A training program calls update() when the weights have changed."""
 
     def __init__(self, w: torch.Tensor, operand: Optional[torch.dtype] = None, backward: bool = True):
         where = "ExpertWeights"
@@ -194,10 +223,8 @@ class ExpertWeights:
         size = forward + (lib.gear_packed_weights_bytes(self.code, *shape, 1) if backward else 0)
         if forward == 0:
             _refuse(where, f"weights of {shape} have no packed form")
-        size = (size + 15) // 16 * 16
-        self.packed = torch.empty(size + 16, dtype=torch.uint8, device=w.device)
-        self.status = self.packed[size:size + 4].view(torch.int32)
-        self.forward = self.packed.data_ptr()
+        self._allocate(size, w.device)
+        self.forward = self.address
         self.transposed = self.forward + forward if backward else None
         self._lay_out(w)
 
@@ -213,27 +240,22 @@ class ExpertWeights:
         self._lay_out(w)
 
 
-def _offsets(off: Optional[torch.Tensor], experts: int, status: Optional[torch.Tensor], where: str):
-    if off is None:
-        if experts != 1:
-            _refuse(where, "off may only be left out where there is one expert")
-        return status
-    _vector(off, where, "off", torch.int32, experts + 1)
-    if status is None:
-        return torch.empty(1, dtype=torch.int32, device=off.device)
-    _vector(status, where, "status", torch.int32, 1)
-    return status
-
-
-def _product(where, dtype, x, x_scale, ld_x, packed, w_scale, rows, n, k, experts, off, out, out_dtype, status) -> torch.Tensor:
-    device = x.device
-    status = _offsets(off, experts, status, where)
+def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, rows, n, k, off, out, out_dtype, status, device) -> torch.Tensor:
+    experts = weights.experts
+    if off is not None:
+        _vector(off, where, "off", torch.int32, experts + 1)
+        off = off.data_ptr()
+    elif experts != 1:
+        _refuse(where, "off may only be left out where there is one expert")
+    if status is not None:
+        _vector(status, where, "status", torch.int32, 1)
+        status = status.data_ptr()
     if out is None:
-        out, ld_out = torch.empty((rows, n), dtype=out_dtype, device=device) if out_dtype is not x.dtype else x.new_empty((rows, n)), n
+        out, ld_out = torch.empty((rows, n), dtype=out_dtype, device=device), n
     else:
         ld_out = _matrix(out, where, "out", None, (rows, n))
-    a = gear_expert_args(dtype, _CODE[out.dtype], rows, k, n, experts, x.data_ptr(), x_scale, packed, w_scale, _ptr(off),
-                         out.data_ptr(), ld_x, ld_out, _ptr(status))
+    a = gear_expert_args(dtype, _CODE[out.dtype], rows, k, n, experts, p_x, p_x_scale, packed, p_w_scale, off, out.data_ptr(), ld_x, ld_out,
+                         status or weights.p_status)
     code = lib.gear_expert_product(C.byref(a), _raw_stream(device.index))
     if code:
         _check(code, where)
@@ -243,14 +265,12 @@ def _product(where, dtype, x, x_scale, ld_x, packed, w_scale, rows, n, k, expert
 def gear_matmul8(rows8: Rows8, weights: Weights8, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                  out_dtype: torch.dtype = torch.bfloat16, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """rows8 times the transposed 8-bit weights.  off [experts + 1] (int32, on the GPU): where each expert's rows begin; rows
-    from off[experts] on are not written.  status [1] (int32): GEAR_ERR_RANGE if off is no such list, and nothing is written."""
-    where = "gear_matmul8"
-    rows8.check(where)
+    from off[experts] on are not written.  status [1] (int32; weights.status if not given): GEAR_ERR_RANGE if off is no such
+    list, and nothing is written."""
     if rows8.dim != weights.K:
-        _refuse(where, f"rows of {rows8.dim} for weights of {weights.K}")
-    rows, ld = rows8.q.shape
-    return _product(where, GEAR_E4M3, rows8.q, rows8.scale.data_ptr(), ld, weights.packed.data_ptr(), weights.scale.data_ptr(), rows, weights.N, weights.K,
-                    weights.experts, off, out, out_dtype, weights.status if status is None else status)
+        _refuse("gear_matmul8", f"rows of {rows8.dim} for weights of {weights.K}")
+    return _product("gear_matmul8", GEAR_E4M3, rows8.p_q, rows8.p_scale, rows8.ld, weights, weights.address, weights.p_scale, rows8.rows,
+                    weights.N, weights.K, off, out, out_dtype, status, rows8.device)
 
 
 def gear_expert_matmul(x: torch.Tensor, weights: ExpertWeights, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -258,8 +278,8 @@ def gear_expert_matmul(x: torch.Tensor, weights: ExpertWeights, off: Optional[to
     """x [rows x K] times the transposed weights of each row's expert: [rows x N]; off and status as for gear_matmul8."""
     where = "gear_expert_matmul"
     ld = _matrix(x, where, "x", weights.dtype, (x.shape[0], weights.K))
-    return _product(where, _CODE[x.dtype], x, None, ld, weights.forward, None, x.shape[0], weights.N, weights.K, weights.experts, off, out,
-                    out_dtype or x.dtype, weights.status if status is None else status)
+    return _product(where, weights.code, x.data_ptr(), None, ld, weights, weights.forward, None, x.shape[0], weights.N, weights.K, off, out,
+                    out_dtype or x.dtype, status, x.device)
 
 
 def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -269,8 +289,8 @@ def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[to
     ld = _matrix(dy, where, "dy", weights.dtype, (dy.shape[0], weights.N))
     if weights.transposed is None:
         _refuse(where, "the weights were laid out without backward")
-    return _product(where, _CODE[dy.dtype], dy, None, ld, weights.transposed, None, dy.shape[0], weights.K, weights.N, weights.experts, off,
-                    out, out_dtype or dy.dtype, weights.status if status is None else status)
+    return _product(where, weights.code, dy.data_ptr(), None, ld, weights, weights.transposed, None, dy.shape[0], weights.K, weights.N, off,
+                    out, out_dtype or dy.dtype, status, dy.device)
 
 
 def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
@@ -282,17 +302,23 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     rows, k = x.shape
     n = dy.shape[-1]
     ld_dy = _matrix(dy, where, "dy", x.dtype, (rows, n))
-    experts = 1 if off is None else off.numel() - 1
-    status = _offsets(off, experts, status, where)
+    experts = 1
+    if off is not None:
+        experts = off.numel() - 1
+        _vector(off, where, "off", torch.int32, experts + 1)
+    if status is not None:
+        _vector(status, where, "status", torch.int32, 1)
     if dw is None:
         dw = torch.empty((experts, n, k), dtype=torch.float32, device=device)
     else:
         _vector(dw, where, "dw", torch.float32, experts * n * k)
     dtype = _CODE[x.dtype]
     size = lib.gear_expert_wgrad_workspace_bytes(dtype, rows, experts, n, k)
-    ws = torch.empty(size, dtype=torch.uint8, device=device)
-    a = gear_expert_wgrad_args(dtype, rows, k, n, experts, dy.data_ptr(), x.data_ptr(), _ptr(off), dw.data_ptr(), ld_dy, ld_x, _ptr(status))
-    code = lib.gear_expert_wgrad(C.byref(a), ws.data_ptr(), size, _raw_stream(device.index))
+    ws = torch.empty(size + 4, dtype=torch.uint8, device=device)      # and a word to report into
+    p_ws = ws.data_ptr()
+    a = gear_expert_wgrad_args(dtype, rows, k, n, experts, dy.data_ptr(), x.data_ptr(), _ptr(off), dw.data_ptr(), ld_dy, ld_x,
+                               p_ws + size if status is None else status.data_ptr())
+    code = lib.gear_expert_wgrad(C.byref(a), p_ws, size, _raw_stream(device.index))
     if code:
         _check(code, where)
     return dw
