@@ -2,7 +2,8 @@
 //
 //   norm = sqrt(sum over tensors and elements of g^2),  c = min(1, max_norm / (norm + 1e-6)),  out = c g
 //
-// Two launches, whatever the number of tensors.  The list lies on the device as one entry per tensor; work is cut into
+// Two launches, whatever the number of tensors (one for a list of up to four chunks: us of two launches / one, 6273
+// gradients in four tensors 6.8 / 4.4, 32768 in one 7.5 / 6.0, but 65536 7.5 / 9.1).  The list lies on the device as one entry per tensor; work is cut into
 // chunks of kClipChunk elements that never cross a tensor, and a workgroup finds a chunk's tensor by bisection over the
 // entries' first chunks.  The first launch leaves one fp64 sum per workgroup, the second adds
 // these up in every workgroup (in the same order, so that all get the same factor) and scales.  Memory bound: all elements
@@ -49,7 +50,8 @@ __device__ __forceinline__ int entry_of(const GradEntry *__restrict__ list, int 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kAtOnce = 4;   // pieces of a thread on their way together
 
-template <typename T> __device__ __forceinline__ double square_sum(const T *__restrict__ p, int64_t n) {
+// by kClipThreads threads, of which the caller is number t
+template <typename T> __device__ __forceinline__ double square_sum(const T *__restrict__ p, int64_t n, int t) {
   constexpr int V = 16 / (int)sizeof(T);
   double sum = 0.0;
   auto add = [&](float v) { sum += (double)v * (double)v; };
@@ -66,10 +68,10 @@ template <typename T> __device__ __forceinline__ double square_sum(const T *__re
   };
   // elements before the first 16-byte border, whole pieces, the rest
   const int head = (int)min(n, (int64_t)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T)));
-  if ((int)threadIdx.x < head) add(to_f32(p[threadIdx.x]));
+  if (t < head) add(to_f32(p[t]));
   const int pieces = (int)(n - head) / V;
   const u32x4 *v = reinterpret_cast<const u32x4 *>(p + head);
-  int i = threadIdx.x;
+  int i = t;
   for (; i + (kAtOnce - 1) * kClipThreads < pieces; i += kAtOnce * kClipThreads) {
     u32x4 w[kAtOnce];
 #pragma unroll
@@ -78,33 +80,36 @@ template <typename T> __device__ __forceinline__ double square_sum(const T *__re
     for (int k = 0; k < kAtOnce; ++k) add_piece(w[k]);
   }
   for (; i < pieces; i += kClipThreads) add_piece(v[i]);
-  const int at = head + pieces * V + threadIdx.x;
+  const int at = head + pieces * V + t;
   if (at < n) add(to_f32(p[at]));
   return sum;
 }
 
-__device__ __forceinline__ double block_sum(double v, double *s_sum) {
+template <int THREADS> __device__ __forceinline__ double block_sum(double v, double *s_sum) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, kWave);
   if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x / kWave] = v;
   __syncthreads();
   v = s_sum[0];
 #pragma unroll
-  for (int w = 1; w < kClipThreads / kWave; ++w) v += s_sum[w];
+  for (int w = 1; w < THREADS / kWave; ++w) v += s_sum[w];
   return v;
+}
+
+// the sum of the squares of chunk c: a thread's share
+__device__ __forceinline__ double chunk_squares(const GradEntry *__restrict__ list, int count, int64_t c, int t) {
+  const GradEntry e = list[entry_of(list, count, c)];
+  const int64_t first = (c - e.first_chunk) * kClipChunk, n = min(kClipChunk, e.n - first);
+  return e.dtype == GEAR_BF16 ? square_sum(static_cast<const bf16_t *>(e.src) + first, n, t)
+                              : square_sum(static_cast<const float *>(e.src) + first, n, t);
 }
 
 __global__ void __launch_bounds__(kClipThreads) k_grad_squares(const GradEntry *__restrict__ list, int count, int64_t chunks,
                                                                double *__restrict__ partial) {
   __shared__ double s_sum[kClipThreads / kWave];
   double sum = 0.0;
-  for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const GradEntry e = list[entry_of(list, count, c)];
-    const int64_t first = (c - e.first_chunk) * kClipChunk, n = min(kClipChunk, e.n - first);
-    sum += e.dtype == GEAR_BF16 ? square_sum(static_cast<const bf16_t *>(e.src) + first, n)
-                                : square_sum(static_cast<const float *>(e.src) + first, n);
-  }
-  sum = block_sum(sum, s_sum);
+  for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) sum += chunk_squares(list, count, c, threadIdx.x);
+  sum = block_sum<kClipThreads>(sum, s_sum);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
@@ -119,15 +124,15 @@ template <typename T> __device__ __forceinline__ u32x4 scale_piece(u32x4 w, floa
   return w;
 }
 
-template <typename T> __device__ __forceinline__ void scale_chunk(const T *src, T *dst, int64_t n, float c) {
+template <typename T> __device__ __forceinline__ void scale_chunk(const T *src, T *dst, int64_t n, float c, int t) {
   constexpr int V = 16 / (int)sizeof(T);
   int head = (int)n;   // element by element where source and destination lie differently to 16 bytes
   if ((((uintptr_t)src ^ (uintptr_t)dst) & 15) == 0) head = (int)min(n, (int64_t)(((16 - ((uintptr_t)src & 15)) & 15) / sizeof(T)));
-  for (int i = threadIdx.x; i < head; i += kClipThreads) dst[i] = from_f32<T>(to_f32(src[i]) * c);
+  for (int i = t; i < head; i += kClipThreads) dst[i] = from_f32<T>(to_f32(src[i]) * c);
   const int pieces = (int)(n - head) / V;
   const u32x4 *v = reinterpret_cast<const u32x4 *>(src + head);
   u32x4 *o = reinterpret_cast<u32x4 *>(dst + head);
-  int i = threadIdx.x;
+  int i = t;
   for (; i + (kAtOnce - 1) * kClipThreads < pieces; i += kAtOnce * kClipThreads) {
     u32x4 w[kAtOnce];
 #pragma unroll
@@ -136,8 +141,23 @@ template <typename T> __device__ __forceinline__ void scale_chunk(const T *src, 
     for (int k = 0; k < kAtOnce; ++k) __builtin_nontemporal_store(scale_piece<T>(w[k], c), o + i + k * kClipThreads);
   }
   for (; i < pieces; i += kClipThreads) __builtin_nontemporal_store(scale_piece<T>(v[i], c), o + i);
-  const int at = head + pieces * V + threadIdx.x;
+  const int at = head + pieces * V + t;
   if (at < n) dst[at] = from_f32<T>(to_f32(src[at]) * c);
+}
+
+__device__ __forceinline__ float clip_factor(float norm, float max_norm) {
+  const float ratio = max_norm / (norm + 1e-6f);
+  return ratio > 1.0f ? 1.0f : ratio;   // NaN stays NaN
+}
+
+__device__ __forceinline__ void chunk_scale(const GradEntry *__restrict__ list, int count, int64_t k, float c, int t) {
+  const GradEntry e = list[entry_of(list, count, k)];
+  if (!e.dst || (c == 1.0f && e.src == e.dst)) return;
+  const int64_t first = (k - e.first_chunk) * kClipChunk, n = min(kClipChunk, e.n - first);
+  if (e.dtype == GEAR_BF16)
+    scale_chunk(static_cast<const bf16_t *>(e.src) + first, static_cast<bf16_t *>(e.dst) + first, n, c, t);
+  else
+    scale_chunk(static_cast<const float *>(e.src) + first, static_cast<float *>(e.dst) + first, n, c, t);
 }
 
 // scale: 0, only the norm is wanted (one workgroup)
@@ -147,20 +167,23 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_scale(const GradEntry *__
   __shared__ double s_sum[kClipThreads / kWave];
   double sum = 0.0;
   for (int i = threadIdx.x; i < n_partial; i += kClipThreads) sum += partial[i];
-  const float norm = (float)sqrt(block_sum(sum, s_sum));
+  const float norm = (float)sqrt(block_sum<kClipThreads>(sum, s_sum));
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
   if (!scale) return;
-  const float ratio = max_norm / (norm + 1e-6f);
-  const float c = ratio > 1.0f ? 1.0f : ratio;   // NaN stays NaN
-  for (int64_t k = chunks - 1 - blockIdx.x; k >= 0; k -= gridDim.x) {
-    const GradEntry e = list[entry_of(list, count, k)];
-    if (!e.dst || (c == 1.0f && e.src == e.dst)) continue;
-    const int64_t first = (k - e.first_chunk) * kClipChunk, n = min(kClipChunk, e.n - first);
-    if (e.dtype == GEAR_BF16)
-      scale_chunk(static_cast<const bf16_t *>(e.src) + first, static_cast<bf16_t *>(e.dst) + first, n, c);
-    else
-      scale_chunk(static_cast<const float *>(e.src) + first, static_cast<float *>(e.dst) + first, n, c);
-  }
+  const float c = clip_factor(norm, max_norm);
+  for (int64_t k = chunks - 1 - blockIdx.x; k >= 0; k -= gridDim.x) chunk_scale(list, count, k, c, threadIdx.x);
+}
+
+// Short lists, whose time is that of two launches and not of one workgroup's memory accesses: all of it by one workgroup, kClipThreads threads to a chunk.  All reads for
+// the sum come before the barrier in block_sum, so gradients may be scaled in place.
+constexpr int kShortChunks = 4, kShortThreads = kShortChunks * kClipThreads;
+__global__ void __launch_bounds__(kShortThreads) k_grad_short(const GradEntry *__restrict__ list, int count, int chunks, float max_norm,
+                                                              int scale, float *__restrict__ norm_out) {
+  __shared__ double s_sum[kShortThreads / kWave];
+  const int chunk = threadIdx.x / kClipThreads, t = threadIdx.x % kClipThreads;
+  const float norm = (float)sqrt(block_sum<kShortThreads>(chunk < chunks ? chunk_squares(list, count, chunk, t) : 0.0, s_sum));
+  if (threadIdx.x == 0) *norm_out = norm;
+  if (scale && chunk < chunks) chunk_scale(list, count, chunk, clip_factor(norm, max_norm), t);
 }
 
 gear_status check(const void *list, int32_t count, int64_t chunks, const void *workspace, size_t bytes, const float *norm) {
@@ -175,11 +198,13 @@ gear_status run(const void *list, int32_t count, int64_t chunks, float max_norm,
   const GradEntry *entries = static_cast<const GradEntry *>(list);
   double *partial = static_cast<double *>(workspace);
   const int blocks = clip_blocks(chunks);
-  if (blocks > 0) {
-    hipLaunchKernelGGL(k_grad_squares, dim3(blocks), dim3(kClipThreads), 0, s, entries, count, chunks, partial);
-    if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
+  if (chunks <= kShortChunks) {
+    hipLaunchKernelGGL(k_grad_short, dim3(1), dim3(kShortThreads), 0, s, entries, count, (int)chunks, max_norm, scale, norm);
+    return hipGetLastError() == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
   }
-  hipLaunchKernelGGL(k_grad_scale, dim3(scale && blocks > 0 ? blocks : 1), dim3(kClipThreads), 0, s, entries, count, chunks,
+  hipLaunchKernelGGL(k_grad_squares, dim3(blocks), dim3(kClipThreads), 0, s, entries, count, chunks, partial);
+  if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
+  hipLaunchKernelGGL(k_grad_scale, dim3(scale ? blocks : 1), dim3(kClipThreads), 0, s, entries, count, chunks,
                      partial, blocks, max_norm, scale, norm);
   return hipGetLastError() == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
 }
