@@ -349,12 +349,13 @@ int64_t wgrad_tiles(const WgradShape &t, int N, int K) { return (int64_t)((N + t
 // cut so that one layer gives one whole round, and experts, whose sizes the host does not know, pieces of one and a half
 // fair shares.  us, uncut / cut: 65536 x 1024 x 1152 by one expert 832 / 191, 16384 x 1024 x 1152 by 8 93 / 71.
 int wgrad_cut(int dtype, int64_t rows, int experts, int N, int K) {
-  constexpr int64_t kSlots = 512, kLeast = 512;
+  constexpr int64_t kSlots = 512;
   const int64_t tiles = wgrad_tiles(wgrad_shape(dtype, K), N, K), whole = rows < 1 ? 1 : rows;
   if (experts * tiles >= 2 * kSlots) return (int)whole;
   int64_t cut = experts == 1 ? (rows + kSlots / tiles - 1) / (kSlots / tiles > 0 ? kSlots / tiles : 1) : rows * tiles * 3 / (2 * kSlots);
   cut = (cut + 31) / 32 * 32;
-  if (cut < kLeast) cut = kLeast;
+  const int64_t least = experts == 1 ? 256 : experts * tiles < kSlots ? 512 : 1024;   // what a piece adds and writes has to be worth it
+  if (cut < least) cut = least;
   return (int)(cut < whole ? cut : whole);
 }
 int64_t wgrad_partials(int64_t rows, int experts, int cut) {   // pieces of experts that are cut, at most
