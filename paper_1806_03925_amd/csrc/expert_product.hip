@@ -7,8 +7,8 @@
 // holds where does not matter, as long as both operands hold the same.  In 8 bits a k-block is also what shares a scale:
 // the instruction multiplies by both operands' powers of two itself, so scales cost no vector instruction.
 //
-// Rows of x are copied global -> LDS by DMA, LDS rows of 128 bytes with their pieces XOR-ed by the row's number modulo 8
-// (no bank conflicts); what lies beyond k or beyond the expert's rows is out of the buffer's range and becomes zeros.
+// Rows of x are copied global -> LDS by DMA, LDS rows of 128 bytes with their pieces XOR-ed by half the row's number modulo 8:
+// the sixteen rows that are read at a time, two to the 256 bytes of all banks, then lie in sixteen different places; what lies beyond k or beyond the expert's rows is out of the buffer's range and becomes zeros.
 // Weights come in operand order (k_pack) straight into registers and never pass LDS.
 #include "eight.hpp"
 #include "experts.hpp"
@@ -152,8 +152,9 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   const int row_bytes = a.K * operand_bytes(C::DT);
   const int nk = (row_bytes + kKBlock - 1) / kKBlock;
 
-  // this lane's pieces of the rows it copies: LDS slot lane % 8 of row lane / 8 receives piece (lane % 8) ^ (row % 8)
-  const int piece = (lane & 7) ^ (lane >> 3);
+  // this lane's pieces of the rows it copies: LDS slot lane % 8 of row lane / 8 receives piece (lane % 8) ^ (row / 2 % 8)
+  static_assert(C::WAVES % 2 == 0, "a wavefront copies every second group of eight rows or all: its rows' XOR does not change");
+  const int piece = (lane & 7) ^ (4 * (wave & 1) + (lane >> 4));
   const auto x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.x) + (int64_t)m0 * a.ld_x, 0,
                                                         (int)((m_rows - 1) * a.ld_x) + nk * kKBlock, 0x00020000);
   // rows in 8 bits have zeros behind their end; others end inside a k-block, and what is beyond must not be read as k
@@ -219,7 +220,7 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-  const uint32_t x_rel = lds_base + (uint32_t)(wm * C::WTM * 32 + r) * 128u + (uint32_t)((g ^ (r & 7)) << 4);
+  const uint32_t x_rel = lds_base + (uint32_t)(wm * C::WTM * 32 + r) * 128u + (uint32_t)((g ^ (r >> 1 & 7)) << 4);
 
   scales(0, 0);
 #pragma unroll

@@ -195,24 +195,25 @@ template <typename C> __global__ void __launch_bounds__(C::THREADS) k_expert_wgr
 // through it for 256 cycles of matrix instructions, this one 72 KB for 512.  Two workgroups share a CU, so that one stores
 // its gradient (128 KB) while the other multiplies; and operands are requested a k-step (16 rows) ahead, also across the
 // border of a stage.
-struct WideTile {
-  static constexpr int THREADS = 256, WAVES = 4, TM = 2, TN = 4, BM = 128, BN = 256, KD = 32, STAGES = 3;
+template <int TM_, int TN_, int WAVES_M_, int WAVES_N_, int STAGES_> struct WideTile {
+  static constexpr int TM = TM_, TN = TN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, STAGES = STAGES_, KD = 32;
+  static constexpr int WAVES = WAVES_M * WAVES_N, THREADS = WAVES * kWave, BM = 32 * TM * WAVES_M, BN = 32 * TN * WAVES_N;
   static constexpr int ROW_A = BM * 2, ROW_B = BN * 2, A_BYTES = KD * ROW_A, STAGE_BYTES = A_BYTES + KD * ROW_B;
   static constexpr int DMA_A = A_BYTES / 1024 / WAVES, DMA_B = KD * ROW_B / 1024 / WAVES, DMA_ALL = DMA_A + DMA_B;   // copies of a wavefront
 };
 
-struct WideFrag {
-  u32x2_v a[WideTile::TM][2], b[WideTile::TN][2];   // [32-column tile][rows +0..3 | +4..7 of the lane's eight]
-  __device__ __forceinline__ void fetch(const uint32_t (&at_a)[WideTile::TM], const uint32_t (&at_b)[WideTile::TN], uint32_t so_a, uint32_t so_b) {
+template <typename C> struct WideFrag {
+  u32x2_v a[C::TM][2], b[C::TN][2];   // [32-column tile][rows +0..3 | +4..7 of the lane's eight]
+  __device__ __forceinline__ void fetch(const uint32_t (&at_a)[C::TM], const uint32_t (&at_b)[C::TN], uint32_t so_a, uint32_t so_b) {
 #pragma unroll
-    for (int i = 0; i < WideTile::TM; ++i) {
+    for (int i = 0; i < C::TM; ++i) {
       lds_read_tr<0>(a[i][0], at_a[i] + so_a);
-      lds_read_tr<4 * WideTile::ROW_A>(a[i][1], at_a[i] + so_a);
+      lds_read_tr<4 * C::ROW_A>(a[i][1], at_a[i] + so_a);
     }
 #pragma unroll
-    for (int i = 0; i < WideTile::TN; ++i) {
+    for (int i = 0; i < C::TN; ++i) {
       lds_read_tr<0>(b[i][0], at_b[i] + so_b);
-      lds_read_tr<4 * WideTile::ROW_B>(b[i][1], at_b[i] + so_b);
+      lds_read_tr<4 * C::ROW_B>(b[i][1], at_b[i] + so_b);
     }
   }
   __device__ __forceinline__ void wait() {
@@ -220,17 +221,17 @@ struct WideFrag {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int i = 0; i < WideTile::TM; ++i) landed(a[i][h]);
+      for (int i = 0; i < C::TM; ++i) landed(a[i][h]);
 #pragma unroll
-      for (int i = 0; i < WideTile::TN; ++i) landed(b[i][h]);
+      for (int i = 0; i < C::TN; ++i) landed(b[i][h]);
     }
   }
-  __device__ __forceinline__ void mma(f32x16_v (&acc)[WideTile::TM][WideTile::TN]) {
+  __device__ __forceinline__ void mma(f32x16_v (&acc)[C::TM][C::TN]) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < WideTile::TM; ++i)
+    for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-      for (int j = 0; j < WideTile::TN; ++j) {
+      for (int j = 0; j < C::TN; ++j) {
         const u32x4_v av = {a[i][0].x, a[i][0].y, a[i][1].x, a[i][1].y};
         const u32x4_v bv = {b[j][0].x, b[j][0].y, b[j][1].x, b[j][1].y};
         MFMA_BF16(acc[i][j], av, bv);
@@ -239,23 +240,23 @@ struct WideFrag {
   }
 };
 
-__device__ __forceinline__ void wgrad_wide(const WgradArgs &a, unsigned char *lds) {
-  using C = WideTile;
+template <typename C> __device__ __forceinline__ void wgrad_wide(const WgradArgs &a, unsigned char *lds) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const WgradTile t = wgrad_tile(a, C::BM, C::BN, blockIdx.x, lane);
   if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
   if (!t.have) return;
   const int m0 = t.m0, n0 = t.n0, first = t.first, last = t.last;
-  const int wm = wave >> 1, wn = wave & 1;
+  const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
   const int nk = (last - first + C::KD - 1) / C::KD;
 
   // A copy is four rows of dy (256 bytes) or two of x (512); the slot of a row's 16-byte piece is XOR-ed by 4 (row % 4), so that
   // the four rows that a transposing read touches lie in different quarters of the banks.  Rows beyond the expert's and columns
   // beyond the last row's end are out of the buffer's range and become zeros.
   const int ld_a = (int)a.ld_dy * 2, ld_b = (int)a.ld_x * 2;
-  const int row_a = lane >> 4, piece_a = (lane & 15) ^ (4 * row_a);
-  const int row_b = lane >> 5, piece_b = (lane & 31) ^ (4 * (2 * (wave & 1) + row_b));
-  const int at_a = (4 * wave + row_a) * ld_a + piece_a * 16, at_b = (2 * wave + row_b) * ld_b + piece_b * 16;
+  constexpr int PA = C::ROW_A / 16, PB = C::ROW_B / 16, RA = 64 / PA, RB = 64 / PB;   // pieces of a row, rows of a copy
+  static_assert((PA == 16 || PA == 32) && (PB == 16 || PB == 32) && C::WAVES % 2 == 0, "copies of two rows or four");
+  const int row_a = RA * wave + lane / PA, row_b = RB * wave + lane / PB;
+  const int at_a = row_a * ld_a + ((lane % PA) ^ (4 * (row_a & 3))) * 16, at_b = row_b * ld_b + ((lane % PB) ^ (4 * (row_b & 3))) * 16;
   unsigned char *pa = static_cast<unsigned char *>(const_cast<void *>(a.dy)) + (int64_t)first * ld_a + m0 * 2;
   unsigned char *pb = static_cast<unsigned char *>(const_cast<void *>(a.x)) + (int64_t)first * ld_b + n0 * 2;
   const int width_a = min(C::BM, a.N - m0) * 2, width_b = min(C::BN, a.K - n0) * 2;
@@ -266,10 +267,10 @@ __device__ __forceinline__ void wgrad_wide(const WgradArgs &a, unsigned char *ld
     unsigned char *da = lds + stage * C::STAGE_BYTES + wave * 1024, *db = da + C::A_BYTES;
 #pragma unroll
     for (int i = 0; i < C::DMA_A; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr_t)(da + i * C::WAVES * 1024), 16, at_a + i * 4 * C::WAVES * ld_a, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr_t)(da + i * C::WAVES * 1024), 16, at_a + i * RA * C::WAVES * ld_a, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < C::DMA_B; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr_t)(db + i * C::WAVES * 1024), 16, at_b + i * 2 * C::WAVES * ld_b, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr_t)(db + i * C::WAVES * 1024), 16, at_b + i * RB * C::WAVES * ld_b, 0, 0, 0);
     asm volatile("" ::: "memory");
   };
 #pragma unroll
@@ -294,7 +295,7 @@ __device__ __forceinline__ void wgrad_wide(const WgradArgs &a, unsigned char *ld
     for (int i = 0; i < C::TN; ++i) b_rel[i] = lds_base + C::A_BYTES + row * C::ROW_B + in + (uint32_t)(((wn * C::TN + i) ^ (j >> 2)) << 6);
   }
   if (nk > 0) {
-    WideFrag f[2];
+    WideFrag<C> f[2];
     wait_stages<C::DMA_ALL, C::STAGES - 2>(nk - 1);
     block_barrier();
     f[0].fetch(a_rel, b_rel, 0, 0);
@@ -333,9 +334,9 @@ __device__ __forceinline__ void wgrad_wide(const WgradArgs &a, unsigned char *ld
       }
 }
 
-__global__ void __launch_bounds__(WideTile::THREADS, 2) k_expert_wgrad_wide(WgradArgs a) {
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[WideTile::STAGES * WideTile::STAGE_BYTES];
-  wgrad_wide(a, lds);
+template <typename C> __global__ void __launch_bounds__(C::THREADS, C::TM * C::TN > 8 ? 1 : 2) k_expert_wgrad_wide(WgradArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[C::STAGES * C::STAGE_BYTES];
+  wgrad_wide<C>(a, lds);
 }
 
 // Tiles of a gradient: fp32 64 x 64, bf16 128 x 256, or 128 x 128 where half of those 256 would be empty
@@ -407,7 +408,8 @@ extern "C" gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *
   } else if (shape.bn == 128) {
     if (launch<TnTile<bf16_t, 2, 2, 3>>(w, blocks, s) != hipSuccess) return GEAR_ERR_HIP;
   } else {
-    hipLaunchKernelGGL(k_expert_wgrad_wide, dim3(blocks), dim3(WideTile::THREADS), 0, s, w);
+    using Wide = WideTile<2, 4, 2, 2, 3>;
+    hipLaunchKernelGGL(k_expert_wgrad_wide<Wide>, dim3(blocks), dim3(Wide::THREADS), 0, s, w);
     if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
   }
   if (wgrad_partials(a->rows, a->experts, cut) > 0) {
