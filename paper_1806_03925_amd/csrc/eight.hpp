@@ -114,7 +114,7 @@ __device__ __forceinline__ void unpack8(uint2 q, float scale, float (&v)[8]) {
 // through s_part [TPR / 64] in ascending order.  TPR > 64: every thread of the workgroup takes part.
 template <int TPR> __device__ __forceinline__ float row_sum(float v, float *s_part) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, kWave);
+  for (int o = (TPR < kWave ? TPR : kWave) / 2; o; o >>= 1) v += __shfl_xor(v, o, kWave);
   if constexpr (TPR > kWave) {
     __syncthreads();   // the last sum has been read by everybody
     if ((threadIdx.x & 63) == 0) s_part[threadIdx.x / kWave] = v;

@@ -551,7 +551,8 @@ template <int DT, int TM, int TN, int WAVES, int AHEAD> hipError_t launch_split(
 //   32 x 128 up to 512 tiles, against 64 x 256: 1024 x 2048 bf16 17.0 / 18.6, 4096 x 1024 x 1152 16.2 / 12.4; but not where its many
 //     row tiles each read weights that no L2 holds: 256 x 8192 bf16 144 / 74
 //   64 x 256 below 512 tiles, against 128 x 256: 2048 x 2048 bf16 19.9 / 28.1, 4096 x 2048 36 / 33; and a little over one round of the
-//     larger tiles (two a CU): 16384 x 1024 x 1152 by 64 experts in 8 bits 30.7 / 36.7
+//     larger tiles (two a CU): 16384 x 1024 x 1152 by 64 experts in 8 bits 30.7 / 36.7; again not with large weights: 5842 x 2904 x 4304
+//     by 9 experts bf16 191 / 161
 //   fp32: 64 x 128 by four wavefronts up to 4096 tiles: 16384 x 1024 x 1152 by 8 experts 314 / 407, 65536 x 1024 x 576 584 / 561
 //   up to 128 columns, where wider tiles are half empty: 128 x 128: 65536 x 72 x 320 in 8 bits 7.8 / 9.4
 template <int DT> hipError_t launch_product(const ProductArgs &a, bool f32, hipStream_t s) {
@@ -563,7 +564,7 @@ template <int DT> hipError_t launch_product(const ProductArgs &a, bool f32, hipS
     const int64_t weights = (int64_t)a.N * a.K * operand_bytes(DT);
     if (tiles(32, 128) <= 512 && (weights <= 8 << 20 || a.rows <= 128 * (int64_t)a.experts)) return launch_tile<DT, 1, 1, 2, 3>(a, f32, s);
     if (a.N <= 128) return launch_tile<DT, 2, 2, 2, 2>(a, f32, s);
-    if (tiles(64, 256) < 512 || (tiles(128, 256) > 512 && tiles(128, 256) <= 640)) return launch_tile<DT, 2, 1, 4, 2>(a, f32, s);
+    if (tiles(64, 256) < 512 || (tiles(128, 256) > 512 && tiles(128, 256) <= 640 && weights <= 8 << 20)) return launch_tile<DT, 2, 1, 4, 2>(a, f32, s);
   }
   return launch_tile<DT, 4, 1, 4, 1>(a, f32, s);
 }

@@ -55,7 +55,7 @@ __device__ __forceinline__ WgradTile wgrad_tile(const WgradArgs &a, int bm, int 
     const int rows = lane < a.experts ? a.off[lane + 1] - a.off[lane] : -1, mine = lane < a.experts ? pieces_of(rows, a.cut) : 0;
     int before = 0;   // pieces of the experts with more rows
     for (int j = 0; j < a.experts; ++j) {
-      const int other = __shfl(rows, j, kWave), pieces = __shfl(mine, j, kWave);
+      const int other = __builtin_amdgcn_readlane(rows, j), pieces = __builtin_amdgcn_readlane(mine, j);
       before += other > rows || (other == rows && j < lane) ? pieces : 0;
     }
     const unsigned long long m = __ballot(want >= before && want < before + mine);

@@ -19,10 +19,10 @@ namespace {
 template <typename T, int TPR, int PER, bool NORM>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_args a) {
   constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
-  __shared__ float s_part[TPR / kWave];
+  __shared__ float s_part[TPR > kWave ? TPR / kWave : 1];
   const int t = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
-  if (ROWS > 1 && row >= a.rows) return;   // a whole wavefront, and no barrier below where a row is one wavefront's
+  if (ROWS > 1 && row >= a.rows) return;   // all threads of a row, which only exchange among themselves
   const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
   const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.ld_residual : nullptr;
   float h[PER][8];
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_arg
 template <typename T, int TPR, int PER>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm_backward(gear_norm_backward_args a, float *__restrict__ partial) {
   constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
-  __shared__ float s_part[TPR / kWave];
+  __shared__ float s_part[TPR > kWave ? TPR / kWave : 1];
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float dg[PER][8];
 #pragma unroll
@@ -201,12 +201,17 @@ bool shape_ok(int64_t rows, int32_t dim, int32_t dtype) {
          (dtype == GEAR_F32 || dtype == GEAR_BF16);
 }
 
-// Threads of a row: a wavefront up to 2048 columns, as many as hold the row in at most 32 values each beyond.
+// Threads of a row: a quarter or half of a wavefront for rows that a whole one would not fill (42115 x 144 fp32 backward 35.5 / 22.9 us), a
+// wavefront up to 2048 columns, as many as hold the row in at most 32 values each beyond.
 template <typename T, bool NORM> hipError_t launch_norm(const gear_norm_args &a, hipStream_t s) {
-  const unsigned rows4 = (unsigned)((a.rows + 3) / 4), rows1 = (unsigned)a.rows;
-#define GEAR_NORM(TPR, PER)                                                                                        \
-  hipLaunchKernelGGL((k_rmsnorm<T, TPR, PER, NORM>), dim3(TPR == 64 ? rows4 : rows1), dim3(TPR < 256 ? 256 : TPR), 0, s, a)
-  if (a.dim <= 512)
+#define GEAR_NORM(TPR, PER)                                                                                                 \
+  hipLaunchKernelGGL((k_rmsnorm<T, TPR, PER, NORM>), dim3((unsigned)(TPR < 256 ? (a.rows * TPR + 255) / 256 : a.rows)),     \
+                     dim3(TPR < 256 ? 256 : TPR), 0, s, a)
+  if (a.dim <= 128)
+    GEAR_NORM(16, 1);
+  else if (a.dim <= 256)
+    GEAR_NORM(32, 1);
+  else if (a.dim <= 512)
     GEAR_NORM(64, 1);
   else if (a.dim <= 1024)
     GEAR_NORM(64, 2);
@@ -229,7 +234,8 @@ template <typename T, bool NORM> hipError_t launch_norm(const gear_norm_args &a,
 // bf16 204 / 197 / 228 / 202, 65536 x 1152 131 / 120 / 145 / 123 (5.0 TB/s), 16384 x 1024 28.8 / 28.0 / 28.2 / 31.6; fp32
 // 65536 x 2048 408 / 446 / 409 / 413 (5.3 TB/s), 10001 x 512 19.0 / 19.8 / 20.6 / 22.1.
 int back_blocks(int64_t rows, int32_t dim, int32_t dtype) {
-  const int64_t groups = dim <= 2048 ? (rows + 3) / 4 : rows, most = dtype == GEAR_BF16 ? 768 : 512;
+  const int at_once = dim <= 128 ? 16 : dim <= 256 ? 8 : dim <= 2048 ? 4 : 1;   // rows of a workgroup
+  const int64_t groups = (rows + at_once - 1) / at_once, most = dtype == GEAR_BF16 ? 768 : 512;
   return (int)(groups < most ? groups : most);
 }
 
@@ -237,7 +243,11 @@ template <typename T> hipError_t launch_back(const gear_norm_backward_args &a, f
   const dim3 grid(back_blocks(a.rows, a.dim, a.dtype));
 #define GEAR_BACK(TPR, PER) \
   hipLaunchKernelGGL((k_rmsnorm_backward<T, TPR, PER>), grid, dim3(TPR < 256 ? 256 : TPR), 0, s, a, partial)
-  if (a.dim <= 512)
+  if (a.dim <= 128)
+    GEAR_BACK(16, 1);
+  else if (a.dim <= 256)
+    GEAR_BACK(32, 1);
+  else if (a.dim <= 512)
     GEAR_BACK(64, 1);
   else if (a.dim <= 1024)
     GEAR_BACK(64, 2);
