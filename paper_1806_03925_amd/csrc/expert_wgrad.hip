@@ -346,16 +346,18 @@ struct WgradShape {
 WgradShape wgrad_shape(int dtype, int K) { return dtype == GEAR_F32 ? WgradShape{64, 64} : K <= 128 ? WgradShape{128, 128} : WgradShape{128, 256}; }
 int64_t wgrad_tiles(const WgradShape &t, int N, int K) { return (int64_t)((N + t.bm - 1) / t.bm) * ((K + t.bn - 1) / t.bn); }
 
-// Rows of a piece.  Two workgroups fit on each CU: 512 at a time.  Where all experts' tiles are fewer than two rounds of that, rows are
-// cut so that one layer gives one whole round, and experts, whose sizes the host does not know, pieces of one and a half
-// fair shares.  us, uncut / cut: 65536 x 1024 x 1152 by one expert 832 / 191, 16384 x 1024 x 1152 by 8 93 / 71.
+// Rows of a piece.  Two workgroups fit on each CU: 512 at a time.  (More in fp32, whose two stages leave room for five, which is
+// for short lists, all latency: 2086 x 80 x 8064 by 61 experts 170 us, with four stages 256; pieces for 1024 at a time gain
+// nothing.)  Where all experts' tiles are fewer than two rounds of that, rows are cut so that one layer gives one whole
+// round, and experts, whose sizes the host does not know, pieces of one and a half fair shares.  us, uncut / cut: 65536 x 1024 x
+// 1152 by one expert 832 / 176, 16384 x 1024 x 1152 by 8 93 / 68.
 int wgrad_cut(int dtype, int64_t rows, int experts, int N, int K) {
-  constexpr int64_t kSlots = 512;
+  constexpr int64_t slots = 512;
   const int64_t tiles = wgrad_tiles(wgrad_shape(dtype, K), N, K), whole = rows < 1 ? 1 : rows;
-  if (experts * tiles >= 2 * kSlots) return (int)whole;
-  int64_t cut = experts == 1 ? (rows + kSlots / tiles - 1) / (kSlots / tiles > 0 ? kSlots / tiles : 1) : rows * tiles * 3 / (2 * kSlots);
+  if (experts * tiles >= 2 * slots) return (int)whole;
+  int64_t cut = experts == 1 ? (rows + slots / tiles - 1) / (slots / tiles > 0 ? slots / tiles : 1) : rows * tiles * 3 / (2 * slots);
   cut = (cut + 31) / 32 * 32;
-  const int64_t least = experts == 1 ? 256 : experts * tiles < kSlots ? 512 : 1024;   // what a piece adds and writes has to be worth it
+  const int64_t least = experts == 1 ? 256 : experts * tiles < slots ? 512 : 1024;   // what a piece adds and writes has to be worth it
   if (cut < least) cut = least;
   return (int)(cut < whole ? cut : whole);
 }
@@ -404,7 +406,7 @@ extern "C" gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *
   const int64_t pieces = a->off ? a->experts + a->rows / cut : (a->rows + cut - 1) / cut;
   const unsigned blocks = wgrad_blocks((pieces > 0 ? pieces : 1) * wgrad_tiles(shape, a->N, a->K));
   if (a->dtype == GEAR_F32) {
-    if (launch<TnTile<float, 1, 1, 4>>(w, blocks, s) != hipSuccess) return GEAR_ERR_HIP;
+    if (launch<TnTile<float, 1, 1, 2>>(w, blocks, s) != hipSuccess) return GEAR_ERR_HIP;
   } else if (shape.bn == 128) {
     if (launch<TnTile<bf16_t, 2, 2, 3>>(w, blocks, s) != hipSuccess) return GEAR_ERR_HIP;
   } else {

@@ -21,62 +21,63 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_arg
   constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
   __shared__ float s_part[TPR > kWave ? TPR / kWave : 1];
   const int t = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
-  if (ROWS > 1 && row >= a.rows) return;   // all threads of a row, which only exchange among themselves
-  const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
-  const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.ld_residual : nullptr;
-  float h[PER][8];
-  float sq = 0.0f;
+  // one pass for all but lists of more rows than a launch may have threads for
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
+    const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
+    const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.ld_residual : nullptr;
+    float h[PER][8];
+    float sq = 0.0f;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int c = 8 * (t + TPR * i);
+    for (int i = 0; i < PER; ++i) {
+      const int c = 8 * (t + TPR * i);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[i][j] = 0.0f;
-    if (c < a.dim) {
-      load8(x + c, h[i]);
-      if (NORM && res) {
-        float r[8];
-        load8(res + c, r);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[i][j] += r[j];
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sq += h[i][j] * h[i][j];
-  }
-  float s = 1.0f;
-  if constexpr (NORM) s = 1.0f / sqrtf(row_sum<TPR>(sq, s_part) / (float)a.dim + a.eps);
-  const int64_t ld8 = rows8_ld(a.dim), lds = scales8_ld(a.dim);
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int c = 8 * (t + TPR * i);
-    float y[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = h[i][j];
-    if constexpr (NORM) {
+      for (int j = 0; j < 8; ++j) h[i][j] = 0.0f;
       if (c < a.dim) {
-        if (a.sum) stream8(static_cast<T *>(a.sum) + row * a.ld_sum + c, h[i]);
-        float g[8];
-        load8(a.gain + c, g);
+        load8(x + c, h[i]);
+        if (NORM && res) {
+          float r[8];
+          load8(res + c, r);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = h[i][j] * s * g[j];
+          for (int j = 0; j < 8; ++j) h[i][j] += r[j];
+        }
       }
-    }
-    if (a.q8) {
-      float top = top8(y);
 #pragma unroll
-      for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-      const int e = exponent8(top);
-      const uint2 q = pack8(y, unscale8(e));
-      if (c < ld8) {
-        *reinterpret_cast<uint2 *>(a.q8 + row * ld8 + c) = q;
-        if (t % 16 == 0) a.scale[row * lds + c / kBlock8] = (uint8_t)(e + 127);
-      }
-      unpack8(q, scale8(e), y);
+      for (int j = 0; j < 8; ++j) sq += h[i][j] * h[i][j];
     }
-    if (a.y && c < a.dim) stream8(static_cast<T *>(a.y) + row * a.ld_y + c, y);
+    float s = 1.0f;
+    if constexpr (NORM) s = 1.0f / sqrtf(row_sum<TPR>(sq, s_part) / (float)a.dim + a.eps);
+    const int64_t ld8 = rows8_ld(a.dim), lds = scales8_ld(a.dim);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = 8 * (t + TPR * i);
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = h[i][j];
+      if constexpr (NORM) {
+        if (c < a.dim) {
+          if (a.sum) stream8(static_cast<T *>(a.sum) + row * a.ld_sum + c, h[i]);
+          float g[8];
+          load8(a.gain + c, g);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = h[i][j] * s * g[j];
+        }
+      }
+      if (a.q8) {
+        float top = top8(y);
+#pragma unroll
+        for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+        const int e = exponent8(top);
+        const uint2 q = pack8(y, unscale8(e));
+        if (c < ld8) {
+          *reinterpret_cast<uint2 *>(a.q8 + row * ld8 + c) = q;
+          if (t % 16 == 0) a.scale[row * lds + c / kBlock8] = (uint8_t)(e + 127);
+        }
+        unpack8(q, scale8(e), y);
+      }
+      if (a.y && c < a.dim) stream8(static_cast<T *>(a.y) + row * a.ld_y + c, y);
+    }
+    if (a.q8 && t < lds - ld8 / kBlock8) a.scale[row * lds + ld8 / kBlock8 + t] = 0;   // behind the last block: not used
   }
-  if (a.q8 && t < lds - ld8 / kBlock8) a.scale[row * lds + ld8 / kBlock8 + t] = 0;   // behind the last block: not used
 }
 
 // Backward pass.  A workgroup takes rows blockIdx.x * ROWS + threadIdx.x / TPR + k gridDim.x * ROWS and keeps its share of
@@ -204,9 +205,13 @@ bool shape_ok(int64_t rows, int32_t dim, int32_t dtype) {
 // Threads of a row: a quarter or half of a wavefront for rows that a whole one would not fill (42115 x 144 fp32 backward 35.5 / 22.9 us), a
 // wavefront up to 2048 columns, as many as hold the row in at most 32 values each beyond.
 template <typename T, bool NORM> hipError_t launch_norm(const gear_norm_args &a, hipStream_t s) {
-#define GEAR_NORM(TPR, PER)                                                                                                 \
-  hipLaunchKernelGGL((k_rmsnorm<T, TPR, PER, NORM>), dim3((unsigned)(TPR < 256 ? (a.rows * TPR + 255) / 256 : a.rows)),     \
-                     dim3(TPR < 256 ? 256 : TPR), 0, s, a)
+  constexpr int64_t kMost = 1 << 21;   // workgroups: threads are counted in 32 bits
+#define GEAR_NORM(TPR, PER)                                                                                            \
+  do {                                                                                                                 \
+    const int64_t blocks = TPR < 256 ? (a.rows * TPR + 255) / 256 : a.rows;                                            \
+    hipLaunchKernelGGL((k_rmsnorm<T, TPR, PER, NORM>), dim3((unsigned)(blocks < kMost ? blocks : kMost)),              \
+                       dim3(TPR < 256 ? 256 : TPR), 0, s, a);                                                          \
+  } while (0)
   if (a.dim <= 128)
     GEAR_NORM(16, 1);
   else if (a.dim <= 256)

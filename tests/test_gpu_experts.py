@@ -604,3 +604,14 @@ def test_refusals(g):
         with pytest.raises(g.GearError) as e:
             call()
         assert e.value.code == g.GEAR_ERR_INVALID, i
+
+
+def test_more_rows_than_threads_of_a_launch(g):
+    """2^21 workgroups of a row each and some more: the first ones take a second row."""
+    rows = (1 << 21) + 5
+    x = torch.zeros(rows, 2056, dtype=BF16, device="cuda")
+    tail = torch.randn(6, 2056, device="cuda", generator=gen(12)).to(BF16)
+    x[-6:] = tail
+    gain = torch.ones(2056, device="cuda")
+    g.gear_rmsnorm(x, gain, 1e-6, out=g.NormOutput(None, x, None))
+    assert torch.equal(x[-6:], g.gear_rmsnorm(tail, gain, 1e-6).y) and not x[:-6].any()
