@@ -22,7 +22,12 @@ struct WgradTile {
   bool have, bad;
 };
 
+// An expert's rows are as many pieces as its rows need at `cut` rows each, all of them as long, in whole stages.
 __device__ __forceinline__ int pieces_of(int rows, int cut) { return max((rows + cut - 1) / cut, 1); }   // no rows: zeros to write
+__device__ __forceinline__ int piece_rows(int rows, int cut) {
+  const int pieces = pieces_of(rows, cut);
+  return ((rows + pieces - 1) / pieces + 31) / 32 * 32;
+}
 
 // partial results in front of those of expert e: the pieces of all experts before it that are cut
 __device__ __forceinline__ int partials_before(const int32_t *__restrict__ off, int e, int cut, int lane) {
@@ -82,7 +87,8 @@ __device__ __forceinline__ WgradTile wgrad_tile(const WgradArgs &a, int bm, int 
   if (e < 0) return r;
   const int first = a.off ? a.off[e] : 0, last = a.off ? a.off[e + 1] : a.rows;
   r.m0 = tile / k_tiles * bm, r.n0 = tile % k_tiles * bn, r.have = true;
-  r.first = first + piece * a.cut, r.last = r.first + min(last - r.first, a.cut);
+  const int step = piece_rows(last - first, a.cut);
+  r.first = min(last, first + piece * step), r.last = r.first + min(last - r.first, step);   // rounding up may leave the last piece nothing
   r.dst = a.dw + (int64_t)e * a.N * a.K;
   if (last - first > a.cut) {
     const int before = a.off ? __builtin_amdgcn_readfirstlane(partials_before(a.off, e, a.cut, lane)) : 0;
@@ -92,6 +98,7 @@ __device__ __forceinline__ WgradTile wgrad_tile(const WgradArgs &a, int bm, int 
 }
 
 // dw of the experts that were cut: their pieces in ascending order
+constexpr int kAtOnce = 8;
 __global__ void __launch_bounds__(256) k_wgrad_sum(WgradArgs a) {
   const int lane = threadIdx.x & 63, e = blockIdx.y;
   if (a.off && !offsets_ok(a.off, a.experts, a.rows, lane)) return;
@@ -103,9 +110,12 @@ __global__ void __launch_bounds__(256) k_wgrad_sum(WgradArgs a) {
   float4 *o = reinterpret_cast<float4 *>(a.dw) + e * vec;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < vec; i += (int64_t)gridDim.x * 256) {
     float4 v = p[i];
-    for (int z = 1; z < pieces; ++z) {
-      const float4 w = p[z * vec + i];
-      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    for (int z = 1; z < pieces; z += kAtOnce) {   // several on their way at a time, added in ascending order
+      float4 w[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) w[k] = z + k < pieces ? p[(z + k) * vec + i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) v.x += w[k].x, v.y += w[k].y, v.z += w[k].z, v.w += w[k].w;
     }
     o[i] = v;
   }
@@ -349,13 +359,14 @@ int64_t wgrad_tiles(const WgradShape &t, int N, int K) { return (int64_t)((N + t
 // Rows of a piece.  Two workgroups fit on each CU: 512 at a time.  (More in fp32, whose two stages leave room for five, which is
 // for short lists, all latency: 2086 x 80 x 8064 by 61 experts 170 us, with four stages 256; pieces for 1024 at a time gain
 // nothing.)  Where all experts' tiles are fewer than two rounds of that, rows are cut so that one layer gives one whole
-// round, and experts, whose sizes the host does not know, pieces of one and a half fair shares.  us, uncut / cut: 65536 x 1024 x
-// 1152 by one expert 832 / 176, 16384 x 1024 x 1152 by 8 93 / 68.
+// round, and experts, whose sizes the host does not know, pieces of up to two fair shares (fp32 one and a half).  us, uncut / cut:
+// 65536 x 1024 x 1152 by one expert 832 / 180, 16384 x 1024 x 1152 by 8 uneven ones 93 / 74, by 8 even ones 64 (one and a half
+// fair shares: 72 and 94), fp32 16384 x 512 x 576 by 8 103 (two: 135).
 int wgrad_cut(int dtype, int64_t rows, int experts, int N, int K) {
   constexpr int64_t slots = 512;
   const int64_t tiles = wgrad_tiles(wgrad_shape(dtype, K), N, K), whole = rows < 1 ? 1 : rows;
   if (experts * tiles >= 2 * slots) return (int)whole;
-  int64_t cut = experts == 1 ? (rows + slots / tiles - 1) / (slots / tiles > 0 ? slots / tiles : 1) : rows * tiles * 3 / (2 * slots);
+  int64_t cut = experts == 1 ? (rows + slots / tiles - 1) / (slots / tiles > 0 ? slots / tiles : 1) : rows * tiles * (dtype == GEAR_F32 ? 3 : 4) / (2 * slots);
   cut = (cut + 31) / 32 * 32;
   const int64_t least = experts == 1 ? 256 : experts * tiles < slots ? 512 : 1024;   // what a piece adds and writes has to be worth it
   if (cut < least) cut = least;

@@ -330,9 +330,11 @@ extern "C" gear_status gear_rmsnorm_backward(const gear_norm_backward_args *a, v
     if (workspace_bytes < gear_norm_backward_workspace_bytes(a->rows, a->dim)) return GEAR_ERR_CAPACITY;
     partial = static_cast<float *>(workspace);
   }
+  const bool alone = a->dgain && back_blocks(a->rows, a->dim, a->dtype) == 1;   // one workgroup's share is the sum
+  if (alone) partial = a->dgain;
   const hipError_t err = a->dtype == GEAR_BF16 ? launch_back<bf16_t>(*a, partial, s) : launch_back<float>(*a, partial, s);
   if (err != hipSuccess) return GEAR_ERR_HIP;
-  if (a->dgain) {
+  if (a->dgain && !alone) {
     hipLaunchKernelGGL(k_sum_rows, dim3((a->dim + 63) / 64), dim3(1024), 0, s, partial, back_blocks(a->rows, a->dim, a->dtype), a->dim, a->dgain);
     if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
   }
