@@ -117,9 +117,26 @@ __device__ __forceinline__ void store_tile(const f32x16_v (&acc)[C::WTM][TN], bf
                 make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
         }
     }
-  } else {   // through a patch of 32 rows x 64 columns, so that a lane stores 16 bytes and a row leaves as one 128-byte line
+  } else {   // through a patch of 32 rows x 64 columns, so that a lane stores 16 bytes and a row leaves as 128 bytes
     bf16_t *o = static_cast<bf16_t *>(out);
     const int prow = lane >> 3, cv = (lane & 7) * 8;
+    // Past the L2, which keeps the operands that other tiles share, where these are whole lines: us through it / past it, 65536 x
+    // 1024 x 1152 in 8 bits 71.5 / 67.7, but 30000 x 4240 x 64, whose rows end inside lines that it puts together, 49.5 / 98.6.
+    const bool lines = (ld & 63) == 0 && ((uintptr_t)out & 127) == 0;
+    auto store = [&](int i, auto past) {
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int row = it * 8 + prow, m = m0 + i * 32 + row;
+        const uint4 v = *reinterpret_cast<const uint4 *>(patch + row * PATCH_LD + cv);
+        u32x4_v *dst = reinterpret_cast<u32x4_v *>(o + m * ld + n0 + cv);
+        if (m < m_end && n0 + cv < N) {
+          if constexpr (decltype(past)::value)
+            __builtin_nontemporal_store(u32x4_v{v.x, v.y, v.z, v.w}, dst);
+          else
+            *dst = u32x4_v{v.x, v.y, v.z, v.w};
+        }
+      }
+    };
 #pragma unroll
     for (int i = 0; i < C::WTM; ++i) {
 #pragma unroll
@@ -129,12 +146,11 @@ __device__ __forceinline__ void store_tile(const f32x16_v (&acc)[C::WTM][TN], bf
           *reinterpret_cast<uint2 *>(patch + c * PATCH_LD + j * 32 + 8 * q + 4 * g) =
               make_uint2(pack_bf16(acc[i][j][4 * q], acc[i][j][4 * q + 1]), pack_bf16(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
       __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int it = 0; it < 4; ++it) {
-        const int row = it * 8 + prow, m = m0 + i * 32 + row;
-        const uint4 v = *reinterpret_cast<const uint4 *>(patch + row * PATCH_LD + cv);
-        if (m < m_end && n0 + cv < N)
-          __builtin_nontemporal_store(u32x4_v{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_v *>(o + m * ld + n0 + cv));
+      if (lines) {
+        store(i, std::true_type{});
+        asm volatile("" ::: "memory");   // the compiler would make one of both kinds of store, the plain one
+      } else {
+        store(i, std::false_type{});
       }
       __builtin_amdgcn_wave_barrier();
     }

@@ -2,8 +2,12 @@
 // number only the device knows.  A workgroup takes one tile of one expert's gradient and walks all of that expert's rows.
 #include "experts.hpp"
 
+#include <type_traits>
+
 namespace gear {
 namespace {
+
+typedef float f32x4_v __attribute__((ext_vector_type(4)));
 
 struct WgradArgs {
   const void *dy, *x;
@@ -329,19 +333,46 @@ template <typename C> __device__ __forceinline__ void wgrad_wide(const WgradArgs
       fill = fill + 1 == C::STAGES ? 0 : fill + 1;
     }
   }
-  float *dst = t.dst;
+  // Results leave through a patch of 32 rows for each wavefront, so that a store instruction writes two rows of 512 bytes, past
+  // the L2, which keeps the operands that other tiles share.  us of 9 experts, straight from the accumulators (128 bytes a row at a
+  // time) / so: 9216 x 4576 x 1720, whose rows end inside lines, 216 / 165, x 4608 x 1792 170 / 158, 65536 x 2048 x 1024 by 64 387 / 371.
+  // Short lists of rows share nothing, and the L2 puts their lines together: 144 x 4576 x 1720 past it 79, through it 53
+  // (but 4608 x 4576 x 1720 111 and 141).
+  static_assert(C::WAVES * 32 * C::TN * 32 * 4 <= C::STAGES * C::STAGE_BYTES && C::TN == 4, "patches fit, rows of 128 columns");
+  wait_vm<0>();
+  __syncthreads();   // all reads of the stages are done
+  float *patch = reinterpret_cast<float *>(lds) + wave * 32 * 32 * C::TN;
   const int c = lane & 31, g = lane >> 5;
-  const int mw = m0 + wm * 32 * C::TM + 4 * g, nw = n0 + wn * 32 * C::TN + c;
-  const bool whole = m0 + C::BM <= a.N && n0 + C::BN <= a.K;   // no test for every store
+  const int n = n0 + wn * 32 * C::TN + 4 * c;
 #pragma unroll
-  for (int i = 0; i < C::TM; ++i)
+  for (int i = 0; i < C::TM; ++i) {
 #pragma unroll
     for (int j = 0; j < C::TN; ++j)
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        const int m = mw + i * 32 + 8 * (q / 4) + q % 4, n = nw + j * 32;
-        if (whole || (m < a.N && n < a.K)) __builtin_nontemporal_store(acc[i][j][q], dst + (int64_t)m * a.K + n);
+      for (int q = 0; q < 16; ++q) patch[(8 * (q / 4) + 4 * g + q % 4) * 128 + j * 32 + c] = acc[i][j][q];
+    __builtin_amdgcn_wave_barrier();
+    const int m = m0 + (wm * C::TM + i) * 32 + g;
+    f32x4_v *dst = reinterpret_cast<f32x4_v *>(t.dst + (int64_t)m * a.K + n);
+    auto store = [&](auto past) {
+#pragma unroll
+      for (int r = 0; r < 32; r += 2) {
+        const f32x4_v v = *reinterpret_cast<const f32x4_v *>(patch + (r + g) * 128 + 4 * c);
+        if (m + r < a.N && n < a.K) {
+          if constexpr (decltype(past)::value)
+            __builtin_nontemporal_store(v, dst + (int64_t)r * a.K / 4);
+          else
+            dst[(int64_t)r * a.K / 4] = v;
+        }
       }
+    };
+    if (last - first > 128) {
+      store(std::true_type{});
+      asm volatile("" ::: "memory");   // the compiler would make one of both kinds of store, the plain one
+    } else {
+      store(std::false_type{});
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 template <typename C> __global__ void __launch_bounds__(C::THREADS, C::TM * C::TN > 8 ? 1 : 2) k_expert_wgrad_wide(WgradArgs a) {
