@@ -323,7 +323,8 @@ gear_status gear_gemm(int32_t dtype, int32_t form, const void *A, const void *B,
  * As elsewhere: device memory of the caller's, no allocation, nothing kept between calls, kernels enqueued on `stream`,
  * results independent of how the device schedules its work.  Widths (dim, K, N) are multiples of 8; the distance
  * between rows (ld_*, in elements) is a multiple of 8 and at least the width, below 2^20; matrices start on 16 bytes.
- * A call on no rows does nothing but what it says it does then.  Sums are fp32 (norms of lists of gradients: fp64).
+ * A call on no rows does nothing but what it says it does then.  Sums are fp32 (norms of lists of gradients
+ * and norms in 8 bits: fp64).
  *
  * 8 bits.  A row of `dim` values in 8 bits is gear_rows8_ld(dim) bytes of e4m3 (4 exponent, 3 fraction bits, largest
  * 448, no infinity), whole blocks of 128 with zeros behind the row's end, and gear_scales8_ld(dim) scale bytes, one for

@@ -86,6 +86,15 @@ __device__ __forceinline__ int exponent8(float top) {
 __device__ __forceinline__ float unscale8(int e) { return __uint_as_float((uint32_t)(127 - e) << 23); }
 __device__ __forceinline__ float scale8(int e) { return __uint_as_float(e == -127 ? 0x00400000u : (uint32_t)(127 + e) << 23); }
 
+// v rounded to odd: towards zero, the last bit set if that lost anything.  What is rounded to fewer bits after that comes out as if v
+// itself had been, and no v is taken for a border (448 2^e, a tie) that it is not on.
+__device__ __forceinline__ float round_odd(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  uint32_t lo = (uint32_t)u;
+  lo = (lo & 0xe0000000u) | ((lo & 0x1fffffffu) ? 0x20000000u : 0u);   // 23 of 52 fraction bits are left
+  return (float)__longlong_as_double((long long)((u & 0xffffffff00000000ull) | lo));
+}
+
 // eight values times 2^-e as e4m3.  Scaled finite values are at most 448, so the conversion never saturates; infinities
 // are turned into NaN first, for which e4m3 has a code.
 __device__ __forceinline__ uint2 pack8(const float (&v)[8], float unscale) {
@@ -112,14 +121,14 @@ __device__ __forceinline__ void unpack8(uint2 q, float scale, float (&v)[8]) {
 
 // Sum over the TPR threads of a row, the same value in all of them: within a wavefront by exchange, between wavefronts
 // through s_part [TPR / 64] in ascending order.  TPR > 64: every thread of the workgroup takes part.
-template <int TPR> __device__ __forceinline__ float row_sum(float v, float *s_part) {
+template <int TPR, typename V> __device__ __forceinline__ V row_sum(V v, V *s_part) {
 #pragma unroll
   for (int o = (TPR < kWave ? TPR : kWave) / 2; o; o >>= 1) v += __shfl_xor(v, o, kWave);
   if constexpr (TPR > kWave) {
     __syncthreads();   // the last sum has been read by everybody
     if ((threadIdx.x & 63) == 0) s_part[threadIdx.x / kWave] = v;
     __syncthreads();
-    v = 0.0f;
+    v = 0;
 #pragma unroll
     for (int w = 0; w < TPR / kWave; ++w) v += s_part[w];
   }

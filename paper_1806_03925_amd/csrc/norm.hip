@@ -5,64 +5,86 @@
 //
 // (dx: y_c depends on h_c directly, s a, and on all of h through s, whose derivative by h_c is -s^3 h_c / dim.)
 // Every call is one pass over its rows: a row stays in the registers of the threads that read it, from the sum of its
-// squares to the last output, so what bounds these kernels is the memory they have to read and write.  10001 x 1152 bf16 with
-// residual into sum, y and 8 bits: 20.3 us, 5.1 TB/s (22.2 with results through the L2).
+// squares to the last output, so what bounds these kernels is the memory they have to read and write (the norm in 8 bits: fp64,
+// see there).
 #include "eight.hpp"
 
 #include <cmath>
+#include <type_traits>
 
 namespace gear {
 namespace {
 
 // A row belongs to TPR threads with PER pieces of eight values each, piece i of thread t at columns 8 (t + TPR i): a
 // wavefront's accesses are contiguous, and 16 neighbouring threads hold a block of 128 columns.
-template <typename T, int TPR, int PER, bool NORM>
+//
+// KIND: what is made of a row, the norm itself, the norm in 8 bits, or the row in 8 bits.  The 8 bits of the norm are rounded once,
+// from fp64: its fp32 value depends in the last bits on how the row was added up, and next to a tie they decide a whole step of the
+// 8 bits, 2^-4 of the value.  10001 x 1152 bf16 with residual into sum, y and 8 bits: 25.3 us, the same
+// reads and writes from fp32 18.9 us (5.4 TB/s): what is over is the arithmetic in fp64.
+enum NormKind { kNorm, kNorm8, kRows8 };
+
+template <typename T, int TPR, int PER, NormKind KIND>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_args a) {
+  using V = typename std::conditional<KIND == kNorm8, double, float>::type;
   constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
-  __shared__ float s_part[TPR > kWave ? TPR / kWave : 1];
+  __shared__ V s_part[TPR > kWave ? TPR / kWave : 1];
   const int t = threadIdx.x % TPR;
   // one pass for all but lists of more rows than a launch may have threads for
   for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
     const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
-    const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.ld_residual : nullptr;
-    float h[PER][8];
-    float sq = 0.0f;
+    const T *res = KIND != kRows8 && a.residual ? static_cast<const T *>(a.residual) + row * a.ld_residual : nullptr;
+    Raw8<T> xs[PER], rs[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = 8 * (t + TPR * i);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[i][j] = 0.0f;
+      xs[i].zero(), rs[i].zero();
       if (c < a.dim) {
-        load8(x + c, h[i]);
-        if (NORM && res) {
-          float r[8];
-          load8(res + c, r);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) h[i][j] += r[j];
-        }
+        xs[i].load(x + c);
+        if (res) rs[i].load(res + c);
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sq += h[i][j] * h[i][j];
     }
-    float s = 1.0f;
-    if constexpr (NORM) s = 1.0f / sqrtf(row_sum<TPR>(sq, s_part) / (float)a.dim + a.eps);
+    auto piece = [&](int i, V (&h)[8]) {
+      float v[8], r[8];
+      xs[i].get(v);
+      rs[i].get(r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = KIND == kRows8 ? (V)v[j] : (V)v[j] + (V)r[j];
+    };
+    V s = 1;
+    if constexpr (KIND != kRows8) {
+      V sq = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        V h[8];
+        piece(i, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sq += h[j] * h[j];
+      }
+      s = (V)1 / sqrt(row_sum<TPR>(sq, s_part) / (V)a.dim + (V)a.eps);
+    }
     const int64_t ld8 = rows8_ld(a.dim), lds = scales8_ld(a.dim);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = 8 * (t + TPR * i);
+      V h[8];
       float y[8];
+      piece(i, h);
+      if (KIND != kRows8 && c < a.dim) {
+        float g[8];
+        load8(a.gain + c, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = h[i][j];
-      if constexpr (NORM) {
-        if (c < a.dim) {
-          if (a.sum) stream8(static_cast<T *>(a.sum) + row * a.ld_sum + c, h[i]);
-          float g[8];
-          load8(a.gain + c, g);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = h[i][j] * s * g[j];
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (KIND == kNorm8)
+            y[j] = round_odd(h[j] * s * (V)g[j]);
+          else
+            y[j] = h[j] * s * g[j];
         }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = (float)h[j];
       }
-      if (a.q8) {
+      if constexpr (KIND != kNorm) {
         float top = top8(y);
 #pragma unroll
         for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
@@ -72,11 +94,18 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_arg
           *reinterpret_cast<uint2 *>(a.q8 + row * ld8 + c) = q;
           if (t % 16 == 0) a.scale[row * lds + c / kBlock8] = (uint8_t)(e + 127);
         }
-        unpack8(q, scale8(e), y);
+        if constexpr (KIND == kNorm8) unpack8(q, scale8(e), y);
       }
-      if (a.y && c < a.dim) stream8(static_cast<T *>(a.y) + row * a.ld_y + c, y);
+      if (KIND == kRows8 || c >= a.dim) continue;
+      if (a.sum) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (float)h[j];
+        stream8(static_cast<T *>(a.sum) + row * a.ld_sum + c, v);
+      }
+      if (a.y) stream8(static_cast<T *>(a.y) + row * a.ld_y + c, y);
     }
-    if (a.q8 && t < lds - ld8 / kBlock8) a.scale[row * lds + ld8 / kBlock8 + t] = 0;   // behind the last block: not used
+    if (KIND != kNorm && t < lds - ld8 / kBlock8) a.scale[row * lds + ld8 / kBlock8 + t] = 0;   // behind the last block: not used
   }
 }
 
@@ -204,12 +233,12 @@ bool shape_ok(int64_t rows, int32_t dim, int32_t dtype) {
 
 // Threads of a row: a quarter or half of a wavefront for rows that a whole one would not fill (42115 x 144 fp32 backward 35.5 / 22.9 us), a
 // wavefront up to 2048 columns, as many as hold the row in at most 32 values each beyond.
-template <typename T, bool NORM> hipError_t launch_norm(const gear_norm_args &a, hipStream_t s) {
+template <typename T, NormKind KIND> hipError_t launch_norm(const gear_norm_args &a, hipStream_t s) {
   constexpr int64_t kMost = 1 << 21;   // workgroups: threads are counted in 32 bits
 #define GEAR_NORM(TPR, PER)                                                                                            \
   do {                                                                                                                 \
     const int64_t blocks = TPR < 256 ? (a.rows * TPR + 255) / 256 : a.rows;                                            \
-    hipLaunchKernelGGL((k_rmsnorm<T, TPR, PER, NORM>), dim3((unsigned)(blocks < kMost ? blocks : kMost)),              \
+    hipLaunchKernelGGL((k_rmsnorm<T, TPR, PER, KIND>), dim3((unsigned)(blocks < kMost ? blocks : kMost)),              \
                        dim3(TPR < 256 ? 256 : TPR), 0, s, a);                                                          \
   } while (0)
   if (a.dim <= 128)
@@ -289,7 +318,9 @@ extern "C" gear_status gear_rmsnorm(const gear_norm_args *a, void *stream) {
   if (a->sum && a->sum == a->y) return GEAR_ERR_INVALID;
   if (!aligned(a->q8, 16) || !aligned(a->scale, 4)) return GEAR_ERR_INVALID;
   hipStream_t s = (hipStream_t)stream;
-  const hipError_t err = a->dtype == GEAR_BF16 ? launch_norm<bf16_t, true>(*a, s) : launch_norm<float, true>(*a, s);
+  const bool bf16 = a->dtype == GEAR_BF16;
+  const hipError_t err = a->q8 ? bf16 ? launch_norm<bf16_t, kNorm8>(*a, s) : launch_norm<float, kNorm8>(*a, s)
+                               : bf16 ? launch_norm<bf16_t, kNorm>(*a, s) : launch_norm<float, kNorm>(*a, s);
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
 }
 
@@ -301,7 +332,7 @@ extern "C" gear_status gear_rows8(const void *x, int32_t dtype, int64_t ld_x, in
   gear_norm_args a = {};
   a.rows = rows, a.dim = dim, a.dtype = dtype, a.x = x, a.ld_x = ld_x, a.q8 = q8, a.scale = scale;
   hipStream_t s = (hipStream_t)stream;
-  const hipError_t err = dtype == GEAR_BF16 ? launch_norm<bf16_t, false>(a, s) : launch_norm<float, false>(a, s);
+  const hipError_t err = dtype == GEAR_BF16 ? launch_norm<bf16_t, kRows8>(a, s) : launch_norm<float, kRows8>(a, s);
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
 }
 

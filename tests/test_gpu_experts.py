@@ -615,3 +615,22 @@ def test_more_rows_than_threads_of_a_launch(g):
     gain = torch.ones(2056, device="cuda")
     g.gear_rmsnorm(x, gain, 1e-6, out=g.NormOutput(None, x, None))
     assert torch.equal(x[-6:], g.gear_rmsnorm(tail, gain, 1e-6).y) and not x[:-6].any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,dim", [(700, 1152), (300, 72), (40, 5000), (9, 12000)])
+def test_norm_in_8_bits_is_rounded_once(g, dtype, rows, dim):
+    """The 8 bits are those nearest to the norm in 64 bits, scales too: 64-bit sums differ in the last bits only, and no value of
+    these lies that near to a border."""
+    r = gen(rows + 2 * dim)
+    x = (torch.randn(rows, dim, device="cuda", generator=r) * torch.exp(torch.randn(rows, 1, device="cuda", generator=r))).to(dtype)
+    res = torch.randn(rows, dim, device="cuda", generator=r).to(dtype)
+    gain = 1 + 0.3 * torch.randn(dim, device="cuda", generator=r)
+    _, y = norm_ref(x, res, gain, float(torch.tensor(1e-6)))
+    out = g.gear_rmsnorm(x, gain, 1e-6, residual=res, q8=True)
+    e = exponents(y)
+    assert torch.equal(out.rows8.scale[:, :e.shape[1]].long() - 127, e)
+    unit = torch.exp2(e.double()).repeat_interleave(128, 1)
+    want = nearest8(torch.nn.functional.pad(y, (0, -dim % 128)) / unit)
+    within(out.rows8.q.view(torch.float8_e4m3fn).double(), want, 0.0)
+    within(out.y, (want * unit)[:, :dim], 0.0)
