@@ -399,7 +399,10 @@ int wgrad_cut(int dtype, int64_t rows, int experts, int N, int K) {
   if (experts * tiles >= 2 * slots) return (int)whole;
   int64_t cut = experts == 1 ? (rows + slots / tiles - 1) / (slots / tiles > 0 ? slots / tiles : 1) : rows * tiles * (dtype == GEAR_F32 ? 3 : 4) / (2 * slots);
   cut = (cut + 31) / 32 * 32;
-  const int64_t least = experts == 1 ? 256 : experts * tiles < slots ? 512 : 1024;   // what a piece adds and writes has to be worth it
+  // What a piece adds and writes has to be worth it.  us with 128 / 256 / 512 rows at least, fp32: 1000 x 72 x 320 by 5 11 / 13 / 14,
+  // 8000 x 64 x 64 by 16 12 / 14 / 19, 1000 x 72 x 320 by one 10 / 12 / 16; bf16: 2000 x 512 x 576 by 8 26 / 19 / 17, 1000 x 1024 x 1152
+  // by one 25 / 22 / 21.
+  const int64_t least = dtype == GEAR_F32 ? 128 : experts == 1 ? 256 : experts * tiles < slots ? 512 : 1024;
   if (cut < least) cut = least;
   return (int)(cut < whole ? cut : whole);
 }

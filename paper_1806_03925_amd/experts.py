@@ -251,7 +251,7 @@ def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, row
         _vector(status, where, "status", torch.int32, 1)
         status = status.data_ptr()
     if out is None:
-        out, ld_out = torch.empty((rows, n), dtype=out_dtype, device=device), n
+        out, ld_out = torch.empty(rows, n, dtype=out_dtype, device=device), n
     else:
         ld_out = _matrix(out, where, "out", None, (rows, n))
     a = gear_expert_args(dtype, _CODE[out.dtype], rows, k, n, experts, p_x, p_x_scale, packed, p_w_scale, off, out.data_ptr(), ld_x, ld_out,
@@ -309,7 +309,7 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     if status is not None:
         _vector(status, where, "status", torch.int32, 1)
     if dw is None:
-        dw = torch.empty((experts, n, k), dtype=torch.float32, device=device)
+        dw = torch.empty(experts, n, k, dtype=torch.float32, device=device)
     else:
         _vector(dw, where, "dw", torch.float32, experts * n * k)
     dtype = _CODE[x.dtype]
