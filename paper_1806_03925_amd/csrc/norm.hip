@@ -20,12 +20,13 @@ namespace {
 //
 // KIND: what is made of a row, the norm itself, the norm in 8 bits, or the row in 8 bits.  The 8 bits of the norm are rounded once,
 // from fp64: its fp32 value depends in the last bits on how the row was added up, and next to a tie they decide a whole step of the
-// 8 bits, 2^-4 of the value.  10001 x 1152 bf16 with residual into sum, y and 8 bits: 25.3 us, the same
-// reads and writes from fp32 18.9 us (5.4 TB/s): what is over is the arithmetic in fp64.
+// 8 bits, 2^-4 of the value.  10001 x 1152 bf16 with residual into sum, y and 8 bits: 23.5 us (24.4 with
+// the registers that the compiler takes by itself, which leave three wavefronts a SIMD), the same reads and writes from fp32 18.9 us
+// (5.4 TB/s): what is over is the arithmetic in fp64.
 enum NormKind { kNorm, kNorm8, kRows8 };
 
 template <typename T, int TPR, int PER, NormKind KIND>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_args a) {
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, KIND == kNorm8 && TPR <= 256 ? 4 : 1) k_rmsnorm(gear_norm_args a) {
   using V = typename std::conditional<KIND == kNorm8, double, float>::type;
   constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
   __shared__ V s_part[TPR > kWave ? TPR / kWave : 1];
@@ -56,6 +57,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_arg
       V sq = 0;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
+        if (i > 0 && 8 * TPR * i >= a.dim) break;
         V h[8];
         piece(i, h);
 #pragma unroll
@@ -67,6 +69,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm(gear_norm_arg
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = 8 * (t + TPR * i);
+      if (i > 0 && 8 * TPR * i >= a.dim) break;
       V h[8];
       float y[8];
       piece(i, h);
