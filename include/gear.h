@@ -345,7 +345,7 @@ int64_t gear_scales8_ld(int32_t dim);
  * Outputs, each NULL where it is not wanted, one at least: sum = h (of `dtype`, may be x or residual itself), y (of
  * `dtype`), and q8 with scale, y in 8 bits.  With both y and q8, y holds what the 8 bits stand for (as far as `dtype`
  * holds it), so that gradients can be taken of what the 8-bit product saw.  y may be x or residual itself unless sum is the same.
- * gain [dim] fp32, 16-byte aligned; eps >= 0; dim at most GEAR_MAX_NORM_DIM.  The norm is that of the unrounded h. */
+ * gain [dim] fp32, 16-byte aligned; eps >= 0; dim at most GEAR_MAX_NORM_DIM.  The norm is that of h before it is rounded to `dtype`. */
 typedef struct {
   int64_t rows;
   int32_t dim, dtype;    /* gear_dtype of x, residual, sum and y */

@@ -20,15 +20,19 @@ namespace {
 //
 // KIND: what is made of a row, the norm itself, the norm in 8 bits, or the row in 8 bits.  The 8 bits of the norm are rounded once,
 // from fp64: its fp32 value depends in the last bits on how the row was added up, and next to a tie they decide a whole step of the
-// 8 bits, 2^-4 of the value.  10001 x 1152 bf16 with residual into sum, y and 8 bits: 23.5 us (24.4 with
-// the registers that the compiler takes by itself, which leave three wavefronts a SIMD), the same reads and writes from fp32 18.9 us
-// (5.4 TB/s): what is over is the arithmetic in fp64.
+// 8 bits, 2^-4 of the value.  10001 x 1152 bf16 with residual into sum, y and 8 bits: 21.7 us, the same reads and writes from fp32
+// 18.9 us (5.4 TB/s): what is over is the arithmetic in fp64.  (h itself is fp32 where x is bf16: exact, unless one of both is 2^16
+// times the other, and off by 2^-24 then.  With that sum in fp64, too, 20000 x 1152 without residual took 38.9 us for 34.3.)
 enum NormKind { kNorm, kNorm8, kRows8 };
 
+// Wavefronts a SIMD that the compiler has to leave room for, which takes fp64 pieces apart again rather than keeping them: 4, us without:
+// 10001 x 1152 bf16 24.4 / 23.5, 15198 x 7664 158 / 140.  Not where pieces are 32 fp32 values: 20000 x 1152 86 with it, 72 without.
+constexpr int simd_waves(NormKind kind, int tpr, int per, int size) { return kind == kNorm8 && tpr <= 256 && (per < 4 || size == 2) ? 4 : 1; }
+
 template <typename T, int TPR, int PER, NormKind KIND>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, KIND == kNorm8 && TPR <= 256 ? 4 : 1) k_rmsnorm(gear_norm_args a) {
+__global__ void __launch_bounds__(TPR <= kWave ? 256 : TPR, simd_waves(KIND, TPR, PER, sizeof(T))) k_rmsnorm(gear_norm_args a) {
   using V = typename std::conditional<KIND == kNorm8, double, float>::type;
-  constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+  constexpr int THREADS = TPR <= kWave ? 256 : TPR, ROWS = THREADS / TPR;
   __shared__ V s_part[TPR > kWave ? TPR / kWave : 1];
   const int t = threadIdx.x % TPR;
   // one pass for all but lists of more rows than a launch may have threads for
@@ -50,7 +54,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, KIND == kNorm8 && TPR <
       xs[i].get(v);
       rs[i].get(r);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[j] = KIND == kRows8 ? (V)v[j] : (V)v[j] + (V)r[j];
+      for (int j = 0; j < 8; ++j) h[j] = KIND == kRows8 ? (V)v[j] : sizeof(T) == 2 ? (V)(v[j] + r[j]) : (V)v[j] + (V)r[j];
     };
     V s = 1;
     if constexpr (KIND != kRows8) {
@@ -115,8 +119,8 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, KIND == kNorm8 && TPR <
 // Backward pass.  A workgroup takes rows blockIdx.x * ROWS + threadIdx.x / TPR + k gridDim.x * ROWS and keeps its share of
 // dgain in registers; what its rows sum to becomes one row of `partial`, added up by k_sum_rows in a fixed order.
 template <typename T, int TPR, int PER>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_rmsnorm_backward(gear_norm_backward_args a, float *__restrict__ partial) {
-  constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+__global__ void __launch_bounds__(TPR <= kWave ? 256 : TPR) k_rmsnorm_backward(gear_norm_backward_args a, float *__restrict__ partial) {
+  constexpr int THREADS = TPR <= kWave ? 256 : TPR, ROWS = THREADS / TPR;
   __shared__ float s_part[TPR > kWave ? TPR / kWave : 1];
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float dg[PER][8];
@@ -235,14 +239,15 @@ bool shape_ok(int64_t rows, int32_t dim, int32_t dtype) {
 }
 
 // Threads of a row: a quarter or half of a wavefront for rows that a whole one would not fill (42115 x 144 fp32 backward 35.5 / 22.9 us), a
-// wavefront up to 2048 columns, as many as hold the row in at most 32 values each beyond.
+// wavefront up to 2048 columns, as many as hold the row in at most 32 values each beyond.  (bf16 in 8 bits up to 4096 with half as many, whose
+// arithmetic is what counts: a wavefront computes whole pieces of 512 columns.  32126 x 2176 142 / 104, but fp32 10000 x 4096 126 / 131.)
 template <typename T, NormKind KIND> hipError_t launch_norm(const gear_norm_args &a, hipStream_t s) {
   constexpr int64_t kMost = 1 << 21;   // workgroups: threads are counted in 32 bits
 #define GEAR_NORM(TPR, PER)                                                                                            \
   do {                                                                                                                 \
-    const int64_t blocks = TPR < 256 ? (a.rows * TPR + 255) / 256 : a.rows;                                            \
+    const int64_t blocks = TPR <= kWave ? (a.rows * TPR + 255) / 256 : a.rows;                                         \
     hipLaunchKernelGGL((k_rmsnorm<T, TPR, PER, KIND>), dim3((unsigned)(blocks < kMost ? blocks : kMost)),              \
-                       dim3(TPR < 256 ? 256 : TPR), 0, s, a);                                                          \
+                       dim3(TPR <= kWave ? 256 : TPR), 0, s, a);                                                       \
   } while (0)
   if (a.dim <= 128)
     GEAR_NORM(16, 1);
@@ -254,9 +259,12 @@ template <typename T, NormKind KIND> hipError_t launch_norm(const gear_norm_args
     GEAR_NORM(64, 2);
   else if (a.dim <= 2048)
     GEAR_NORM(64, 4);
-  else if (a.dim <= 4096)
-    GEAR_NORM(256, 2);
-  else if (a.dim <= 8192)
+  else if (a.dim <= 4096) {
+    if constexpr (KIND == kNorm8 && sizeof(T) == 2)
+      GEAR_NORM(128, 4);
+    else
+      GEAR_NORM(256, 2);
+  } else if (a.dim <= 8192)
     GEAR_NORM(256, 4);
   else if (a.dim <= 32768)
     GEAR_NORM(1024, 4);
@@ -279,7 +287,7 @@ int back_blocks(int64_t rows, int32_t dim, int32_t dtype) {
 template <typename T> hipError_t launch_back(const gear_norm_backward_args &a, float *partial, hipStream_t s) {
   const dim3 grid(back_blocks(a.rows, a.dim, a.dtype));
 #define GEAR_BACK(TPR, PER) \
-  hipLaunchKernelGGL((k_rmsnorm_backward<T, TPR, PER>), grid, dim3(TPR < 256 ? 256 : TPR), 0, s, a, partial)
+  hipLaunchKernelGGL((k_rmsnorm_backward<T, TPR, PER>), grid, dim3(TPR <= kWave ? 256 : TPR), 0, s, a, partial)
   if (a.dim <= 128)
     GEAR_BACK(16, 1);
   else if (a.dim <= 256)

@@ -634,3 +634,19 @@ def test_norm_in_8_bits_is_rounded_once(g, dtype, rows, dim):
     want = nearest8(torch.nn.functional.pad(y, (0, -dim % 128)) / unit)
     within(out.rows8.q.view(torch.float8_e4m3fn).double(), want, 0.0)
     within(out.y, (want * unit)[:, :dim], 0.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,dim", [(5, 2056), (300, 2176), (7, 3584), (33, 4096), (3, 4104)])
+def test_norm_in_8_bits_of_rows_wider_than_a_wavefront(g, dtype, rows, dim):
+    """Rows of several wavefronts, whole and ragged, with and without a residual: 8 bits and scales are those of the norm in 64 bits."""
+    r = gen(7 * rows + dim)
+    x = torch.randn(rows, dim, device="cuda", generator=r).to(dtype)
+    gain = 1 + 0.3 * torch.randn(dim, device="cuda", generator=r)
+    for res in (None, torch.randn(rows, dim, device="cuda", generator=r).to(dtype)):
+        _, y = norm_ref(x, res, gain, float(torch.tensor(1e-6)))
+        out = g.gear_rmsnorm(x, gain, 1e-6, residual=res, y=False, q8=True)
+        e = exponents(y)
+        assert torch.equal(out.rows8.scale[:, :e.shape[1]].long() - 127, e)
+        want = nearest8(torch.nn.functional.pad(y, (0, -dim % 128)) / torch.exp2(e.double()).repeat_interleave(128, 1))
+        within(out.rows8.q.view(torch.float8_e4m3fn).double(), want, 0.0)
