@@ -251,6 +251,8 @@ def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, row
         _vector(status, where, "status", torch.int32, 1)
         status = status.data_ptr()
     if out is None:
+        if out_dtype not in _CODE:
+            _refuse(where, f"out_dtype has to be float32 or bfloat16, not {out_dtype}")
         out, ld_out = torch.empty(rows, n, dtype=out_dtype, device=device), n
     else:
         ld_out = _matrix(out, where, "out", None, (rows, n))
@@ -295,7 +297,8 @@ def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[to
 
 def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
                       status: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """dy_e^T x_e for every expert: [experts x N x K] float32, zeros for one without rows."""
+    """dy_e^T x_e for every expert: [experts x N x K] float32, zeros for one without rows.  off as for gear_matmul8; status [1]
+    (int32): GEAR_ERR_RANGE if it is no such list, and nothing is written."""
     where = "gear_expert_wgrad"
     ld_x = _matrix(x, where, "x")
     device = x.device

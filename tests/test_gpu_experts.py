@@ -650,3 +650,15 @@ def test_norm_in_8_bits_of_rows_wider_than_a_wavefront(g, dtype, rows, dim):
         assert torch.equal(out.rows8.scale[:, :e.shape[1]].long() - 127, e)
         want = nearest8(torch.nn.functional.pad(y, (0, -dim % 128)) / torch.exp2(e.double()).repeat_interleave(128, 1))
         within(out.rows8.q.view(torch.float8_e4m3fn).double(), want, 0.0)
+
+
+def test_products_refuse_results_of_other_types(g):
+    x = torch.zeros(4, 64, device="cuda", dtype=BF16)
+    w = torch.zeros(64, 64, device="cuda", dtype=BF16)
+    for call in (lambda d: g.gear_expert_matmul(x, g.ExpertWeights(w), out_dtype=d), lambda d: g.gear_expert_dgrad(x, g.ExpertWeights(w), out_dtype=d),
+                 lambda d: g.gear_matmul8(g.gear_rows8(x), g.gear_weights8(w), out_dtype=d)):
+        for other in (torch.float16, torch.float64, torch.int32):
+            with pytest.raises(g.GearError):
+                call(other)
+        for right in (F32, BF16):
+            assert not call(right).any()
