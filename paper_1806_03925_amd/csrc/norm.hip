@@ -278,9 +278,12 @@ template <typename T, NormKind KIND> hipError_t launch_norm(const gear_norm_args
 // device at once, three for each CU in bf16 and two in fp32 (registers): us of 512 / 768 / 1024 / 1536 for 65536 x 2048
 // bf16 204 / 197 / 228 / 202, 65536 x 1152 131 / 120 / 145 / 123 (5.0 TB/s), 16384 x 1024 28.8 / 28.0 / 28.2 / 31.6; fp32
 // 65536 x 2048 408 / 446 / 409 / 413 (5.3 TB/s), 10001 x 512 19.0 / 19.8 / 20.6 / 22.1.
+// Few rows are one workgroup's, which leaves dgain itself: two launches / one, from Python, 32 x 512 bf16 (8 rounds of rows) 12.7 / 10.2, 16 x
+// 1152 (4) 12.8 / 9.8, but 32 x 1152 (8) 12.9 / 15.4.
 int back_blocks(int64_t rows, int32_t dim, int32_t dtype) {
   const int at_once = dim <= 128 ? 16 : dim <= 256 ? 8 : dim <= 2048 ? 4 : 1;   // rows of a workgroup
   const int64_t groups = (rows + at_once - 1) / at_once, most = dtype == GEAR_BF16 ? 768 : 512;
+  if (groups <= (dim <= 512 ? 8 : 4)) return 1;
   return (int)(groups < most ? groups : most);
 }
 
