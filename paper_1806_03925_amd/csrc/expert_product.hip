@@ -37,15 +37,18 @@ struct ProductArgs {
   int32_t *status;
 };
 
-// Tile shape: WAVES_M x WAVES_N wavefronts, each 32 WTM rows x 64 columns; both operands are requested AHEAD k-blocks before
-// they are multiplied, and x has one stage more in LDS
-template <int DT_, int WTM_, int WAVES_M_, int WAVES_N_, int AHEAD_> struct ProductTile {
-  static constexpr int DT = DT_, WTM = WTM_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, AHEAD = AHEAD_, STAGES = AHEAD + 1;
+// Tile shape: WAVES_M x WAVES_N wavefronts, each 32 WTM rows x 64 columns.  Both operands are requested a k-block before they are
+// multiplied; more would take the registers that a third workgroup on the CU needs, which hides more (us of two k-blocks / one: 64 x
+// 256 4096 x 1024 x 1152 bf16 13.6 / 13.2, 128 x 128 35092 x 120 x 2840 by 4 in 8 bits 31.8 / 29.9, three / one: 32 x 128 1024 x 2048
+// 17.8 / 17.1, fp32 64 x 128 2086 x 8064 x 80 by 61 87 / 74).
+constexpr int kStages = 2;   // of x in LDS
+template <int DT_, int WTM_, int WAVES_M_, int WAVES_N_> struct ProductTile {
+  static constexpr int DT = DT_, WTM = WTM_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
   static constexpr int WAVES = WAVES_M * WAVES_N, THREADS = WAVES * kWave;
   static constexpr int BM = 32 * WTM * WAVES_M, BN = WN * WAVES_N;
   static constexpr int STAGE_BYTES = BM * kKBlock, DMA = BM / 8 / WAVES;   // copies of a wavefront per stage, eight rows each
   static constexpr int PATCH_BYTES = WAVES * 32 * PATCH_LD * 2;
-  static constexpr int LDS_BYTES = STAGES * STAGE_BYTES > PATCH_BYTES ? STAGES * STAGE_BYTES : PATCH_BYTES;
+  static constexpr int LDS_BYTES = kStages * STAGE_BYTES > PATCH_BYTES ? kStages * STAGE_BYTES : PATCH_BYTES;
   static_assert(DMA * 8 * WAVES == BM, "a copy is eight rows");
 };
 
@@ -183,7 +186,7 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   }
   auto copy = [&](int k) {
     const int kk = min(k, nk - 1);
-    unsigned char *s = lds + (k % C::STAGES) * C::STAGE_BYTES;
+    unsigned char *s = lds + (k % kStages) * C::STAGE_BYTES;
     const bool in = kk * kKBlock + piece * 16 < beyond;
 #pragma unroll
     for (int i = 0; i < C::DMA; ++i)
@@ -196,7 +199,7 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   const int64_t strip = (int64_t)nk * kPackedBlock;
   const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<unsigned char *>(a.packed) + ((int64_t)t.e * n32 + first32) * strip, 0, (int)(min(2, n32 - first32) * strip), 0x00020000);
-  u32x4_v b[C::AHEAD][2][2][TN];   // [k-block modulo AHEAD][half][unit][column tile]
+  u32x4_v b[2][2][TN];   // [half][unit][column tile]
   auto load = [&](u32x4_v (&to)[2][TN], int k, int half) {
     const int at = min(k, nk - 1) * kPackedBlock + half * 2048;
 #pragma unroll
@@ -239,44 +242,30 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   const uint32_t x_rel = lds_base + (uint32_t)(wm * C::WTM * 32 + r) * 128u + (uint32_t)((g ^ (r >> 1 & 7)) << 4);
 
   scales(0, 0);
-#pragma unroll
-  for (int k = 0; k < C::AHEAD; ++k) {
-    copy(k);
-    load(b[k][0], k, 0);
-    load(b[k][1], k, 1);
-  }
+  copy(0);
+  load(b[0], 0, 0);
+  load(b[1], 0, 1);
   auto block = [&](int k, auto which) {
     constexpr int W = decltype(which)::value;
     if (k >= nk) return;
-    // what was issued after the copies of k: 8 loads, and the copies and loads of the blocks between
-    wait_vm<8 + (C::AHEAD - 1) * (C::DMA + 8)>();
+    wait_vm<8>();      // 8 loads were issued after the copies of k
     block_barrier();   // everybody's copies of k have landed, and everybody has read what copy() now overwrites
-    copy(k + C::AHEAD);
-    const uint32_t at = x_rel + (uint32_t)(k % C::STAGES) * C::STAGE_BYTES;
-    u32x4_v (&bk)[2][2][TN] = b[W % C::AHEAD];
-    mma_half<C, W & 3>(acc, at, bk[0], sx[0], sw[0]);
-    load(bk[0], k + C::AHEAD, 0);
-    mma_half<C, W & 3>(acc, at ^ 64u, bk[1], sx[0], sw[0]);
-    load(bk[1], k + C::AHEAD, 1);
+    copy(k + 1);
+    const uint32_t at = x_rel + (uint32_t)(k % kStages) * C::STAGE_BYTES;
+    mma_half<C, W>(acc, at, b[0], sx[0], sw[0]);
+    load(b[0], k + 1, 0);
+    mma_half<C, W>(acc, at ^ 64u, b[1], sx[0], sw[0]);
+    load(b[1], k + 1, 1);
   };
-  auto four = [&](int k, auto first) {
-    constexpr int F = decltype(first)::value;
+  for (int k = 0; k < nk; k += 4) {   // four k-blocks share a word of scales
     scales(1, k + 4);
-    block(k, std::integral_constant<int, F>{});
-    block(k + 1, std::integral_constant<int, F + 1>{});
-    block(k + 2, std::integral_constant<int, F + 2>{});
-    block(k + 3, std::integral_constant<int, F + 3>{});
+    block(k, std::integral_constant<int, 0>{});
+    block(k + 1, std::integral_constant<int, 1>{});
+    block(k + 2, std::integral_constant<int, 2>{});
+    block(k + 3, std::integral_constant<int, 3>{});
 #pragma unroll
     for (int i = 0; i < C::WTM; ++i) sx[0][i] = sx[1][i];
     sw[0] = sw[1];
-  };
-  // bodies of the loop: as many k-blocks as scale words and register sets both divide
-  for (int k = 0; k < nk; k += C::AHEAD == 3 ? 12 : 4) {
-    four(k, std::integral_constant<int, 0>{});
-    if constexpr (C::AHEAD == 3) {
-      four(k + 4, std::integral_constant<int, 4>{});
-      four(k + 8, std::integral_constant<int, 8>{});
-    }
   }
   wait_vm<0>();    // copies beyond the end have landed too: LDS becomes the patches
   __syncthreads();
@@ -528,9 +517,9 @@ hipError_t launch_pack(const void *w, int experts, int N, int K, void *packed, v
   return hipGetLastError();
 }
 
-template <int DT, int WTM, int WAVES_M, int WAVES_N, int AHEAD>
+template <int DT, int WTM, int WAVES_M, int WAVES_N>
 hipError_t launch_tile(const ProductArgs &a, bool f32, hipStream_t s) {
-  using C = ProductTile<DT, WTM, WAVES_M, WAVES_N, AHEAD>;
+  using C = ProductTile<DT, WTM, WAVES_M, WAVES_N>;
   // as many row tiles as there can be (every expert may end inside one), one at least: it looks at the offsets
   const int64_t m_tiles = ((int64_t)a.rows + C::BM - 1) / C::BM + (a.off ? a.experts - 1 : 0);
   const dim3 grid((unsigned)(m_tiles > 0 ? m_tiles * ((a.N + C::BN - 1) / C::BN) : 1));
@@ -562,27 +551,29 @@ template <int DT, int TM, int TN, int WAVES, int AHEAD> hipError_t launch_split(
 
 // Which shape: the largest that still gives the device something to do, by the number of tiles (with experts, of about how
 // many: half a tile more for each).  us measured, K = N where one is given, smaller / larger shape of each border:
-//   few tiles, up to 256 of 32 x 32 (one for each CU), against 32 x 128: 256 x 1024 x 1152 bf16 6.7 / 7.3, 64 x 4096 8 bits 10.2 /
-//     15.0; above, 512 x 1024 x 1152 bf16 11.4 / 7.4.  fp32, whose products are slow, up to 1024: 512 x 2048 55 / 66, 1024 x 2048 108 / 75
-//   32 x 128 up to 512 tiles, against 64 x 256: 1024 x 2048 bf16 17.0 / 18.6, 4096 x 1024 x 1152 16.2 / 12.4; but not where its many
-//     row tiles each read weights that no L2 holds: 256 x 8192 bf16 144 / 74
-//   64 x 256 below 512 tiles, against 128 x 256: 2048 x 2048 bf16 19.9 / 28.1, 4096 x 2048 36 / 33; and a little over one round of the
-//     larger tiles (two a CU): 16384 x 1024 x 1152 by 64 experts in 8 bits 30.7 / 36.7; again not with large weights: 5842 x 2904 x 4304
-//     by 9 experts bf16 191 / 161
-//   fp32: 64 x 128 by four wavefronts up to 4096 tiles: 16384 x 1024 x 1152 by 8 experts 314 / 407, 65536 x 1024 x 576 584 / 561
-//   up to 128 columns, where wider tiles are half empty: 128 x 128: 65536 x 72 x 320 in 8 bits 7.8 / 9.4
+//   few tiles, up to 256 of 32 x 32 (one for each CU), against 32 x 128: 256 x 1024 x 1152 bf16 7.3 / 7.6, 64 x 4096 8 bits 10.5 /
+//     10.3; above, 512 x 1024 x 1152 bf16 11.9 / 7.8.  fp32, whose products are slow, up to 1024, against 64 x 128: 512 x 2048 53.5 /
+//     70.0, 1024 x 2048 98.8 / 74.6
+//   32 x 128 up to 256 tiles, then 64 x 128 up to as many: 1024 x 1024 x 4096 bf16 25.2 / 27.1, 1024 x 2048 16.9 / 14.9, 256 x 8192
+//     54.4 / 50.3; where experts have few rows only above 512: 1000 x 1024 by 32 15.9 / 18.2
+//   64 x 256 above, against 32 x 128 and 64 x 128: 1500 x 2048 x 1024 bf16 12.0 / 13.6 / 14.2, 2000 x 2048 20.2 / 28.2 / 25.0, up to 512
+//     tiles, against 128 x 256: 2048 x 2048 bf16 19.9 / 28.1, 4096 x 2048 34.4 / 33.8
+//   fp32: 64 x 128 by four wavefronts: 16384 x 1024 x 1152 by 8 experts 308 / 405, but 65536 x 1024 x 576 577 / 557
+//   up to 128 columns, and up to 384 where 256 are too few, of which wider tiles leave a quarter or more empty: 128 x 128, against 64 x 256:
+//     65536 x 72 x 320 in 8 bits 9.2 / 11.3, 9000 x 264 x 2000 bf16 22.3 / 29.2
 template <int DT> hipError_t launch_product(const ProductArgs &a, bool f32, hipStream_t s) {
   auto tiles = [&](int bm, int bn) { return ((int64_t)(a.rows + bm - 1) / bm + (a.off ? a.experts / 2 : 0)) * ((a.N + bn - 1) / bn); };
   if (tiles(32, 32) <= (DT == GEAR_F32 ? 1024 : 256)) return launch_split<DT, 1, 1, 4, 2>(a, f32, s);
   if constexpr (DT == GEAR_F32) {
-    if (tiles(64, 128) <= 4096) return launch_tile<DT, 1, 2, 2, 3>(a, f32, s);
+    return launch_tile<DT, 1, 2, 2>(a, f32, s);
   } else {
-    const int64_t weights = (int64_t)a.N * a.K * operand_bytes(DT);
-    if (tiles(32, 128) <= 512 && (weights <= 8 << 20 || a.rows <= 128 * (int64_t)a.experts)) return launch_tile<DT, 1, 1, 2, 3>(a, f32, s);
-    if (a.N <= 128) return launch_tile<DT, 2, 2, 2, 2>(a, f32, s);
-    if (tiles(64, 256) < 512 || (tiles(128, 256) > 512 && tiles(128, 256) <= 640 && weights <= 8 << 20)) return launch_tile<DT, 2, 1, 4, 2>(a, f32, s);
+    const int64_t narrow = tiles(32, 128);
+    if (narrow <= 256 || (narrow <= 512 && a.rows < 256 * (int64_t)a.experts)) return launch_tile<DT, 1, 1, 2>(a, f32, s);
+    if (narrow <= 512) return launch_tile<DT, 1, 2, 2>(a, f32, s);
+    if (a.N <= 128 || (a.N > 256 && a.N <= 384)) return launch_tile<DT, 2, 2, 2>(a, f32, s);
+    if (tiles(64, 256) < 512) return launch_tile<DT, 2, 1, 4>(a, f32, s);
+    return launch_tile<DT, 4, 1, 4>(a, f32, s);
   }
-  return launch_tile<DT, 4, 1, 4, 1>(a, f32, s);
 }
 
 }  // namespace

@@ -662,3 +662,12 @@ def test_products_refuse_results_of_other_types(g):
                 call(other)
         for right in (F32, BF16):
             assert not call(right).any()
+
+
+@pytest.mark.parametrize("sizes,n,k", [([1, 1300, 230], 776, 200), ([1500, 0, 30], 1160, 72), ([2200, 0, 7000, 41], 264, 136), ([5300, 301], 376, 64),
+                                       ([4000, 90, 33], 584, 136), ([9000, 129, 0, 7200], 1160, 72)])
+def test_products_between_few_tiles_and_many(g, sizes, n, k):
+    """Ragged rows of as many as each shape of tile is meant for, one at a time: 64 x 128 (twice), 128 x 128 (twice), 64 x 256 and 128 x 256."""
+    for dtype in (F32, BF16):
+        test_expert_products(g, dtype, sizes, n, k)
+    test_products_in_8_bits(g, sizes, n, k)
