@@ -101,27 +101,41 @@ __device__ __forceinline__ WgradTile wgrad_tile(const WgradArgs &a, int bm, int 
   return r;
 }
 
-// dw of the experts that were cut: their pieces in ascending order
+// dw of the experts that were cut: their pieces in ascending order, in SHARES equal shares whose sums are added in that order, too
 constexpr int kAtOnce = 8;
-__global__ void __launch_bounds__(256) k_wgrad_sum(WgradArgs a) {
+template <int SHARES> __global__ void __launch_bounds__(256) k_wgrad_sum(WgradArgs a) {
+  constexpr int COLS = 256 / SHARES;
+  __shared__ float4 s_sum[SHARES > 1 ? SHARES : 1][COLS];
   const int lane = threadIdx.x & 63, e = blockIdx.y;
   if (a.off && !offsets_ok(a.off, a.experts, a.rows, lane)) return;
   const int rows = a.off ? a.off[e + 1] - a.off[e] : a.rows;
   if (rows <= a.cut) return;
   const int before = a.off ? __builtin_amdgcn_readfirstlane(partials_before(a.off, e, a.cut, lane)) : 0, pieces = pieces_of(rows, a.cut);
+  const int share = threadIdx.x / COLS, col = threadIdx.x % COLS, each = (pieces + SHARES - 1) / SHARES, last = min(pieces, (share + 1) * each);
   const int64_t vec = (int64_t)a.N * a.K / 4;
   const float4 *p = reinterpret_cast<const float4 *>(a.partial) + before * vec;
   float4 *o = reinterpret_cast<float4 *>(a.dw) + e * vec;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < vec; i += (int64_t)gridDim.x * 256) {
-    float4 v = p[i];
-    for (int z = 1; z < pieces; z += kAtOnce) {   // several on their way at a time, added in ascending order
-      float4 w[kAtOnce];
+  for (int64_t i0 = (int64_t)blockIdx.x * COLS; i0 < vec; i0 += (int64_t)gridDim.x * COLS) {
+    const int64_t i = i0 + col;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (i < vec) {
+      for (int z = share * each; z < last; z += kAtOnce) {   // several on their way at a time, added in ascending order
+        float4 w[kAtOnce];
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) w[k] = z + k < pieces ? p[(z + k) * vec + i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = 0; k < kAtOnce; ++k) w[k] = z + k < last ? p[(z + k) * vec + i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) v.x += w[k].x, v.y += w[k].y, v.z += w[k].z, v.w += w[k].w;
+        for (int k = 0; k < kAtOnce; ++k) v.x += w[k].x, v.y += w[k].y, v.z += w[k].z, v.w += w[k].w;
+      }
     }
-    o[i] = v;
+    if constexpr (SHARES > 1) {
+      __syncthreads();   // the last sums have been read
+      s_sum[share][col] = v;
+      __syncthreads();
+      if (share > 0) continue;
+#pragma unroll
+      for (int k = 1; k < SHARES; ++k) v.x += s_sum[k][col].x, v.y += s_sum[k][col].y, v.z += s_sum[k][col].z, v.w += s_sum[k][col].w;
+    }
+    if (i < vec) o[i] = v;
   }
 }
 // workgroups for `tiles` tiles: whole rounds of kSpread tiles on every XCD
@@ -460,8 +474,15 @@ extern "C" gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *
     if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
   }
   if (wgrad_partials(a->rows, a->experts, cut) > 0) {
-    const int64_t vec = (int64_t)a->N * a->K / 4, want = (vec + 255) / 256;
-    hipLaunchKernelGGL(k_wgrad_sum, dim3((unsigned)(want < 4096 ? want : 4096), (unsigned)a->experts), dim3(256), 0, s, w);
+    const int64_t vec = (int64_t)a->N * a->K / 4;
+    // few columns are few workgroups, each with a long walk: us by one share / 16, 65536 x 72 x 128 bf16 34 / 16, 9000 x 320 x 72 14 / 12, but
+    // 30000 x 1024 x 128 by 4 28 / 36
+    if (vec * a->experts <= 16384) {
+      hipLaunchKernelGGL(k_wgrad_sum<16>, dim3((unsigned)((vec + 15) / 16), (unsigned)a->experts), dim3(256), 0, s, w);
+    } else {
+      const int64_t want = (vec + 255) / 256;
+      hipLaunchKernelGGL(k_wgrad_sum<1>, dim3((unsigned)(want < 4096 ? want : 4096), (unsigned)a->experts), dim3(256), 0, s, w);
+    }
     if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
   }
   return GEAR_OK;

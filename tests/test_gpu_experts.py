@@ -671,3 +671,15 @@ def test_products_between_few_tiles_and_many(g, sizes, n, k):
     for dtype in (F32, BF16):
         test_expert_products(g, dtype, sizes, n, k)
     test_products_in_8_bits(g, sizes, n, k)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,n,k", [(20011, 72, 128), (9000, 8, 8), (40000, 72, 320), (33000, 264, 320)])
+def test_weight_gradient_of_long_lists_and_few_columns(g, dtype, rows, n, k):
+    """Many pieces of a small gradient, added up in shares; the same again, bit for bit."""
+    r = gen(rows + n)
+    dy, x = (torch.randn(rows, w, device="cuda", generator=r).to(dtype) for w in (n, k))
+    a, b = dy.double(), x.double()
+    dw = g.gear_expert_wgrad(dy, x)
+    within(dw[0], a.t().contiguous() @ b, (rows + 8) * 2 * U * (a.abs().t().contiguous() @ b.abs()))
+    assert torch.equal(dw, g.gear_expert_wgrad(dy, x))
