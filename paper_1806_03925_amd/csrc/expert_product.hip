@@ -46,6 +46,7 @@ template <int DT_, int WTM_, int WAVES_M_, int WAVES_N_> struct ProductTile {
   static constexpr int DT = DT_, WTM = WTM_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
   static constexpr int WAVES = WAVES_M * WAVES_N, THREADS = WAVES * kWave;
   static constexpr int BM = 32 * WTM * WAVES_M, BN = WN * WAVES_N;
+  static constexpr bool HALVES = BM == 128 && BN == 256;
   static constexpr int STAGE_BYTES = BM * kKBlock, DMA = BM / 8 / WAVES;   // copies of a wavefront per stage, eight rows each
   static constexpr int PATCH_BYTES = WAVES * 32 * PATCH_LD * 2;
   static constexpr int LDS_BYTES = kStages * STAGE_BYTES > PATCH_BYTES ? kStages * STAGE_BYTES : PATCH_BYTES;
@@ -160,14 +161,12 @@ __device__ __forceinline__ void store_tile(const f32x16_v (&acc)[C::WTM][TN], bf
   }
 }
 
-template <typename C, bool F32> __device__ __forceinline__ void product_tile(const ProductArgs &a, unsigned char *lds) {
+template <typename C, bool F32> __device__ __forceinline__ void product_tile(const ProductArgs &a, const ExpertTile &t, unsigned char *lds) {
+  const int m0 = t.m0 + max(t.part, 0) * C::BM;
+  if (m0 >= t.m_end) return;   // the second half of a tile that has no more rows than the first
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
-  const int n_tiles = (a.N + C::BN - 1) / C::BN;
-  const ExpertTile t = expert_tile(a.off, a.experts, a.rows, C::BM, n_tiles, blockIdx.x, lane);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
-  if (!t.have) return;
-  const int m0 = t.m0, n0 = t.n_tile * C::BN, m_rows = min(C::BM, t.m_end - m0);
+  const int n0 = t.n_tile * C::BN, m_rows = min(C::BM, t.m_end - m0);
   const int row_bytes = a.K * operand_bytes(C::DT);
   const int nk = (row_bytes + kKBlock - 1) / kKBlock;
 
@@ -273,9 +272,23 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
                      n0 + wn * WN, a.N, lane);
 }
 
+template <typename C> __device__ __forceinline__ ExpertTile look(const ProductArgs &a, bool halves) {
+  const ExpertTile t = expert_tile(a.off, a.experts, a.rows, C::BM, (a.N + C::BN - 1) / C::BN, blockIdx.x, threadIdx.x & 63, halves);
+  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
+  return t;
+}
+
 template <typename C, bool F32> __global__ void __launch_bounds__(C::THREADS, 2) k_expert_product(ProductArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host's pass does not know copies of 16 bytes into LDS
+  using Half = ProductTile<C::DT, C::HALVES ? C::WTM / 2 : C::WTM, C::WAVES_M, C::WAVES_N>;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[C::LDS_BYTES];
-  product_tile<C, F32>(a, lds);
+  const ExpertTile t = look<C>(a, C::HALVES);
+  if (!t.have) return;
+  if (C::HALVES && t.part >= 0)
+    product_tile<Half, F32>(a, t, lds);
+  else
+    product_tile<C, F32>(a, t, lds);
+#endif
 }
 
 // ---- few tiles ----------------------------------------------------------------------------------------------------
@@ -295,9 +308,7 @@ template <typename C> struct SplitBlock {   // operands of a k-block in register
 template <typename C, bool F32> __device__ __forceinline__ void split_tile(const ProductArgs &a, float *sums) {
   constexpr int DT = C::DT, TM_ = C::TM, TN_ = C::TN;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n_tiles = (a.N + C::BN - 1) / C::BN;
-  const ExpertTile t = expert_tile(a.off, a.experts, a.rows, C::BM, n_tiles, blockIdx.x, lane);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
+  const ExpertTile t = look<C>(a, false);
   if (!t.have) return;
   const int m0 = t.m0, n0 = t.n_tile * C::BN, m_rows = min(C::BM, t.m_end - m0);
   const int row_bytes = a.K * operand_bytes(DT), nk = (row_bytes + kKBlock - 1) / kKBlock;
@@ -522,7 +533,7 @@ hipError_t launch_tile(const ProductArgs &a, bool f32, hipStream_t s) {
   using C = ProductTile<DT, WTM, WAVES_M, WAVES_N>;
   // as many row tiles as there can be (every expert may end inside one), one at least: it looks at the offsets
   const int64_t m_tiles = ((int64_t)a.rows + C::BM - 1) / C::BM + (a.off ? a.experts - 1 : 0);
-  const dim3 grid((unsigned)(m_tiles > 0 ? m_tiles * ((a.N + C::BN - 1) / C::BN) : 1));
+  const dim3 grid((unsigned)((m_tiles > 0 ? m_tiles * ((a.N + C::BN - 1) / C::BN) : 1) + (C::HALVES ? kHalved : 0)));
   if constexpr (DT == GEAR_F32) {
     hipLaunchKernelGGL((k_expert_product<C, true>), grid, dim3(C::THREADS), 0, s, a);
   } else {

@@ -6,11 +6,19 @@
 namespace gear {
 namespace {
 
-// The tile of a workgroup: rows [m0, m_end) of expert e from m0 on, column tile n_tile.  bad: off is not a CSR index.
+// The tile of a workgroup: rows [m0, m_end) of expert e from m0 on, column tile n_tile; of its rows the first half (part 0), the second
+// (1) or all (-1).  bad: off is not a CSR index.
 struct ExpertTile {
   int e, m0, m_end, n_tile;
   bool have, bad;
+  int part;
 };
+
+// Workgroups of the largest shape of tile that the device runs at a time, two for each CU.  If a few tiles are left for a last round,
+// each of them is two workgroups' (`halves`: the shape allows it), at most one for each CU, so that it is over sooner.  us whole / in halves:
+// 17408 x 1024 x 1152 bf16 (32 tiles left) 46.3 / 41.6, 20480 x 1024 x 1152 (128) 47.7 / 43.5, 9216 x 2048 x 4096 (64) 145 / 133; with
+// about 150 left, 16384 x 1152 x 1024 by 8 experts, 44.7 / 47.5.
+constexpr int kSlots = 512, kHalved = kSlots / 4;
 
 __device__ __forceinline__ int wave_add(int v) {
 #pragma unroll
@@ -43,12 +51,20 @@ __device__ __forceinline__ TileAt tile_at(int t, int m_tiles, int n_tiles) {
 // neighbouring ones have been gathered on one XCD.  Every wavefront looks at all offsets, 64 at a time, so that all
 // workgroups agree on whether they are a CSR index.
 __device__ __forceinline__ ExpertTile expert_tile(const int32_t *__restrict__ off, int experts, int rows, int edge, int n_tiles,
-                                                  int block, int lane) {
-  ExpertTile r = {0, 0, 0, 0, false, false};
+                                                  int block, int lane, bool halves) {
+  ExpertTile r = {0, 0, 0, 0, false, false, -1};
+  auto tile_of = [&](int tiles) {   // the tile that `block` works on, or one beyond them
+    const int whole = tiles / kSlots * kSlots, rest = tiles - whole;
+    if (!halves || whole == 0 || rest > kHalved || block < whole) return block;
+    if (block >= whole + 2 * rest) return tiles;
+    r.part = block >= whole + rest;
+    return block - r.part * rest;
+  };
   if (!off) {
     const int m_tiles = (rows + edge - 1) / edge;
-    if (block >= m_tiles * n_tiles) return r;
-    const TileAt t = tile_at(xcd_remap(block, m_tiles * n_tiles), m_tiles, n_tiles);
+    const int tile = tile_of(m_tiles * n_tiles);
+    if (tile >= m_tiles * n_tiles) return r;
+    const TileAt t = tile_at(xcd_remap(tile, m_tiles * n_tiles), m_tiles, n_tiles);
     r.m0 = t.m * edge, r.m_end = rows, r.n_tile = t.n, r.have = true;
     return r;
   }
@@ -62,8 +78,9 @@ __device__ __forceinline__ ExpertTile expert_tile(const int32_t *__restrict__ of
   }
   r.bad = bad;
   total = __builtin_amdgcn_readfirstlane(total);   // the same in all lanes: what follows from it is scalar
-  if (bad || block >= total * n_tiles) return r;
-  const TileAt t = tile_at(xcd_remap(block, total * n_tiles), total, n_tiles);
+  const int tile = tile_of(total * n_tiles);
+  if (bad || tile >= total * n_tiles) return r;
+  const TileAt t = tile_at(xcd_remap(tile, total * n_tiles), total, n_tiles);
   const int want = t.m;
   int before = 0;
   for (int e0 = 0; e0 < experts; e0 += kWave) {

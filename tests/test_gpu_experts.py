@@ -683,3 +683,10 @@ def test_weight_gradient_of_long_lists_and_few_columns(g, dtype, rows, n, k):
     dw = g.gear_expert_wgrad(dy, x)
     within(dw[0], a.t().contiguous() @ b, (rows + 8) * 2 * U * (a.abs().t().contiguous() @ b.abs()))
     assert torch.equal(dw, g.gear_expert_wgrad(dy, x))
+
+
+@pytest.mark.parametrize("sizes,n,k", [([16384 + 40], 1024, 64), ([8000, 0, 8500, 130], 1024, 72), ([9000, 7400, 1], 1032, 136), ([33000], 1000, 64)])
+def test_products_whose_last_round_is_halved(g, sizes, n, k):
+    """A little more than one round (or two) of the largest tiles, the last of them with few rows and with many."""
+    test_expert_products(g, BF16, sizes, n, k)
+    test_products_in_8_bits(g, sizes, n, k)
