@@ -569,13 +569,17 @@ template <int DT, int TM, int TN, int WAVES, int AHEAD> hipError_t launch_split(
 //     54.4 / 50.3; where experts have few rows only above 512: 1000 x 1024 by 32 15.9 / 18.2
 //   64 x 256 above, against 32 x 128 and 64 x 128: 1500 x 2048 x 1024 bf16 12.0 / 13.6 / 14.2, 2000 x 2048 20.2 / 28.2 / 25.0, up to 512
 //     tiles, against 128 x 256: 2048 x 2048 bf16 19.9 / 28.1, 4096 x 2048 34.4 / 33.8
-//   fp32: 64 x 128 by four wavefronts: 16384 x 1024 x 1152 by 8 experts 308 / 405, but 65536 x 1024 x 576 577 / 557
+//   fp32: 64 x 128 by four wavefronts: 16384 x 1024 x 1152 by 8 experts 308 / 405, but 65536 x 1024 x 576 577 / 557; 32 x 64 split over k,
+//     which moves more, where rounds of one 64 x 128 for each CU would be less than three quarters full: 1441 x 1880 x 5736 by 2 (360
+//     tiles) 295 / 340, 4000 x 512 x 576 by 8 (268) 33.7 / 40.5, 3000 x 1024 (376) 63.9 / 65.3, but 1600 x 2048 x 1024 (400) 71.4 / 66.9
 //   up to 128 columns, and up to 384 where 256 are too few, of which wider tiles leave a quarter or more empty: 128 x 128, against 64 x 256:
 //     65536 x 72 x 320 in 8 bits 9.2 / 11.3, 9000 x 264 x 2000 bf16 22.3 / 29.2
 template <int DT> hipError_t launch_product(const ProductArgs &a, bool f32, hipStream_t s) {
   auto tiles = [&](int bm, int bn) { return ((int64_t)(a.rows + bm - 1) / bm + (a.off ? a.experts / 2 : 0)) * ((a.N + bn - 1) / bn); };
   if (tiles(32, 32) <= (DT == GEAR_F32 ? 1024 : 256)) return launch_split<DT, 1, 1, 4, 2>(a, f32, s);
   if constexpr (DT == GEAR_F32) {
+    const int64_t count = tiles(64, 128), empty = (count + 255) / 256 * 256 - count;
+    if (empty > count / 3) return launch_split<DT, 1, 2, 4, 1>(a, f32, s);
     return launch_tile<DT, 1, 2, 2>(a, f32, s);
   } else {
     const int64_t narrow = tiles(32, 128);
