@@ -690,3 +690,10 @@ def test_products_whose_last_round_is_halved(g, sizes, n, k):
     """A little more than one round (or two) of the largest tiles, the last of them with few rows and with many."""
     test_expert_products(g, BF16, sizes, n, k)
     test_products_in_8_bits(g, sizes, n, k)
+
+
+@pytest.mark.parametrize("sizes,n,k", [([300, 41], 520, 3104), ([70, 0, 200], 776, 6152), ([129], 1160, 6200)])
+def test_products_of_few_tiles_and_long_rows(g, sizes, n, k):
+    """Tiles that are split over k: rows of 48 k-blocks of 128 bytes and more, whole and not."""
+    test_expert_products(g, BF16, sizes, n, k)
+    test_products_in_8_bits(g, sizes, n, k)
