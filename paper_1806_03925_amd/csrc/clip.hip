@@ -3,10 +3,10 @@
 //   norm = sqrt(sum over tensors and elements of g^2),  c = min(1, max_norm / (norm + 1e-6)),  out = c g
 //
 // Two launches, whatever the number of tensors (one for a list of up to four chunks: us of two launches / one, 6273
-// gradients in four tensors 6.8 / 4.4, 32768 in one 7.5 / 6.0, but 65536 7.5 / 9.1).  The list lies on the device as one entry per tensor; work is cut into
-// chunks of kClipChunk elements that never cross a tensor, and a workgroup finds a chunk's tensor by bisection over the
-// entries' first chunks.  The first launch leaves one fp64 sum per workgroup, the second adds
-// these up in every workgroup (in the same order, so that all get the same factor) and scales.  Memory bound: all elements
+// gradients in four tensors 6.8 / 4.4, 32768 in one 7.5 / 6.0, but 65536 7.5 / 9.1).  The list lies on the device as one
+// entry per tensor; work is cut into chunks of kClipChunk elements that never cross a tensor, and a workgroup finds a
+// chunk's tensor by bisection over the entries' first chunks.  The first launch leaves one fp64 sum per workgroup, the
+// second adds these up in every workgroup (in the same order, so that all get the same factor) and scales.  Memory bound: all elements
 // are read once for the norm, and read and written once more to be scaled, since the factor is not known before; the
 // second pass walks its chunks backwards and finds in the cache what the first has read last.  400 M gradients (1.07 GB, bf16 and
 // fp32) 681 us, 4.7 TB/s of the 3.2 GB; 704 forwards, 737 with results through the L2, 761 with neighbouring chunks to a workgroup.
@@ -174,8 +174,8 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_scale(const GradEntry *__
   for (int64_t k = chunks - 1 - blockIdx.x; k >= 0; k -= gridDim.x) chunk_scale(list, count, k, c, threadIdx.x);
 }
 
-// Short lists, whose time is that of two launches and not of one workgroup's memory accesses: all of it by one workgroup, kClipThreads threads to a chunk.  All reads for
-// the sum come before the barrier in block_sum, so gradients may be scaled in place.
+// Short lists, whose time is that of two launches and not of one workgroup's memory accesses: all of it by one
+// workgroup, kClipThreads threads to a chunk.  All reads for the sum come before the barrier in block_sum, so gradients may be scaled in place.
 constexpr int kShortChunks = 4, kShortThreads = kShortChunks * kClipThreads;
 __global__ void __launch_bounds__(kShortThreads) k_grad_short(const GradEntry *__restrict__ list, int count, int chunks, float max_norm,
                                                               int scale, float *__restrict__ norm_out) {

@@ -8,7 +8,8 @@
 // the instruction multiplies by both operands' powers of two itself, so scales cost no vector instruction.
 //
 // Rows of x are copied global -> LDS by DMA, LDS rows of 128 bytes with their pieces XOR-ed by half the row's number modulo 8:
-// the sixteen rows that are read at a time, two to the 256 bytes of all banks, then lie in sixteen different places; what lies beyond k or beyond the expert's rows is out of the buffer's range and becomes zeros.
+// the sixteen rows that are read at a time, two to the 256 bytes of all banks, then lie in sixteen different places; what lies
+// beyond k or beyond the expert's rows is out of the buffer's range and becomes zeros.
 // Weights come in operand order (k_pack) straight into registers and never pass LDS.
 #include "eight.hpp"
 #include "experts.hpp"
@@ -38,7 +39,7 @@ struct ProductArgs {
 };
 
 // Tile shape: WAVES_M x WAVES_N wavefronts, each 32 WTM rows x 64 columns.  Both operands are requested a k-block before they are
-// multiplied; more would take the registers that a third workgroup on the CU needs, which hides more (us of two k-blocks / one: 64 x
+// multiplied; more would take the registers that another workgroup on the CU needs, which hides more (us of two k-blocks / one: 64 x
 // 256 4096 x 1024 x 1152 bf16 13.6 / 13.2, 128 x 128 35092 x 120 x 2840 by 4 in 8 bits 31.8 / 29.9, three / one: 32 x 128 1024 x 2048
 // 17.8 / 17.1, fp32 64 x 128 2086 x 8064 x 80 by 61 87 / 74).
 constexpr int kStages = 2;   // of x in LDS
@@ -343,7 +344,8 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
     for (int u = 0; u < 4; ++u) {
 #pragma unroll
       for (int j = 0; j < TN_; ++j)
-        b.w[j][u] = __builtin_bit_cast(u32x4_v, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc, j * (int)strip + lane * 16, kk * kPackedBlock + u * 1024, 0));
+        b.w[j][u] = __builtin_bit_cast(u32x4_v, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc, j * (int)strip + lane * 16,
+                                                                                      kk * kPackedBlock + u * 1024, 0));
       const bool in = kk * kKBlock + (2 * u + g) * 16 < beyond;
 #pragma unroll
       for (int i = 0; i < TM_; ++i)

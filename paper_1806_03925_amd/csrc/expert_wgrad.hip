@@ -411,7 +411,8 @@ int wgrad_cut(int dtype, int64_t rows, int experts, int N, int K) {
   constexpr int64_t slots = 512;
   const int64_t tiles = wgrad_tiles(wgrad_shape(dtype, K), N, K), whole = rows < 1 ? 1 : rows;
   if (experts * tiles >= 2 * slots) return (int)whole;
-  int64_t cut = experts == 1 ? (rows + slots / tiles - 1) / (slots / tiles > 0 ? slots / tiles : 1) : rows * tiles * (dtype == GEAR_F32 ? 3 : 4) / (2 * slots);
+  const int64_t at_once = tiles < slots ? slots / tiles : 1;
+  int64_t cut = experts == 1 ? (rows + at_once - 1) / at_once : rows * tiles * (dtype == GEAR_F32 ? 3 : 4) / (2 * slots);
   cut = (cut + 31) / 32 * 32;
   // What a piece adds and writes has to be worth it.  us with 128 / 256 / 512 rows at least, fp32: 1000 x 72 x 320 by 5 11 / 13 / 14,
   // 8000 x 64 x 64 by 16 12 / 14 / 19, 1000 x 72 x 320 by one 10 / 12 / 16; bf16: 2000 x 512 x 576 by 8 26 / 19 / 17, 1000 x 1024 x 1152
@@ -480,8 +481,9 @@ extern "C" gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *
     if (vec * a->experts <= 16384) {
       hipLaunchKernelGGL(k_wgrad_sum<16>, dim3((unsigned)((vec + 15) / 16), (unsigned)a->experts), dim3(256), 0, s, w);
     } else {
-      const int64_t want = (vec + 255) / 256;
-      hipLaunchKernelGGL(k_wgrad_sum<1>, dim3((unsigned)(want < 4096 ? want : 4096), (unsigned)a->experts), dim3(256), 0, s, w);
+      // 4096 in all, as those of experts that are not cut have nothing to do: 16384 x 1024 x 1152 by 8 69 / 67
+      const int64_t want = (vec + 255) / 256, most = 4096 / a->experts + 1;
+      hipLaunchKernelGGL(k_wgrad_sum<1>, dim3((unsigned)(want < most ? want : most), (unsigned)a->experts), dim3(256), 0, s, w);
     }
     if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
   }
