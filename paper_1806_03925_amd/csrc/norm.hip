@@ -200,33 +200,35 @@ __global__ void __launch_bounds__(TPR <= kWave ? 256 : TPR) k_rmsnorm_backward(g
   }
 }
 
-// out[c] = sum of partial[r][c], r < n, always in the same order.  A workgroup takes 64 columns, 16 threads of four a row, 64
-// rows at a time: few workgroups, so each has to have many rows on their way.  us for 1024 rows of 1024: 4; by 16 x 16
-// threads with one column each 20.
+// out[c] = sum of partial[r][c], r < n, always in the same order.  A workgroup takes 32 columns, eight threads of four a row, 128
+// rows at a time: few workgroups, so each has to have many rows on their way.  us of the whole backward pass of 16384 x 1024 bf16 (768 rows
+// here) with 64 / 32 / 16 columns: 28.2 / 27.4 / 27.5; this launch with one column of a row to a thread, 16 rows at a time, 20 for 4.
+constexpr int kSumCols = 32;
 __global__ void __launch_bounds__(1024) k_sum_rows(const float *__restrict__ partial, int n, int dim, float *__restrict__ out) {
-  __shared__ __attribute__((aligned(16))) float s[64][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 15) * 4, r0 = threadIdx.x >> 4;
+  constexpr int COLS = kSumCols, T = COLS / 4, ROWS = 1024 / T, PARTS = 1024 / COLS, EACH = ROWS / PARTS;   // threads to a row, rows at a time
+  __shared__ __attribute__((aligned(16))) float s[ROWS][COLS];
+  const int c = blockIdx.x * COLS + (threadIdx.x % T) * 4, r0 = threadIdx.x / T;
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   if (c < dim) {
 #pragma unroll 4
-    for (int r = r0; r < n; r += 64) {
+    for (int r = r0; r < n; r += ROWS) {
       const float4 p = *reinterpret_cast<const float4 *>(partial + (size_t)r * dim + c);
       v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
     }
   }
-  *reinterpret_cast<float4 *>(&s[r0][(threadIdx.x & 15) * 4]) = v;
+  *reinterpret_cast<float4 *>(&s[r0][(threadIdx.x % T) * 4]) = v;
   __syncthreads();
-  const int col = threadIdx.x & 63, q = threadIdx.x >> 6;
+  const int col = threadIdx.x % COLS, q = threadIdx.x / COLS;
   float sum = 0.0f;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) sum += s[q * 4 + r][col];
+  for (int r = 0; r < EACH; ++r) sum += s[q * EACH + r][col];
   __syncthreads();
   s[q][col] = sum;
   __syncthreads();
-  if (q == 0 && blockIdx.x * 64 + col < dim) {
+  if (q == 0 && blockIdx.x * COLS + col < dim) {
 #pragma unroll
-    for (int r = 1; r < 16; ++r) sum += s[r][col];
-    out[blockIdx.x * 64 + col] = sum;
+    for (int r = 1; r < PARTS; ++r) sum += s[r][col];
+    out[blockIdx.x * COLS + col] = sum;
   }
 }
 
@@ -380,7 +382,7 @@ extern "C" gear_status gear_rmsnorm_backward(const gear_norm_backward_args *a, v
   const hipError_t err = a->dtype == GEAR_BF16 ? launch_back<bf16_t>(*a, partial, s) : launch_back<float>(*a, partial, s);
   if (err != hipSuccess) return GEAR_ERR_HIP;
   if (a->dgain && !alone) {
-    hipLaunchKernelGGL(k_sum_rows, dim3((a->dim + 63) / 64), dim3(1024), 0, s, partial, back_blocks(a->rows, a->dim, a->dtype), a->dim, a->dgain);
+    hipLaunchKernelGGL(k_sum_rows, dim3((a->dim + kSumCols - 1) / kSumCols), dim3(1024), 0, s, partial, back_blocks(a->rows, a->dim, a->dtype), a->dim, a->dgain);
     if (hipGetLastError() != hipSuccess) return GEAR_ERR_HIP;
   }
   return GEAR_OK;
