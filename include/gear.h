@@ -345,7 +345,9 @@ int64_t gear_scales8_ld(int32_t dim);
  * Outputs, each NULL where it is not wanted, one at least: sum = h (of `dtype`, may be x or residual itself), y (of
  * `dtype`), and q8 with scale, y in 8 bits.  With both y and q8, y holds what the 8 bits stand for (as far as `dtype`
  * holds it), so that gradients can be taken of what the 8-bit product saw.  y may be x or residual itself unless sum is the same.
- * gain [dim] fp32, 16-byte aligned; eps >= 0; dim at most GEAR_MAX_NORM_DIM.  The norm is that of h before it is rounded to `dtype`. */
+ * gain [dim] fp32, 16-byte aligned; eps >= 0; dim at most GEAR_MAX_NORM_DIM.  The norm is that of h before it is rounded to `dtype`.
+ * Squares and their sum are fp32 (without q8) and have to lie in its range: rows of a root mean square up to 7e16 (at any dim), and from
+ * 1e-18 where eps is smaller than their squares. */
 typedef struct {
   int64_t rows;
   int32_t dim, dtype;    /* gear_dtype of x, residual, sum and y */
@@ -359,7 +361,8 @@ typedef struct {
 gear_status gear_rmsnorm(const gear_norm_args *a, void *stream);
 
 /* Backward pass at h (the forward pass's sum, or x): with s = (mean(h^2) + eps)^-1/2 and a = dy * gain
- *   dx = s a - h s^3 mean(a h) + dsum        (dsum, what flows into h itself; may be NULL)
+ *   dx = s a - h s^3 mean(a h) + dsum        (dsum, what flows into h itself; may be NULL; s^3 is not formed: h may be as large or small
+ *                                             as the norm in fp32 takes it)
  *   dgain = sum over rows of dy h s          ([dim] fp32, 16-byte aligned; may be NULL)
  * dx is the gradient of both x and residual; it may be dy or dsum itself.  workspace (256-byte aligned) as
  * gear_norm_backward_workspace_bytes says; not needed where dgain is NULL.  No rows: dgain is zero. */
