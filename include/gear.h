@@ -401,7 +401,8 @@ gear_status gear_pack_weights(const void *w, int32_t src_dtype, int32_t operand_
  * x [rows x K] of `dtype` (GEAR_E4M3: ld_x in bytes, at least gear_rows8_ld(K) and a multiple of 16; x_scale
  * [rows x gear_scales8_ld(K)], 4-byte aligned).  out [rows x N] of out_dtype: fp32, or bf16 where dtype is not GEAR_F32.
  * status (device word, may be NULL where off is): GEAR_ERR_RANGE if off is not as said, and out is then left as it was;
- * otherwise 0. */
+ * otherwise 0, or what it was before where keep_status is not 0: many calls, on any streams, may then share a word that holds an error
+ * until the caller clears it. */
 typedef struct {
   int32_t dtype, out_dtype;
   int64_t rows;
@@ -414,6 +415,7 @@ typedef struct {
   void *out;
   int64_t ld_x, ld_out;
   int32_t *status;
+  int32_t keep_status;
 } gear_expert_args;
 gear_status gear_expert_product(const gear_expert_args *a, void *stream);
 

@@ -7,8 +7,8 @@ from .binding import (  # noqa: F401
     gear_workspace_region, lib, make_config,
 )
 from .experts import (  # noqa: F401
-    ExpertWeights, GradList, NormOutput, Rows8, Weights8, gear_clip_grads, gear_expert_dgrad, gear_expert_matmul, gear_expert_wgrad,
-    gear_grad_norm, gear_matmul8, gear_rmsnorm, gear_rmsnorm_backward, gear_rows8, gear_weights8,
+    ExpertWeights, GradList, NormOutput, Rows8, Weights8, gear_clip_grads, gear_expert_dgrad, gear_expert_matmul, gear_expert_status,
+    gear_expert_wgrad, gear_grad_norm, gear_matmul8, gear_rmsnorm, gear_rmsnorm_backward, gear_rows8, gear_weights8,
 )
 
 

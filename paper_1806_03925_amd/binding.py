@@ -81,7 +81,7 @@ class gear_expert_args(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("out_dtype", C.c_int32), ("rows", C.c_int64), ("K", C.c_int32), ("N", C.c_int32),
                 ("experts", C.c_int32), ("x", C.c_void_p), ("x_scale", C.c_void_p), ("packed", C.c_void_p),
                 ("w_scale", C.c_void_p), ("off", C.c_void_p), ("out", C.c_void_p), ("ld_x", C.c_int64), ("ld_out", C.c_int64),
-                ("status", C.c_void_p)]
+                ("status", C.c_void_p), ("keep_status", C.c_int32)]
 
 
 class gear_expert_wgrad_args(C.Structure):

@@ -36,6 +36,7 @@ struct ProductArgs {
   int64_t ld_x, ld_out;   // bytes, elements
   int rows, K, N, experts;
   int32_t *status;
+  int keep_status;
 };
 
 // Tile shape: WAVES_M x WAVES_N wavefronts, each 32 WTM rows x 64 columns.  Both operands are requested a k-block before they are
@@ -275,7 +276,7 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
 
 template <typename C> __device__ __forceinline__ ExpertTile look(const ProductArgs &a, bool halves) {
   const ExpertTile t = expert_tile(a.off, a.experts, a.rows, C::BM, (a.N + C::BN - 1) / C::BN, blockIdx.x, threadIdx.x & 63, halves);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
+  report(t.bad, a.status, a.keep_status);
   return t;
 }
 
@@ -656,7 +657,8 @@ extern "C" gear_status gear_expert_product(const gear_expert_args *a, void *stre
   hipStream_t s = (hipStream_t)stream;
   if (a->rows == 0 && !a->off && !a->status) return GEAR_OK;
   const ProductArgs p = {static_cast<const unsigned char *>(a->x), a->x_scale, static_cast<const unsigned char *>(a->packed), a->w_scale,
-                         a->off, a->out, a->ld_x * size, a->ld_out, (int)a->rows, a->K, a->N, a->experts, a->status};
+                         a->off, a->out, a->ld_x * size, a->ld_out, (int)a->rows, a->K, a->N, a->experts, a->status,
+                         a->keep_status};
   const bool f32 = a->out_dtype == GEAR_F32;
   const hipError_t err = a->dtype == GEAR_E4M3   ? launch_product<GEAR_E4M3>(p, f32, s)
                          : a->dtype == GEAR_BF16 ? launch_product<GEAR_BF16>(p, f32, s)

@@ -36,6 +36,11 @@ __device__ __forceinline__ bool offsets_ok(const int32_t *__restrict__ off, int 
   return !bad;
 }
 
+// Offsets that are no CSR index are reported by one thread; those that are only where nobody shares the word (gear.h).
+__device__ __forceinline__ void report(bool bad, int32_t *status, int keep) {
+  if (status && blockIdx.x == 0 && threadIdx.x == 0 && (bad || !keep)) *status = bad ? GEAR_ERR_RANGE : GEAR_OK;
+}
+
 // Tile t of m_tiles x n_tiles: kGroupRows row tiles are walked down, column by column, before the next ones.  The 64 tiles
 // that an XCD works on at a time then read 8 strips of rows and 8 of weights through its L2, not two and 32.
 constexpr int kGroupRows = 8;

@@ -43,6 +43,28 @@ def _vector(t: torch.Tensor, where: str, name: str, dtype: torch.dtype, n: int) 
         _refuse(where, f"{name} has to be {n} contiguous {dtype} on the GPU")
 
 
+_words = {}      # GPU -> the word that calls without a status of their own report into, and its address
+
+
+def _word(index: int, where: str) -> Tuple[torch.Tensor, int]:
+    found = _words.get(index)
+    if found is None:
+        if torch.cuda.is_current_stream_capturing():
+            _refuse(where, "the first report of this GPU cannot be made while a graph is captured: give it a status, or call gear_expert_status before")
+        with torch.inference_mode(False):
+            word = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
+        torch.cuda.current_stream(index).synchronize()      # any stream may report from now on
+        found = _words.setdefault(index, (word, word.data_ptr()))
+    return found
+
+
+def gear_expert_status(device=None) -> torch.Tensor:
+    """The word [1] (int32) of a GPU that products which are given no status report into: GEAR_ERR_RANGE once offsets were no
+    list of rows, and until the caller clears it (zero_()); 0 before.  Calls that work leave it alone, so any streams share it."""
+    device = torch.device("cuda" if device is None else device)
+    return _word(torch.cuda.current_device() if device.index is None else device.index, "gear_expert_status")[0]
+
+
 class Rows8:
     """Rows in 8 bits: q [rows x gear_rows8_ld(dim)] (bytes of e4m3), scale [rows x gear_scales8_ld(dim)] (exponent + 127)."""
     __slots__ = ("rows", "dim", "ld", "device", "_q", "_scale", "_room", "p_q", "p_scale")
@@ -174,18 +196,18 @@ def _weights(w: torch.Tensor, where: str) -> Tuple[int, int, int]:
 
 
 class _Packed:
-    """Memory of weights laid out for the products, and behind them a word that the products report into."""
+    """Memory of weights laid out for the products."""
 
     def _allocate(self, size: int, device) -> None:
-        size = (size + 255) // 256 * 256
-        self.packed = torch.empty(size + 4, dtype=torch.uint8, device=device)
+        self.packed = torch.empty(size, dtype=torch.uint8, device=device)
         self.address = self.packed.data_ptr()
-        self.p_status = self.address + size
+        if device.index not in _words and not torch.cuda.is_current_stream_capturing():
+            _word(device.index, "weights")                  # there when products are captured
 
     @property
     def status(self) -> torch.Tensor:
-        """What the last product that was given no word of its own reported."""
-        return self.packed[-4:].view(torch.int32)
+        """gear_expert_status of the weights' GPU."""
+        return gear_expert_status(self.packed.device)
 
 
 class Weights8(_Packed):
@@ -247,9 +269,12 @@ def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, row
         off = off.data_ptr()
     elif experts != 1:
         _refuse(where, "off may only be left out where there is one expert")
+    keep = 0
     if status is not None:
         _vector(status, where, "status", torch.int32, 1)
         status = status.data_ptr()
+    elif off is not None:
+        status, keep = _word(device.index, where)[1], 1
     if out is None:
         if out_dtype not in _CODE:
             _refuse(where, f"out_dtype has to be float32 or bfloat16, not {out_dtype}")
@@ -257,7 +282,7 @@ def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, row
     else:
         ld_out = _matrix(out, where, "out", None, (rows, n))
     a = gear_expert_args(dtype, _CODE[out.dtype], rows, k, n, experts, p_x, p_x_scale, packed, p_w_scale, off, out.data_ptr(), ld_x, ld_out,
-                         status or weights.p_status)
+                         status, keep)
     code = lib.gear_expert_product(C.byref(a), _raw_stream(device.index))
     if code:
         _check(code, where)

@@ -43,3 +43,56 @@ def test_norm_backward_of_rows_of_zeros_and_next_to_no_eps(g, eps):
     got, got_gain = g.gear_rmsnorm_backward(h, gain, dy, eps)
     within(got, dx, 4 * norm_bound(520, F32) * scale)
     within(got_gain, dgain, (norm_bound(520, F32) + 14 * U) * total)
+
+
+# ---- reports of offsets that are no list ------------------------------------------------------------------------------
+def operands(sizes, n, k):
+    r = gen(n + k)
+    rows = sum(sizes)
+    off = torch.tensor([0] + sizes).cumsum(0).to(torch.int32).cuda()
+    draw = lambda *s: torch.randn(s, device="cuda", generator=r).to(BF16)
+    return draw(rows, k), draw(rows, n), draw(len(sizes), n, k), off
+
+
+def dirty_memory():
+    """Blocks of all sizes that weights are laid out in, left full of ones to whoever is given them next."""
+    torch.cuda.synchronize()
+    blocks = [torch.full((1 << p,), 255, dtype=torch.uint8, device="cuda") for p in range(9, 22) for _ in range(8)]
+    torch.cuda.synchronize()
+    del blocks
+
+
+def test_weights_report_nothing_before_the_first_product(g):
+    _, _, w, _ = operands([3, 4], 72, 64)
+    for _ in range(3):
+        dirty_memory()
+        assert g.ExpertWeights(w).status.item() == 0 and g.gear_weights8(w).status.item() == 0
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_a_product_that_works_does_not_erase_the_report_of_one_that_did_not(g, kind):
+    x, dy, w, good = operands([50, 50], 72, 64)
+    bad = torch.tensor([0, 60, 50], dtype=torch.int32, device="cuda")
+    weights = g.ExpertWeights(w) if kind == "bf16" else g.gear_weights8(w)
+    call = (lambda off: g.gear_expert_matmul(x, weights, off)) if kind == "bf16" else (lambda off: g.gear_matmul8(g.gear_rows8(x), weights, off))
+    try:
+        call(good)
+        assert weights.status.item() == 0
+        call(bad)
+        call(good)
+        if kind == "bf16":
+            g.gear_expert_dgrad(dy, weights, good)
+        assert weights.status.item() == g.GEAR_ERR_RANGE
+    finally:
+        weights.status.zero_()
+    call(good)
+    assert weights.status.item() == 0                       # cleared by the caller, and only by the caller
+
+
+def test_a_status_of_ones_own_is_written_by_every_product(g):
+    x, _, w, good = operands([50, 50], 72, 64)
+    weights, status = g.ExpertWeights(w), torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    g.gear_expert_matmul(x, weights, good, status=status)
+    assert status.item() == 0
+    g.gear_expert_matmul(x, weights, good + 1, status=status)
+    assert status.item() == g.GEAR_ERR_RANGE and weights.status.item() == 0
