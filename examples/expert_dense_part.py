@@ -109,6 +109,8 @@ def run(steps: int, kinds: int = 5, dim: int = 72, expiry: int = 2, verbose: boo
         losses.append(st.loss.clone())
         if verbose:
             print(f"step {step}: loss {losses[-1].item():.6f}, averaged gradients {int(st.n_ready.item())}, their norm {norms[-1].item():.2e}", flush=True)
+    if int(g.gear_expert_status().item()) != g.GEAR_OK:       # of all products and weight gradients above
+        raise g.GearError(int(g.gear_expert_status().item()), "offsets of a list of images")
     return st, dense, torch.cat(losses), torch.stack(norms)
 
 

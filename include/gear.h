@@ -420,8 +420,8 @@ typedef struct {
 gear_status gear_expert_product(const gear_expert_args *a, void *stream);
 
 /* dw_e [N x K] = dy_e^T x_e over the rows of every expert, dw [experts x N x K] fp32 contiguous, 16-byte aligned (zeros
- * for an expert without rows).  dy [rows x N] and x [rows x K] of `dtype` (GEAR_F32 or GEAR_BF16); off and status as
- * above, a bad off leaves dw as it was.  workspace (256-byte aligned) as gear_expert_wgrad_workspace_bytes says. */
+ * for an expert without rows).  dy [rows x N] and x [rows x K] of `dtype` (GEAR_F32 or GEAR_BF16); off, status and
+ * keep_status as above, a bad off leaves dw as it was.  workspace (256-byte aligned) as gear_expert_wgrad_workspace_bytes says. */
 typedef struct {
   int32_t dtype;
   int64_t rows;
@@ -431,6 +431,7 @@ typedef struct {
   float *dw;
   int64_t ld_dy, ld_x;
   int32_t *status;
+  int32_t keep_status;
 } gear_expert_wgrad_args;
 size_t gear_expert_wgrad_workspace_bytes(int32_t dtype, int64_t rows, int32_t experts, int32_t N, int32_t K);
 gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *workspace, size_t workspace_bytes, void *stream);

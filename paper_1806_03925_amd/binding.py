@@ -87,7 +87,7 @@ class gear_expert_args(C.Structure):
 class gear_expert_wgrad_args(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("rows", C.c_int64), ("K", C.c_int32), ("N", C.c_int32), ("experts", C.c_int32),
                 ("dy", C.c_void_p), ("x", C.c_void_p), ("off", C.c_void_p), ("dw", C.c_void_p), ("ld_dy", C.c_int64),
-                ("ld_x", C.c_int64), ("status", C.c_void_p)]
+                ("ld_x", C.c_int64), ("status", C.c_void_p), ("keep_status", C.c_int32)]
 
 
 class gear_grad_tensor(C.Structure):

@@ -18,6 +18,7 @@ struct WgradArgs {
   int32_t *status;
   float *partial;        // [pieces of experts that are cut][N x K]
   int cut;               // rows of a piece
+  int keep_status;
 };
 
 struct WgradTile {
@@ -147,7 +148,7 @@ template <typename C> __global__ void __launch_bounds__(C::THREADS) k_expert_wgr
   __shared__ __attribute__((aligned(1024))) unsigned char lds[C::STAGES * C::STAGE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const WgradTile t = wgrad_tile(a, C::BM, C::BN, blockIdx.x, lane);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
+  report(t.bad, a.status, a.keep_status);
   if (!t.have) return;
   const int m0 = t.m0, n0 = t.n0, first = t.first, last = t.last;
 
@@ -271,7 +272,7 @@ template <typename C> struct WideFrag {
 template <typename C> __device__ __forceinline__ void wgrad_wide(const WgradArgs &a, unsigned char *lds) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const WgradTile t = wgrad_tile(a, C::BM, C::BN, blockIdx.x, lane);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = t.bad ? GEAR_ERR_RANGE : GEAR_OK;
+  report(t.bad, a.status, a.keep_status);
   if (!t.have) return;
   const int m0 = t.m0, n0 = t.n0, first = t.first, last = t.last;
   const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
@@ -461,7 +462,7 @@ extern "C" gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *
   const int cut = wgrad_cut(a->dtype, a->rows, a->experts, a->N, a->K);
   const WgradShape shape = wgrad_shape(a->dtype, a->K);
   const WgradArgs w = {a->dy, a->x, a->off, a->dw, a->ld_dy, a->ld_x, (int)a->rows, a->K, a->N, a->experts, a->status,
-                       static_cast<float *>(workspace), cut};
+                       static_cast<float *>(workspace), cut, a->keep_status};
   hipStream_t s = (hipStream_t)stream;
   const int64_t pieces = a->off ? a->experts + a->rows / cut : (a->rows + cut - 1) / cut;
   const unsigned blocks = wgrad_blocks((pieces > 0 ? pieces : 1) * wgrad_tiles(shape, a->N, a->K));

@@ -59,8 +59,9 @@ def _word(index: int, where: str) -> Tuple[torch.Tensor, int]:
 
 
 def gear_expert_status(device=None) -> torch.Tensor:
-    """The word [1] (int32) of a GPU that products which are given no status report into: GEAR_ERR_RANGE once offsets were no
-    list of rows, and until the caller clears it (zero_()); 0 before.  Calls that work leave it alone, so any streams share it."""
+    """The word [1] (int32) of a GPU that products and weight gradients report into when they are given no status: GEAR_ERR_RANGE
+    once offsets were no list of rows, until the caller clears it (zero_()); 0 before.  Calls that work leave it alone, so any
+    streams share it."""
     device = torch.device("cuda" if device is None else device)
     return _word(torch.cuda.current_device() if device.index is None else device.index, "gear_expert_status")[0]
 
@@ -323,7 +324,8 @@ def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[to
 def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
                       status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dy_e^T x_e for every expert: [experts x N x K] float32, zeros for one without rows.  off as for gear_matmul8; status [1]
-    (int32): GEAR_ERR_RANGE if it is no such list, and nothing is written."""
+    (int32): GEAR_ERR_RANGE if it is no such list, and nothing is written, otherwise 0; without it the error is left in
+    gear_expert_status."""
     where = "gear_expert_wgrad"
     ld_x = _matrix(x, where, "x")
     device = x.device
@@ -334,19 +336,22 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     if off is not None:
         experts = off.numel() - 1
         _vector(off, where, "off", torch.int32, experts + 1)
+    keep, p_status = 0, None
     if status is not None:
         _vector(status, where, "status", torch.int32, 1)
+        p_status = status.data_ptr()
+    elif off is not None:
+        p_status, keep = _word(device.index, where)[1], 1
     if dw is None:
         dw = torch.empty(experts, n, k, dtype=torch.float32, device=device)
     else:
         _vector(dw, where, "dw", torch.float32, experts * n * k)
     dtype = _CODE[x.dtype]
     size = lib.gear_expert_wgrad_workspace_bytes(dtype, rows, experts, n, k)
-    ws = torch.empty(size + 4, dtype=torch.uint8, device=device)      # and a word to report into
-    p_ws = ws.data_ptr()
+    ws = torch.empty(size, dtype=torch.uint8, device=device)
     a = gear_expert_wgrad_args(dtype, rows, k, n, experts, dy.data_ptr(), x.data_ptr(), _ptr(off), dw.data_ptr(), ld_dy, ld_x,
-                               p_ws + size if status is None else status.data_ptr())
-    code = lib.gear_expert_wgrad(C.byref(a), p_ws, size, _raw_stream(device.index))
+                               p_status, keep)
+    code = lib.gear_expert_wgrad(C.byref(a), ws.data_ptr(), size, _raw_stream(device.index))
     if code:
         _check(code, where)
     return dw

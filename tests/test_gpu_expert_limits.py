@@ -96,3 +96,45 @@ def test_a_status_of_ones_own_is_written_by_every_product(g):
     assert status.item() == 0
     g.gear_expert_matmul(x, weights, good + 1, status=status)
     assert status.item() == g.GEAR_ERR_RANGE and weights.status.item() == 0
+
+
+def test_a_weight_gradient_reports_without_a_status_of_its_own(g):
+    x, dy, w, good = operands([50, 50], 72, 64)
+    word = g.gear_expert_status()
+    want = g.gear_expert_wgrad(dy, x, good)
+    assert word.item() == 0 and g.gear_expert_status(x.device) is word
+    try:
+        dw = torch.full((2, 72, 64), 7.0, device="cuda")
+        g.gear_expert_wgrad(dy, x, torch.tensor([0, 60, 50], dtype=torch.int32, device="cuda"), dw=dw)
+        assert torch.equal(g.gear_expert_wgrad(dy, x, good), want)
+        g.gear_expert_matmul(x, g.ExpertWeights(w), good)
+        assert word.item() == g.GEAR_ERR_RANGE and (dw == 7).all()
+    finally:
+        word.zero_()
+    g.gear_expert_wgrad(dy, x, good)
+    assert word.item() == 0
+
+
+def test_reports_from_a_graph_and_from_two_streams(g):
+    """Every replay reports; calls that work, on whatever stream, leave the report alone."""
+    x, dy, w, good = operands([50, 50], 72, 64)
+    weights, word, off = g.ExpertWeights(w), g.gear_expert_status(), good.clone()
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        g.gear_expert_matmul(x, weights, off)
+        g.gear_expert_wgrad(dy, x, off)
+    try:
+        for wrong in (False, True, False, True):
+            off.copy_(good + 1 if wrong else good)
+            graph.replay()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                for _ in range(3):
+                    g.gear_expert_matmul(x, weights, good)
+            torch.cuda.synchronize()
+            assert word.item() == (g.GEAR_ERR_RANGE if wrong else 0)
+            word.zero_()
+    finally:
+        word.zero_()
