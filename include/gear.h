@@ -454,8 +454,9 @@ gear_status gear_grad_list_pack(const gear_grad_tensor *tensors, int32_t count, 
 size_t gear_grad_workspace_bytes(int64_t chunks);
 gear_status gear_grad_norm(const void *list, int32_t count, int64_t chunks, void *workspace, size_t workspace_bytes,
                            float *norm, void *stream);
-/* The same, and dst = c src for every tensor with c = min(1, max_norm / (norm + 1e-6)), max_norm > 0.  A norm that is
- * infinite makes c 0, one that is NaN makes c NaN. */
+/* The same, and dst = c src for every tensor with c = min(1, max_norm / (norm + 1e-6)), max_norm > 0, from the norm in fp64:
+ * gradients that are finite are scaled by it also where fp32 can only report an infinite norm.  An infinity among the gradients makes
+ * c 0, a NaN makes c NaN. */
 gear_status gear_clip_grads(const void *list, int32_t count, int64_t chunks, float max_norm, void *workspace,
                             size_t workspace_bytes, float *norm, void *stream);
 

@@ -145,9 +145,10 @@ template <typename T> __device__ __forceinline__ void scale_chunk(const T *src, 
   if (at < n) dst[at] = from_f32<T>(to_f32(src[at]) * c);
 }
 
-__device__ __forceinline__ float clip_factor(float norm, float max_norm) {
-  const float ratio = max_norm / (norm + 1e-6f);
-  return ratio > 1.0f ? 1.0f : ratio;   // NaN stays NaN
+// from the norm in fp64: fp32 may not hold that of gradients which are finite
+__device__ __forceinline__ float clip_factor(double norm, float max_norm) {
+  const double ratio = (double)max_norm / (norm + 1e-6);
+  return ratio > 1.0 ? 1.0f : (float)ratio;   // NaN stays NaN
 }
 
 __device__ __forceinline__ void chunk_scale(const GradEntry *__restrict__ list, int count, int64_t k, float c, int t) {
@@ -167,8 +168,8 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_scale(const GradEntry *__
   __shared__ double s_sum[kClipThreads / kWave];
   double sum = 0.0;
   for (int i = threadIdx.x; i < n_partial; i += kClipThreads) sum += partial[i];
-  const float norm = (float)sqrt(block_sum<kClipThreads>(sum, s_sum));
-  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+  const double norm = sqrt(block_sum<kClipThreads>(sum, s_sum));
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   if (!scale) return;
   const float c = clip_factor(norm, max_norm);
   for (int64_t k = chunks - 1 - blockIdx.x; k >= 0; k -= gridDim.x) chunk_scale(list, count, k, c, threadIdx.x);
@@ -181,8 +182,8 @@ __global__ void __launch_bounds__(kShortThreads) k_grad_short(const GradEntry *_
                                                               int scale, float *__restrict__ norm_out) {
   __shared__ double s_sum[kShortThreads / kWave];
   const int chunk = threadIdx.x / kClipThreads, t = threadIdx.x % kClipThreads;
-  const float norm = (float)sqrt(block_sum<kShortThreads>(chunk < chunks ? chunk_squares(list, count, chunk, t) : 0.0, s_sum));
-  if (threadIdx.x == 0) *norm_out = norm;
+  const double norm = sqrt(block_sum<kShortThreads>(chunk < chunks ? chunk_squares(list, count, chunk, t) : 0.0, s_sum));
+  if (threadIdx.x == 0) *norm_out = (float)norm;
   if (scale && chunk < chunks) chunk_scale(list, count, chunk, clip_factor(norm, max_norm), t);
 }
 

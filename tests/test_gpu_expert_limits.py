@@ -138,3 +138,20 @@ def test_reports_from_a_graph_and_from_two_streams(g):
             word.zero_()
     finally:
         word.zero_()
+
+
+# ---- clipping -------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n", [40, 20_000, 200_000])
+def test_clipping_of_gradients_whose_norm_fp32_does_not_hold(g, n):
+    """Each gradient is finite and so is the norm in 64 bits; the reported fp32 norm is infinite, what is clipped is not lost.  One
+    rounding of c and one of the result, either of which may be below the normal numbers: 2^-149."""
+    a, b = torch.full((n,), 3.0e38, device="cuda"), torch.full((7,), -1.0e38, device="cuda", dtype=BF16)
+    norm = math.sqrt(sum(t.double().square().sum().item() for t in (a, b)))
+    out = [torch.empty_like(a), torch.empty_like(b)]
+    limit = 100.0
+    c = limit / norm
+    assert norm > 3.5e38 and c < 1
+    got = g.gear_clip_grads(g.GradList([a, b], out), limit)
+    assert got.item() == math.inf
+    for t, o in zip((a, b), out):
+        within(o, t.double() * c, torch.full_like(t.double(), 2.0 ** -149) + (4 * U + HALF[t.dtype] + 2.0 ** -149 / c) * c * t.double().abs())
