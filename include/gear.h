@@ -437,8 +437,9 @@ size_t gear_expert_wgrad_workspace_bytes(int32_t dtype, int64_t rows, int32_t ex
 gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
 /* A list of gradients, for their global norm and for clipping.  The caller describes its tensors on the host (contiguous,
- * n >= 0 elements, aligned to an element; dst may be src or another tensor, not one that overlaps it in part, and may be
- * NULL where only the norm is wanted), gear_grad_list_pack writes the list's device form into host memory
+ * n >= 0 elements, aligned to an element; dst may be src or another tensor, and may be NULL where only the norm is wanted.
+ * No dst may share memory with its src in part, with another entry's dst or with another entry's src: who scales an element first
+ * would be chance.  gear_grad_list_pack does not look for that, the caller knows its tensors), gear_grad_list_pack writes the list's device form into host memory
  * (gear_grad_list_bytes(count) bytes) and the caller copies that to the device (16-byte aligned) and keeps it as long as
  * the tensors live where they are.  chunks (out): pieces of work in the list, handed to the calls below. */
 typedef struct {

@@ -3,6 +3,7 @@ memory, marshalling.  Matrices are [rows x width] with neighbouring columns next
 Calls enqueue on the current stream and do not synchronise."""
 from __future__ import annotations
 
+import bisect
 import ctypes as C
 from typing import NamedTuple, Optional, Sequence, Tuple
 
@@ -357,10 +358,27 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     return dw
 
 
+def _share_memory(src: Sequence[Tuple[int, int]], dst: Sequence[Tuple[int, int]]) -> bool:
+    """Whether a range (address, bytes) of dst meets another one of dst, or one of src other than all of its own."""
+    at = sorted((a, a + n, i) for i, (a, n) in enumerate(dst) if n > 0)
+    if any(a[1] > b[0] for a, b in zip(at, at[1:])):
+        return True
+    ends = [a[1] for a in at]
+    for i, (a, n) in enumerate(src):
+        k = bisect.bisect_right(ends, a)
+        while n > 0 and k < len(at) and at[k][0] < a + n:
+            if at[k] != (a, a + n, i):
+                return True
+            k += 1
+    return False
+
+
 class GradList:
     """A list of gradients for gear_grad_norm and gear_clip_grads; `out` (the tensors that receive the clipped gradients) is
     the gradients themselves unless given.  Holds for as long as the tensors keep their memory: build it once, or again when
-    a gradient has been replaced."""
+    a gradient has been replaced.  Elements that two workgroups would scale, or one reads while another writes them, are
+    refused: list a tensor that is used twice once.  (Without `out` such a list has its norm, but cannot be clipped.)  Calls
+    on one list share its workspace: they come one after another."""
 
     def __init__(self, grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
         where = "GradList"
@@ -372,6 +390,12 @@ class GradList:
             _need(all(t.is_cuda and t.is_contiguous() and t.dtype in _CODE for t in (g, o)) and g.dtype == o.dtype and g.numel() == o.numel(),
                   where, "contiguous float32 or bfloat16 tensors on the GPU, each as large as the one that receives it")
             e.src, e.dst, e.n, e.dtype = g.data_ptr() or None, o.data_ptr() or None, g.numel(), _CODE[g.dtype]
+        where_of = lambda tensors: [(t.data_ptr(), t.numel() * t.element_size()) for t in tensors]
+        self.clips = not _share_memory(where_of(self.grads), where_of(self.out))
+        if not self.clips:
+            _need(out is None, where, "a tensor that receives clipped gradients shares memory with another one of the list")
+            for e in entries:
+                e.dst = None
         host = torch.empty(lib.gear_grad_list_bytes(len(self.grads)), dtype=torch.uint8)
         chunks = C.c_int64()
         _check(lib.gear_grad_list_pack(entries, len(self.grads), host.data_ptr(), C.byref(chunks)), where)
@@ -398,6 +422,7 @@ def gear_grad_norm(grads: GradList, norm: Optional[torch.Tensor] = None) -> torc
 
 def gear_clip_grads(grads: GradList, max_norm: float, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scales the gradients of the list so that their norm is at most max_norm; returns the norm [1] that they had."""
+    _need(grads.clips, "gear_clip_grads", "tensors of the list share memory")
     norm = _norm_word(norm, grads, "gear_clip_grads")
     what, room = grads.plan
     _check(lib.gear_clip_grads(*what, max_norm, *room, norm.data_ptr(), _raw_stream(norm.device.index)), "gear_clip_grads")

@@ -155,3 +155,24 @@ def test_clipping_of_gradients_whose_norm_fp32_does_not_hold(g, n):
     assert got.item() == math.inf
     for t, o in zip((a, b), out):
         within(o, t.double() * c, torch.full_like(t.double(), 2.0 ** -149) + (4 * U + HALF[t.dtype] + 2.0 ** -149 / c) * c * t.double().abs())
+
+
+def test_lists_whose_tensors_share_memory(g):
+    a, b = torch.randn(1000, device="cuda", generator=gen(1)), torch.randn(1000, device="cuda", generator=gen(2))
+    before, room = a.clone(), torch.empty(2000, device="cuda")
+    norm = a.double().norm().item()
+    twice = g.GradList([a, a])
+    assert abs(g.gear_grad_norm(twice).item() - math.sqrt(2) * norm) <= 2 * U * 2 * norm
+    for refused in (lambda: g.gear_clip_grads(twice, norm / 2), lambda: g.gear_clip_grads(g.GradList([a, a[500:]]), 1.0),
+                    lambda: g.GradList([a, b], [room[:1000], room[999:1999]]), lambda: g.GradList([a, b], [b, a]),
+                    lambda: g.GradList([room[:1000]], [room[1:1001]])):
+        with pytest.raises(g.GearError) as e:
+            refused()
+        assert e.value.code == g.GEAR_ERR_INVALID
+    assert torch.equal(a, before)
+    g.gear_clip_grads(g.GradList([a, a], [room[:1000], room[1000:]]), norm / 2)       # twice into two places
+    c = norm / 2 / (math.sqrt(2) * norm + 1e-6)
+    for part in (room[:1000], room[1000:]):
+        within(part, a.double() * c, 4 * U * c * a.double().abs())
+    g.gear_clip_grads(g.GradList([room[:1000], room[1000:]]), norm / 4)               # neighbours in place
+    assert abs(room.double().norm().item() - norm / 4) <= 1e-5 * norm
