@@ -1,6 +1,6 @@
 """The operators of a Dense Part made of experts (include/gear.h) on PyTorch tensors: argument checks, output and workspace
 memory, marshalling.  Matrices are [rows x width] with neighbouring columns next to each other; rows may lie further apart.
-Calls enqueue on the current stream and do not synchronise."""
+All tensors of a call are on the current GPU.  Calls enqueue on its current stream and do not synchronise."""
 from __future__ import annotations
 
 import bisect
@@ -15,6 +15,7 @@ from .binding import (GEAR_BF16, GEAR_E4M3, GEAR_ERR_INVALID, GEAR_F32, GearErro
 _CODE = {torch.float32: GEAR_F32, torch.bfloat16: GEAR_BF16}
 _BYTE = (torch.uint8, torch.float8_e4m3fn)
 _raw_stream = torch._C._cuda_getCurrentRawStream   # of current_stream(), without the object around it: these calls are short
+_current_gpu = torch._C._cuda_getDevice            # asked for once there is a tensor on a GPU
 
 
 def _refuse(where: str, what: str) -> None:
@@ -26,11 +27,18 @@ def _need(ok: bool, where: str, what: str) -> None:
         _refuse(where, what)
 
 
-def _matrix(t: torch.Tensor, where: str, name: str, dtype: Optional[torch.dtype] = None, shape=None) -> int:
-    """Checks a matrix on the device and returns the distance between its rows."""
+def _gpu(index: int, where: str, name: str) -> int:
+    """The GPU of a call, whose tensors all have to be on it: the current one, as kernels run there."""
+    if index < 0 or index != _current_gpu():
+        _refuse(where, f"{name} has to be on the current GPU")
+    return index
+
+
+def _matrix(t: torch.Tensor, gpu: int, where: str, name: str, dtype: Optional[torch.dtype] = None, shape=None) -> int:
+    """Checks a matrix and returns the distance between its rows."""
     size = t.shape
-    if not t.is_cuda or len(size) != 2 or (t.dtype is not dtype if dtype is not None else t.dtype not in _CODE):
-        _refuse(where, f"{name} has to be a matrix on the GPU of {dtype or 'float32 or bfloat16'}")
+    if t.get_device() != gpu or len(size) != 2 or (t.dtype is not dtype if dtype is not None else t.dtype not in _CODE):
+        _refuse(where, f"{name} has to be a matrix on GPU {gpu} of {dtype or 'float32 or bfloat16'}")
     if shape is not None and size != shape:
         _refuse(where, f"{name} has to be {tuple(shape)}, not {tuple(size)}")
     apart = t.stride()
@@ -39,9 +47,9 @@ def _matrix(t: torch.Tensor, where: str, name: str, dtype: Optional[torch.dtype]
     return apart[0] if size[0] > 1 else size[1]
 
 
-def _vector(t: torch.Tensor, where: str, name: str, dtype: torch.dtype, n: int) -> None:
-    if not t.is_cuda or t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
-        _refuse(where, f"{name} has to be {n} contiguous {dtype} on the GPU")
+def _vector(t: torch.Tensor, gpu: int, where: str, name: str, dtype: torch.dtype, n: int) -> None:
+    if t.get_device() != gpu or t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(where, f"{name} has to be {n} contiguous {dtype} on GPU {gpu}")
 
 
 _words = {}      # GPU -> the word that calls without a status of their own report into, and its address
@@ -75,8 +83,8 @@ class Rows8:
         rows = q.shape[0]
         if not q.is_cuda or q.dtype not in _BYTE or q.shape != (rows, (dim + 127) // 128 * 128) or not q.is_contiguous():
             _refuse("Rows8", "q has to be [rows x gear_rows8_ld(dim)] contiguous bytes on the GPU")
-        if not scale.is_cuda or scale.dtype is not torch.uint8 or scale.shape != (rows, (dim + 511) // 512 * 4) or not scale.is_contiguous():
-            _refuse("Rows8", "scale has to be [rows x gear_scales8_ld(dim)] contiguous bytes on the GPU")
+        if scale.device != q.device or scale.dtype is not torch.uint8 or scale.shape != (rows, (dim + 511) // 512 * 4) or not scale.is_contiguous():
+            _refuse("Rows8", "scale has to be [rows x gear_scales8_ld(dim)] contiguous bytes on q's GPU")
         self.rows, self.dim, self.ld, self.device = rows, dim, q.shape[1], q.device
         self._q, self._scale, self._room, self.p_q, self.p_scale = q, scale, None, q.data_ptr(), scale.data_ptr()
 
@@ -115,24 +123,25 @@ def gear_rmsnorm(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Opti
     """Norm of h = x + residual: the sum (where there is a residual), the norm times gain (`y`), the same in 8 bits (`q8`).
     out: memory for the results (any of its fields may be None) instead of new tensors; sum may be residual or x itself."""
     where = "gear_rmsnorm"
-    ld_x = _matrix(x, where, "x")
+    gpu = _gpu(x.get_device(), where, "x")
+    ld_x = _matrix(x, gpu, where, "x")
     dtype, device, shape = x.dtype, x.device, x.shape
     rows, dim = shape
-    _vector(gain, where, "gain", torch.float32, dim)
+    _vector(gain, gpu, where, "gain", torch.float32, dim)
     o_sum, o_y, r8 = out if out is not None else (None, None, None)
     p_res = p_sum = p_y = p_q = p_scale = None
     ld_r = ld_s = ld_y = 0
     if residual is not None:
-        ld_r, p_res = _matrix(residual, where, "residual", dtype, shape), residual.data_ptr()
+        ld_r, p_res = _matrix(residual, gpu, where, "residual", dtype, shape), residual.data_ptr()
     if o_sum is not None:
-        ld_s, p_sum = _matrix(o_sum, where, "sum", dtype, shape), o_sum.data_ptr()
+        ld_s, p_sum = _matrix(o_sum, gpu, where, "sum", dtype, shape), o_sum.data_ptr()
     elif residual is not None:
         o_sum = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
         ld_s, p_sum = dim, o_sum.data_ptr()
     if not y:
         o_y = None
     elif o_y is not None:
-        ld_y, p_y = _matrix(o_y, where, "y", dtype, shape), o_y.data_ptr()
+        ld_y, p_y = _matrix(o_y, gpu, where, "y", dtype, shape), o_y.data_ptr()
     else:
         o_y = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
         ld_y, p_y = dim, o_y.data_ptr()
@@ -141,11 +150,11 @@ def gear_rmsnorm(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Opti
     else:
         if r8 is None:
             r8 = Rows8.empty(rows, dim, device)
-        elif r8.dim != dim or r8.rows != rows:
-            _refuse(where, "rows8 has another shape than x")
+        elif r8.dim != dim or r8.rows != rows or r8.device.index != gpu:
+            _refuse(where, "rows8 has another shape than x or is on another GPU")
         p_q, p_scale = r8.p_q, r8.p_scale
     a = gear_norm_args(rows, dim, _CODE[dtype], eps, x.data_ptr(), p_res, gain.data_ptr(), p_sum, p_y, ld_x, ld_r, ld_s, ld_y, p_q, p_scale)
-    code = lib.gear_rmsnorm(C.byref(a), _raw_stream(device.index))
+    code = lib.gear_rmsnorm(C.byref(a), _raw_stream(gpu))
     if code:
         _check(code, where)
     return NormOutput(o_sum, o_y, r8)
@@ -155,24 +164,25 @@ def gear_rmsnorm_backward(h: torch.Tensor, gain: torch.Tensor, dy: torch.Tensor,
                           dx: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dx, dgain) of the norm at h, dsum (what flows into the sum itself) added to dx; dx may be dy or dsum."""
     where = "gear_rmsnorm_backward"
+    gpu = _gpu(h.get_device(), where, "h")
     dtype, device, shape = h.dtype, h.device, h.shape
-    ld_h, ld_dy = _matrix(h, where, "h"), _matrix(dy, where, "dy", dtype, shape)
+    ld_h, ld_dy = _matrix(h, gpu, where, "h"), _matrix(dy, gpu, where, "dy", dtype, shape)
     rows, dim = shape
-    _vector(gain, where, "gain", torch.float32, dim)
-    ld_ds = _matrix(dsum, where, "dsum", dtype, shape) if dsum is not None else 0
+    _vector(gain, gpu, where, "gain", torch.float32, dim)
+    ld_ds = _matrix(dsum, gpu, where, "dsum", dtype, shape) if dsum is not None else 0
     if dx is None:
         dx, ld_dx = torch.empty_like(h) if h.is_contiguous() else h.new_empty(shape), dim
     else:
-        ld_dx = _matrix(dx, where, "dx", dtype, shape)
+        ld_dx = _matrix(dx, gpu, where, "dx", dtype, shape)
     if dgain is None:
         dgain = torch.empty_like(gain)
     else:
-        _vector(dgain, where, "dgain", torch.float32, dim)
+        _vector(dgain, gpu, where, "dgain", torch.float32, dim)
     size = lib.gear_norm_backward_workspace_bytes(rows, dim)
     ws = torch.empty(size, dtype=torch.uint8, device=device)
     a = gear_norm_backward_args(rows, dim, _CODE[dtype], eps, h.data_ptr(), dy.data_ptr(), _ptr(dsum), gain.data_ptr(), dx.data_ptr(),
                                 dgain.data_ptr(), ld_h, ld_dy, ld_ds, ld_dx)
-    code = lib.gear_rmsnorm_backward(C.byref(a), ws.data_ptr(), size, _raw_stream(device.index))
+    code = lib.gear_rmsnorm_backward(C.byref(a), ws.data_ptr(), size, _raw_stream(gpu))
     if code:
         _check(code, where)
     return dx, dgain
@@ -181,19 +191,21 @@ def gear_rmsnorm_backward(h: torch.Tensor, gain: torch.Tensor, dy: torch.Tensor,
 def gear_rows8(x: torch.Tensor, out: Optional[Rows8] = None) -> Rows8:
     """x in 8 bits, a scale for every row and 128 columns."""
     where = "gear_rows8"
-    ld = _matrix(x, where, "x")
+    gpu = _gpu(x.get_device(), where, "x")
+    ld = _matrix(x, gpu, where, "x")
     rows, dim = x.shape
     if out is None:
         out = Rows8.empty(rows, dim, x.device)
-    elif out.dim != dim or out.rows != rows:
-        _refuse(where, "out has another shape than x")
-    _check(lib.gear_rows8(x.data_ptr(), _CODE[x.dtype], ld, rows, dim, out.p_q, out.p_scale, _raw_stream(x.device.index)), where)
+    elif out.dim != dim or out.rows != rows or out.device.index != gpu:
+        _refuse(where, "out has another shape than x or is on another GPU")
+    _check(lib.gear_rows8(x.data_ptr(), _CODE[x.dtype], ld, rows, dim, out.p_q, out.p_scale, _raw_stream(gpu)), where)
     return out
 
 
 def _weights(w: torch.Tensor, where: str) -> Tuple[int, int, int]:
-    if not w.is_cuda or w.dim() not in (2, 3) or w.dtype not in _CODE or not w.is_contiguous():
-        _refuse(where, "w has to be contiguous [experts x N x K] or [N x K] on the GPU, float32 or bfloat16")
+    _gpu(w.get_device(), where, "w")
+    if w.dim() not in (2, 3) or w.dtype not in _CODE or not w.is_contiguous():
+        _refuse(where, "w has to be contiguous [experts x N x K] or [N x K], float32 or bfloat16")
     return (1, *w.shape) if len(w.shape) == 2 else tuple(w.shape)
 
 
@@ -201,10 +213,11 @@ class _Packed:
     """Memory of weights laid out for the products."""
 
     def _allocate(self, size: int, device) -> None:
+        self.gpu = device.index
         self.packed = torch.empty(size, dtype=torch.uint8, device=device)
         self.address = self.packed.data_ptr()
-        if device.index not in _words and not torch.cuda.is_current_stream_capturing():
-            _word(device.index, "weights")                  # there when products are captured
+        if self.gpu not in _words and not torch.cuda.is_current_stream_capturing():
+            _word(self.gpu, "weights")                  # there when products are captured
 
     @property
     def status(self) -> torch.Tensor:
@@ -224,7 +237,7 @@ class Weights8(_Packed):
         self._allocate(size + scales, w.device)
         self.p_scale = self.address + size
         _check(lib.gear_pack_weights(w.data_ptr(), _CODE[w.dtype], GEAR_E4M3, *shape, self.address, None, self.p_scale,
-                                     _raw_stream(w.device.index)), where)
+                                     _raw_stream(self.gpu)), where)
 
 
 def gear_weights8(w: torch.Tensor) -> Weights8:
@@ -254,38 +267,40 @@ class ExpertWeights(_Packed):
 
     def _lay_out(self, w: torch.Tensor) -> None:
         code = lib.gear_pack_weights(w.data_ptr(), _CODE[w.dtype], self.code, self.experts, self.N, self.K, self.forward, self.transposed, None,
-                                     _raw_stream(w.device.index))
+                                     _raw_stream(self.gpu))
         if code:
             _check(code, "ExpertWeights")
 
     def update(self, w: torch.Tensor) -> None:
-        if _weights(w, "ExpertWeights.update") != (self.experts, self.N, self.K):
-            _refuse("ExpertWeights.update", "w has another shape than before")
+        if _weights(w, "ExpertWeights.update") != (self.experts, self.N, self.K) or w.get_device() != self.gpu:
+            _refuse("ExpertWeights.update", "w has another shape than before or is on another GPU")
         self._lay_out(w)
 
 
 def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, rows, n, k, off, out, out_dtype, status, device) -> torch.Tensor:
-    experts = weights.experts
+    experts, gpu = weights.experts, device.index
+    if weights.gpu != gpu:
+        _refuse(where, "rows and weights are on different GPUs")
     if off is not None:
-        _vector(off, where, "off", torch.int32, experts + 1)
+        _vector(off, gpu, where, "off", torch.int32, experts + 1)
         off = off.data_ptr()
     elif experts != 1:
         _refuse(where, "off may only be left out where there is one expert")
     keep = 0
     if status is not None:
-        _vector(status, where, "status", torch.int32, 1)
+        _vector(status, gpu, where, "status", torch.int32, 1)
         status = status.data_ptr()
     elif off is not None:
-        status, keep = _word(device.index, where)[1], 1
+        status, keep = _word(gpu, where)[1], 1
     if out is None:
         if out_dtype not in _CODE:
             _refuse(where, f"out_dtype has to be float32 or bfloat16, not {out_dtype}")
         out, ld_out = torch.empty(rows, n, dtype=out_dtype, device=device), n
     else:
-        ld_out = _matrix(out, where, "out", None, (rows, n))
+        ld_out = _matrix(out, gpu, where, "out", None, (rows, n))
     a = gear_expert_args(dtype, _CODE[out.dtype], rows, k, n, experts, p_x, p_x_scale, packed, p_w_scale, off, out.data_ptr(), ld_x, ld_out,
                          status, keep)
-    code = lib.gear_expert_product(C.byref(a), _raw_stream(device.index))
+    code = lib.gear_expert_product(C.byref(a), _raw_stream(gpu))
     if code:
         _check(code, where)
     return out
@@ -296,6 +311,7 @@ def gear_matmul8(rows8: Rows8, weights: Weights8, off: Optional[torch.Tensor] = 
     """rows8 times the transposed 8-bit weights.  off [experts + 1] (int32, on the GPU): where each expert's rows begin; rows
     from off[experts] on are not written.  status [1] (int32; weights.status if not given): GEAR_ERR_RANGE if off is no such
     list, and nothing is written."""
+    _gpu(rows8.device.index, "gear_matmul8", "rows8")
     if rows8.dim != weights.K:
         _refuse("gear_matmul8", f"rows of {rows8.dim} for weights of {weights.K}")
     return _product("gear_matmul8", GEAR_E4M3, rows8.p_q, rows8.p_scale, rows8.ld, weights, weights.address, weights.p_scale, rows8.rows,
@@ -306,7 +322,7 @@ def gear_expert_matmul(x: torch.Tensor, weights: ExpertWeights, off: Optional[to
                        out_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows x K] times the transposed weights of each row's expert: [rows x N]; off and status as for gear_matmul8."""
     where = "gear_expert_matmul"
-    ld = _matrix(x, where, "x", weights.dtype, (x.shape[0], weights.K))
+    ld = _matrix(x, _gpu(x.get_device(), where, "x"), where, "x", weights.dtype, (x.shape[0], weights.K))
     return _product(where, weights.code, x.data_ptr(), None, ld, weights, weights.forward, None, x.shape[0], weights.N, weights.K, off, out,
                     out_dtype or x.dtype, status, x.device)
 
@@ -315,7 +331,7 @@ def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[to
                       out_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dy [rows x N] times the weights of each row's expert: the gradient [rows x K] of gear_expert_matmul's x."""
     where = "gear_expert_dgrad"
-    ld = _matrix(dy, where, "dy", weights.dtype, (dy.shape[0], weights.N))
+    ld = _matrix(dy, _gpu(dy.get_device(), where, "dy"), where, "dy", weights.dtype, (dy.shape[0], weights.N))
     if weights.transposed is None:
         _refuse(where, "the weights were laid out without backward")
     return _product(where, weights.code, dy.data_ptr(), None, ld, weights, weights.transposed, None, dy.shape[0], weights.K, weights.N, off,
@@ -328,31 +344,32 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     (int32): GEAR_ERR_RANGE if it is no such list, and nothing is written, otherwise 0; without it the error is left in
     gear_expert_status."""
     where = "gear_expert_wgrad"
-    ld_x = _matrix(x, where, "x")
+    gpu = _gpu(x.get_device(), where, "x")
+    ld_x = _matrix(x, gpu, where, "x")
     device = x.device
     rows, k = x.shape
     n = dy.shape[-1]
-    ld_dy = _matrix(dy, where, "dy", x.dtype, (rows, n))
+    ld_dy = _matrix(dy, gpu, where, "dy", x.dtype, (rows, n))
     experts = 1
     if off is not None:
         experts = off.numel() - 1
-        _vector(off, where, "off", torch.int32, experts + 1)
+        _vector(off, gpu, where, "off", torch.int32, experts + 1)
     keep, p_status = 0, None
     if status is not None:
-        _vector(status, where, "status", torch.int32, 1)
+        _vector(status, gpu, where, "status", torch.int32, 1)
         p_status = status.data_ptr()
     elif off is not None:
-        p_status, keep = _word(device.index, where)[1], 1
+        p_status, keep = _word(gpu, where)[1], 1
     if dw is None:
         dw = torch.empty(experts, n, k, dtype=torch.float32, device=device)
     else:
-        _vector(dw, where, "dw", torch.float32, experts * n * k)
+        _vector(dw, gpu, where, "dw", torch.float32, experts * n * k)
     dtype = _CODE[x.dtype]
     size = lib.gear_expert_wgrad_workspace_bytes(dtype, rows, experts, n, k)
     ws = torch.empty(size, dtype=torch.uint8, device=device)
     a = gear_expert_wgrad_args(dtype, rows, k, n, experts, dy.data_ptr(), x.data_ptr(), _ptr(off), dw.data_ptr(), ld_dy, ld_x,
                                p_status, keep)
-    code = lib.gear_expert_wgrad(C.byref(a), ws.data_ptr(), size, _raw_stream(device.index))
+    code = lib.gear_expert_wgrad(C.byref(a), ws.data_ptr(), size, _raw_stream(gpu))
     if code:
         _check(code, where)
     return dw
@@ -385,10 +402,11 @@ class GradList:
         _need(len(grads) > 0 and (out is None or len(out) == len(grads)), where, "a list of tensors, and as many to receive them")
         self.grads = list(grads)
         self.out = self.grads if out is None else list(out)
+        self.gpu = _gpu(self.grads[0].get_device(), where, "the first gradient")
         entries = (gear_grad_tensor * len(self.grads))()
         for e, g, o in zip(entries, self.grads, self.out):
-            _need(all(t.is_cuda and t.is_contiguous() and t.dtype in _CODE for t in (g, o)) and g.dtype == o.dtype and g.numel() == o.numel(),
-                  where, "contiguous float32 or bfloat16 tensors on the GPU, each as large as the one that receives it")
+            _need(all(t.get_device() == self.gpu and t.is_contiguous() and t.dtype in _CODE for t in (g, o)) and g.dtype == o.dtype and g.numel() == o.numel(),
+                  where, "contiguous float32 or bfloat16 tensors on one GPU, each as large as the one that receives it")
             e.src, e.dst, e.n, e.dtype = g.data_ptr() or None, o.data_ptr() or None, g.numel(), _CODE[g.dtype]
         where_of = lambda tensors: [(t.data_ptr(), t.numel() * t.element_size()) for t in tensors]
         self.clips = not _share_memory(where_of(self.grads), where_of(self.out))
@@ -406,9 +424,10 @@ class GradList:
 
 
 def _norm_word(norm: Optional[torch.Tensor], grads: GradList, where: str) -> torch.Tensor:
+    _gpu(grads.gpu, where, "grads")
     if norm is None:
         return torch.empty((), dtype=torch.float32, device=grads.list.device)
-    _vector(norm, where, "norm", torch.float32, 1)
+    _vector(norm, grads.gpu, where, "norm", torch.float32, 1)
     return norm
 
 
@@ -416,7 +435,7 @@ def gear_grad_norm(grads: GradList, norm: Optional[torch.Tensor] = None) -> torc
     """The norm [1] of all gradients of the list together."""
     norm = _norm_word(norm, grads, "gear_grad_norm")
     what, room = grads.plan
-    _check(lib.gear_grad_norm(*what, *room, norm.data_ptr(), _raw_stream(norm.device.index)), "gear_grad_norm")
+    _check(lib.gear_grad_norm(*what, *room, norm.data_ptr(), _raw_stream(grads.gpu)), "gear_grad_norm")
     return norm
 
 
@@ -425,5 +444,5 @@ def gear_clip_grads(grads: GradList, max_norm: float, norm: Optional[torch.Tenso
     _need(grads.clips, "gear_clip_grads", "tensors of the list share memory")
     norm = _norm_word(norm, grads, "gear_clip_grads")
     what, room = grads.plan
-    _check(lib.gear_clip_grads(*what, max_norm, *room, norm.data_ptr(), _raw_stream(norm.device.index)), "gear_clip_grads")
+    _check(lib.gear_clip_grads(*what, max_norm, *room, norm.data_ptr(), _raw_stream(grads.gpu)), "gear_clip_grads")
     return norm

@@ -3,8 +3,9 @@ import itertools
 import random
 
 import pytest
+import torch
 
-from paper_1806_03925_amd import experts
+from paper_1806_03925_amd import binding as b, experts
 
 
 @pytest.mark.parametrize("src,dst,shared", [
@@ -36,3 +37,95 @@ def test_memory_that_gradients_share_against_every_pair():
         assert experts._share_memory(src, dst) is bool(want), (src, dst)
         seen.add(bool(want))
     assert seen == {True, False}
+
+
+# ---- tensors of several GPUs: stand-ins without memory that say which GPU they are on -----------------------------------------
+PLACES = itertools.count(1 << 20, 1 << 16)
+
+
+class OnGpu(torch.Tensor):
+    gpu = 0
+    is_cuda = True
+    device = property(lambda t: torch.device("cuda", t.gpu))
+    get_device = lambda t: t.gpu
+    data_ptr = lambda t: t.at
+
+
+def on(gpu, *shape, dtype=torch.bfloat16):
+    t = torch.empty(shape, dtype=dtype, device="meta").as_subclass(OnGpu)
+    t.gpu, t.at = gpu, next(PLACES)
+    return t
+
+
+class NothingRuns:
+    def __getattr__(self, name):
+        raise AssertionError(f"{name} was called")
+
+
+def expert_weights(gpu, kind=experts.ExpertWeights):
+    w = object.__new__(kind)
+    w.experts, w.N, w.K, w.dtype, w.code, w.gpu = 2, 72, 64, torch.bfloat16, b.GEAR_BF16, gpu
+    w.address = w.forward = w.transposed = w.p_scale = w.p_status = 1 << 20
+    return w
+
+
+def rows8(gpu, dim=64):
+    return experts.Rows8(on(gpu, 4, 128, dtype=torch.uint8), on(gpu, 4, 4, dtype=torch.uint8), dim)
+
+
+F32, I32 = torch.float32, torch.int32
+MOVED = {   # call -> its tensors: each of them on the other GPU once, all others on this one
+    "rmsnorm": (dict(x=lambda d: on(d, 4, 64), gain=lambda d: on(d, 64, dtype=F32), residual=lambda d: on(d, 4, 64), sum=lambda d: on(d, 4, 64),
+                     y=lambda d: on(d, 4, 64), rows8=rows8),
+                lambda x, gain, residual, sum, y, rows8: experts.gear_rmsnorm(x, gain, 1e-6, residual, True, True, experts.NormOutput(sum, y, rows8))),
+    "backward": (dict(h=lambda d: on(d, 4, 64), gain=lambda d: on(d, 64, dtype=F32), dy=lambda d: on(d, 4, 64), dsum=lambda d: on(d, 4, 64),
+                      dx=lambda d: on(d, 4, 64), dgain=lambda d: on(d, 64, dtype=F32)),
+                 lambda h, gain, dy, dsum, dx, dgain: experts.gear_rmsnorm_backward(h, gain, dy, 1e-6, dsum, dx, dgain)),
+    "rows8": (dict(x=lambda d: on(d, 4, 64), out=rows8), lambda x, out: experts.gear_rows8(x, out)),
+    "matmul8": (dict(r=rows8, w=lambda d: expert_weights(d, experts.Weights8), off=lambda d: on(d, 3, dtype=I32), out=lambda d: on(d, 4, 72),
+                     status=lambda d: on(d, 1, dtype=I32)),
+                lambda r, w, off, out, status: experts.gear_matmul8(r, w, off, out, status=status)),
+    "matmul": (dict(x=lambda d: on(d, 4, 64), w=expert_weights, off=lambda d: on(d, 3, dtype=I32), out=lambda d: on(d, 4, 72),
+                    status=lambda d: on(d, 1, dtype=I32)),
+               lambda x, w, off, out, status: experts.gear_expert_matmul(x, w, off, out, status=status)),
+    "dgrad": (dict(dy=lambda d: on(d, 4, 72), w=expert_weights, off=lambda d: on(d, 3, dtype=I32), out=lambda d: on(d, 4, 64),
+                   status=lambda d: on(d, 1, dtype=I32)),
+              lambda dy, w, off, out, status: experts.gear_expert_dgrad(dy, w, off, out, status=status)),
+    "wgrad": (dict(dy=lambda d: on(d, 4, 72), x=lambda d: on(d, 4, 64), off=lambda d: on(d, 3, dtype=I32), dw=lambda d: on(d, 2, 72, 64, dtype=F32),
+                   status=lambda d: on(d, 1, dtype=I32)),
+              lambda dy, x, off, dw, status: experts.gear_expert_wgrad(dy, x, off, dw, status)),
+    "update": (dict(w=lambda d: on(d, 2, 72, 64), weights=expert_weights), lambda w, weights: weights.update(w)),
+    "list": (dict(g=lambda d: on(d, 8), h=lambda d: on(d, 8), o=lambda d: on(d, 8), p=lambda d: on(d, 8)),
+             lambda g, h, o, p: experts.GradList([g, h], [o, p])),
+}
+
+
+@pytest.mark.parametrize("call,moved", [(c, m) for c, (tensors, _) in MOVED.items() for m in tensors])
+def test_tensors_of_several_gpus_are_refused(monkeypatch, call, moved):
+    monkeypatch.setattr(experts, "lib", NothingRuns())
+    monkeypatch.setattr(experts, "_current_gpu", lambda: 0, raising=False)
+    tensors, run = MOVED[call]
+    with pytest.raises(b.GearError) as e:
+        run(**{name: make(int(name == moved)) for name, make in tensors.items()})
+    assert e.value.code == b.GEAR_ERR_INVALID
+
+
+@pytest.mark.parametrize("call", MOVED)
+def test_tensors_of_a_gpu_that_is_not_the_current_one_are_refused(monkeypatch, call):
+    """Kernels are launched on the current GPU: neither its streams nor its memory are those of the tensors."""
+    monkeypatch.setattr(experts, "lib", NothingRuns())
+    monkeypatch.setattr(experts, "_current_gpu", lambda: 0, raising=False)
+    tensors, run = MOVED[call]
+    with pytest.raises(b.GearError) as e:
+        run(**{name: make(1) for name, make in tensors.items()})
+    assert e.value.code == b.GEAR_ERR_INVALID
+
+
+@pytest.mark.parametrize("call", MOVED)
+def test_tensors_of_one_gpu_are_taken(monkeypatch, call):
+    """The stand-ins above are refused for where they are and nothing else."""
+    monkeypatch.setattr(experts, "lib", NothingRuns())
+    monkeypatch.setattr(experts, "_current_gpu", lambda: 0, raising=False)
+    tensors, run = MOVED[call]
+    with pytest.raises(AssertionError, match="was called"):
+        run(**{name: make(0) for name, make in tensors.items()})
