@@ -80,7 +80,7 @@ class Rows8:
     __slots__ = ("rows", "dim", "ld", "device", "_q", "_scale", "_room", "p_q", "p_scale")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, dim: int):
-        rows = q.shape[0]
+        rows = q.shape[0] if q.dim() else 0
         if not q.is_cuda or q.dtype not in _BYTE or q.shape != (rows, (dim + 127) // 128 * 128) or not q.is_contiguous():
             _refuse("Rows8", "q has to be [rows x gear_rows8_ld(dim)] contiguous bytes on the GPU")
         if scale.device != q.device or scale.dtype is not torch.uint8 or scale.shape != (rows, (dim + 511) // 512 * 4) or not scale.is_contiguous():
@@ -322,7 +322,9 @@ def gear_expert_matmul(x: torch.Tensor, weights: ExpertWeights, off: Optional[to
                        out_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows x K] times the transposed weights of each row's expert: [rows x N]; off and status as for gear_matmul8."""
     where = "gear_expert_matmul"
-    ld = _matrix(x, _gpu(x.get_device(), where, "x"), where, "x", weights.dtype, (x.shape[0], weights.K))
+    ld = _matrix(x, _gpu(x.get_device(), where, "x"), where, "x", weights.dtype)
+    if x.shape[1] != weights.K:
+        _refuse(where, f"rows of {x.shape[1]} for weights of {weights.K}")
     return _product(where, weights.code, x.data_ptr(), None, ld, weights, weights.forward, None, x.shape[0], weights.N, weights.K, off, out,
                     out_dtype or x.dtype, status, x.device)
 
@@ -331,7 +333,9 @@ def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[to
                       out_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dy [rows x N] times the weights of each row's expert: the gradient [rows x K] of gear_expert_matmul's x."""
     where = "gear_expert_dgrad"
-    ld = _matrix(dy, _gpu(dy.get_device(), where, "dy"), where, "dy", weights.dtype, (dy.shape[0], weights.N))
+    ld = _matrix(dy, _gpu(dy.get_device(), where, "dy"), where, "dy", weights.dtype)
+    if dy.shape[1] != weights.N:
+        _refuse(where, f"rows of {dy.shape[1]} for weights of {weights.N} outputs")
     if weights.transposed is None:
         _refuse(where, "the weights were laid out without backward")
     return _product(where, weights.code, dy.data_ptr(), None, ld, weights, weights.transposed, None, dy.shape[0], weights.K, weights.N, off,
@@ -347,12 +351,16 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     gpu = _gpu(x.get_device(), where, "x")
     ld_x = _matrix(x, gpu, where, "x")
     device = x.device
+    ld_dy = _matrix(dy, gpu, where, "dy", x.dtype)
     rows, k = x.shape
-    n = dy.shape[-1]
-    ld_dy = _matrix(dy, gpu, where, "dy", x.dtype, (rows, n))
+    n = dy.shape[1]
+    if dy.shape[0] != rows:
+        _refuse(where, f"dy has {dy.shape[0]} rows and x {rows}")
     experts = 1
     if off is not None:
         experts = off.numel() - 1
+        if experts < 1:
+            _refuse(where, "off has to hold a begin and an end at least")
         _vector(off, gpu, where, "off", torch.int32, experts + 1)
     keep, p_status = 0, None
     if status is not None:

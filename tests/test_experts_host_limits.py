@@ -129,3 +129,23 @@ def test_tensors_of_one_gpu_are_taken(monkeypatch, call):
     tensors, run = MOVED[call]
     with pytest.raises(AssertionError, match="was called"):
         run(**{name: make(0) for name, make in tensors.items()})
+
+
+@pytest.mark.parametrize("call", [
+    lambda: experts.gear_expert_wgrad(on(0, 4, 72), on(0, 4, 64), on(0, 0, dtype=I32)),             # no offset at all
+    lambda: experts.gear_expert_wgrad(on(0, 4, 72), on(0, 4, 64), on(0, 1, dtype=I32)),             # of no expert
+    lambda: experts.gear_expert_wgrad(on(0), on(0, 4, 64)),
+    lambda: experts.gear_expert_wgrad(on(0, 4, 72), on(0)),
+    lambda: experts.gear_expert_matmul(on(0), expert_weights(0), on(0, 3, dtype=I32)),
+    lambda: experts.gear_expert_dgrad(on(0), expert_weights(0), on(0, 3, dtype=I32)),
+    lambda: experts.gear_rmsnorm(on(0), on(0, 64, dtype=F32), 1e-6),
+    lambda: experts.gear_rmsnorm_backward(on(0), on(0, 64, dtype=F32), on(0), 1e-6),
+    lambda: experts.gear_rows8(on(0)),
+    lambda: experts.gear_weights8(on(0)),
+    lambda: experts.Rows8(on(0, dtype=torch.uint8), on(0, dtype=torch.uint8), 64)])
+def test_tensors_without_dimensions_and_lists_without_entries(monkeypatch, call):
+    monkeypatch.setattr(experts, "lib", NothingRuns())
+    monkeypatch.setattr(experts, "_current_gpu", lambda: 0)
+    with pytest.raises(b.GearError) as e:
+        call()
+    assert e.value.code == b.GEAR_ERR_INVALID
