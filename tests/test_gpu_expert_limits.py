@@ -176,3 +176,40 @@ def test_lists_whose_tensors_share_memory(g):
         within(part, a.double() * c, 4 * U * c * a.double().abs())
     g.gear_clip_grads(g.GradList([room[:1000], room[1000:]]), norm / 4)               # neighbours in place
     assert abs(room.double().norm().item() - norm / 4) <= 1e-5 * norm
+
+
+# ---- many experts, some of whose rows are cut into pieces ---------------------------------------------------------------
+MANY = [[i % 3 for i in range(70)], [1] * 131]
+MANY[0][3], MANY[0][64], MANY[0][69] = 3000, 2500, 4100
+MANY[1][0], MANY[1][66], MANY[1][130] = 5000, 1800, 2600
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,k", [(8, 8), (40, 136), (72, 128), (136, 320)])
+@pytest.mark.parametrize("sizes", MANY)
+def test_weight_gradients_of_more_than_64_experts_some_of_them_long(g, dtype, n, k, sizes):
+    """More experts than one look at the offsets finds: pieces, and the partial results before them, behind the 64th too."""
+    r = gen(n + k)
+    rows = sum(sizes)
+    dy, x = (torch.randn(rows, w, device="cuda", generator=r).to(dtype) for w in (n, k))
+    off = torch.tensor([0] + sizes).cumsum(0).to(torch.int32).cuda()
+    dw = g.gear_expert_wgrad(dy, x, off)
+    at = 0
+    for e, m in enumerate(sizes):
+        a, b = dy[at:at + m].double(), x[at:at + m].double()
+        within(dw[e], a.t().contiguous() @ b, (m + 8) * 2 * U * (a.abs().t().contiguous() @ b.abs()))
+        at += m
+    assert torch.equal(dw, g.gear_expert_wgrad(dy, x, off))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,dim", [(1, 72), (9, 1152), (5000, 264), (700, 2056)])
+def test_norm_backward_without_the_gradient_of_the_gain(g, dtype, rows, dim):
+    """dgain = NULL needs no workspace and leaves dx as it is with one."""
+    r = gen(rows + dim)
+    h, dy = (torch.randn(rows, dim, device="cuda", generator=r).to(dtype) for _ in range(2))
+    gain, dx = 1 + 0.3 * torch.randn(dim, device="cuda", generator=r), torch.empty_like(h)
+    a = g.binding.gear_norm_backward_args(rows, dim, g.GEAR_F32 if dtype is F32 else g.GEAR_BF16, 1e-5, h.data_ptr(), dy.data_ptr(), None,
+                                          gain.data_ptr(), dx.data_ptr(), None, dim, dim, 0, dim)
+    assert g.lib.gear_rmsnorm_backward(C.byref(a), None, 0, torch.cuda.current_stream().cuda_stream) == g.GEAR_OK
+    assert torch.equal(dx, g.gear_rmsnorm_backward(h, gain, dy, 1e-5)[0])
