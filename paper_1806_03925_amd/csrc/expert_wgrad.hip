@@ -464,7 +464,8 @@ extern "C" gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *
   const WgradArgs w = {a->dy, a->x, a->off, a->dw, a->ld_dy, a->ld_x, (int)a->rows, a->K, a->N, a->experts, a->status,
                        static_cast<float *>(workspace), cut, a->keep_status};
   hipStream_t s = (hipStream_t)stream;
-  const int64_t pieces = a->off ? a->experts + a->rows / cut : (a->rows + cut - 1) / cut;
+  // rows that are not cut add no piece: the largest gradients have as many tiles as a launch may have threads for
+  const int64_t pieces = a->off ? a->experts + (cut < a->rows ? a->rows / cut : 0) : (a->rows + cut - 1) / cut;
   const unsigned blocks = wgrad_blocks((pieces > 0 ? pieces : 1) * wgrad_tiles(shape, a->N, a->K));
   if (a->dtype == GEAR_F32) {
     if (launch<TnTile<float, 1, 1, 2>>(w, blocks, s) != hipSuccess) return GEAR_ERR_HIP;

@@ -213,3 +213,20 @@ def test_norm_backward_without_the_gradient_of_the_gain(g, dtype, rows, dim):
                                           gain.data_ptr(), dx.data_ptr(), None, dim, dim, 0, dim)
     assert g.lib.gear_rmsnorm_backward(C.byref(a), None, 0, torch.cuda.current_stream().cuda_stream) == g.GEAR_OK
     assert torch.equal(dx, g.gear_rmsnorm_backward(h, gain, dy, 1e-5)[0])
+
+
+def test_a_weight_gradient_of_as_many_tiles_as_there_may_be(g):
+    """2^23 tiles of 64 x 64, 137 GB of them: 2^31 threads, and as many again would be more than a launch takes."""
+    torch.cuda.empty_cache()
+    n, k = (1 << 20) - 8, 1 << 15
+    if torch.cuda.mem_get_info()[0] < 4 * n * k + (8 << 30):
+        pytest.skip("needs 146 GB of the GPU's memory")
+    dy, x = torch.randn(1, n, device="cuda", generator=gen(1)), torch.randn(1, k, device="cuda", generator=gen(2))
+    dw = g.gear_expert_wgrad(dy, x, torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
+    for at in (0, 12_345, n - 1):
+        assert torch.equal(dw[0, at], dy[0, at] * x[0])     # one product each: nothing is added
+    for at in (0, 777, k - 1):
+        assert torch.equal(dw[0, :, at], dy[0] * x[0, at])
+    assert g.gear_expert_status().item() == 0
+    del dw
+    torch.cuda.empty_cache()
