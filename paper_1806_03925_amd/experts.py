@@ -77,7 +77,7 @@ def gear_expert_status(device=None) -> torch.Tensor:
 
 class Rows8:
     """Rows in 8 bits: q [rows x gear_rows8_ld(dim)] (bytes of e4m3), scale [rows x gear_scales8_ld(dim)] (exponent + 127)."""
-    __slots__ = ("rows", "dim", "ld", "device", "_q", "_scale", "_room", "p_q", "p_scale")
+    __slots__ = ("rows", "dim", "ld", "device", "gpu", "_q", "_scale", "_room", "p_q", "p_scale")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, dim: int):
         rows = q.shape[0] if q.dim() else 0
@@ -85,14 +85,14 @@ class Rows8:
             _refuse("Rows8", "q has to be [rows x gear_rows8_ld(dim)] contiguous bytes on the GPU")
         if scale.device != q.device or scale.dtype is not torch.uint8 or scale.shape != (rows, (dim + 511) // 512 * 4) or not scale.is_contiguous():
             _refuse("Rows8", "scale has to be [rows x gear_scales8_ld(dim)] contiguous bytes on q's GPU")
-        self.rows, self.dim, self.ld, self.device = rows, dim, q.shape[1], q.device
+        self.rows, self.dim, self.ld, self.device, self.gpu = rows, dim, q.shape[1], q.device, q.get_device()
         self._q, self._scale, self._room, self.p_q, self.p_scale = q, scale, None, q.data_ptr(), scale.data_ptr()
 
     @staticmethod
     def empty(rows: int, dim: int, device) -> "Rows8":
         """One allocation for both; the tensors are made when somebody asks for them."""
         r = object.__new__(Rows8)
-        r.rows, r.dim, r.ld, r.device = rows, dim, (dim + 127) // 128 * 128, device
+        r.rows, r.dim, r.ld, r.device, r.gpu = rows, dim, (dim + 127) // 128 * 128, device, device.index
         r._q = r._scale = None
         r._room = torch.empty(rows * (r.ld + (dim + 511) // 512 * 4), dtype=torch.uint8, device=device)
         r.p_q = r._room.data_ptr()
@@ -150,7 +150,7 @@ def gear_rmsnorm(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Opti
     else:
         if r8 is None:
             r8 = Rows8.empty(rows, dim, device)
-        elif r8.dim != dim or r8.rows != rows or r8.device.index != gpu:
+        elif r8.dim != dim or r8.rows != rows or r8.gpu != gpu:
             _refuse(where, "rows8 has another shape than x or is on another GPU")
         p_q, p_scale = r8.p_q, r8.p_scale
     a = gear_norm_args(rows, dim, _CODE[dtype], eps, x.data_ptr(), p_res, gain.data_ptr(), p_sum, p_y, ld_x, ld_r, ld_s, ld_y, p_q, p_scale)
@@ -196,7 +196,7 @@ def gear_rows8(x: torch.Tensor, out: Optional[Rows8] = None) -> Rows8:
     rows, dim = x.shape
     if out is None:
         out = Rows8.empty(rows, dim, x.device)
-    elif out.dim != dim or out.rows != rows or out.device.index != gpu:
+    elif out.dim != dim or out.rows != rows or out.gpu != gpu:
         _refuse(where, "out has another shape than x or is on another GPU")
     _check(lib.gear_rows8(x.data_ptr(), _CODE[x.dtype], ld, rows, dim, out.p_q, out.p_scale, _raw_stream(gpu)), where)
     return out
@@ -277,8 +277,8 @@ class ExpertWeights(_Packed):
         self._lay_out(w)
 
 
-def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, rows, n, k, off, out, out_dtype, status, device) -> torch.Tensor:
-    experts, gpu = weights.experts, device.index
+def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, rows, n, k, off, out, out_dtype, status, gpu) -> torch.Tensor:
+    experts = weights.experts
     if weights.gpu != gpu:
         _refuse(where, "rows and weights are on different GPUs")
     if off is not None:
@@ -295,7 +295,7 @@ def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, row
     if out is None:
         if out_dtype not in _CODE:
             _refuse(where, f"out_dtype has to be float32 or bfloat16, not {out_dtype}")
-        out, ld_out = torch.empty(rows, n, dtype=out_dtype, device=device), n
+        out, ld_out = torch.empty(rows, n, dtype=out_dtype, device=gpu), n
     else:
         ld_out = _matrix(out, gpu, where, "out", None, (rows, n))
     a = gear_expert_args(dtype, _CODE[out.dtype], rows, k, n, experts, p_x, p_x_scale, packed, p_w_scale, off, out.data_ptr(), ld_x, ld_out,
@@ -311,35 +311,39 @@ def gear_matmul8(rows8: Rows8, weights: Weights8, off: Optional[torch.Tensor] = 
     """rows8 times the transposed 8-bit weights.  off [experts + 1] (int32, on the GPU): where each expert's rows begin; rows
     from off[experts] on are not written.  status [1] (int32; weights.status if not given): GEAR_ERR_RANGE if off is no such
     list, and nothing is written."""
-    _gpu(rows8.device.index, "gear_matmul8", "rows8")
+    gpu = _gpu(rows8.gpu, "gear_matmul8", "rows8")
     if rows8.dim != weights.K:
         _refuse("gear_matmul8", f"rows of {rows8.dim} for weights of {weights.K}")
     return _product("gear_matmul8", GEAR_E4M3, rows8.p_q, rows8.p_scale, rows8.ld, weights, weights.address, weights.p_scale, rows8.rows,
-                    weights.N, weights.K, off, out, out_dtype, status, rows8.device)
+                    weights.N, weights.K, off, out, out_dtype, status, gpu)
 
 
 def gear_expert_matmul(x: torch.Tensor, weights: ExpertWeights, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                        out_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows x K] times the transposed weights of each row's expert: [rows x N]; off and status as for gear_matmul8."""
     where = "gear_expert_matmul"
-    ld = _matrix(x, _gpu(x.get_device(), where, "x"), where, "x", weights.dtype)
-    if x.shape[1] != weights.K:
-        _refuse(where, f"rows of {x.shape[1]} for weights of {weights.K}")
-    return _product(where, weights.code, x.data_ptr(), None, ld, weights, weights.forward, None, x.shape[0], weights.N, weights.K, off, out,
-                    out_dtype or x.dtype, status, x.device)
+    gpu = _gpu(x.get_device(), where, "x")
+    ld = _matrix(x, gpu, where, "x", weights.dtype)
+    rows, k = x.shape
+    if k != weights.K:
+        _refuse(where, f"rows of {k} for weights of {weights.K}")
+    return _product(where, weights.code, x.data_ptr(), None, ld, weights, weights.forward, None, rows, weights.N, k, off, out,
+                    out_dtype or weights.dtype, status, gpu)
 
 
 def gear_expert_dgrad(dy: torch.Tensor, weights: ExpertWeights, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                       out_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dy [rows x N] times the weights of each row's expert: the gradient [rows x K] of gear_expert_matmul's x."""
     where = "gear_expert_dgrad"
-    ld = _matrix(dy, _gpu(dy.get_device(), where, "dy"), where, "dy", weights.dtype)
-    if dy.shape[1] != weights.N:
-        _refuse(where, f"rows of {dy.shape[1]} for weights of {weights.N} outputs")
+    gpu = _gpu(dy.get_device(), where, "dy")
+    ld = _matrix(dy, gpu, where, "dy", weights.dtype)
+    rows, n = dy.shape
+    if n != weights.N:
+        _refuse(where, f"rows of {n} for weights of {weights.N} outputs")
     if weights.transposed is None:
         _refuse(where, "the weights were laid out without backward")
-    return _product(where, weights.code, dy.data_ptr(), None, ld, weights, weights.transposed, None, dy.shape[0], weights.K, weights.N, off,
-                    out, out_dtype or dy.dtype, status, dy.device)
+    return _product(where, weights.code, dy.data_ptr(), None, ld, weights, weights.transposed, None, rows, weights.K, n, off, out,
+                    out_dtype or weights.dtype, status, gpu)
 
 
 def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
@@ -350,12 +354,11 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     where = "gear_expert_wgrad"
     gpu = _gpu(x.get_device(), where, "x")
     ld_x = _matrix(x, gpu, where, "x")
-    device = x.device
     ld_dy = _matrix(dy, gpu, where, "dy", x.dtype)
     rows, k = x.shape
-    n = dy.shape[1]
-    if dy.shape[0] != rows:
-        _refuse(where, f"dy has {dy.shape[0]} rows and x {rows}")
+    rows_dy, n = dy.shape
+    if rows_dy != rows:
+        _refuse(where, f"dy has {rows_dy} rows and x {rows}")
     experts = 1
     if off is not None:
         experts = off.numel() - 1
@@ -369,12 +372,12 @@ def gear_expert_wgrad(dy: torch.Tensor, x: torch.Tensor, off: Optional[torch.Ten
     elif off is not None:
         p_status, keep = _word(gpu, where)[1], 1
     if dw is None:
-        dw = torch.empty(experts, n, k, dtype=torch.float32, device=device)
+        dw = torch.empty(experts, n, k, dtype=torch.float32, device=gpu)
     else:
         _vector(dw, gpu, where, "dw", torch.float32, experts * n * k)
     dtype = _CODE[x.dtype]
     size = lib.gear_expert_wgrad_workspace_bytes(dtype, rows, experts, n, k)
-    ws = torch.empty(size, dtype=torch.uint8, device=device)
+    ws = torch.empty(size, dtype=torch.uint8, device=gpu)
     a = gear_expert_wgrad_args(dtype, rows, k, n, experts, dy.data_ptr(), x.data_ptr(), _ptr(off), dw.data_ptr(), ld_dy, ld_x,
                                p_status, keep)
     code = lib.gear_expert_wgrad(C.byref(a), ws.data_ptr(), size, _raw_stream(gpu))
