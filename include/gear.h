@@ -323,7 +323,7 @@ gear_status gear_gemm(int32_t dtype, int32_t form, const void *A, const void *B,
  * As elsewhere: device memory of the caller's, no allocation, nothing kept between calls, kernels enqueued on `stream`,
  * results independent of how the device schedules its work.  Widths (dim, K, N) are multiples of 8; the distance
  * between rows (ld_*, in elements) is a multiple of 8 and at least the width, below 2^20; matrices start on 16 bytes.
- * A call on no rows does nothing but what it says it does then.  Sums are fp32 (norms of lists of gradients
+ * At most 2^30 rows.  A call on no rows does nothing but what it says it does then.  Sums are fp32 (norms of lists of gradients
  * and norms in 8 bits: fp64).
  *
  * 8 bits.  A row of `dim` values in 8 bits is gear_rows8_ld(dim) bytes of e4m3 (4 exponent, 3 fraction bits, largest
@@ -333,7 +333,8 @@ gear_status gear_gemm(int32_t dtype, int32_t form, const void *A, const void *B,
  * loses nothing and what is rounded (to nearest, ties to even) is only the value's fraction.  Infinities and NaN
  * become NaN and do not count for the scale.  The matrix instruction takes the scales as they are.  It adds eight
  * neighbouring products at once and keeps of each what is at least 2^-13 of the largest one's power of two; everything
- * beyond these eight is added in fp32. */
+ * beyond these eight is added in fp32.  Of random rows that is 1.5e-5 of the result (576 to 4096 columns; the rounding of the
+ * operands to 8 bits: 4e-2), so results in fp32 are no more exact than that. */
 #define GEAR_E4M3 2            /* beside gear_dtype, where a call says that it takes it: 8 bits with scales */
 #define GEAR_MAX_NORM_DIM 65536
 #define GEAR_MAX_EXPERTS 1024
@@ -379,7 +380,7 @@ typedef struct {
 size_t gear_norm_backward_workspace_bytes(int64_t rows, int32_t dim);
 gear_status gear_rmsnorm_backward(const gear_norm_backward_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
-/* x [rows x dim] (dtype, ld_x) in 8 bits: q8 and scale as above. */
+/* x [rows x dim] (dtype, ld_x; dim at most GEAR_MAX_NORM_DIM) in 8 bits: q8 and scale as above. */
 gear_status gear_rows8(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t dim, uint8_t *q8, uint8_t *scale,
                        void *stream);
 
@@ -439,7 +440,8 @@ gear_status gear_expert_wgrad(const gear_expert_wgrad_args *a, void *workspace, 
 /* A list of gradients, for their global norm and for clipping.  The caller describes its tensors on the host (contiguous,
  * n >= 0 elements, aligned to an element; dst may be src or another tensor, and may be NULL where only the norm is wanted.
  * No dst may share memory with its src in part, with another entry's dst or with another entry's src: who scales an element first
- * would be chance.  gear_grad_list_pack does not look for that, the caller knows its tensors), gear_grad_list_pack writes the list's device form into host memory
+ * would be chance.  gear_grad_list_pack does not look for that, the caller knows its tensors), gear_grad_list_pack writes the
+ * list's device form into host memory
  * (gear_grad_list_bytes(count) bytes) and the caller copies that to the device (16-byte aligned) and keeps it as long as
  * the tensors live where they are.  chunks (out): pieces of work in the list, handed to the calls below. */
 typedef struct {

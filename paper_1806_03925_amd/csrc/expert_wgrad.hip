@@ -1,5 +1,6 @@
 // Weight gradients grouped by expert, dW_e = dy_e^T x_e over the rows of every expert: a contraction over the rows, whose
-// number only the device knows.  A workgroup takes one tile of one expert's gradient and walks all of that expert's rows.
+// number only the device knows.  A workgroup takes one tile of one expert's gradient and walks that expert's rows, or a piece of
+// them: long experts are cut, and what their pieces add up to is summed afterwards.
 #include "experts.hpp"
 
 #include <type_traits>
@@ -220,8 +221,8 @@ template <typename C> __global__ void __launch_bounds__(C::THREADS) k_expert_wgr
 }
 
 // ---- bf16: 128 x 256 by four wavefronts of 64 x 128 ----------------------------------------------------------------
-// Both operands pass LDS, and LDS bounds this product: of 32 rows a tile of 128 x 128 (four wavefronts of 64 x 64) moves 48 KB
-// through it for 256 cycles of matrix instructions, this one 72 KB for 512.  Two workgroups share a CU, so that one stores
+// Both operands pass LDS, whose 128 bytes a cycle bound the loop: of 32 rows a tile of 128 x 128 (four wavefronts of 64 x 64) moves 48 KB
+// through it for 256 cycles of matrix instructions (these are busy 0.67 of the time at most), this one 72 KB for 512 (0.89).  Two workgroups share a CU, so that one stores
 // its gradient (128 KB) while the other multiplies; and operands are requested a k-step (16 rows) ahead, also across the
 // border of a stage.
 template <int TM_, int TN_, int WAVES_M_, int WAVES_N_, int STAGES_> struct WideTile {

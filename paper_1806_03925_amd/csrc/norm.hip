@@ -7,7 +7,12 @@
 // leaves fp32's range where h is 1e13 or 1e-13 and is never formed.)
 // Every call is one pass over its rows: a row stays in the registers of the threads that read it, from the sum of its
 // squares to the last output, so what bounds these kernels is the memory they have to read and write (the norm in 8 bits: fp64,
-// see there).
+// see there).  That holds up to 8192 columns (but for two registers of a bf16 row in 8 bits).  Wider rows are 1024 threads', which have 128
+// registers each and keep part of a row in scratch memory; registers spilled up to 32768 columns / beyond, and TB/s of the bytes that a call
+// has to move at 4096 x 16384 / 1024 x 65536:
+//   backward bf16 45 / 265, 2.8 / 1.0; fp32 79 / 442, 3.6 / 1.5 (5.0 and 4.7 at 4096 x 8192)
+//   8 bits   bf16 none / 36, 3.9 / 2.6; fp32 6 / 145, 4.7 / 2.3 (5.3 and 5.1)
+//   norm     bf16 none, 6.7 / 5.8; fp32 none / 41, 4.2 / 3.7 (6.7 and 5.7)
 #include "eight.hpp"
 
 #include <cmath>
@@ -278,10 +283,11 @@ template <typename T, NormKind KIND> hipError_t launch_norm(const gear_norm_args
   return hipGetLastError();
 }
 
-// Workgroups of the backward pass: rows are shared out to them, each leaves one row of partial sums.  As many as are on the
-// device at once, three for each CU in bf16 and two in fp32 (registers): us of 512 / 768 / 1024 / 1536 for 65536 x 2048
-// bf16 204 / 197 / 228 / 202, 65536 x 1152 131 / 120 / 145 / 123 (5.0 TB/s), 16384 x 1024 28.8 / 28.0 / 28.2 / 31.6; fp32
-// 65536 x 2048 408 / 446 / 409 / 413 (5.3 TB/s), 10001 x 512 19.0 / 19.8 / 20.6 / 22.1.
+// Workgroups of the backward pass: rows are shared out to them, each leaves one row of partial sums.  768 in bf16 and 512 in fp32, which are
+// those that are on the device at once for 1025 to 2048 and 4097 to 8192 columns, three and two for each CU (registers; others leave room for
+// four and more, wider rows for one): us of 512 / 768 / 1024 for 65536 x 2048 bf16 178 / 160 / 197, 8192 x 8192 91 / 84 / 103, 16384 x 4096
+// 93 / 80 / 81, 30000 x 1024 38 / 35 / 35, but 65536 x 512 46 / 41 / 37; fp32 65536 x 2048 309 / 347 / 308, 8192 x 8192 169 / 190 / 173, 16384 x
+// 4096 160 / 156 / 162, 65536 x 512 67 / 70 / 70, but 100000 x 264 76 / 59 / 54: narrow rows could do with more of them.
 // Few rows are one workgroup's, which leaves dgain itself: two launches / one, from Python, 32 x 512 bf16 (8 rounds of rows) 12.7 / 10.2, 16 x
 // 1152 (4) 12.8 / 9.8, but 32 x 1152 (8) 12.9 / 15.4.
 int back_blocks(int64_t rows, int32_t dim, int32_t dtype) {

@@ -1,6 +1,9 @@
 """The operators of a Dense Part made of experts (include/gear.h) on PyTorch tensors: argument checks, output and workspace
 memory, marshalling.  Matrices are [rows x width] with neighbouring columns next to each other; rows may lie further apart.
-All tensors of a call are on the current GPU.  Calls enqueue on its current stream and do not synchronise."""
+All tensors of a call are on the current GPU.  Calls enqueue on its current stream and do not synchronise.
+
+These calls are no part of PyTorch's autograd: results have no history, also where an input requires a gradient.  Gradients
+are calls of their own (gear_rmsnorm_backward, gear_expert_dgrad, gear_expert_wgrad) that the program puts together."""
 from __future__ import annotations
 
 import bisect
@@ -309,8 +312,9 @@ def _product(where, dtype, p_x, p_x_scale, ld_x, weights, packed, p_w_scale, row
 def gear_matmul8(rows8: Rows8, weights: Weights8, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                  out_dtype: torch.dtype = torch.bfloat16, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """rows8 times the transposed 8-bit weights.  off [experts + 1] (int32, on the GPU): where each expert's rows begin; rows
-    from off[experts] on are not written.  status [1] (int32; weights.status if not given): GEAR_ERR_RANGE if off is no such
-    list, and nothing is written."""
+    from off[experts] on are not written.  status [1] (int32): GEAR_ERR_RANGE if off is no such list, and nothing is written,
+    otherwise 0; without it the error is left in gear_expert_status.  Sums of eight neighbouring columns keep fewer bits than
+    fp32 (include/gear.h): 1.5e-5 of the result, which out_dtype=float32 shows."""
     gpu = _gpu(rows8.gpu, "gear_matmul8", "rows8")
     if rows8.dim != weights.K:
         _refuse("gear_matmul8", f"rows of {rows8.dim} for weights of {weights.K}")
