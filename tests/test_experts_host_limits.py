@@ -149,3 +149,25 @@ def test_tensors_without_dimensions_and_lists_without_entries(monkeypatch, call)
     with pytest.raises(b.GearError) as e:
         call()
     assert e.value.code == b.GEAR_ERR_INVALID
+
+
+def test_a_first_report_is_not_made_while_a_graph_is_captured(monkeypatch):
+    """The word would belong to the graph, and be cleared by its replays: a call that needs it says so, one with a status of its own does not
+    need it, nor one without offsets."""
+    monkeypatch.setattr(experts, "lib", NothingRuns())
+    monkeypatch.setattr(experts, "_current_gpu", lambda: 0)
+    monkeypatch.setattr(experts, "_words", {})
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    x, dy, off, status = on(0, 4, 64), on(0, 4, 72), on(0, 3, dtype=I32), on(0, 1, dtype=I32)
+    out, dw, weights = on(0, 4, 72), on(0, 2, 72, 64, dtype=F32), expert_weights(0)
+    for call in (lambda: experts.gear_expert_matmul(x, weights, off, out), lambda: experts.gear_expert_wgrad(dy, x, off, dw)):
+        with pytest.raises(b.GearError) as e:
+            call()
+        assert e.value.code == b.GEAR_ERR_INVALID
+    weights.experts = 1
+    for call in (lambda: experts.gear_expert_matmul(x, weights, None, out), lambda: experts.gear_expert_wgrad(dy, x, off, dw, status)):
+        with pytest.raises(AssertionError, match="was called"):
+            call()
+    weights.experts = 2
+    with pytest.raises(AssertionError, match="was called"):
+        experts.gear_expert_matmul(x, weights, off, out, status=status)
