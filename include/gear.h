@@ -463,6 +463,135 @@ gear_status gear_grad_norm(const void *list, int32_t count, int64_t chunks, void
 gear_status gear_clip_grads(const void *list, int32_t count, int64_t chunks, float max_norm, void *workspace,
                             size_t workspace_bytes, float *norm, void *stream);
 
+/* ---- Rows that choose their experts ------------------------------------------------------------------------------
+ * A Dense Part whose rows go to experts by learned scores: the choice and its gradient, the rows' way to their experts and
+ * back and its gradients (Section 3, step 6), for the products above.  The rules of that section hold (widths, distances between rows,
+ * alignment); only logits may have any width, distance and alignment of their elements.
+ *
+ * Scores of a row are the softmax or the sigmoid of its logits.  An expert is eligible where its logit is not -inf and its bias
+ * neither -inf nor NaN; a row with a NaN logit (softmax: or +inf) has no eligible expert and NaN for all its weights.  Experts are ordered
+ * by score + bias in fp64, without a bias by logit, ties by the lowest number.  Experts may come in groups of equal size, one
+ * group's behind the other's: a group's value is the largest score + bias in it, or the sum of the two largest (of as many as
+ * are eligible), and only experts of the groups_kept groups of the largest values (ties by the lowest number) can be chosen.  The k first are chosen; a slot for which
+ * no eligible expert is left holds expert -1 and weighs 0.  The weight of an expert is its score, without the bias, divided by
+ * the sum of the chosen ones' if `renormalise`, times scale.
+ *
+ * Pairs (row, slot) that have an expert are lined up by expert, then row, then slot: place is where, off [experts + 1] where every
+ * expert's begin, as gear_expert_product takes it; place is -1 for a slot without an expert. */
+#define GEAR_SCORE_SOFTMAX 0
+#define GEAR_SCORE_SIGMOID 1
+#define GEAR_MAX_CHOSEN 32
+#define GEAR_MAX_GROUPS 64
+
+/* rows * k is at most 2^30.  n (device word, may be NULL): rows from *n on are padding, whatever they hold, and have no expert.  off and place may
+ * both be NULL where only the choice is wanted; the workspace (256-byte aligned, gear_route_workspace_bytes) is not needed then.
+ * scale > 0.  No rows: off is all zeros. */
+typedef struct {
+  int64_t rows;
+  int32_t experts, k, dtype;              /* gear_dtype of the logits */
+  int32_t score, groups, groups_kept, group_best;   /* group_best: 1 the largest, 2 the sum of two; groups = 1: no groups */
+  int32_t renormalise;
+  float scale;
+  const void *logits;                     /* [rows x experts] */
+  int64_t ld_logits;
+  const float *bias;                      /* [experts], may be NULL */
+  const int32_t *n;
+  int32_t *expert;                        /* [rows x k], best first */
+  float *weight;                          /* [rows x k] */
+  int32_t *off, *place;                   /* [experts + 1], [rows x k] */
+} gear_route_args;
+size_t gear_route_workspace_bytes(int64_t rows, int32_t experts, int32_t k, int32_t groups);
+gear_status gear_route(const gear_route_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradient of the weights with respect to the logits, the choice held fixed: dlogits [rows x experts] of the logits' type, every
+ * element written.  expert and weight are what gear_route left; experts of a row are distinct.  dweight is not read as a number where a slot has no
+ * expert; rows without any expert have zeros, rows whose weights hold a NaN have NaN.  dlogits may not be logits. */
+typedef struct {
+  int64_t rows;
+  int32_t experts, k, dtype;
+  int32_t score, renormalise;
+  float scale;
+  const void *logits;
+  int64_t ld_logits;
+  const int32_t *expert;
+  const float *weight, *dweight;          /* [rows x k] */
+  void *dlogits;
+  int64_t ld_dlogits;
+} gear_route_backward_args;
+gear_status gear_route_backward(const gear_route_backward_args *a, void *stream);
+
+/* Rows to their experts: xs[place[r, j]] = x[r], a copy for every slot that has a place.  xs [rows * k x dim] of x's type.  Rows of xs that
+ * are nobody's place (from off[experts] on) are left as they were.  Places outside [0, rows * k) are taken for none, here and below;
+ * places other than gear_route's have to be distinct.  rows * k is at most 2^30. */
+gear_status gear_expert_gather(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t dim, const int32_t *place, int32_t k,
+                               void *xs, int64_t ld_xs, void *stream);
+
+/* Back again: out[r] = residual[r] + sum over j of weight[r, j] y[place[r, j]], added up in fp32 in the order of the slots.  residual may
+ * be NULL (nothing), weight may be NULL (1 each: the gradient of gear_expert_gather, y being that of xs and residual what flows
+ * into x itself).  A slot without a place counts as a row of zeros: a NaN weight makes the row NaN, other weights nothing.
+ * out may be residual itself, but not y. */
+typedef struct {
+  int64_t rows;
+  int32_t dim, k, dtype;                  /* gear_dtype of y, residual and out */
+  const void *y, *residual;
+  const int32_t *place;
+  const float *weight;
+  void *out;
+  int64_t ld_y, ld_residual, ld_out;
+} gear_expert_combine_args;
+gear_status gear_expert_combine(const gear_expert_combine_args *a, void *stream);
+
+/* Its gradients: dy[place[r, j]] = weight[r, j] dout[r] (rows that are nobody's place are left as they were; dy may be y itself, or NULL),
+ * dweight[r, j] = dout[r] . y[place[r, j]] in fp32, 0 for a slot without a place (may be NULL).  The residual's gradient is dout. */
+typedef struct {
+  int64_t rows;
+  int32_t dim, k, dtype;                  /* gear_dtype of dout, y and dy */
+  const void *dout, *y;
+  const int32_t *place;
+  const float *weight;
+  void *dy;
+  float *dweight;
+  int64_t ld_dout, ld_y, ld_dy;
+} gear_expert_combine_backward_args;
+gear_status gear_expert_combine_backward(const gear_expert_combine_backward_args *a, void *stream);
+
+/* ---- Products in 8-bit integers ---------------------------------------------------------------------------------------
+ * A row of `dim` values v as integers q with one scale: scale = max|v| / 127 (fp32), q the integer nearest to 127 v / max|v|, ties to
+ * even, so q scale stands for v.  A row of zeros has scale 0; a row that holds an infinity or a NaN has integers 0 and scale
+ * NaN, and so has everything made from it.  The same for weights, a scale for every output's [K] weights.  Sums are exact (32-bit integers: K is
+ * at most 65536), so a product is off by its operands' rounding to 8 bits and three roundings of fp32.  Rows take gear_rows8_ld(dim) bytes, zeros behind
+ * their end. */
+
+/* x [rows x dim] in 8-bit integers.  place NULL (k then 1): row r of q and scale is x[r].  Otherwise x[r] goes to row place[r, j] for every
+ * slot that has a place, as gear_expert_gather does it; q and scale have rows * k rows then. */
+gear_status gear_rows_i8(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t dim, const int32_t *place, int32_t k, int8_t *q,
+                         float *scale, void *stream);
+
+/* Weights for gear_product_i8: w [experts x N x K] contiguous, GEAR_F32 or GEAR_BF16, made into integers with a scale for every output (scale
+ * [experts x N] is written), or GEAR_I8, integers already (scale is the caller's and not touched; -128 is allowed).  packed: gear_packed_i8_bytes,
+ * 16-byte aligned (0 bytes on a bad argument); scale 16-byte aligned. */
+#define GEAR_I8 3                         /* beside gear_dtype, for these weights alone */
+size_t gear_packed_i8_bytes(int32_t experts, int32_t N, int32_t K);
+gear_status gear_pack_weights_i8(const void *w, int32_t src_dtype, int32_t experts, int32_t N, int32_t K, int8_t *packed, float *scale, void *stream);
+
+/* out[r, n] = x_scale[r] w_scale[e, n] sum over k of x[r, k] w_e[n, k] for the rows of every expert: off, status, keep_status and out as for
+ * gear_expert_product; x rows of ld_x bytes, at least gear_rows8_ld(K) and a multiple of 16. */
+typedef struct {
+  int32_t out_dtype;
+  int64_t rows;
+  int32_t K, N, experts;
+  const int8_t *x;
+  const float *x_scale;                   /* [rows] */
+  const int8_t *packed;
+  const float *w_scale;                   /* [experts x N], 16-byte aligned */
+  const int32_t *off;
+  void *out;
+  int64_t ld_x, ld_out;
+  int32_t *status;
+  int32_t keep_status;
+} gear_i8_args;
+gear_status gear_product_i8(const gear_i8_args *a, void *stream);
+
 /* Per-kernel timing of a step, for benchmarks.  gear_profile_create allocates a fixed pool of HIP
  * events on the current device (host memory; NULL on failure), gear_profile_destroy releases it.
  * After a gear_step that was given the profile and after the stream has been synchronised,

@@ -10,6 +10,10 @@ from .experts import (  # noqa: F401
     ExpertWeights, GradList, NormOutput, Rows8, Weights8, gear_clip_grads, gear_expert_dgrad, gear_expert_matmul, gear_expert_status,
     gear_expert_wgrad, gear_grad_norm, gear_matmul8, gear_rmsnorm, gear_rmsnorm_backward, gear_rows8, gear_weights8,
 )
+from .routing import (  # noqa: F401
+    Route, RowsI8, WeightsI8, gear_expert_combine, gear_expert_combine_backward, gear_expert_gather, gear_expert_gather_i8, gear_matmul_i8,
+    gear_route, gear_route_backward, gear_rows_i8, gear_weights_i8,
+)
 
 
 def config_for(wl, max_batch=None, max_nnz=None):

@@ -15,7 +15,9 @@ import torch
 
 GEAR_MAX_LAYERS = 8
 GEAR_OK, GEAR_ERR_INVALID, GEAR_ERR_RANGE, GEAR_ERR_CAPACITY, GEAR_ERR_HIP = range(5)
-GEAR_F32, GEAR_BF16, GEAR_E4M3 = 0, 1, 2
+GEAR_F32, GEAR_BF16, GEAR_E4M3, GEAR_I8 = 0, 1, 2, 3
+GEAR_SCORE_SOFTMAX, GEAR_SCORE_SIGMOID = 0, 1
+GEAR_MAX_CHOSEN, GEAR_MAX_GROUPS = 32, 64
 DTYPE_CODE = {"f32": GEAR_F32, "bf16": GEAR_BF16}
 TORCH_DTYPE = {GEAR_F32: torch.float32, GEAR_BF16: torch.bfloat16}
 
@@ -30,6 +32,8 @@ EXPORTS = (
     "gear_packed_weights_bytes", "gear_weight_scales_bytes", "gear_pack_weights", "gear_expert_product",
     "gear_expert_wgrad_workspace_bytes", "gear_expert_wgrad", "gear_grad_list_bytes", "gear_grad_list_pack",
     "gear_grad_workspace_bytes", "gear_grad_norm", "gear_clip_grads",
+    "gear_route_workspace_bytes", "gear_route", "gear_route_backward", "gear_expert_gather", "gear_expert_combine",
+    "gear_expert_combine_backward", "gear_rows_i8", "gear_packed_i8_bytes", "gear_pack_weights_i8", "gear_product_i8",
     "gear_gemm", "gear_profile_create", "gear_profile_destroy", "gear_profile_count", "gear_profile_span",
     "gear_debug_fail_launch", "gear_debug_helper_idle", "gear_status_string",
 )
@@ -92,6 +96,37 @@ class gear_expert_wgrad_args(C.Structure):
 
 class gear_grad_tensor(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
+class gear_route_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("experts", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("score", C.c_int32), ("groups", C.c_int32),
+                ("groups_kept", C.c_int32), ("group_best", C.c_int32), ("renormalise", C.c_int32), ("scale", C.c_float), ("logits", C.c_void_p),
+                ("ld_logits", C.c_int64), ("bias", C.c_void_p), ("n", C.c_void_p), ("expert", C.c_void_p), ("weight", C.c_void_p),
+                ("off", C.c_void_p), ("place", C.c_void_p)]
+
+
+class gear_route_backward_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("experts", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("score", C.c_int32),
+                ("renormalise", C.c_int32), ("scale", C.c_float), ("logits", C.c_void_p), ("ld_logits", C.c_int64), ("expert", C.c_void_p),
+                ("weight", C.c_void_p), ("dweight", C.c_void_p), ("dlogits", C.c_void_p), ("ld_dlogits", C.c_int64)]
+
+
+class gear_expert_combine_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("y", C.c_void_p), ("residual", C.c_void_p),
+                ("place", C.c_void_p), ("weight", C.c_void_p), ("out", C.c_void_p), ("ld_y", C.c_int64), ("ld_residual", C.c_int64),
+                ("ld_out", C.c_int64)]
+
+
+class gear_expert_combine_backward_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("dout", C.c_void_p), ("y", C.c_void_p),
+                ("place", C.c_void_p), ("weight", C.c_void_p), ("dy", C.c_void_p), ("dweight", C.c_void_p), ("ld_dout", C.c_int64),
+                ("ld_y", C.c_int64), ("ld_dy", C.c_int64)]
+
+
+class gear_i8_args(C.Structure):
+    _fields_ = [("out_dtype", C.c_int32), ("rows", C.c_int64), ("K", C.c_int32), ("N", C.c_int32), ("experts", C.c_int32), ("x", C.c_void_p),
+                ("x_scale", C.c_void_p), ("packed", C.c_void_p), ("w_scale", C.c_void_p), ("off", C.c_void_p), ("out", C.c_void_p),
+                ("ld_x", C.c_int64), ("ld_out", C.c_int64), ("status", C.c_void_p), ("keep_status", C.c_int32)]
 
 
 class gear_step_out(C.Structure):
@@ -199,6 +234,26 @@ def _load() -> C.CDLL:
     lib.gear_grad_norm.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
     lib.gear_clip_grads.restype = C.c_int
     lib.gear_clip_grads.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+    lib.gear_route_workspace_bytes.restype = C.c_size_t
+    lib.gear_route_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32]
+    lib.gear_route.restype = C.c_int
+    lib.gear_route.argtypes = [C.POINTER(gear_route_args), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.gear_route_backward.restype = C.c_int
+    lib.gear_route_backward.argtypes = [C.POINTER(gear_route_backward_args), C.c_void_p]
+    lib.gear_expert_gather.restype = C.c_int
+    lib.gear_expert_gather.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.gear_expert_combine.restype = C.c_int
+    lib.gear_expert_combine.argtypes = [C.POINTER(gear_expert_combine_args), C.c_void_p]
+    lib.gear_expert_combine_backward.restype = C.c_int
+    lib.gear_expert_combine_backward.argtypes = [C.POINTER(gear_expert_combine_backward_args), C.c_void_p]
+    lib.gear_rows_i8.restype = C.c_int
+    lib.gear_rows_i8.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.gear_packed_i8_bytes.restype = C.c_size_t
+    lib.gear_packed_i8_bytes.argtypes = [C.c_int32] * 3
+    lib.gear_pack_weights_i8.restype = C.c_int
+    lib.gear_pack_weights_i8.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.gear_product_i8.restype = C.c_int
+    lib.gear_product_i8.argtypes = [C.POINTER(gear_i8_args), C.c_void_p]
     lib.gear_profile_create.restype = C.c_void_p
     lib.gear_profile_create.argtypes = []
     lib.gear_profile_destroy.restype = None

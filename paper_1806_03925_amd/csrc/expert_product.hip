@@ -1,11 +1,13 @@
-// Products of rows with the weights of their expert, out[r] = x[r] W_e^T, in fp32, bf16 and 8 bits, for training (forward,
-// and dX on transposed weights) and for serving.  Off by row tiles that end with their expert, a layer is one expert.
+// Products of rows with the weights of their expert, out[r] = x[r] W_e^T, in fp32, bf16, 8 bits and 8-bit integers, for training
+// (forward, and dX on transposed weights; fp32 and bf16) and for serving.  Off by row tiles that end with their expert, a layer is one expert.
 //
-// All three types are one kernel, because 128 bytes of a row are 32, 64 or 128 values of k: a k-block.  It is eight
+// All types are one kernel, because 128 bytes of a row are 32, 64 or 128 values of k: a k-block.  It is eight
 // 16-byte pieces, and "unit" u of it is piece 2u for one half of a wavefront and piece 2u + 1 for the other.  A unit is
-// four v_mfma_f32_32x32x2_f32, one v_mfma_f32_32x32x16_bf16, or half of a v_mfma_scale_f32_32x32x64_f8f6f4; which k a lane
+// four v_mfma_f32_32x32x2_f32, one v_mfma_f32_32x32x16_bf16 or v_mfma_i32_32x32x32_i8, or half of a
+// v_mfma_scale_f32_32x32x64_f8f6f4; which k a lane
 // holds where does not matter, as long as both operands hold the same.  In 8 bits a k-block is also what shares a scale:
-// the instruction multiplies by both operands' powers of two itself, so scales cost no vector instruction.
+// the instruction multiplies by both operands' powers of two itself, so scales cost no vector instruction.  Integers are added up
+// exactly, in 32 bits (127^2 65536 < 2^31), and a row's and an output's scale multiply what comes out.
 //
 // Rows of x are copied global -> LDS by DMA, LDS rows of 128 bytes with their pieces XOR-ed by half the row's number modulo 8:
 // the sixteen rows that are read at a time, two to the 256 bytes of all banks, then lie in sixteen different places; what lies
@@ -24,13 +26,17 @@ typedef int i32x8_v __attribute__((ext_vector_type(8)));
 constexpr int kKBlock = 128;           // bytes
 constexpr int kPackedBlock = 32 * kKBlock;   // bytes of packed weights for 32 outputs and a k-block
 
-__host__ __device__ constexpr int operand_bytes(int dtype) { return dtype == GEAR_E4M3 ? 1 : dtype == GEAR_BF16 ? 2 : 4; }
+__host__ __device__ constexpr int operand_bytes(int dtype) { return dtype == GEAR_F32 ? 4 : dtype == GEAR_BF16 ? 2 : 1; }
+
+typedef int i32x4_v __attribute__((ext_vector_type(4)));
+typedef int i32x16_v __attribute__((ext_vector_type(16)));
+template <int DT> using AccOf = std::conditional_t<DT == GEAR_I8, i32x16_v, f32x16_v>;   // sums of a 32 x 32 tile
 
 struct ProductArgs {
   const unsigned char *x;
-  const uint8_t *x_scale;
+  const uint8_t *x_scale;   // GEAR_I8: floats, one for each row
   const unsigned char *packed;
-  const uint8_t *w_scale;
+  const uint8_t *w_scale;   // GEAR_I8: floats, one for each output of an expert
   const int32_t *off;
   void *out;
   int64_t ld_x, ld_out;   // bytes, elements
@@ -55,9 +61,14 @@ template <int DT_, int WTM_, int WAVES_M_, int WAVES_N_> struct ProductTile {
   static_assert(DMA * 8 * WAVES == BM, "a copy is eight rows");
 };
 
+// rows x, weights w: a unit of each
+__device__ __forceinline__ i32x16_v mfma_i8(i32x16_v acc, const u32x4_v &x, const u32x4_v &w) {
+  return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_v, w), __builtin_bit_cast(i32x4_v, x), acc, 0, 0, 0);
+}
+
 // One unit pair (half a k-block): rows from LDS, weights b[unit][column tile] from registers.
 template <typename C, int WHICH>
-__device__ __forceinline__ void mma_half(f32x16_v (&acc)[C::WTM][TN], uint32_t addr, const u32x4_v (&b)[2][TN],
+__device__ __forceinline__ void mma_half(AccOf<C::DT> (&acc)[C::WTM][TN], uint32_t addr, const u32x4_v (&b)[2][TN],
                                          const uint32_t (&sx)[C::WTM], uint32_t sw) {
   u32x4_v p[C::WTM], q[C::WTM];
   const uint32_t a0 = addr, a1 = addr ^ 32u;
@@ -91,6 +102,9 @@ __device__ __forceinline__ void mma_half(f32x16_v (&acc)[C::WTM][TN], uint32_t a
       } else if constexpr (C::DT == GEAR_BF16) {
         MFMA_BF16_T(acc[i][j], p[i], b[0][j]);
         MFMA_BF16_T(acc[i][j], q[i], b[1][j]);
+      } else if constexpr (C::DT == GEAR_I8) {
+        acc[i][j] = mfma_i8(acc[i][j], p[i], b[0][j]);
+        acc[i][j] = mfma_i8(acc[i][j], q[i], b[1][j]);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -178,7 +192,7 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   const auto x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.x) + (int64_t)m0 * a.ld_x, 0,
                                                         (int)((m_rows - 1) * a.ld_x) + nk * kKBlock, 0x00020000);
   // rows in 8 bits have zeros behind their end; others end inside a k-block, and what is beyond must not be read as k
-  const int beyond = C::DT == GEAR_E4M3 ? nk * kKBlock : row_bytes;
+  const int beyond = operand_bytes(C::DT) == 1 ? nk * kKBlock : row_bytes;
   int x_at[C::DMA];
 #pragma unroll
   for (int i = 0; i < C::DMA; ++i) {
@@ -232,13 +246,13 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
     }
   };
 
-  f32x16_v acc[C::WTM][TN];
+  AccOf<C::DT> acc[C::WTM][TN];
 #pragma unroll
   for (int i = 0; i < C::WTM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
   const uint32_t x_rel = lds_base + (uint32_t)(wm * C::WTM * 32 + r) * 128u + (uint32_t)((g ^ (r >> 1 & 7)) << 4);
 
@@ -270,8 +284,31 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   }
   wait_vm<0>();    // copies beyond the end have landed too: LDS becomes the patches
   __syncthreads();
-  store_tile<C, F32>(acc, reinterpret_cast<bf16_t *>(lds) + wave * 32 * PATCH_LD, a.out, a.ld_out, m0 + wm * 32 * C::WTM, t.m_end,
-                     n0 + wn * WN, a.N, lane);
+  auto store = [&](const f32x16_v (&v)[C::WTM][TN]) {
+    store_tile<C, F32>(v, reinterpret_cast<bf16_t *>(lds) + wave * 32 * PATCH_LD, a.out, a.ld_out, m0 + wm * 32 * C::WTM, t.m_end, n0 + wn * WN,
+                       a.N, lane);
+  };
+  if constexpr (C::DT == GEAR_I8) {
+    const float *x_of = reinterpret_cast<const float *>(a.x_scale) + m0, *w_of = reinterpret_cast<const float *>(a.w_scale) + (int64_t)t.e * a.N;
+    float xr[C::WTM];
+#pragma unroll
+    for (int i = 0; i < C::WTM; ++i) xr[i] = x_of[min(wm * 32 * C::WTM + i * 32 + r, m_rows - 1)];
+    f32x16_v v[C::WTM][TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 wn4 = *reinterpret_cast<const float4 *>(w_of + min(n0 + wn * WN + j * 32 + 8 * q + 4 * g, a.N - 4));
+        const float wc[4] = {wn4.x, wn4.y, wn4.z, wn4.w};
+#pragma unroll
+        for (int i = 0; i < C::WTM; ++i)
+#pragma unroll
+          for (int h = 0; h < 4; ++h) v[i][j][4 * q + h] = (float)acc[i][j][4 * q + h] * xr[i] * wc[h];
+      }
+    store(v);
+  } else {
+    store(acc);
+  }
 }
 
 template <typename C> __device__ __forceinline__ ExpertTile look(const ProductArgs &a, bool halves) {
@@ -314,7 +351,7 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
   if (!t.have) return;
   const int m0 = t.m0, n0 = t.n_tile * C::BN, m_rows = min(C::BM, t.m_end - m0);
   const int row_bytes = a.K * operand_bytes(DT), nk = (row_bytes + kKBlock - 1) / kKBlock;
-  const int beyond = DT == GEAR_E4M3 ? nk * kKBlock : row_bytes;
+  const int beyond = operand_bytes(DT) == 1 ? nk * kKBlock : row_bytes;
   const int r = lane & 31, g = lane >> 5;
   const auto x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.x) + (int64_t)m0 * a.ld_x, 0,
                                                         (int)((m_rows - 1) * a.ld_x) + nk * kKBlock, 0x00020000);
@@ -332,13 +369,13 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
     for (int i = 0; i < TM_; ++i) xs[i] = a.x_scale + (int64_t)(m0 + min(i * 32 + r, m_rows - 1)) * lds8;
     ws = a.w_scale + ((int64_t)t.e * ((a.N + kBlock8 - 1) / kBlock8) + n0 / kBlock8) * lds8;
   }
-  f32x16_v acc[TM_][TN_];
+  AccOf<DT> acc[TM_][TN_];
 #pragma unroll
   for (int i = 0; i < TM_; ++i)
 #pragma unroll
     for (int j = 0; j < TN_; ++j)
 #pragma unroll
-      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
   auto load = [&](SplitBlock<C> &b, int k) {   // past the end: the last block once more, which is not multiplied
     const int kk = min(k, nk - 1);
 #pragma unroll
@@ -374,6 +411,9 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
         } else if constexpr (DT == GEAR_BF16) {
 #pragma unroll
           for (int u = 0; u < 4; ++u) MFMA_BF16_T(acc[i][j], b.x[i][u], b.w[j][u]);
+        } else if constexpr (DT == GEAR_I8) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) acc[i][j] = mfma_i8(acc[i][j], b.x[i][u], b.w[j][u]);
         } else {
 #pragma unroll
           for (int u = 0; u < 4; ++u)
@@ -394,6 +434,7 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
     }
   }
   // [wavefront][tile][element / 4][lane] of four values each: four consecutive columns of row lane % 32
+  using Four = std::conditional_t<DT == GEAR_I8, int4, float4>;
   constexpr int PARTS = TM_ * TN_ * 4;
 #pragma unroll
   for (int i = 0; i < TM_; ++i)
@@ -401,19 +442,25 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
     for (int j = 0; j < TN_; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<float4 *>(sums + (((wave * TM_ + i) * TN_ + j) * 256 + q * 64 + lane) * 4) =
-            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        *reinterpret_cast<Four *>(sums + (((wave * TM_ + i) * TN_ + j) * 256 + q * 64 + lane) * 4) =
+            Four{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
   __syncthreads();
   for (int part = wave; part < PARTS; part += C::WAVES) {
     const int q = part & 3, j = (part >> 2) % TN_, i = (part >> 2) / TN_;
-    float4 v = *reinterpret_cast<const float4 *>(sums + (part * 64 + lane) * 4);
+    Four sum = *reinterpret_cast<const Four *>(sums + (part * 64 + lane) * 4);
 #pragma unroll
     for (int w = 1; w < C::WAVES; ++w) {
-      const float4 o = *reinterpret_cast<const float4 *>(sums + ((w * PARTS + part) * 64 + lane) * 4);
-      v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+      const Four o = *reinterpret_cast<const Four *>(sums + ((w * PARTS + part) * 64 + lane) * 4);
+      sum.x += o.x, sum.y += o.y, sum.z += o.z, sum.w += o.w;
     }
     const int m = i * 32 + r, n = n0 + j * 32 + 8 * q + 4 * g;
     if (m < m_rows && n < a.N) {
+      float4 v = make_float4((float)sum.x, (float)sum.y, (float)sum.z, (float)sum.w);
+      if constexpr (DT == GEAR_I8) {
+        const float xr = reinterpret_cast<const float *>(a.x_scale)[m0 + m];
+        const float4 wc = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(a.w_scale) + (int64_t)t.e * a.N + n);
+        v.x = v.x * xr * wc.x, v.y = v.y * xr * wc.y, v.z = v.z * xr * wc.z, v.w = v.w * xr * wc.w;
+      }
       if constexpr (F32)
         *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + (m0 + m) * a.ld_out + n) = v;
       else
@@ -664,4 +711,24 @@ extern "C" gear_status gear_expert_product(const gear_expert_args *a, void *stre
                          : a->dtype == GEAR_BF16 ? launch_product<GEAR_BF16>(p, f32, s)
                                                  : launch_product<GEAR_F32>(p, f32, s);
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
+}
+
+extern "C" gear_status gear_product_i8(const gear_i8_args *a, void *stream) {
+  if (!a || a->experts < 1 || a->experts > GEAR_MAX_EXPERTS || a->N < 8 || a->N % 8 || a->N >= (1 << 20) || a->K < 8 || a->K % 8 ||
+      a->K > GEAR_MAX_NORM_DIM || a->rows < 0 || a->rows > (1 << 30))
+    return GEAR_ERR_INVALID;
+  if (a->out_dtype != GEAR_F32 && a->out_dtype != GEAR_BF16) return GEAR_ERR_INVALID;
+  if (!a->packed || ((uintptr_t)a->packed & 15) || !a->w_scale || ((uintptr_t)a->w_scale & 15) || (a->off ? !a->status : a->experts != 1))
+    return GEAR_ERR_INVALID;
+  if (((a->rows + 127) / 128 + a->experts) * ((a->N + 127) / 128) > (1 << 23)) return GEAR_ERR_INVALID;   // as above
+  if (a->rows > 0) {
+    if (!a->x || !a->out || ((uintptr_t)a->x & 15) || ((uintptr_t)a->out & 15) || !a->x_scale || ((uintptr_t)a->x_scale & 3)) return GEAR_ERR_INVALID;
+    if (a->ld_x < rows8_ld(a->K) || a->ld_x % 16 || a->ld_x >= (1 << 20)) return GEAR_ERR_INVALID;
+    if (a->ld_out < a->N || a->ld_out % 8 || a->ld_out >= (1 << 20)) return GEAR_ERR_INVALID;
+  }
+  if (a->rows == 0 && !a->off && !a->status) return GEAR_OK;
+  const ProductArgs p = {reinterpret_cast<const unsigned char *>(a->x), reinterpret_cast<const uint8_t *>(a->x_scale),
+                         reinterpret_cast<const unsigned char *>(a->packed), reinterpret_cast<const uint8_t *>(a->w_scale), a->off, a->out,
+                         a->ld_x, a->ld_out, (int)a->rows, a->K, a->N, a->experts, a->status, a->keep_status};
+  return launch_product<GEAR_I8>(p, a->out_dtype == GEAR_F32, (hipStream_t)stream) == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
 }

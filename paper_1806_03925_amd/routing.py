@@ -1,0 +1,347 @@
+"""Rows that choose their experts, and products in 8-bit integers (include/gear.h), on PyTorch tensors: argument checks, output
+and workspace memory, marshalling, by the rules of experts.py.  All tensors of a call are on the current GPU, calls enqueue on its
+current stream and do not synchronise, and results have no autograd history: gradients are calls of their own."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from .binding import (GEAR_I8, GEAR_SCORE_SIGMOID, GEAR_SCORE_SOFTMAX, _check, gear_expert_combine_args,
+                      gear_expert_combine_backward_args, gear_i8_args, gear_route_args, gear_route_backward_args, lib)
+from .experts import _CODE, _Packed, _gpu, _matrix, _raw_stream, _refuse, _vector, _weights, _word
+
+_SCORE = {"softmax": GEAR_SCORE_SOFTMAX, "sigmoid": GEAR_SCORE_SIGMOID}
+
+
+class Route:
+    """Where rows go.  expert [rows x k] (int32, best first; -1: none), weight [rows x k] (float32), place [rows x k] (int32: the
+    pair's row in the order of experts; -1: none), off [experts + 1] (int32: where each expert's rows begin).  gear_route makes one;
+    a program may put one together from tensors of its own, whose places have to be distinct."""
+    __slots__ = ("rows", "k", "experts", "gpu", "p_expert", "p_weight", "p_place", "p_off", "_room", "_expert", "_weight", "_place", "_off")
+
+    def __init__(self, expert: torch.Tensor, weight: torch.Tensor, place: torch.Tensor, off: torch.Tensor):
+        where = "Route"
+        self.gpu = _gpu(expert.get_device(), where, "expert")
+        if expert.dim() != 2 or expert.shape[1] < 1 or off.dim() != 1 or off.numel() < 2:
+            _refuse(where, "expert has to be [rows x k] and off [experts + 1]")
+        self.rows, self.k = expert.shape
+        self.experts = off.numel() - 1
+        for t, name, dtype in ((expert, "expert", torch.int32), (weight, "weight", torch.float32), (place, "place", torch.int32)):
+            if t.shape != expert.shape:
+                _refuse(where, f"{name} has to be {tuple(expert.shape)}, not {tuple(t.shape)}")
+            _vector(t, self.gpu, where, name, dtype, self.rows * self.k)
+        _vector(off, self.gpu, where, "off", torch.int32, self.experts + 1)
+        self._room = None
+        self._expert, self._weight, self._place, self._off = expert, weight, place, off
+        self.p_expert, self.p_weight, self.p_place, self.p_off = (t.data_ptr() for t in (expert, weight, place, off))
+
+    @staticmethod
+    def _empty(rows: int, k: int, experts: int, gpu: int) -> "Route":
+        """One allocation for all four; the tensors are made when somebody asks for them."""
+        r = object.__new__(Route)
+        r.rows, r.k, r.experts, r.gpu = rows, k, experts, gpu
+        r._expert = r._weight = r._place = r._off = None
+        r._room = torch.empty(3 * rows * k + experts + 1, dtype=torch.int32, device=gpu)
+        r.p_expert = r._room.data_ptr()
+        step = 4 * rows * k
+        r.p_weight, r.p_place, r.p_off = r.p_expert + step, r.p_expert + 2 * step, r.p_expert + 3 * step
+        return r
+
+    def _part(self, i: int) -> torch.Tensor:
+        k = self.k
+        return self._room.as_strided((self.rows, k), (k, 1), i * self.rows * k)
+
+    @property
+    def expert(self) -> torch.Tensor:
+        if self._expert is None:
+            self._expert = self._part(0)
+        return self._expert
+
+    @property
+    def weight(self) -> torch.Tensor:
+        if self._weight is None:
+            self._weight = self._part(1).view(torch.float32)
+        return self._weight
+
+    @property
+    def place(self) -> torch.Tensor:
+        if self._place is None:
+            self._place = self._part(2)
+        return self._place
+
+    @property
+    def off(self) -> torch.Tensor:
+        if self._off is None:
+            self._off = self._room.as_strided((self.experts + 1,), (1,), 3 * self.rows * self.k)
+        return self._off
+
+
+def _logits(t: torch.Tensor, where: str, name: str, dtype=None, shape=None) -> int:
+    """Checks a matrix of logits, of any width, and returns the distance between its rows."""
+    return _matrix(t, _gpu(t.get_device(), where, name), where, name, dtype, shape)
+
+
+def gear_route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optional[torch.Tensor] = None, groups: int = 1, groups_kept: int = 1,
+               group_best: int = 1, renormalise: bool = True, scale: float = 1.0, n: Optional[torch.Tensor] = None) -> Route:
+    """The k experts of every row of logits [rows x experts] (float32 or bfloat16), their weights, and the order of all pairs by
+    expert.  score: "softmax" or "sigmoid" of the logits.  bias [experts] (float32) is added to the scores for the choice, not for
+    the weights.  groups > 1: experts come in groups, of which the groups_kept best may be chosen from, by the sum of their
+    group_best (1 or 2) best.  renormalise: weights are divided by their sum.  n [1] (int32): rows from n on are padding and go
+    nowhere.  Experts with a logit or bias of -inf are not chosen (include/gear.h has all of the definition)."""
+    where = "gear_route"
+    ld = _logits(logits, where, "logits")
+    rows, experts = logits.shape
+    gpu = logits.get_device()
+    code = _SCORE.get(score)
+    if code is None:
+        _refuse(where, f"score has to be softmax or sigmoid, not {score}")
+    if bias is not None:
+        _vector(bias, gpu, where, "bias", torch.float32, experts)
+        bias = bias.data_ptr()
+    if n is not None:
+        _vector(n, gpu, where, "n", torch.int32, 1)
+        n = n.data_ptr()
+    size = lib.gear_route_workspace_bytes(rows, experts, k, groups)
+    if size == 0:
+        _refuse(where, f"{k} of {experts} experts in {groups} groups for {rows} rows")
+    r = Route._empty(rows, k, experts, gpu)
+    ws = torch.empty(size, dtype=torch.uint8, device=gpu)
+    a = gear_route_args(rows, experts, k, _CODE[logits.dtype], code, groups, groups_kept, group_best, 1 if renormalise else 0, scale,
+                        logits.data_ptr(), ld, bias, n, r.p_expert, r.p_weight, r.p_off, r.p_place)
+    status = lib.gear_route(C.byref(a), ws.data_ptr(), size, _raw_stream(gpu))
+    if status:
+        _check(status, where)
+    return r
+
+
+def gear_route_backward(logits: torch.Tensor, route: Route, dweight: torch.Tensor, score: str = "softmax", renormalise: bool = True,
+                        scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient [rows x experts] of the logits from that of the route's weights; score, renormalise and scale as gear_route had
+    them.  `out` may not be the logits themselves."""
+    where = "gear_route_backward"
+    ld = _logits(logits, where, "logits")
+    gpu, dtype, shape = logits.get_device(), logits.dtype, logits.shape
+    rows, experts = shape
+    if route.rows != rows or route.experts != experts or route.gpu != gpu:
+        _refuse(where, "the route is of other logits")
+    code = _SCORE.get(score)
+    if code is None:
+        _refuse(where, f"score has to be softmax or sigmoid, not {score}")
+    _vector(dweight, gpu, where, "dweight", torch.float32, rows * route.k)
+    if out is None:
+        out, ld_out = torch.empty(shape, dtype=dtype, device=gpu), experts
+    else:
+        ld_out = _matrix(out, gpu, where, "out", dtype, shape)
+        if rows and out.data_ptr() == logits.data_ptr():
+            _refuse(where, "out may not be the logits themselves")
+    a = gear_route_backward_args(rows, experts, route.k, _CODE[dtype], code, 1 if renormalise else 0, scale, logits.data_ptr(), ld, route.p_expert,
+                                 route.p_weight, dweight.data_ptr(), out.data_ptr(), ld_out)
+    status = lib.gear_route_backward(C.byref(a), _raw_stream(gpu))
+    if status:
+        _check(status, where)
+    return out
+
+
+def _of_route(t: torch.Tensor, route: Route, rows: int, where: str, name: str, dtype=None, dim: Optional[int] = None) -> int:
+    """Checks a matrix of `rows` rows on the route's GPU, the current one."""
+    ld = _matrix(t, _gpu(route.gpu, where, "the route"), where, name, dtype)
+    if t.shape[0] != rows or (dim is not None and t.shape[1] != dim):
+        _refuse(where, f"{name} has to be {(rows, dim if dim is not None else t.shape[1])}, not {tuple(t.shape)}")
+    return ld
+
+
+def gear_expert_gather(x: torch.Tensor, route: Route, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [rows x dim] copied to every place that the route gives its rows: [rows * k x dim] for gear_expert_matmul with route.off.  Rows
+    from route.off[experts] on are not written.  Its gradient is gear_expert_combine(dxs, route, weighted=False)."""
+    where = "gear_expert_gather"
+    ld = _of_route(x, route, route.rows, where, "x")
+    dim, places = x.shape[1], route.rows * route.k
+    if out is None:
+        out, ld_out = torch.empty(places, dim, dtype=x.dtype, device=route.gpu), dim
+    else:
+        ld_out = _of_route(out, route, places, where, "out", x.dtype, dim)
+    status = lib.gear_expert_gather(x.data_ptr(), _CODE[x.dtype], ld, route.rows, dim, route.p_place, route.k, out.data_ptr(), ld_out,
+                                    _raw_stream(route.gpu))
+    if status:
+        _check(status, where)
+    return out
+
+
+def gear_expert_combine(y: torch.Tensor, route: Route, weighted: bool = True, residual: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The way back: residual + the sum of the rows' places in y [rows * k x dim], each times its weight (weighted=False: 1).  out
+    may be residual itself."""
+    where = "gear_expert_combine"
+    rows, places = route.rows, route.rows * route.k
+    ld_y = _of_route(y, route, places, where, "y")
+    dtype, dim = y.dtype, y.shape[1]
+    ld_r, p_r = 0, None
+    if residual is not None:
+        ld_r, p_r = _of_route(residual, route, rows, where, "residual", dtype, dim), residual.data_ptr()
+    if out is None:
+        out, ld_out = torch.empty(rows, dim, dtype=dtype, device=route.gpu), dim
+    else:
+        ld_out = _of_route(out, route, rows, where, "out", dtype, dim)
+    a = gear_expert_combine_args(rows, dim, route.k, _CODE[dtype], y.data_ptr(), p_r, route.p_place, route.p_weight if weighted else None, out.data_ptr(),
+                                 ld_y, ld_r, ld_out)
+    status = lib.gear_expert_combine(C.byref(a), _raw_stream(route.gpu))
+    if status:
+        _check(status, where)
+    return out
+
+
+def gear_expert_combine_backward(dout: torch.Tensor, y: torch.Tensor, route: Route, dy: Optional[torch.Tensor] = None,
+                                 dweight: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dy, dweight) of gear_expert_combine with weights: dy [rows * k x dim], of which rows from route.off[experts] on are not
+    written (dy may be y itself), and dweight [rows x k] (float32).  The residual's gradient is dout."""
+    where = "gear_expert_combine_backward"
+    rows, places = route.rows, route.rows * route.k
+    ld_dout = _of_route(dout, route, rows, where, "dout")
+    dtype, dim = dout.dtype, dout.shape[1]
+    ld_y = _of_route(y, route, places, where, "y", dtype, dim)
+    if dy is None:
+        dy, ld_dy = torch.empty(places, dim, dtype=dtype, device=route.gpu), dim
+    else:
+        ld_dy = _of_route(dy, route, places, where, "dy", dtype, dim)
+    if dweight is None:
+        dweight = torch.empty(rows, route.k, dtype=torch.float32, device=route.gpu)
+    else:
+        _vector(dweight, route.gpu, where, "dweight", torch.float32, places)
+    a = gear_expert_combine_backward_args(rows, dim, route.k, _CODE[dtype], dout.data_ptr(), y.data_ptr(), route.p_place, route.p_weight, dy.data_ptr(),
+                                          dweight.data_ptr(), ld_dout, ld_y, ld_dy)
+    status = lib.gear_expert_combine_backward(C.byref(a), _raw_stream(route.gpu))
+    if status:
+        _check(status, where)
+    return dy, dweight
+
+
+# ---- 8-bit integers ---------------------------------------------------------------------------------------------------
+class RowsI8:
+    """Rows in 8-bit integers: q [rows x gear_rows8_ld(dim)] (int8, zeros behind a row's end), scale [rows] (float32)."""
+    __slots__ = ("rows", "dim", "ld", "gpu", "_q", "_scale", "_room", "p_q", "p_scale")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, dim: int):
+        where = "RowsI8"
+        self.gpu = _gpu(q.get_device(), where, "q")
+        rows = q.shape[0] if q.dim() else 0
+        if q.dtype is not torch.int8 or dim < 1 or q.shape != (rows, (dim + 127) // 128 * 128) or not q.is_contiguous():
+            _refuse(where, "q has to be [rows x gear_rows8_ld(dim)] contiguous int8")
+        _vector(scale, self.gpu, where, "scale", torch.float32, rows)
+        self.rows, self.dim, self.ld = rows, dim, q.shape[1]
+        self._q, self._scale, self._room, self.p_q, self.p_scale = q, scale, None, q.data_ptr(), scale.data_ptr()
+
+    @staticmethod
+    def empty(rows: int, dim: int, gpu: int) -> "RowsI8":
+        """One allocation for both; the tensors are made when somebody asks for them."""
+        r = object.__new__(RowsI8)
+        r.rows, r.dim, r.ld, r.gpu = rows, dim, (dim + 127) // 128 * 128, gpu
+        r._q = r._scale = None
+        r._room = torch.empty(rows * (r.ld + 4), dtype=torch.int8, device=gpu)
+        r.p_q = r._room.data_ptr()
+        r.p_scale = r.p_q + rows * r.ld
+        return r
+
+    @property
+    def q(self) -> torch.Tensor:
+        if self._q is None:
+            self._q = self._room[:self.rows * self.ld].view(self.rows, self.ld)
+        return self._q
+
+    @property
+    def scale(self) -> torch.Tensor:
+        if self._scale is None:
+            self._scale = self._room[self.rows * self.ld:].view(torch.float32)
+        return self._scale
+
+
+def _rows_i8(x: torch.Tensor, ld: int, rows: int, place: Optional[int], k: int, out: Optional[RowsI8], gpu: int, where: str) -> RowsI8:
+    dim = x.shape[1]
+    if out is None:
+        out = RowsI8.empty(rows * k, dim, gpu)
+    elif out.dim != dim or out.rows != rows * k or out.gpu != gpu:
+        _refuse(where, "out has another shape than the rows or is on another GPU")
+    status = lib.gear_rows_i8(x.data_ptr(), _CODE[x.dtype], ld, rows, dim, place, k, out.p_q, out.p_scale, _raw_stream(gpu))
+    if status:
+        _check(status, where)
+    return out
+
+
+def gear_rows_i8(x: torch.Tensor, out: Optional[RowsI8] = None) -> RowsI8:
+    """x [rows x dim] in 8-bit integers, a scale for every row."""
+    where = "gear_rows_i8"
+    gpu = _gpu(x.get_device(), where, "x")
+    return _rows_i8(x, _matrix(x, gpu, where, "x"), x.shape[0], None, 1, out, gpu, where)
+
+
+def gear_expert_gather_i8(x: torch.Tensor, route: Route, out: Optional[RowsI8] = None) -> RowsI8:
+    """gear_expert_gather and gear_rows_i8 in one: rows from route.off[experts] on are not written."""
+    where = "gear_expert_gather_i8"
+    ld = _of_route(x, route, route.rows, where, "x")
+    return _rows_i8(x, ld, route.rows, route.p_place, route.k, out, route.gpu, where)
+
+
+class WeightsI8(_Packed):
+    """Weights in 8-bit integers with a scale [experts x N] for every output, laid out for gear_matmul_i8 (gear_weights_i8 makes them)."""
+
+    def __init__(self, w: torch.Tensor, scale: Optional[torch.Tensor] = None):
+        where = "gear_weights_i8"
+        if scale is None:
+            self.experts, self.N, self.K = shape = _weights(w, where)
+            code = _CODE[w.dtype]
+        else:
+            _gpu(w.get_device(), where, "w")
+            if w.dim() not in (2, 3) or w.dtype is not torch.int8 or not w.is_contiguous():
+                _refuse(where, "w with a scale has to be contiguous int8 [experts x N x K] or [N x K]")
+            self.experts, self.N, self.K = shape = (1, *w.shape) if w.dim() == 2 else tuple(w.shape)
+            _vector(scale, w.get_device(), where, "scale", torch.float32, shape[0] * shape[1])
+            code = GEAR_I8
+        size = lib.gear_packed_i8_bytes(*shape)
+        if size == 0:
+            _refuse(where, f"weights of {shape} have no packed form")
+        self._allocate(size, w.device)
+        self.scale = torch.empty(shape[:2], dtype=torch.float32, device=w.device) if scale is None else scale.reshape(shape[:2]).clone()
+        self.p_scale = self.scale.data_ptr()
+        _check(lib.gear_pack_weights_i8(w.data_ptr(), code, *shape, self.address, self.p_scale, _raw_stream(self.gpu)), where)
+
+
+def gear_weights_i8(w: torch.Tensor, scale: Optional[torch.Tensor] = None) -> WeightsI8:
+    """w ([experts x N x K] or [N x K], float32 or bfloat16) in 8-bit integers, a scale for every output; or w in int8 already, with its
+    scale [experts x N]."""
+    return WeightsI8(w, scale)
+
+
+def gear_matmul_i8(rows: RowsI8, weights: WeightsI8, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   out_dtype: torch.dtype = torch.bfloat16, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """rows times the transposed weights of each row's expert, [rows x N]: integers added up exactly, then scaled.  off, status and rows from
+    off[experts] on as for gear_matmul8."""
+    where = "gear_matmul_i8"
+    gpu, n, experts = _gpu(rows.gpu, where, "rows"), weights.N, weights.experts
+    if rows.dim != weights.K:
+        _refuse(where, f"rows of {rows.dim} for weights of {weights.K}")
+    if weights.gpu != gpu:
+        _refuse(where, "rows and weights are on different GPUs")
+    if off is not None:
+        _vector(off, gpu, where, "off", torch.int32, experts + 1)
+        off = off.data_ptr()
+    elif experts != 1:
+        _refuse(where, "off may only be left out where there is one expert")
+    keep = 0
+    if status is not None:
+        _vector(status, gpu, where, "status", torch.int32, 1)
+        status = status.data_ptr()
+    elif off is not None:
+        status, keep = _word(gpu, where)[1], 1
+    if out is None:
+        if out_dtype not in _CODE:
+            _refuse(where, f"out_dtype has to be float32 or bfloat16, not {out_dtype}")
+        out, ld_out = torch.empty(rows.rows, n, dtype=out_dtype, device=gpu), n
+    else:
+        ld_out = _matrix(out, gpu, where, "out", None, (rows.rows, n))
+    a = gear_i8_args(_CODE[out.dtype], rows.rows, weights.K, n, experts, rows.p_q, rows.p_scale, weights.address, weights.p_scale, off,
+                     out.data_ptr(), rows.ld, ld_out, status, keep)
+    code = lib.gear_product_i8(C.byref(a), _raw_stream(gpu))
+    if code:
+        _check(code, where)
+    return out
