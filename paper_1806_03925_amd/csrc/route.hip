@@ -2,8 +2,14 @@
 // gradient (gear.h has the definitions).
 //
 // A row is a team of LPR lanes' (16, 32 or 64 of one wavefront), V logits a lane, all in registers from the one time they are
-// read.  Scores are fp64: what decides the choice is score + bias, and two experts' sums lie closer together than fp32 resolves
-// in one row of some hundred thousand.  A choice is k times the largest over the team, ties to the lowest index.
+// read.  What decides the choice is score + bias, and two experts' sums lie closer together than fp32 resolves in one row of some
+// hundred thousand.  So the choice is made twice at most: from fp32, with a bound on its error, and again by the definition, in
+// fp64, by the wavefronts that have a row with two neighbours in its order closer than that.
+//
+// The choice from fp32.  Values become whole numbers of the same order (`sortable`) whose last bits say which of the lane's values
+// they are, so that a comparison moves both in one instruction.  A lane sorts its own by a network; then k + 1 times the largest of
+// the team's first ones is taken, by rotations within 16 lanes, and its lane moves on to its next.  (k times the largest of all V
+// in fp64 instead: 114 us for 65536 rows of 256 with a bias, k = 8.)
 //
 // The order of the pairs is a counting sort by expert.  A workgroup takes a run of rows and counts its experts; a second launch
 // with the same runs finds from all counts where each run's pairs begin, ranks them (equal experts in a wavefront by ballots,
@@ -18,7 +24,7 @@ namespace gear {
 namespace {
 
 constexpr int kMaxRuns = 256;        // one for each CU
-constexpr int kRouteThreads = 1024, kGroupedThreads = 256;
+constexpr int kRouteThreads = 1024, kGroupedThreads = 512;   // at most
 constexpr int kMaxGroups = GEAR_MAX_GROUPS;
 
 struct RouteArgs {
@@ -31,60 +37,118 @@ struct RouteArgs {
   const int32_t *n;
   int32_t *expert;
   float *weight;
-  int32_t *off, *place, *count;      // count [runs x experts]
+  int32_t *off, *place, *count;      // count [experts x runs, a multiple of four]
 };
 
-template <int LPR> __device__ __forceinline__ double team_add(double v) {
-#pragma unroll
-  for (int o = LPR / 2; o; o >>= 1) v += __shfl_xor(v, o, kWave);
+__host__ __device__ constexpr int runs_ld(int runs) { return (runs + 3) / 4 * 4; }
+
+// ---- over a team: every lane gets the result, and every lane of the wavefront takes part -------------------------------
+template <int N> __device__ __forceinline__ int rotate(int v) { return __builtin_amdgcn_update_dpp(v, v, 0x120 + N, 0xf, 0xf, false); }   // in 16 lanes
+template <int N> __device__ __forceinline__ float rotate(float v) { return __int_as_float(rotate<N>(__float_as_int(v))); }
+template <int LPR, typename V, typename F> __device__ __forceinline__ V team(V v, F &&f) {
+  v = f(v, rotate<8>(v));
+  v = f(v, rotate<4>(v));
+  v = f(v, rotate<2>(v));
+  v = f(v, rotate<1>(v));
+  if constexpr (LPR > 16) v = f(v, __shfl_xor(v, 16, kWave));
+  if constexpr (LPR > 32) v = f(v, __shfl_xor(v, 32, kWave));
   return v;
 }
 template <int LPR> __device__ __forceinline__ float team_max(float v) {
-#pragma unroll
-  for (int o = LPR / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
-  return v;
+  return team<LPR>(v, [](float x, float y) { return fmaxf(x, y); });
 }
-template <int LPR> __device__ __forceinline__ bool team_any(bool v) {
-  int x = v;
-#pragma unroll
-  for (int o = LPR / 2; o; o >>= 1) x |= __shfl_xor(x, o, kWave);
-  return x != 0;
+template <int LPR> __device__ __forceinline__ int team_max(int v) {
+  return team<LPR>(v, [](int x, int y) { return max(x, y); });
 }
+template <int LPR> __device__ __forceinline__ float team_add(float v) {
+  return team<LPR>(v, [](float x, float y) { return x + y; });
+}
+template <int LPR> __device__ __forceinline__ uint64_t team_ballot(bool v) {   // of this lane's team, its first lane in bit 0
+  const uint64_t m = __ballot(v);
+  if constexpr (LPR == 64) return m;
+  return m >> (threadIdx.x & 63 & ~(LPR - 1)) & ((1ull << LPR) - 1);
+}
+template <int LPR> __device__ __forceinline__ bool team_any(bool v) { return team_ballot<LPR>(v) != 0; }
 
-// the largest of a team's (value, index), the lower index of equals; `with` goes along
+// the largest of a wavefront's (value, index), the lower index of equals
 struct Best {
   double value;
   int index;
-  float with;
 };
-template <int LPR> __device__ __forceinline__ Best team_best(Best b) {
+__device__ __forceinline__ Best wave_best(Best b) {
 #pragma unroll
-  for (int o = LPR / 2; o; o >>= 1) {
+  for (int o = kWave / 2; o; o >>= 1) {
     const double v = __shfl_xor(b.value, o, kWave);
     const int i = __shfl_xor(b.index, o, kWave);
-    const float w = __shfl_xor(b.with, o, kWave);
-    if (v > b.value || (v == b.value && i < b.index)) b = {v, i, w};
+    if (v > b.value || (v == b.value && i < b.index)) b = {v, i};
   }
   return b;
 }
 
-// Sigmoid and softmax of a logit, up to a factor that is the same for all of `top`'s row where `relative`: no sum of such
-// scores vanishes, however small they are.  Softmax: exp(l - top), relative or not.
-__device__ __forceinline__ double score_of(float l, bool softmax, double top, bool relative) {
-  const double v = (double)l;
-  if (softmax) return exp(v - top);
-  if (v > 0.0) return 1.0 / (1.0 + exp(-v));
-  const double shift = relative && top < 0.0 ? top : 0.0;
-  return exp(v - shift) / (1.0 + exp(v));
+// ---- scores ---------------------------------------------------------------------------------------------------------
+// in fp64, for the choice: softmax without its sum, or sigmoid
+__device__ __forceinline__ double exact_score(float l, bool softmax, float top) {
+  return softmax ? exp((double)l - (double)top) : 1.0 / (1.0 + exp(-(double)l));
 }
+// in fp32: exp(l - top); sigmoid.  Off by (|l - top| + 4) 2^-24 of themselves.
+__device__ __forceinline__ float quick_exp(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504f); }
+__device__ __forceinline__ float quick_score(float l, bool softmax, float top) {
+  return softmax ? quick_exp(l - top) : __builtin_amdgcn_rcpf(1.0f + quick_exp(-l));
+}
+// A chosen expert's share: its score up to a factor that is the same for all of its row where `relative`.  No sum of such scores
+// vanishes then, however small they are, when `top` is the largest chosen logit.
+__device__ __forceinline__ float share(float l, bool softmax, float top, bool relative) {
+  if (softmax) return expf(l - top);
+  if (l > 0.0f) return 1.0f / (1.0f + expf(-l));
+  const float shift = relative ? fminf(top, 0.0f) : 0.0f;
+  return expf(l - shift) / (1.0f + expf(l));
+}
+
+// ---- whole numbers in the order of floats ------------------------------------------------------------------------------
+constexpr int kNobody = -2147483647 - 1;   // below every float's
+__device__ __forceinline__ int sortable(float f) {
+  const int b = __float_as_int(f + 0.0f);   // -0 is 0
+  return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float unsorted(int s) { return __int_as_float(s ^ ((s >> 31) & 0x7fffffff)); }
+
+// descending, by odd-even merges
+template <int V> struct Sorter {
+  template <int I, int J> static __device__ __forceinline__ void exchange(int (&k)[V]) {
+    const int a = max(k[I], k[J]), b = min(k[I], k[J]);
+    k[I] = a, k[J] = b;
+  }
+  template <int I, int END, int STEP, int R> static __device__ __forceinline__ void row(int (&k)[V]) {
+    if constexpr (I + R < END) {
+      exchange<I, I + R>(k);
+      row<I + STEP, END, STEP, R>(k);
+    }
+  }
+  template <int LO, int N, int R> static __device__ __forceinline__ void merge(int (&k)[V]) {
+    if constexpr (2 * R < N) {
+      merge<LO, N, 2 * R>(k);
+      merge<LO + R, N, 2 * R>(k);
+      row<LO + R, LO + N, 2 * R, R>(k);
+    } else {
+      exchange<LO, LO + R>(k);
+    }
+  }
+  template <int LO = 0, int N = V> static __device__ __forceinline__ void sort(int (&k)[V]) {
+    if constexpr (N > 1) {
+      sort<LO, N / 2>(k);
+      sort<LO + N / 2, N / 2>(k);
+      merge<LO, N, 1>(k);
+    }
+  }
+};
 
 // ---- order of the pairs -------------------------------------------------------------------------------------------
 // Places of the pairs of rows [first, last), those of run number `run`.  On entry s_wave[e] is the number of expert e's pairs in all
-// runs and s_base[e] that in the runs before this one.  s_base, s_wave: experts and kRankers x experts words of LDS.
-constexpr int kRankers = 8;          // wavefronts that rank pairs: as many as counts of 1024 experts fit in LDS
-template <int THREADS> __device__ void places(const RouteArgs &a, int run, int64_t first, int64_t last, int32_t *s_base, int32_t *s_wave) {
-  constexpr int WAVES = THREADS / kWave < kRankers ? THREADS / kWave : kRankers;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E = a.experts;
+// runs and s_base[e] that in the runs before this one.  s_base, s_wave: experts and rankers x experts words of LDS.
+__host__ __device__ constexpr int rankers_of(int experts) { return experts <= 512 ? 16 : 8; }   // wavefronts that rank: their counts fit in LDS
+
+__device__ __forceinline__ void places(const RouteArgs &a, int run, int64_t first, int64_t last, int32_t *s_base, int32_t *s_wave) {
+  const int threads = blockDim.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E = a.experts, waves = min(threads / kWave, rankers_of(E));
   __syncthreads();
   if (wave == 0) {   // where each expert begins
     int begin = 0;
@@ -105,230 +169,382 @@ template <int THREADS> __device__ void places(const RouteArgs &a, int run, int64
     if (run == 0 && lane == 0) a.off[E] = begin;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < WAVES * E; i += THREADS) s_wave[i] = 0;
+  for (int i = threadIdx.x; i < waves * E; i += threads) s_wave[i] = 0;
   __syncthreads();
-  // a wavefront takes every pair from `from` on, 64 at a time: first it counts, then it places
-  const int64_t pairs = (last - first) * a.k, per = (pairs + WAVES - 1) / WAVES;
+  // a wavefront's pairs one behind the other, 64 at a time, four times 64 requested together: first it counts, then it places
+  const int64_t pairs = (last - first) * a.k, per = (pairs + waves - 1) / waves;
   const int64_t begin = first * a.k + min(wave * per, pairs);
-  const int64_t end = wave < WAVES ? first * a.k + min((wave + 1) * per, pairs) : begin;
-  int32_t *mine = s_wave + min(wave, WAVES - 1) * E;
-  int bits = 0;
-  while ((1 << bits) < E) ++bits;
+  const int64_t end = wave < waves ? first * a.k + min((wave + 1) * per, pairs) : begin;
+  int32_t *mine = s_wave + min(wave, waves - 1) * E;
   auto walk = [&](auto &&then) {
-    for (int64_t i0 = begin; i0 < end; i0 += kWave) {
-      const int64_t i = i0 + lane;
-      const int e = i < end ? a.expert[i] : -1;
-      uint64_t same = __ballot(e >= 0);
-      for (int b = 0; b < bits; ++b) {
-        const uint64_t set = __ballot((e >> b) & 1);
-        same &= (e >> b) & 1 ? set : ~set;
+    constexpr int AHEAD = 4;
+    for (int64_t i0 = begin; i0 < end; i0 += AHEAD * kWave) {
+      int e[AHEAD];
+#pragma unroll
+      for (int p = 0; p < AHEAD; ++p) {
+        const int64_t i = i0 + p * kWave + lane;
+        e[p] = i < end ? a.expert[i] : -1;
       }
-      const int rank = __popcll(same & ((1ull << lane) - 1));
-      then(i, e, rank, __popcll(same), i < end);
+#pragma unroll
+      for (int p = 0; p < AHEAD; ++p)
+        if (i0 + p * kWave < end) then(i0 + p * kWave + lane, e[p]);
     }
   };
-  walk([&](int64_t, int e, int rank, int all, bool) {
-    if (e >= 0 && rank == 0) mine[e] += all;   // one lane for each expert
+  walk([&](int64_t, int e) {
+    if (e >= 0) atomicAdd(mine + e, 1);
   });
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += THREADS) {
+  for (int e = threadIdx.x; e < E; e += threads) {
     int at = s_base[e];
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < waves; ++w) {
       const int c = s_wave[w * E + e];
       s_wave[w * E + e] = at;
       at += c;
     }
   }
   __syncthreads();
-  walk([&](int64_t i, int e, int rank, int all, bool in) {
+  int bits = 0;
+  while ((1 << bits) < E) ++bits;
+  walk([&](int64_t i, int e) {
+    uint64_t same = __ballot(e >= 0);   // lanes of the same expert
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t set = __ballot((e >> b) & 1);
+      same &= (e >> b) & 1 ? set : ~set;
+    }
+    const int rank = __popcll(same & ((1ull << lane) - 1));
     int at = -1;
     if (e >= 0) at = mine[e] + rank;
     asm volatile("" ::: "memory");   // every lane has read before one adds
-    if (e >= 0 && rank == 0) mine[e] += all;
-    if (in) a.place[i] = at;
+    if (e >= 0 && rank == 0) mine[e] += __popcll(same);
+    if (i < end) a.place[i] = at;
   });
+}
+
+// The choice of one row by the definition, in fp64, by a whole wavefront: lane j gets the j-th expert, -1 where there is none.  The row is
+// read again: its values in fp64 are few for 64 lanes, and nobody keeps registers for them who does not need them.
+template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int choose_exactly(const RouteArgs &a, int64_t row, float top) {
+  constexpr int V = MAX_E / kWave;
+  const double kNone = -INFINITY;
+  const int lane = threadIdx.x & 63, E = a.experts;
+  const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+  float lg[V];
+  double order[V], sum = 1.0;
+#pragma unroll
+  for (int v = 0; v < V; ++v) lg[v] = v * kWave + lane < E ? to_f32(x[v * kWave + lane]) : -INFINITY;
+  if (a.softmax && (a.bias || GROUPED)) {
+    sum = 0.0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum += exact_score(lg[v], true, top);
+#pragma unroll
+    for (int o = kWave / 2; o; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int e = v * kWave + lane;
+    const float bias = a.bias && e < E ? a.bias[e] : 0.0f;
+    order[v] = !(lg[v] > -INFINITY && bias > -INFINITY) ? kNone
+               : a.bias || GROUPED                      ? exact_score(lg[v], a.softmax, top) / sum + (double)bias
+                                                        : (double)lg[v];
+  }
+  if constexpr (GROUPED) {
+    const int per = E / a.groups;
+    double mine = kNone;    // lane q: group q's value
+    for (int q = 0; q < a.groups; ++q) {
+      Best one = {kNone, MAX_E}, two = {kNone, MAX_E};
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int e = v * kWave + lane;
+        if (e >= q * per && e < (q + 1) * per && order[v] > one.value) one = {order[v], e};
+      }
+      one = wave_best(one);
+      if (a.best == 2) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int e = v * kWave + lane;
+          if (e >= q * per && e < (q + 1) * per && e != one.index && order[v] > two.value) two = {order[v], e};
+        }
+        two = wave_best(two);
+      }
+      if (lane == q) mine = two.value > kNone ? one.value + two.value : one.value;
+    }
+    uint64_t keep = 0;
+    for (int j = 0; j < a.kept; ++j) {
+      const Best b = wave_best({mine, lane});
+      if (b.value > kNone) keep |= 1ull << b.index;
+      if (lane == b.index) mine = kNone;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int e = min(v * kWave + lane, E - 1);
+      if (!(keep >> (e / per) & 1)) order[v] = kNone;
+      if (order[v] > kNone && !a.bias) order[v] = (double)lg[v];
+    }
+  }
+  int chosen = -1;
+  for (int j = 0; j < a.k; ++j) {
+    Best b = {kNone, MAX_E};
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (order[v] > b.value) b = {order[v], v * kWave + lane};
+    b = wave_best(b);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (v * kWave + lane == b.index) order[v] = kNone;
+    if (lane == j && b.value > kNone) chosen = b.index;
+  }
+  return chosen;
 }
 
 template <typename T, int LPR, int V, bool WIDE, bool GROUPED>
 __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_route(RouteArgs a) {
-  constexpr int THREADS = GROUPED ? kGroupedThreads : kRouteThreads, TEAMS = THREADS / LPR, MAX_E = LPR * V;
-  constexpr int SLOTS = LPR < GEAR_MAX_CHOSEN ? GEAR_MAX_CHOSEN / LPR : 1;   // of a lane
+  constexpr int MAX_E = LPR * V, SLOTS = LPR < GEAR_MAX_CHOSEN ? GEAR_MAX_CHOSEN / LPR : 1;   // of a lane
+  constexpr bool HALF = sizeof(T) == 2;
   static_assert(!WIDE || V % 4 == 0, "four neighbouring logits a load");
   extern __shared__ int32_t s_words[];                          // [experts] counts, then what places() needs
-  __shared__ double s_value[GROUPED ? TEAMS * MAX_E : 1], s_group[GROUPED ? TEAMS * kMaxGroups : 1];
-  const double kNone = -INFINITY;
-  const int l = threadIdx.x % LPR, team = threadIdx.x / LPR, E = a.experts;
-  for (int e = threadIdx.x; e < E; e += THREADS) s_words[e] = 0;
+  __shared__ float s_value[GROUPED ? kGroupedThreads * V : 1];
+  const int threads = blockDim.x, teams = threads / LPR;
+  const int l = threadIdx.x % LPR, my_team = threadIdx.x / LPR, lane0_of_mine = threadIdx.x & 63 & ~(LPR - 1), E = a.experts;
+  for (int e = threadIdx.x; e < E; e += threads) s_words[e] = 0;
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * a.run, last = min(a.rows, first + a.run);
-  const int64_t used = a.n ? min(a.rows, (int64_t)max(*a.n, 0)) : a.rows;
-  auto index = [&](int v) { return WIDE ? (v / 4) * (LPR * 4) + l * 4 + v % 4 : v * LPR + l; };
-  float bias[V];
+  const int64_t used = min(last, a.n ? (int64_t)max(*a.n, 0) : last);
+  auto index_of = [&](int v, int lane) { return WIDE ? (v / 4) * (LPR * 4) + lane * 4 + v % 4 : v * LPR + lane; };
+  auto index = [&](int v) { return index_of(v, l); };
+  float bias[V];                              // -inf where it may not be chosen
 #pragma unroll
-  for (int v = 0; v < V; ++v) bias[v] = a.bias && index(v) < E ? a.bias[index(v)] : 0.0f;
+  for (int v = 0; v < V; ++v) {
+    bias[v] = a.bias && index(v) < E ? a.bias[index(v)] : 0.0f;
+    if (!(bias[v] > -INFINITY)) bias[v] = -INFINITY;
+  }
+  const bool scores = a.bias || GROUPED;      // the choice looks at them
+  const bool whole = HALF && !a.bias;         // logits of 16 bits decide: a number holds one and its expert, and nothing is approximate
 
-  for (int64_t row0 = first; row0 < last; row0 += TEAMS) {
-    const int64_t row = row0 + team;
-    const bool have = row < min(last, used);
-    const T *x = static_cast<const T *>(a.logits) + row * a.ld;
-    float lg[V];
+  auto load = [&](float (&lg)[V], int64_t row) {
 #pragma unroll
     for (int v = 0; v < V; ++v) lg[v] = -INFINITY;
-    if (have) {
-      if constexpr (WIDE) {
+    if (row >= used) return;
+    const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+    if constexpr (WIDE) {
 #pragma unroll
-        for (int v = 0; v < V; v += 4)
-          if (index(v) < E) {
-            if constexpr (sizeof(T) == 4) {
-              const float4 f = *reinterpret_cast<const float4 *>(x + index(v));
-              lg[v] = f.x, lg[v + 1] = f.y, lg[v + 2] = f.z, lg[v + 3] = f.w;
-            } else {
-              const uint2 f = *reinterpret_cast<const uint2 *>(x + index(v));
-              lg[v] = __uint_as_float(f.x << 16), lg[v + 1] = __uint_as_float(f.x & 0xffff0000u);
-              lg[v + 2] = __uint_as_float(f.y << 16), lg[v + 3] = __uint_as_float(f.y & 0xffff0000u);
-            }
+      for (int v = 0; v < V; v += 4)
+        if (index(v) < E) {
+          if constexpr (!HALF) {
+            const float4 f = *reinterpret_cast<const float4 *>(x + index(v));
+            lg[v] = f.x, lg[v + 1] = f.y, lg[v + 2] = f.z, lg[v + 3] = f.w;
+          } else {
+            const uint2 f = *reinterpret_cast<const uint2 *>(x + index(v));
+            lg[v] = __uint_as_float(f.x << 16), lg[v + 1] = __uint_as_float(f.x & 0xffff0000u);
+            lg[v + 2] = __uint_as_float(f.y << 16), lg[v + 3] = __uint_as_float(f.y & 0xffff0000u);
           }
-      } else {
+        }
+    } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (index(v) < E) lg[v] = to_f32(x[index(v)]);
-      }
+      for (int v = 0; v < V; ++v)
+        if (index(v) < E) lg[v] = to_f32(x[index(v)]);
     }
+  };
+  float lg[V], ahead[V];
+  load(ahead, first + my_team);
+  for (int64_t row0 = first; row0 < last; row0 += teams) {
+    const int64_t row = row0 + my_team;
+#pragma unroll
+    for (int v = 0; v < V; ++v) lg[v] = ahead[v];
+    if (row0 + teams < last) load(ahead, row + teams);
     bool broken = false;
     float top = -INFINITY;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      broken |= lg[v] != lg[v] || (a.softmax && lg[v] == INFINITY);
+      broken |= lg[v] != lg[v];
       top = fmaxf(top, lg[v]);
     }
-    broken = team_any<LPR>(broken);
     top = team_max<LPR>(top);
+    broken = team_any<LPR>(broken) || (a.softmax && top == INFINITY);
     const bool empty = broken || top == -INFINITY;   // no expert for this row, whatever the biases
-    double sum = 1.0;
-    if (a.softmax && (a.bias || GROUPED || !a.renormalise)) {
-      sum = 0.0;
+    const float from = empty ? 0.0f : top;
+    float inv = 1.0f;                                // of the sum of exp(l - top)
+    float value[V];
+    if (scores || (a.softmax && !a.renormalise)) {
+      float sum = 0.0f;
 #pragma unroll
-      for (int v = 0; v < V; ++v) sum += empty ? 0.0 : score_of(lg[v], true, top, false);
-      sum = team_add<LPR>(sum);
+      for (int v = 0; v < V; ++v) {
+        value[v] = quick_score(lg[v], a.softmax, from);
+        sum += value[v];
+      }
+      if (a.softmax) inv = empty ? 0.0f : 1.0f / team_add<LPR>(sum);
+#pragma unroll
+      for (int v = 0; v < V; ++v) value[v] = value[v] * inv + bias[v];
     }
-    double order[V];
+    // Two values of the same true order are at most this far the wrong way round: scores are off by (|l - top| + 8) 2^-23 of themselves (sum included), of which the
+    // largest has 2^-20 at most, and values by their rounding and the bits that say where they are from
+    const float off_scores = (a.softmax ? inv : 1.0f) * 0x1p-18f;
+    bool unsure = false;
+    uint64_t keep = ~0ull;
+    if constexpr (GROUPED) {
+      const int per = E / a.groups;
+      float *mine = s_value + my_team * MAX_E;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (index(v) < E) mine[index(v)] = !empty && fminf(lg[v], bias[v]) > -INFINITY ? value[v] : -INFINITY;
+      asm volatile("" ::: "memory");   // a team is part of one wavefront, whose LDS accesses come in order
+      __builtin_amdgcn_wave_barrier();
+      int worth[kMaxGroups / LPR];
+#pragma unroll
+      for (int i = 0; i < kMaxGroups / LPR; ++i) {
+        const int q = l + i * LPR;
+        worth[i] = kNobody;
+        if (q < a.groups) {
+          float one = -INFINITY, two = -INFINITY;
+          for (int c = 0; c < per; ++c) {
+            const float v = mine[q * per + c];
+            two = fmaxf(two, fminf(one, v));
+            one = fmaxf(one, v);
+          }
+          if (one > -INFINITY) worth[i] = (sortable(a.best == 2 && two > -INFINITY ? one + two : one) & ~(kMaxGroups - 1)) | (kMaxGroups - 1 - q);
+        }
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+      keep = 0;
+      int before = kNobody;
+      for (int j = 0; j <= a.kept; ++j) {
+        int best = worth[0];
+#pragma unroll
+        for (int i = 1; i < kMaxGroups / LPR; ++i) best = max(best, worth[i]);
+        best = team_max<LPR>(best);
+        if (best == kNobody) continue;
+        if (j < a.kept) {
+          keep |= 1ull << (kMaxGroups - 1 - (best & (kMaxGroups - 1)));
+          before = best;
+        } else {   // only between the last that is kept and the first that is not does the order matter
+          const float x = unsorted(before & ~(kMaxGroups - 1)), y = unsorted(best & ~(kMaxGroups - 1));
+          unsure = !(x - y > 0x1p-14f * fmaxf(fabsf(x), fabsf(y)) + 4.0f * off_scores);
+        }
+#pragma unroll
+        for (int i = 0; i < kMaxGroups / LPR; ++i)
+          if (worth[i] == best) worth[i] = kNobody;
+      }
+    }
+    int number[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const bool ok = !empty && lg[v] > -INFINITY && bias[v] > -INFINITY;
-      double value = (double)lg[v];
-      if (GROUPED || a.bias) {
-        value = score_of(lg[v], a.softmax, top, false) / sum + (double)bias[v];
-        if (GROUPED && index(v) < E) s_value[team * MAX_E + index(v)] = ok ? value : kNone;
-        if (!a.bias) value = (double)lg[v];
-      }
-      order[v] = ok ? value : kNone;
+      bool ok = !empty && fminf(lg[v], bias[v]) > -INFINITY;
+      if constexpr (GROUPED) ok = ok && (keep >> (min(index(v), E - 1) / (E / a.groups)) & 1);
+      const int s = sortable(a.bias ? value[v] : lg[v]);
+      number[v] = !ok ? kNobody : whole ? (s & ~0xffff) | (0xffff - index(v)) : (s & ~(V - 1)) | (V - 1 - v);
     }
-    if constexpr (GROUPED) {
-      __syncthreads();
-      const int per = E / a.groups;
-      for (int q = l; q < a.groups; q += LPR) {
-        double one = kNone, two = kNone;
-        for (int i = 0; i < per; ++i) {
-          const double v = s_value[team * MAX_E + q * per + i];
-          two = v > one ? one : fmax(two, v);
-          one = fmax(one, v);
-        }
-        s_group[team * kMaxGroups + q] = a.best == 2 && two > kNone ? one + two : one;
-      }
-      __syncthreads();
-      double mine[kMaxGroups / LPR];
-#pragma unroll
-      for (int i = 0; i < kMaxGroups / LPR; ++i) mine[i] = l + i * LPR < a.groups ? s_group[team * kMaxGroups + l + i * LPR] : kNone;
-      uint64_t keep = 0;
-      for (int j = 0; j < a.kept; ++j) {
-        Best b = {kNone, kMaxGroups, 0.0f};
-#pragma unroll
-        for (int i = 0; i < kMaxGroups / LPR; ++i)
-          if (mine[i] > b.value) b = {mine[i], l + i * LPR, 0.0f};
-        b = team_best<LPR>(b);
-        if (!(b.value > kNone)) break;
-        keep |= 1ull << b.index;
-#pragma unroll
-        for (int i = 0; i < kMaxGroups / LPR; ++i)
-          if (l + i * LPR == b.index) mine[i] = kNone;
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (index(v) < E && !(keep >> (index(v) / per) & 1)) order[v] = kNone;
-    }
+    Sorter<V>::sort(number);
     int chosen[SLOTS];
-    float logit[SLOTS];
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s) chosen[s] = -1, logit[s] = -INFINITY;
-    for (int j = 0; j < a.k; ++j) {
-      Best b = {kNone, MAX_E, 0.0f};
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (order[v] > b.value) b = {order[v], index(v), lg[v]};
-      b = team_best<LPR>(b);
-      if (!(b.value > kNone)) break;     // the same for the whole team
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (index(v) == b.index) order[v] = kNone;
+    for (int s = 0; s < SLOTS; ++s) chosen[s] = -1;
+    int before = kNobody;
+    const int last_j = whole ? a.k - 1 : a.k;        // one more, to see how far it is
+    for (int j = 0; j <= last_j; ++j) {
+      const int best = team_max<LPR>(number[0]);
+      const bool hit = number[0] == best && best != kNobody;
+      int at;
+      if (whole) {
+        at = best == kNobody ? -1 : 0xffff - (best & 0xffff);
+      } else {
+        const uint64_t from_lanes = team_ballot<LPR>(hit);
+        at = from_lanes ? index_of(V - 1 - (best & (V - 1)), __builtin_ctzll(from_lanes | 1ull << 63)) : -1;
+        if (from_lanes & (from_lanes - 1)) unsure = true;                   // two lanes' numbers are the same
+        if (j > 0 && from_lanes) {
+          const float x = unsorted(before & ~(V - 1)), y = unsorted(best & ~(V - 1));
+          if (!(x - y > (a.bias ? 0x1p-17f * fmaxf(fabsf(x), fabsf(y)) + off_scores : 0.0f))) unsure = true;
+        }
+        before = best;
+      }
 #pragma unroll
       for (int s = 0; s < SLOTS; ++s)
-        if (j == l + s * LPR) chosen[s] = b.index, logit[s] = b.with;
+        if (j < a.k && j == l + s * LPR) chosen[s] = at;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int stay = number[v], next = v + 1 < V ? number[v + 1] : kNobody;   // values: a choice of elements would become an array in scratch
+        number[v] = hit ? next : stay;
+      }
+    }
+    for (uint64_t left = __ballot(unsure); left;) {   // by the definition, team by team
+      const int lane0 = __builtin_ctzll(left) & ~(LPR - 1);
+      left &= LPR == 64 ? 0 : ~(((1ull << (LPR & 63)) - 1) << lane0);
+      const int pick = choose_exactly<T, (MAX_E < kWave ? kWave : MAX_E), GROUPED>(a, row + lane0 / LPR - lane0_of_mine / LPR, __shfl(top, lane0, kWave));
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s) {
+        const int at = __shfl(pick, l + s * LPR, kWave);
+        if (lane0 == lane0_of_mine) chosen[s] = at;
+      }
     }
     // weights
-    double highest = (double)top;
-    if (a.renormalise) {
-      float m = logit[0];
+    const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+    float logit[SLOTS], w[SLOTS], highest = top, total = 0.0f;
 #pragma unroll
-      for (int s = 1; s < SLOTS; ++s) m = fmaxf(m, logit[s]);
-      highest = (double)team_max<LPR>(m);
+    for (int s = 0; s < SLOTS; ++s) logit[s] = chosen[s] >= 0 ? to_f32(x[chosen[s]]) : -INFINITY;
+    if (a.renormalise) {
+      highest = logit[0];
+#pragma unroll
+      for (int s = 1; s < SLOTS; ++s) highest = fmaxf(highest, logit[s]);
+      highest = team_max<LPR>(highest);
     }
-    double w[SLOTS], total = 0.0;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
-      w[s] = chosen[s] >= 0 ? score_of(logit[s], a.softmax, highest, a.renormalise) : 0.0;
+      w[s] = chosen[s] >= 0 ? share(logit[s], a.softmax, highest, a.renormalise) : 0.0f;
       total += w[s];
     }
-    total = a.renormalise ? team_add<LPR>(total) : sum;
+    const float factor = a.renormalise ? a.scale / team_add<LPR>(total) : a.scale * inv;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       const int j = l + s * LPR;
       if (row < last && j < a.k) {
         a.expert[row * a.k + j] = chosen[s];
-        a.weight[row * a.k + j] = broken ? NAN : chosen[s] >= 0 ? (float)((double)a.scale * w[s] / total) : 0.0f;
+        a.weight[row * a.k + j] = broken ? NAN : chosen[s] >= 0 ? w[s] * factor : 0.0f;
         if (chosen[s] >= 0) atomicAdd(&s_words[chosen[s]], 1);
       }
     }
-    if constexpr (GROUPED) __syncthreads();   // s_value and s_group have been read
   }
   if (!a.off) return;
   __syncthreads();
   if (gridDim.x > 1) {
-    for (int e = threadIdx.x; e < E; e += THREADS) a.count[(int64_t)blockIdx.x * E + e] = s_words[e];
+    for (int e = threadIdx.x; e < E; e += threads) a.count[e * runs_ld(gridDim.x) + blockIdx.x] = s_words[e];
     return;
   }
-  for (int e = threadIdx.x; e < E; e += THREADS) {
+  for (int e = threadIdx.x; e < E; e += threads) {
     s_words[E + e] = s_words[e];
     s_words[e] = 0;
   }
-  places<THREADS>(a, 0, first, last, s_words, s_words + E);
+  places(a, 0, first, last, s_words, s_words + E);
 }
 
-constexpr int kPlaceThreads = 512;
+// A wavefront takes an expert's counts, four runs a lane.
+constexpr int kPlaceThreads = 1024;
 __global__ void __launch_bounds__(kPlaceThreads) k_places(RouteArgs a) {
   extern __shared__ int32_t s_words[];
+  static_assert(kMaxRuns == 4 * kWave, "four runs a lane");
   const int64_t first = (int64_t)blockIdx.x * a.run, last = min(a.rows, first + a.run);
-  const int E = a.experts, runs = gridDim.x, run = blockIdx.x;
-  for (int e = threadIdx.x; e < E; e += kPlaceThreads) {
-    int before = 0, all = 0;
-    for (int r = 0; r < runs; ++r) {
-      const int c = a.count[r * E + e];
-      all += c;
-      before += r < run ? c : 0;
+  const int E = a.experts, runs = gridDim.x, run = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int WAVES = kPlaceThreads / kWave, AHEAD = 8;
+  for (int e0 = wave; e0 < E; e0 += WAVES * AHEAD) {
+    int4 c[AHEAD];
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      const int e = e0 + p * WAVES;
+      c[p] = make_int4(0, 0, 0, 0);
+      if (e < E && 4 * lane < runs) c[p] = *reinterpret_cast<const int4 *>(a.count + e * runs_ld(runs) + 4 * lane);
     }
-    s_words[e] = before;
-    s_words[E + e] = all;
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      const int e = e0 + p * WAVES, r[4] = {c[p].x, c[p].y, c[p].z, c[p].w};
+      int before = 0, all = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (4 * lane + i < runs) all += r[i];
+        if (4 * lane + i < run) before += r[i];
+      }
+      auto add = [](int x, int y) { return x + y; };
+      all = team<64>(all, add);
+      before = team<64>(before, add);
+      if (lane == 0 && e < E) s_words[e] = before, s_words[E + e] = all;
+    }
   }
-  places<kPlaceThreads>(a, run, first, last, s_words, s_words + E);
+  places(a, run, first, last, s_words, s_words + E);
 }
 
 // ---- gradient -----------------------------------------------------------------------------------------------------
@@ -347,12 +563,6 @@ struct RouteBackArgs {
   const float *weight, *dweight;
   void *dlogits;
 };
-
-template <int LPR> __device__ __forceinline__ float team_addf(float v) {
-#pragma unroll
-  for (int o = LPR / 2; o; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
-}
 
 template <typename T, int LPR, int V, bool WIDE> __global__ void __launch_bounds__(256) k_route_back(RouteBackArgs a) {
   constexpr int TEAMS = 256 / LPR, MAX_E = LPR * V, SLOTS = LPR < GEAR_MAX_CHOSEN ? GEAR_MAX_CHOSEN / LPR : 1;
@@ -390,7 +600,7 @@ template <typename T, int LPR, int V, bool WIDE> __global__ void __launch_bounds
     }
     broken = team_any<LPR>(broken);
     some = team_any<LPR>(some);      // else the row is padding, whatever its logits hold, or has no expert: zeros
-    inner = team_addf<LPR>(inner);
+    inner = team_add<LPR>(inner);
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
@@ -421,8 +631,8 @@ template <typename T, int LPR, int V, bool WIDE> __global__ void __launch_bounds
         sum += lg[v];
         dot += lg[v] * d[v];
       }
-      sum = team_addf<LPR>(sum);
-      dot = team_addf<LPR>(dot);
+      sum = team_add<LPR>(sum);
+      dot = team_add<LPR>(dot);
       const float inv = none ? 0.0f : 1.0f / sum;
 #pragma unroll
       for (int v = 0; v < V; ++v) d[v] = lg[v] * inv * (d[v] - dot * inv);
@@ -446,14 +656,16 @@ template <typename F> hipError_t by_experts(int experts, F &&call) {
 }
 
 struct Runs {
-  int run, count;
+  int run, count, threads;
 };
-// Runs of rows: as many as there are CUs, of whole passes of a workgroup over its rows.
+// Runs of rows: as many as there are CUs at most, of whole passes of a workgroup over its rows; a batch that fits in one has no more threads
+// than its rows need (one row of 64: 9.1 us by 1024 threads).
 Runs runs_of(int64_t rows, int experts, bool grouped) {
-  const int lpr = experts <= 256 ? 16 : experts <= 512 ? 32 : 64, teams = (grouped ? kGroupedThreads : kRouteThreads) / lpr;
+  const int lpr = experts <= 256 ? 16 : experts <= 512 ? 32 : 64, most = grouped ? kGroupedThreads : kRouteThreads, teams = most / lpr;
   const int64_t passes = (rows + teams - 1) / teams, each = (passes + kMaxRuns - 1) / kMaxRuns;
   const int64_t run = (each > 0 ? each : 1) * teams;
-  return {(int)run, (int)(rows > 0 ? (rows + run - 1) / run : 1)};
+  const int threads = rows >= teams ? most : rows > 0 ? (int)((rows * lpr + kWave - 1) / kWave * kWave) : kWave;
+  return {(int)run, (int)(rows > 0 ? (rows + run - 1) / run : 1), threads};
 }
 
 bool sizes_ok(int64_t rows, int32_t experts, int32_t k) {
@@ -461,16 +673,15 @@ bool sizes_ok(int64_t rows, int32_t experts, int32_t k) {
          rows * k <= (1 << 30);
 }
 
-template <typename T, bool WIDE, bool GROUPED> hipError_t launch_route(const RouteArgs &a, int runs, hipStream_t s) {
+template <typename T, bool WIDE, bool GROUPED> hipError_t launch_route(const RouteArgs &a, const Runs &runs, hipStream_t s) {
   return by_experts(a.experts, [&](auto lpr, auto v) {
-    constexpr int THREADS = GROUPED ? kGroupedThreads : kRouteThreads;
-    const size_t lds = (size_t)a.experts * (1 + (runs == 1 ? kRankers : 0)) * 4;
-    hipLaunchKernelGGL((k_route<T, decltype(lpr)::value, decltype(v)::value, WIDE, GROUPED>), dim3(runs), dim3(THREADS), lds, s, a);
+    const size_t lds = (size_t)a.experts * (1 + (runs.count == 1 ? rankers_of(a.experts) : 0)) * 4;
+    hipLaunchKernelGGL((k_route<T, decltype(lpr)::value, decltype(v)::value, WIDE, GROUPED>), dim3(runs.count), dim3(runs.threads), lds, s, a);
     return hipGetLastError();
   });
 }
 
-template <typename T> hipError_t launch_route_of(const RouteArgs &a, int runs, bool wide, hipStream_t s) {
+template <typename T> hipError_t launch_route_of(const RouteArgs &a, const Runs &runs, bool wide, hipStream_t s) {
   if (a.groups > 1) return wide ? launch_route<T, true, true>(a, runs, s) : launch_route<T, false, true>(a, runs, s);
   return wide ? launch_route<T, true, false>(a, runs, s) : launch_route<T, false, false>(a, runs, s);
 }
@@ -491,7 +702,7 @@ using namespace gear;
 
 extern "C" size_t gear_route_workspace_bytes(int64_t rows, int32_t experts, int32_t k, int32_t groups) {
   if (!sizes_ok(rows, experts, k) || groups < 1) return 0;
-  return ((size_t)runs_of(rows, experts, groups > 1).count * experts * 4 + 255) / 256 * 256;
+  return ((size_t)runs_ld(runs_of(rows, experts, groups > 1).count) * experts * 4 + 255) / 256 * 256;
 }
 
 extern "C" gear_status gear_route(const gear_route_args *a, void *workspace, size_t workspace_bytes, void *stream) {
@@ -519,9 +730,9 @@ extern "C" gear_status gear_route(const gear_route_args *a, void *workspace, siz
   const RouteArgs p = {a->rows, a->ld_logits, r.run, a->experts, a->k, a->score == GEAR_SCORE_SOFTMAX, a->groups, a->groups_kept, a->group_best,
                        a->renormalise != 0, a->scale, a->logits, a->bias, a->n, a->expert, a->weight, a->off, a->place, (int32_t *)workspace};
   const bool wide = a->experts % 4 == 0 && a->ld_logits % 4 == 0 && ((uintptr_t)a->logits & (4 * size - 1)) == 0;
-  hipError_t err = a->dtype == GEAR_F32 ? launch_route_of<float>(p, r.count, wide, s) : launch_route_of<bf16_t>(p, r.count, wide, s);
+  hipError_t err = a->dtype == GEAR_F32 ? launch_route_of<float>(p, r, wide, s) : launch_route_of<bf16_t>(p, r, wide, s);
   if (err == hipSuccess && a->off && r.count > 1) {
-    hipLaunchKernelGGL(k_places, dim3(r.count), dim3(kPlaceThreads), (size_t)a->experts * (1 + kRankers) * 4, s, p);
+    hipLaunchKernelGGL(k_places, dim3(r.count), dim3(kPlaceThreads), (size_t)a->experts * (1 + rankers_of(a->experts)) * 4, s, p);
     err = hipGetLastError();
   }
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
