@@ -6,10 +6,12 @@
 // hundred thousand.  So the choice is made twice at most: from fp32, with a bound on its error, and again by the definition, in
 // fp64, by the wavefronts that have a row with two neighbours in its order closer than that.
 //
-// The choice from fp32.  Values become whole numbers of the same order (`sortable`) whose last bits say which of the lane's values
-// they are, so that a comparison moves both in one instruction.  A lane sorts its own by a network; then k + 1 times the largest of
-// the team's first ones is taken, by rotations within 16 lanes, and its lane moves on to its next.  (k times the largest of all V
-// in fp64 instead: 114 us for 65536 rows of 256 with a bias, k = 8.)
+// The choice from fp32.  A value becomes a whole number: how far it lies above a bound under the k-th, in 2^-21 of the way to the
+// largest, and behind that its expert's tag, so that one comparison moves both and equal ones come in the order of their experts.  The
+// conversion keeps the order, if not every difference, so only neighbours with the same or (where scores are added up) too
+// near numbers are in doubt.  A lane sorts its own by a network.  Where k is at most 8, teams then merge lists of 8 lane by lane,
+// log2(LPR) times, and keep the best of what falls off; else k + 1 times the largest of the team's first ones is taken and its lane moves
+// on.  Bound by these instructions.
 //
 // The order of the pairs is a counting sort by expert.  A workgroup takes a run of rows and counts its experts; a second launch
 // with the same runs finds from all counts where each run's pairs begin, ranks them (equal experts in a wavefront by ballots,
@@ -56,6 +58,9 @@ template <int LPR, typename V, typename F> __device__ __forceinline__ V team(V v
 }
 template <int LPR> __device__ __forceinline__ float team_max(float v) {
   return team<LPR>(v, [](float x, float y) { return fmaxf(x, y); });
+}
+template <int LPR> __device__ __forceinline__ float team_min(float v) {
+  return team<LPR>(v, [](float x, float y) { return fminf(x, y); });
 }
 template <int LPR> __device__ __forceinline__ int team_max(int v) {
   return team<LPR>(v, [](int x, int y) { return max(x, y); });
@@ -112,6 +117,27 @@ __device__ __forceinline__ int sortable(float f) {
 }
 __device__ __forceinline__ float unsorted(int s) { return __int_as_float(s ^ ((s >> 31) & 0x7fffffff)); }
 
+// ---- whole numbers that say whose they are ------------------------------------------------------------------------------
+constexpr int kTagBits = 10, kTag = (1 << kTagBits) - 1;      // the lower of equal values' experts has the larger tag
+static_assert(GEAR_MAX_EXPERTS <= kTag + 1, "an expert's number fits");
+constexpr float kSteps = 2097150.0f;                          // 2^21 - 2
+__device__ __forceinline__ bool is_somebody(int number) { return number > kTag; }
+__device__ __forceinline__ int expert_of(int number) { return kTag - (number & kTag); }
+// v, or -inf who may not be chosen; from `bound` (1) to the largest (2^21 - 1), 0 below
+__device__ __forceinline__ int number_of(float v, float bound, float steps, int expert) {
+  return (int)fmaxf(fmaf(v - bound, steps, 1.0f), 0.0f) << kTagBits | (kTag - expert);
+}
+
+template <int CTRL> __device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
+// the other half of a group of 2 << STEP lanes, in some order: what it holds is the same in all of its lanes
+template <int STEP> __device__ __forceinline__ int across(int v) {
+  if constexpr (STEP == 0) return moved<0xb1>(v);         // lanes 1 0 3 2
+  if constexpr (STEP == 1) return moved<0x4e>(v);         // lanes 2 3 0 1
+  if constexpr (STEP == 2) return moved<0x141>(v);        // eight lanes backwards
+  if constexpr (STEP == 3) return moved<0x140>(v);        // sixteen
+  return __shfl_xor(v, 1 << STEP, kWave);
+}
+
 // descending, by odd-even merges
 template <int V> struct Sorter {
   template <int I, int J> static __device__ __forceinline__ void exchange(int (&k)[V]) {
@@ -141,6 +167,32 @@ template <int V> struct Sorter {
     }
   }
 };
+
+// The first eight of two lanes' lists of eight, and the largest of all that are in neither of their lists.
+constexpr int kList = 8;
+template <int STEP, int LPR> __device__ __forceinline__ void merge_lists(int (&mine)[kList], int &rest) {
+  if constexpr ((1 << STEP) < LPR) {
+    int all[kList];
+    rest = max(rest, across<STEP>(rest));
+#pragma unroll
+    for (int i = 0; i < kList; ++i) {
+      const int other = across<STEP>(mine[kList - 1 - i]);
+      all[i] = max(mine[i], other);
+      rest = max(rest, min(mine[i], other));
+    }
+#pragma unroll
+    for (int apart = kList / 2; apart; apart /= 2)   // they fall, then rise: halves against each other
+#pragma unroll
+      for (int i = 0; i < kList; ++i)
+        if (!(i & apart)) {
+          const int a = max(all[i], all[i + apart]), b = min(all[i], all[i + apart]);
+          all[i] = a, all[i + apart] = b;
+        }
+#pragma unroll
+    for (int i = 0; i < kList; ++i) mine[i] = all[i];
+    merge_lists<STEP + 1, LPR>(mine, rest);
+  }
+}
 
 // ---- order of the pairs -------------------------------------------------------------------------------------------
 // Places of the pairs of rows [first, last), those of run number `run`.  On entry s_wave[e] is the number of expert e's pairs in all
@@ -172,52 +224,59 @@ __device__ __forceinline__ void places(const RouteArgs &a, int run, int64_t firs
   for (int i = threadIdx.x; i < waves * E; i += threads) s_wave[i] = 0;
   __syncthreads();
   // a wavefront's pairs one behind the other, 64 at a time, four times 64 requested together: first it counts, then it places
+  constexpr int AHEAD = 4;
   const int64_t pairs = (last - first) * a.k, per = (pairs + waves - 1) / waves;
   const int64_t begin = first * a.k + min(wave * per, pairs);
   const int64_t end = wave < waves ? first * a.k + min((wave + 1) * per, pairs) : begin;
   int32_t *mine = s_wave + min(wave, waves - 1) * E;
-  auto walk = [&](auto &&then) {
-    constexpr int AHEAD = 4;
-    for (int64_t i0 = begin; i0 < end; i0 += AHEAD * kWave) {
-      int e[AHEAD];
+  int e[AHEAD];
+  auto request = [&](int64_t i0) {
 #pragma unroll
-      for (int p = 0; p < AHEAD; ++p) {
-        const int64_t i = i0 + p * kWave + lane;
-        e[p] = i < end ? a.expert[i] : -1;
-      }
-#pragma unroll
-      for (int p = 0; p < AHEAD; ++p)
-        if (i0 + p * kWave < end) then(i0 + p * kWave + lane, e[p]);
+    for (int p = 0; p < AHEAD; ++p) {
+      const int64_t i = i0 + p * kWave + lane;
+      e[p] = i < end ? a.expert[i] : -1;
     }
   };
-  walk([&](int64_t, int e) {
-    if (e >= 0) atomicAdd(mine + e, 1);
-  });
+  for (int64_t i0 = begin; i0 < end; i0 += AHEAD * kWave) {
+    request(i0);
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p)
+      if (e[p] >= 0) atomicAdd(mine + e[p], 1);
+  }
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += threads) {
-    int at = s_base[e];
-    for (int w = 0; w < waves; ++w) {
-      const int c = s_wave[w * E + e];
-      s_wave[w * E + e] = at;
-      at += c;
+  for (int x = threadIdx.x; x < E; x += threads) {
+    int c[16], at = s_base[x];
+    static_assert(rankers_of(1) == 16, "all counts requested together");
+#pragma unroll
+    for (int w = 0; w < 16; ++w) c[w] = w < waves ? s_wave[w * E + x] : 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      if (w < waves) s_wave[w * E + x] = at;
+      at += c[w];
     }
   }
   __syncthreads();
   int bits = 0;
   while ((1 << bits) < E) ++bits;
-  walk([&](int64_t i, int e) {
-    uint64_t same = __ballot(e >= 0);   // lanes of the same expert
-    for (int b = 0; b < bits; ++b) {
-      const uint64_t set = __ballot((e >> b) & 1);
-      same &= (e >> b) & 1 ? set : ~set;
+  for (int64_t i0 = begin; i0 < end; i0 += AHEAD * kWave) {
+    if (end - begin > AHEAD * kWave) request(i0);   // else they are still there
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      const int64_t i = i0 + p * kWave + lane;
+      if (i0 + p * kWave >= end) break;
+      uint64_t same = __ballot(e[p] >= 0);   // lanes of the same expert
+      for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((e[p] >> b) & 1);
+        same &= (e[p] >> b) & 1 ? set : ~set;
+      }
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      int at = -1;
+      if (e[p] >= 0) at = mine[e[p]] + rank;
+      asm volatile("" ::: "memory");   // every lane has read before one adds
+      if (e[p] >= 0 && rank == 0) mine[e[p]] += __popcll(same);
+      if (i < end) a.place[i] = at;
     }
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    int at = -1;
-    if (e >= 0) at = mine[e] + rank;
-    asm volatile("" ::: "memory");   // every lane has read before one adds
-    if (e >= 0 && rank == 0) mine[e] += __popcll(same);
-    if (i < end) a.place[i] = at;
-  });
+  }
 }
 
 // The choice of one row by the definition, in fp64, by a whole wavefront: lane j gets the j-th expert, -1 where there is none.  The row is
@@ -295,11 +354,11 @@ template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int ch
   return chosen;
 }
 
-template <typename T, int LPR, int V, bool WIDE, bool GROUPED>
+template <typename T, int LPR, int V, bool WIDE, bool GROUPED, bool FEW>   // FEW: k is at most kList
 __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_route(RouteArgs a) {
-  constexpr int MAX_E = LPR * V, SLOTS = LPR < GEAR_MAX_CHOSEN ? GEAR_MAX_CHOSEN / LPR : 1;   // of a lane
-  constexpr bool HALF = sizeof(T) == 2;
+  constexpr int MAX_E = LPR * V, SLOTS = !FEW && LPR < GEAR_MAX_CHOSEN ? GEAR_MAX_CHOSEN / LPR : 1;   // of a lane
   static_assert(!WIDE || V % 4 == 0, "four neighbouring logits a load");
+  static_assert(GEAR_MAX_EXPERTS <= 1024 && LPR >= kList, "a tag's bits; a lane for each of a list");
   extern __shared__ int32_t s_words[];                          // [experts] counts, then what places() needs
   __shared__ float s_value[GROUPED ? kGroupedThreads * V : 1];
   const int threads = blockDim.x, teams = threads / LPR;
@@ -308,8 +367,7 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * a.run, last = min(a.rows, first + a.run);
   const int64_t used = min(last, a.n ? (int64_t)max(*a.n, 0) : last);
-  auto index_of = [&](int v, int lane) { return WIDE ? (v / 4) * (LPR * 4) + lane * 4 + v % 4 : v * LPR + lane; };
-  auto index = [&](int v) { return index_of(v, l); };
+  auto index = [&](int v) { return WIDE ? (v / 4) * (LPR * 4) + l * 4 + v % 4 : v * LPR + l; };
   float bias[V];                              // -inf where it may not be chosen
 #pragma unroll
   for (int v = 0; v < V; ++v) {
@@ -317,9 +375,9 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
     if (!(bias[v] > -INFINITY)) bias[v] = -INFINITY;
   }
   const bool scores = a.bias || GROUPED;      // the choice looks at them
-  const bool whole = HALF && !a.bias;         // logits of 16 bits decide: a number holds one and its expert, and nothing is approximate
 
-  auto load = [&](float (&lg)[V], int64_t row) {
+  float lg[V];
+  auto load = [&](int64_t row) {
 #pragma unroll
     for (int v = 0; v < V; ++v) lg[v] = -INFINITY;
     if (row >= used) return;
@@ -328,7 +386,7 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
 #pragma unroll
       for (int v = 0; v < V; v += 4)
         if (index(v) < E) {
-          if constexpr (!HALF) {
+          if constexpr (sizeof(T) == 4) {
             const float4 f = *reinterpret_cast<const float4 *>(x + index(v));
             lg[v] = f.x, lg[v + 1] = f.y, lg[v + 2] = f.z, lg[v + 3] = f.w;
           } else {
@@ -343,20 +401,15 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
         if (index(v) < E) lg[v] = to_f32(x[index(v)]);
     }
   };
-  float lg[V], ahead[V];
-  load(ahead, first + my_team);
+  load(first + my_team);
   for (int64_t row0 = first; row0 < last; row0 += teams) {
     const int64_t row = row0 + my_team;
-#pragma unroll
-    for (int v = 0; v < V; ++v) lg[v] = ahead[v];
-    if (row0 + teams < last) load(ahead, row + teams);
     bool broken = false;
     float top = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      broken |= lg[v] != lg[v];
-      top = fmaxf(top, lg[v]);
-    }
+    for (int v = 0; v < V; v += 2) broken |= __builtin_isunordered(lg[v], lg[v + 1]);   // either is NaN
+#pragma unroll
+    for (int v = 0; v < V; ++v) top = fmaxf(top, lg[v]);
     top = team_max<LPR>(top);
     broken = team_any<LPR>(broken) || (a.softmax && top == INFINITY);
     const bool empty = broken || top == -INFINITY;   // no expert for this row, whatever the biases
@@ -372,11 +425,11 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
       }
       if (a.softmax) inv = empty ? 0.0f : 1.0f / team_add<LPR>(sum);
 #pragma unroll
-      for (int v = 0; v < V; ++v) value[v] = value[v] * inv + bias[v];
+      for (int v = 0; v < V; ++v) value[v] = fmaf(value[v], inv, bias[v]);
     }
-    // Two values of the same true order are at most this far the wrong way round: scores are off by (|l - top| + 8) 2^-23 of themselves (sum included), of which the
-    // largest has 2^-20 at most, and values by their rounding and the bits that say where they are from
-    const float off_scores = (a.softmax ? inv : 1.0f) * 0x1p-18f;
+    // How far apart two values have to be at least to be in their true order.  A softmax in fp32 is off by s (d + 13) 2^-23, d = top - l (argument, exponential, sum
+    // and quotient), which is largest at the row's largest score `inv`: 2^-19 of it.  A sigmoid is off by 2^-22.
+    const float apart = a.softmax ? inv * 0x1p-18f : 0x1p-20f;
     bool unsure = false;
     uint64_t keep = ~0ull;
     if constexpr (GROUPED) {
@@ -394,6 +447,7 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
         worth[i] = kNobody;
         if (q < a.groups) {
           float one = -INFINITY, two = -INFINITY;
+#pragma unroll 4
           for (int c = 0; c < per; ++c) {
             const float v = mine[q * per + c];
             two = fmaxf(two, fminf(one, v));
@@ -415,52 +469,89 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
         if (j < a.kept) {
           keep |= 1ull << (kMaxGroups - 1 - (best & (kMaxGroups - 1)));
           before = best;
-        } else {   // only between the last that is kept and the first that is not does the order matter
+        } else {   // only between the last that is kept and the first that is not does the order matter; six bits are the group's number
           const float x = unsorted(before & ~(kMaxGroups - 1)), y = unsorted(best & ~(kMaxGroups - 1));
-          unsure = !(x - y > 0x1p-14f * fmaxf(fabsf(x), fabsf(y)) + 4.0f * off_scores);
+          unsure = !(x - y > 0x1p-15f * fmaxf(fabsf(x), fabsf(y)) + 2.0f * apart);
         }
 #pragma unroll
         for (int i = 0; i < kMaxGroups / LPR; ++i)
           if (worth[i] == best) worth[i] = kNobody;
       }
     }
-    int number[V];
+    // what decides, -inf where it may not be chosen
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      bool ok = !empty && fminf(lg[v], bias[v]) > -INFINITY;
-      if constexpr (GROUPED) ok = ok && (keep >> (min(index(v), E - 1) / (E / a.groups)) & 1);
-      const int s = sortable(a.bias ? value[v] : lg[v]);
-      number[v] = !ok ? kNobody : whole ? (s & ~0xffff) | (0xffff - index(v)) : (s & ~(V - 1)) | (V - 1 - v);
+      if (!a.bias)
+        value[v] = lg[v];
+      else if (!(lg[v] > -INFINITY))
+        value[v] = -INFINITY;
+      if constexpr (GROUPED)
+        if (!(keep >> (min(index(v), E - 1) / (E / a.groups)) & 1)) value[v] = -INFINITY;
     }
+    if (row0 + teams < last) load(row + teams);     // on their way while these are sorted
+    float high = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < V; ++v) high = fmaxf(high, value[v]);
+    // Every lane's largest is at least the bound: LPR values are, 16 at least, more than the k + 1 that a list of eight is about.  Where a lane
+    // has none, or k is larger, nobody eligible lies below the bound.
+    float bound = team_min<LPR>(high);
+    high = team_max<LPR>(high);
+    if (!FEW || __any(!(bound > -INFINITY))) {
+      float low = INFINITY;
+#pragma unroll
+      for (int v = 0; v < V; ++v) low = fminf(low, value[v] > -INFINITY ? value[v] : INFINITY);
+      low = team_min<LPR>(low);
+      if (!FEW || !(bound > -INFINITY)) bound = low;
+    }
+    const float range = high - bound, steps = fminf(kSteps / range, 0x1p127f);   // range 0: those below are still below 1
+    int number[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) number[v] = number_of(value[v], bound, steps, index(v));
     Sorter<V>::sort(number);
+    // x before y in the order, y somebody: is that in doubt?  Sums of scores and biases: if they are `apart` or less, or their own rounding.
+    // Logits: if their numbers are the same but they may not be.  All are where the range is none; logits of 16 bits, which differ by 2^-8 of themselves,
+    // are unless they are next to nothing.
+    const int near = a.bias ? (int)fminf((apart + 0x1p-22f * fmaxf(fabsf(high), fabsf(bound))) * steps, 0x1p22f) + 2 : 0;
+    auto doubt = [&](int x, int y) {
+      const int ahead = (x >> kTagBits) - (y >> kTagBits);
+      if (ahead > near) return false;
+      if (a.bias) return true;
+      if (sizeof(T) == 2 && fabsf(bound + (float)(x >> kTagBits) * (range * 0x1p-21f)) > range * 0x1p-10f) return false;
+      return range != 0.0f;
+    };
+    unsure = !empty && (unsure || !(range < INFINITY));
     int chosen[SLOTS];
+    if constexpr (FEW) {
+      int list[kList], rest = V > kList ? number[V > kList ? kList : 0] : 0;
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s) chosen[s] = -1;
-    int before = kNobody;
-    const int last_j = whole ? a.k - 1 : a.k;        // one more, to see how far it is
-    for (int j = 0; j <= last_j; ++j) {
-      const int best = team_max<LPR>(number[0]);
-      const bool hit = number[0] == best && best != kNobody;
-      int at;
-      if (whole) {
-        at = best == kNobody ? -1 : 0xffff - (best & 0xffff);
-      } else {
-        const uint64_t from_lanes = team_ballot<LPR>(hit);
-        at = from_lanes ? index_of(V - 1 - (best & (V - 1)), __builtin_ctzll(from_lanes | 1ull << 63)) : -1;
-        if (from_lanes & (from_lanes - 1)) unsure = true;                   // two lanes' numbers are the same
-        if (j > 0 && from_lanes) {
-          const float x = unsorted(before & ~(V - 1)), y = unsorted(best & ~(V - 1));
-          if (!(x - y > (a.bias ? 0x1p-17f * fmaxf(fabsf(x), fabsf(y)) + off_scores : 0.0f))) unsure = true;
-        }
-        before = best;
+      for (int i = 0; i < kList; ++i) list[i] = i < V ? number[i < V ? i : 0] : 0;
+      merge_lists<0, LPR>(list, rest);
+      int mine = list[0], next = list[1];   // of lane l: the l-th and the one behind it
+#pragma unroll
+      for (int i = 1; i < kList; ++i) {
+        const int x = list[i], y = i + 1 < kList ? list[i + 1 < kList ? i + 1 : 0] : rest;
+        if (l == i) mine = x, next = y;
       }
+      const bool is = !empty && l < a.k && is_somebody(mine);
+      chosen[0] = is ? expert_of(mine) : -1;
+      if (is && is_somebody(next) && doubt(mine, next)) unsure = true;
+    } else {
 #pragma unroll
-      for (int s = 0; s < SLOTS; ++s)
-        if (j < a.k && j == l + s * LPR) chosen[s] = at;
+      for (int s = 0; s < SLOTS; ++s) chosen[s] = -1;
+      int before = 0;
+      for (int j = 0; j <= a.k; ++j) {        // one more, to see how far it is
+        const int best = team_max<LPR>(number[0]);
+        const bool hit = number[0] == best, is = !empty && is_somebody(best);
+        if (is && j > 0 && doubt(before, best)) unsure = true;
+        before = best;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int stay = number[v], next = v + 1 < V ? number[v + 1] : kNobody;   // values: a choice of elements would become an array in scratch
-        number[v] = hit ? next : stay;
+        for (int s = 0; s < SLOTS; ++s)
+          if (is && j < a.k && j == l + s * LPR) chosen[s] = expert_of(best);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int stay = number[v], next = v + 1 < V ? number[v + 1] : 0;   // values: a choice of elements would become an array in scratch
+          number[v] = hit ? next : stay;
+        }
       }
     }
     for (uint64_t left = __ballot(unsure); left;) {   // by the definition, team by team
@@ -469,7 +560,7 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
       const int pick = choose_exactly<T, (MAX_E < kWave ? kWave : MAX_E), GROUPED>(a, row + lane0 / LPR - lane0_of_mine / LPR, __shfl(top, lane0, kWave));
 #pragma unroll
       for (int s = 0; s < SLOTS; ++s) {
-        const int at = __shfl(pick, l + s * LPR, kWave);
+        const int at = __shfl(pick, (l + s * LPR) & 63, kWave);
         if (lane0 == lane0_of_mine) chosen[s] = at;
       }
     }
@@ -676,7 +767,11 @@ bool sizes_ok(int64_t rows, int32_t experts, int32_t k) {
 template <typename T, bool WIDE, bool GROUPED> hipError_t launch_route(const RouteArgs &a, const Runs &runs, hipStream_t s) {
   return by_experts(a.experts, [&](auto lpr, auto v) {
     const size_t lds = (size_t)a.experts * (1 + (runs.count == 1 ? rankers_of(a.experts) : 0)) * 4;
-    hipLaunchKernelGGL((k_route<T, decltype(lpr)::value, decltype(v)::value, WIDE, GROUPED>), dim3(runs.count), dim3(runs.threads), lds, s, a);
+    constexpr int LPR = decltype(lpr)::value, V = decltype(v)::value;
+    if (a.k <= kList)
+      hipLaunchKernelGGL((k_route<T, LPR, V, WIDE, GROUPED, true>), dim3(runs.count), dim3(runs.threads), lds, s, a);
+    else
+      hipLaunchKernelGGL((k_route<T, LPR, V, WIDE, GROUPED, false>), dim3(runs.count), dim3(runs.threads), lds, s, a);
     return hipGetLastError();
   });
 }
