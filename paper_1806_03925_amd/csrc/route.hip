@@ -45,7 +45,7 @@ struct RouteArgs {
 __host__ __device__ constexpr int runs_ld(int runs) { return (runs + 3) / 4 * 4; }
 
 // ---- over a team: every lane gets the result, and every lane of the wavefront takes part -------------------------------
-template <int N> __device__ __forceinline__ int rotate(int v) { return __builtin_amdgcn_update_dpp(v, v, 0x120 + N, 0xf, 0xf, false); }   // in 16 lanes
+template <int N> __device__ __forceinline__ int rotate(int v) { return __builtin_amdgcn_mov_dpp(v, 0x120 + N, 0xf, 0xf, true); }   // in 16 lanes
 template <int N> __device__ __forceinline__ float rotate(float v) { return __int_as_float(rotate<N>(__float_as_int(v))); }
 template <int LPR, typename V, typename F> __device__ __forceinline__ V team(V v, F &&f) {
   v = f(v, rotate<8>(v));
@@ -95,11 +95,8 @@ __device__ __forceinline__ Best wave_best(Best b) {
 __device__ __forceinline__ double exact_score(float l, bool softmax, float top) {
   return softmax ? exp((double)l - (double)top) : 1.0 / (1.0 + exp(-(double)l));
 }
-// in fp32: exp(l - top); sigmoid.  Off by (|l - top| + 4) 2^-24 of themselves.
+// in fp32, off by (|v| + 2) 2^-23 of itself
 __device__ __forceinline__ float quick_exp(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504f); }
-__device__ __forceinline__ float quick_score(float l, bool softmax, float top) {
-  return softmax ? quick_exp(l - top) : __builtin_amdgcn_rcpf(1.0f + quick_exp(-l));
-}
 // A chosen expert's share: its score up to a factor that is the same for all of its row where `relative`.  No sum of such scores
 // vanishes then, however small they are, when `top` is the largest chosen logit.
 __device__ __forceinline__ float share(float l, bool softmax, float top, bool relative) {
@@ -128,7 +125,7 @@ __device__ __forceinline__ int number_of(float v, float bound, float steps, int 
   return (int)fmaxf(fmaf(v - bound, steps, 1.0f), 0.0f) << kTagBits | (kTag - expert);
 }
 
-template <int CTRL> __device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
+template <int CTRL> __device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
 // the other half of a group of 2 << STEP lanes, in some order: what it holds is the same in all of its lanes
 template <int STEP> __device__ __forceinline__ int across(int v) {
   if constexpr (STEP == 0) return moved<0xb1>(v);         // lanes 1 0 3 2
@@ -417,13 +414,18 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
     float inv = 1.0f;                                // of the sum of exp(l - top)
     float value[V];
     if (scores || (a.softmax && !a.renormalise)) {
-      float sum = 0.0f;
+      if (a.softmax) {
+        float sum = 0.0f;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        value[v] = quick_score(lg[v], a.softmax, from);
-        sum += value[v];
+        for (int v = 0; v < V; ++v) {
+          value[v] = quick_exp(lg[v] - from);
+          sum += value[v];
+        }
+        inv = empty ? 0.0f : 1.0f / team_add<LPR>(sum);
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) value[v] = __builtin_amdgcn_rcpf(1.0f + quick_exp(-lg[v]));
       }
-      if (a.softmax) inv = empty ? 0.0f : 1.0f / team_add<LPR>(sum);
 #pragma unroll
       for (int v = 0; v < V; ++v) value[v] = fmaf(value[v], inv, bias[v]);
     }
@@ -526,12 +528,15 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
 #pragma unroll
       for (int i = 0; i < kList; ++i) list[i] = i < V ? number[i < V ? i : 0] : 0;
       merge_lists<0, LPR>(list, rest);
-      int mine = list[0], next = list[1];   // of lane l: the l-th and the one behind it
-#pragma unroll
-      for (int i = 1; i < kList; ++i) {
-        const int x = list[i], y = i + 1 < kList ? list[i + 1 < kList ? i + 1 : 0] : rest;
-        if (l == i) mine = x, next = y;
-      }
+      // lane l's: the l-th and the one behind it, by the bits of l
+      auto pick = [&](int a0, int a1, int a2, int a3, int a4, int a5, int a6, int a7) {
+        const int b0 = l & 1 ? a1 : a0, b1 = l & 1 ? a3 : a2, b2 = l & 1 ? a5 : a4, b3 = l & 1 ? a7 : a6;
+        const int c0 = l & 2 ? b1 : b0, c1 = l & 2 ? b3 : b2;
+        return l & 4 ? c1 : c0;
+      };
+      static_assert(kList == 8, "three bits");
+      const int mine = pick(list[0], list[1], list[2], list[3], list[4], list[5], list[6], list[7]);
+      const int next = pick(list[1], list[2], list[3], list[4], list[5], list[6], list[7], rest);
       const bool is = !empty && l < a.k && is_somebody(mine);
       chosen[0] = is ? expert_of(mine) : -1;
       if (is && is_somebody(next) && doubt(mine, next)) unsure = true;
