@@ -39,10 +39,12 @@ struct RouteArgs {
   const int32_t *n;
   int32_t *expert;
   float *weight;
-  int32_t *off, *place, *count;      // count [experts x runs, a multiple of four]
+  int32_t *off, *place;
+  void *count;                       // [experts x runs_ld] of 16 bits, of 32 where a run has more rows than that holds
 };
 
-__host__ __device__ constexpr int runs_ld(int runs) { return (runs + 3) / 4 * 4; }
+__host__ __device__ constexpr int runs_ld(int runs) { return (runs + 7) / 8 * 8; }
+__host__ __device__ constexpr bool narrow(int run) { return run <= 0xffff; }   // an expert is chosen once a row
 
 // ---- over a team: every lane gets the result, and every lane of the wavefront takes part -------------------------------
 template <int N> __device__ __forceinline__ int rotate(int v) { return __builtin_amdgcn_mov_dpp(v, 0x120 + N, 0xf, 0xf, true); }   // in 16 lanes
@@ -75,17 +77,34 @@ template <int LPR> __device__ __forceinline__ uint64_t team_ballot(bool v) {   /
 }
 template <int LPR> __device__ __forceinline__ bool team_any(bool v) { return team_ballot<LPR>(v) != 0; }
 
-// the largest of a wavefront's (value, index), the lower index of equals
+// over a wavefront, in fp64: within 16 lanes by rotations, then the four
+template <int N> __device__ __forceinline__ double rotate(double v) { return __hiloint2double(rotate<N>(__double2hiint(v)), rotate<N>(__double2loint(v))); }
+template <typename F> __device__ __forceinline__ double wave_of(double v, F &&f) {
+  v = f(v, rotate<8>(v));
+  v = f(v, rotate<4>(v));
+  v = f(v, rotate<2>(v));
+  v = f(v, rotate<1>(v));
+  double r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), 16 * i), __builtin_amdgcn_readlane(__double2loint(v), 16 * i));
+  return f(f(r[0], r[1]), f(r[2], r[3]));
+}
+// The largest of values [v][lane] and its number 64 v + lane, the lowest of equals; -1 where all are -inf.
 struct Best {
   double value;
   int index;
 };
-__device__ __forceinline__ Best wave_best(Best b) {
+template <int V> __device__ __forceinline__ Best wave_best(const double (&value)[V]) {
+  double high = value[0];
 #pragma unroll
-  for (int o = kWave / 2; o; o >>= 1) {
-    const double v = __shfl_xor(b.value, o, kWave);
-    const int i = __shfl_xor(b.index, o, kWave);
-    if (v > b.value || (v == b.value && i < b.index)) b = {v, i};
+  for (int v = 1; v < V; ++v) high = fmax(high, value[v]);
+  Best b = {wave_of(high, [](double x, double y) { return fmax(x, y); }), -1};
+  if (!(b.value > -INFINITY)) return b;
+#pragma unroll
+  for (int v = V - 1; v >= 0; --v) {
+    const uint64_t m = __ballot(value[v] == b.value);
+    if (m) b.index = v * kWave + __builtin_ctzll(m);
   }
   return b;
 }
@@ -291,8 +310,7 @@ template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int ch
     sum = 0.0;
 #pragma unroll
     for (int v = 0; v < V; ++v) sum += exact_score(lg[v], true, top);
-#pragma unroll
-    for (int o = kWave / 2; o; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    sum = wave_of(sum, [](double x, double y) { return x + y; });
   }
 #pragma unroll
   for (int v = 0; v < V; ++v) {
@@ -304,30 +322,31 @@ template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int ch
   }
   if constexpr (GROUPED) {
     const int per = E / a.groups;
-    double mine = kNone;    // lane q: group q's value
+    double worth[1] = {kNone};    // lane q: group q's value
     for (int q = 0; q < a.groups; ++q) {
-      Best one = {kNone, MAX_E}, two = {kNone, MAX_E};
+      double in[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int e = v * kWave + lane;
-        if (e >= q * per && e < (q + 1) * per && order[v] > one.value) one = {order[v], e};
+        in[v] = e >= q * per && e < (q + 1) * per ? order[v] : kNone;
       }
-      one = wave_best(one);
+      const Best one = wave_best(in);
+      double sum_of_two = one.value;
       if (a.best == 2) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const int e = v * kWave + lane;
-          if (e >= q * per && e < (q + 1) * per && e != one.index && order[v] > two.value) two = {order[v], e};
-        }
-        two = wave_best(two);
+        for (int v = 0; v < V; ++v)
+          if (v * kWave + lane == one.index) in[v] = kNone;
+        const Best two = wave_best(in);
+        if (two.index >= 0) sum_of_two += two.value;
       }
-      if (lane == q) mine = two.value > kNone ? one.value + two.value : one.value;
+      if (lane == q) worth[0] = sum_of_two;
     }
     uint64_t keep = 0;
     for (int j = 0; j < a.kept; ++j) {
-      const Best b = wave_best({mine, lane});
-      if (b.value > kNone) keep |= 1ull << b.index;
-      if (lane == b.index) mine = kNone;
+      const Best b = wave_best(worth);
+      if (b.index < 0) break;
+      keep |= 1ull << b.index;
+      if (lane == b.index) worth[0] = kNone;
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -338,15 +357,12 @@ template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int ch
   }
   int chosen = -1;
   for (int j = 0; j < a.k; ++j) {
-    Best b = {kNone, MAX_E};
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (order[v] > b.value) b = {order[v], v * kWave + lane};
-    b = wave_best(b);
+    const Best b = wave_best(order);
+    if (b.index < 0) break;
 #pragma unroll
     for (int v = 0; v < V; ++v)
       if (v * kWave + lane == b.index) order[v] = kNone;
-    if (lane == j && b.value > kNone) chosen = b.index;
+    if (lane == j) chosen = b.index;
   }
   return chosen;
 }
@@ -599,7 +615,13 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
   if (!a.off) return;
   __syncthreads();
   if (gridDim.x > 1) {
-    for (int e = threadIdx.x; e < E; e += threads) a.count[e * runs_ld(gridDim.x) + blockIdx.x] = s_words[e];
+    for (int e = threadIdx.x; e < E; e += threads) {
+      const int at = e * runs_ld(gridDim.x) + blockIdx.x;
+      if (narrow(a.run))
+        static_cast<uint16_t *>(a.count)[at] = (uint16_t)s_words[e];
+      else
+        static_cast<int32_t *>(a.count)[at] = s_words[e];
+    }
     return;
   }
   for (int e = threadIdx.x; e < E; e += threads) {
@@ -609,35 +631,39 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
   places(a, 0, first, last, s_words, s_words + E);
 }
 
-// A wavefront takes an expert's counts, four runs a lane.
+// Sixteen bytes of an expert's counts a lane: LANES lanes have those of all runs, a wavefront takes 64 / LANES experts at a time.  Every workgroup
+// reads all counts, 256 KB of 32 bits for 256 runs and experts, which is what 16 bits are for.
 constexpr int kPlaceThreads = 1024;
-__global__ void __launch_bounds__(kPlaceThreads) k_places(RouteArgs a) {
+template <typename T> __global__ void __launch_bounds__(kPlaceThreads) k_places(RouteArgs a) {
   extern __shared__ int32_t s_words[];
-  static_assert(kMaxRuns == 4 * kWave, "four runs a lane");
+  constexpr int EACH = 16 / sizeof(T), LANES = kMaxRuns / EACH, AT_ONCE = kPlaceThreads / LANES, AHEAD = 8;
+  static_assert(LANES == 32 || LANES == 64, "a part of a wavefront, or all of it");
   const int64_t first = (int64_t)blockIdx.x * a.run, last = min(a.rows, first + a.run);
-  const int E = a.experts, runs = gridDim.x, run = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  constexpr int WAVES = kPlaceThreads / kWave, AHEAD = 8;
-  for (int e0 = wave; e0 < E; e0 += WAVES * AHEAD) {
-    int4 c[AHEAD];
+  const int E = a.experts, runs = gridDim.x, run = blockIdx.x, l = threadIdx.x % LANES;
+  for (int e0 = 0; e0 < E; e0 += AT_ONCE * AHEAD) {
+    uint4 c[AHEAD];
 #pragma unroll
     for (int p = 0; p < AHEAD; ++p) {
-      const int e = e0 + p * WAVES;
-      c[p] = make_int4(0, 0, 0, 0);
-      if (e < E && 4 * lane < runs) c[p] = *reinterpret_cast<const int4 *>(a.count + e * runs_ld(runs) + 4 * lane);
+      const int e = e0 + p * AT_ONCE + threadIdx.x / LANES;
+      c[p] = make_uint4(0u, 0u, 0u, 0u);
+      if (e < E && EACH * l < runs) c[p] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.count) + e * runs_ld(runs) + EACH * l);
     }
 #pragma unroll
     for (int p = 0; p < AHEAD; ++p) {
-      const int e = e0 + p * WAVES, r[4] = {c[p].x, c[p].y, c[p].z, c[p].w};
+      if (e0 + p * AT_ONCE >= E) break;
+      const int e = e0 + p * AT_ONCE + threadIdx.x / LANES;
+      const uint32_t w[4] = {c[p].x, c[p].y, c[p].z, c[p].w};
       int before = 0, all = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (4 * lane + i < runs) all += r[i];
-        if (4 * lane + i < run) before += r[i];
+      for (int i = 0; i < EACH; ++i) {
+        const int n = EACH == 4 ? (int)w[i & 3] : (int)(w[i / 2 & 3] >> (16 * (i & 1)) & 0xffffu);
+        if (EACH * l + i < runs) all += n;
+        if (EACH * l + i < run) before += n;
       }
       auto add = [](int x, int y) { return x + y; };
-      all = team<64>(all, add);
-      before = team<64>(before, add);
-      if (lane == 0 && e < E) s_words[e] = before, s_words[E + e] = all;
+      all = team<LANES>(all, add);
+      before = team<LANES>(before, add);
+      if (l == 0 && e < E) s_words[e] = before, s_words[E + e] = all;
     }
   }
   places(a, run, first, last, s_words, s_words + E);
@@ -802,7 +828,8 @@ using namespace gear;
 
 extern "C" size_t gear_route_workspace_bytes(int64_t rows, int32_t experts, int32_t k, int32_t groups) {
   if (!sizes_ok(rows, experts, k) || groups < 1) return 0;
-  return ((size_t)runs_ld(runs_of(rows, experts, groups > 1).count) * experts * 4 + 255) / 256 * 256;
+  const Runs r = runs_of(rows, experts, groups > 1);
+  return ((size_t)runs_ld(r.count) * experts * (narrow(r.run) ? 2 : 4) + 255) / 256 * 256;
 }
 
 extern "C" gear_status gear_route(const gear_route_args *a, void *workspace, size_t workspace_bytes, void *stream) {
@@ -828,11 +855,15 @@ extern "C" gear_status gear_route(const gear_route_args *a, void *workspace, siz
   }
   hipStream_t s = (hipStream_t)stream;
   const RouteArgs p = {a->rows, a->ld_logits, r.run, a->experts, a->k, a->score == GEAR_SCORE_SOFTMAX, a->groups, a->groups_kept, a->group_best,
-                       a->renormalise != 0, a->scale, a->logits, a->bias, a->n, a->expert, a->weight, a->off, a->place, (int32_t *)workspace};
+                       a->renormalise != 0, a->scale, a->logits, a->bias, a->n, a->expert, a->weight, a->off, a->place, workspace};
   const bool wide = a->experts % 4 == 0 && a->ld_logits % 4 == 0 && ((uintptr_t)a->logits & (4 * size - 1)) == 0;
   hipError_t err = a->dtype == GEAR_F32 ? launch_route_of<float>(p, r, wide, s) : launch_route_of<bf16_t>(p, r, wide, s);
   if (err == hipSuccess && a->off && r.count > 1) {
-    hipLaunchKernelGGL(k_places, dim3(r.count), dim3(kPlaceThreads), (size_t)a->experts * (1 + rankers_of(a->experts)) * 4, s, p);
+    const size_t lds = (size_t)a->experts * (1 + rankers_of(a->experts)) * 4;
+    if (narrow(r.run))
+      hipLaunchKernelGGL(k_places<uint16_t>, dim3(r.count), dim3(kPlaceThreads), lds, s, p);
+    else
+      hipLaunchKernelGGL(k_places<int32_t>, dim3(r.count), dim3(kPlaceThreads), lds, s, p);
     err = hipGetLastError();
   }
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;

@@ -179,7 +179,7 @@ def test_no_rows(g):
     assert g.gear_route_backward(torch.empty(0, 24, device="cuda"), r, torch.empty(0, 3, device="cuda")).shape == (0, 24)
 
 
-@pytest.mark.parametrize("rows,experts,k", [(1025, 7, 3), (5000, 1024, 4), (20_001, 40, 3), (70_000, 256, 1), (300_000, 3, 2), (16_385, 300, 8), (65_536, 64, 2)])
+@pytest.mark.parametrize("rows,experts,k", [(1025, 7, 3), (5000, 1024, 4), (20_001, 40, 3), (70_000, 256, 1), (300_000, 3, 2), (16_385, 300, 8), (65_536, 64, 2), (17_000_000, 3, 1)])
 def test_order_of_many_runs(g, rows, experts, k):
     """The order from the choice, by torch's stable sort."""
     r = gen(rows)
