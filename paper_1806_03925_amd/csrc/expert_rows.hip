@@ -12,89 +12,162 @@
 namespace gear {
 namespace {
 
-// A row belongs to TPR threads, thread t takes pieces t, t + TPR, ... of eight values.
-template <int TPR> struct Team {
-  static constexpr int THREADS = TPR <= kWave ? 256 : TPR, ROWS = THREADS / TPR;
-};
-
 // the place of a pair, -1 where it has none within [0, places)
 __device__ __forceinline__ int64_t place_of(const int32_t *__restrict__ place, int64_t pair, int64_t places) {
   const int p = place[pair];
   return p >= 0 && p < places ? p : -1;
 }
 
+// ---- one thread for eight values of a row -------------------------------------------------------------------------------
+// Threads are numbered through all rows, so that no row's width leaves any of them idle.
+constexpr int kPieceThreads = 256;
+struct Piece {
+  int64_t row;
+  int c;
+};
+// the one of this thread in chunk number `chunk` of kPieceThreads pieces; row >= rows behind the last
+__device__ __forceinline__ Piece piece_of(int64_t chunk, int pieces, float one_over) {
+  const int64_t at = chunk * kPieceThreads, row0 = at / pieces;             // the same in all lanes
+  const int local = (int)(at - row0 * pieces) + (int)threadIdx.x;          // below 2^13 + 2^8: the quotient below is exact
+  const int down = (int)(((float)local + 0.5f) * one_over);
+  return {row0 + down, 8 * (local - down * pieces)};
+}
+
 struct GatherArgs {
   int64_t rows, ld_x, ld_xs;
   int dim, k;
+  float one_over;           // the row's pieces
+  int64_t chunks;
   const void *x;
   const int32_t *place;
   void *xs;
 };
-template <typename T, int TPR> __global__ void __launch_bounds__(Team<TPR>::THREADS) k_gather(GatherArgs a) {
-  const int t = threadIdx.x % TPR;
-  for (int64_t row = (int64_t)blockIdx.x * Team<TPR>::ROWS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * Team<TPR>::ROWS) {
-    const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
-    for (int c = 8 * t; c < a.dim; c += 8 * TPR) {
-      float v[8];
-      load8(x + c, v);
-      for (int j = 0; j < a.k; ++j) {
-        const int64_t p = place_of(a.place, row * a.k + j, a.rows * a.k);
-        if (p >= 0) store8(static_cast<T *>(a.xs) + p * a.ld_xs + c, v);
+template <typename T> __global__ void __launch_bounds__(kPieceThreads) k_gather(GatherArgs a) {
+  for (int64_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+    const Piece t = piece_of(chunk, a.dim / 8, a.one_over);
+    if (t.row >= a.rows) continue;
+    constexpr int PIECES = 8 * (int)sizeof(T) / 16;
+    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.x) + t.row * a.ld_x + t.c);
+    const uint4 lo = src[0], hi = src[PIECES - 1];
+    for (int j0 = 0; j0 < a.k; j0 += 4) {
+      int64_t p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[j] = j0 + j < a.k ? place_of(a.place, t.row * a.k + j0 + j, a.rows * a.k) : -1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (p[j] < 0) continue;
+        uint4 *dst = reinterpret_cast<uint4 *>(static_cast<T *>(a.xs) + p[j] * a.ld_xs + t.c);
+        dst[0] = lo;
+        if constexpr (PIECES > 1) dst[1] = hi;
       }
     }
   }
 }
 
-template <typename T, int TPR> __global__ void __launch_bounds__(Team<TPR>::THREADS) k_combine(gear_expert_combine_args a) {
-  const int t = threadIdx.x % TPR;
-  for (int64_t row = (int64_t)blockIdx.x * Team<TPR>::ROWS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * Team<TPR>::ROWS) {
-    for (int c = 8 * t; c < a.dim; c += 8 * TPR) {
-      float sum[8];
+struct CombineArgs {
+  gear_expert_combine_args a;
+  float one_over;
+  int64_t chunks;
+};
+template <typename T> __global__ void __launch_bounds__(kPieceThreads) k_combine(CombineArgs args) {
+  const gear_expert_combine_args &a = args.a;
+  for (int64_t chunk = blockIdx.x; chunk < args.chunks; chunk += gridDim.x) {
+    const Piece t = piece_of(chunk, a.dim / 8, args.one_over);
+    if (t.row >= a.rows) continue;
+    Raw8<T> res;
+    res.zero();
+    if (a.residual) res.load(static_cast<const T *>(a.residual) + t.row * a.ld_residual + t.c);
+    float sum[8];
+    for (int j0 = 0; j0 < a.k; j0 += 4) {   // four places on their way at a time
+      int64_t p[4];
+      float w[4];
+      Raw8<T> y[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-      if (a.residual) load8(static_cast<const T *>(a.residual) + row * a.ld_residual + c, sum);
-      for (int j = 0; j < a.k; ++j) {
-        const int64_t p = place_of(a.place, row * a.k + j, a.rows * a.k);
-        const float w = a.weight ? a.weight[row * a.k + j] : 1.0f;
+      for (int j = 0; j < 4; ++j) {
+        const int64_t pair = t.row * a.k + j0 + j;
+        const bool in = j0 + j < a.k;
+        p[j] = in ? place_of(a.place, pair, a.rows * a.k) : -1;
+        w[j] = !in ? 0.0f : a.weight ? a.weight[pair] : 1.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        y[j].zero();
+        if (p[j] >= 0) y[j].load(static_cast<const T *>(a.y) + p[j] * a.ld_y + t.c);
+      }
+      if (j0 == 0) res.get(sum);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
         float v[8];
+        y[j].get(v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        if (p >= 0) load8(static_cast<const T *>(a.y) + p * a.ld_y + c, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += w * v[i];
+        for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[j], v[i], sum[i]);
       }
-      store8(static_cast<T *>(a.out) + row * a.ld_out + c, sum);
     }
+    store8(static_cast<T *>(a.out) + t.row * a.ld_out + t.c, sum);
   }
 }
 
-template <typename T, int TPR> __global__ void __launch_bounds__(Team<TPR>::THREADS) k_combine_back(gear_expert_combine_backward_args a) {
+// ---- one team for a row -----------------------------------------------------------------------------------------------
+// A row belongs to TPR threads, with PER pieces of eight values each in registers: piece i of thread t at columns 8 (t + TPR i).
+template <int TPR> struct Team {
+  static constexpr int THREADS = TPR <= kWave ? 256 : TPR, ROWS = THREADS / TPR;
+};
+
+// dout stays in registers while the row's places go by, two at a time.
+template <typename T, int TPR, int PER> __global__ void __launch_bounds__(Team<TPR>::THREADS) k_combine_back(gear_expert_combine_backward_args a) {
   __shared__ float s_part[TPR > kWave ? TPR / kWave : 1];
+  constexpr int AHEAD = PER * sizeof(T) <= 8 ? 2 : 1;
   const int t = threadIdx.x % TPR;
   for (int64_t row0 = (int64_t)blockIdx.x * Team<TPR>::ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * Team<TPR>::ROWS) {
     const int64_t row = row0 + threadIdx.x / TPR;
     if (TPR <= kWave && row >= a.rows) continue;
-    for (int j = 0; j < a.k; ++j) {
-      const int64_t p = place_of(a.place, row * a.k + j, a.rows * a.k);
-      const float w = a.weight[row * a.k + j];
-      float dot = 0.0f;
-      if (p >= 0) {
-        for (int c = 8 * t; c < a.dim; c += 8 * TPR) {
-          float d[8], y[8];
-          load8(static_cast<const T *>(a.dout) + row * a.ld_dout + c, d);
-          if (a.dweight) {
-            load8(static_cast<const T *>(a.y) + p * a.ld_y + c, y);
+    Raw8<T> d[PER];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dot += d[i] * y[i];
-          }
+    for (int i = 0; i < PER; ++i) {
+      const int c = 8 * (t + TPR * i);
+      d[i].zero();
+      if (c < a.dim) d[i].load(static_cast<const T *>(a.dout) + row * a.ld_dout + c);
+    }
+    for (int j0 = 0; j0 < a.k; j0 += AHEAD) {
+      int64_t p[AHEAD];
+      float w[AHEAD];
+      Raw8<T> y[AHEAD][PER];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[i] *= w;
-          if (a.dy) store8(static_cast<T *>(a.dy) + p * a.ld_dy + c, d);
-        }
+      for (int j = 0; j < AHEAD; ++j) {
+        const int64_t pair = row * a.k + j0 + j;
+        const bool in = j0 + j < a.k;
+        p[j] = in ? place_of(a.place, pair, a.rows * a.k) : -1;
+        w[j] = in ? a.weight[pair] : 0.0f;
       }
-      if (a.dweight) {
-        dot = row_sum<TPR>(dot, s_part);
-        if (t == 0) a.dweight[row * a.k + j] = p >= 0 ? dot : 0.0f;
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int c = 8 * (t + TPR * i);
+          y[j][i].zero();
+          if (a.dweight && p[j] >= 0 && c < a.dim) y[j][i].load(static_cast<const T *>(a.y) + p[j] * a.ld_y + c);
+        }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        float dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int c = 8 * (t + TPR * i);
+          float dv[8], yv[8];
+          d[i].get(dv);
+          y[j][i].get(yv);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dot = fmaf(dv[e], yv[e], dot);
+          if (a.dy && p[j] >= 0 && c < a.dim) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dv[e] *= w[j];
+            store8(static_cast<T *>(a.dy) + p[j] * a.ld_dy + c, dv);
+          }
+        }
+        if (a.dweight) {
+          dot = row_sum<TPR>(dot, s_part);
+          if (t == 0 && j0 + j < a.k) a.dweight[row * a.k + j0 + j] = p[j] >= 0 ? dot : 0.0f;   // not 0 * NaN where there is no place
+        }
       }
     }
   }
@@ -115,10 +188,39 @@ constexpr uint32_t kInfinite = 0x7f800000u;
 __device__ __forceinline__ float scale127(uint32_t top) {   // of a row, from the bits of its largest magnitude
   return top >= kInfinite ? NAN : (float)((double)__uint_as_float(top) / 127.0);
 }
-__device__ __forceinline__ uint2 pack_i8(const float (&v)[8], float top) {
-  uint32_t w[2] = {0u, 0u};
+
+// How a row's values become integers: v * factor in fp32, off by less than 127 2^-23, decides where that is not within kTie of a tie; else, or
+// where the factor is no ordinary number, the quotient in fp64 does.
+constexpr float kTie = 0x1p-15f;
+struct Quantise {
+  float top, factor;
+  bool always;            // in fp64
+};
+__device__ __forceinline__ Quantise quantise_of(uint32_t top) {
+  const float t = top >= kInfinite ? 0.0f : __uint_as_float(top);
+  const bool small = t < 0x1p-100f;
+  return {t, small ? 0.0f : 127.0f / t, small && t > 0.0f};
+}
+__device__ __forceinline__ uint2 pack_i8(const float (&v)[8], const Quantise &q) {
+  constexpr float kWhole = 12582912.0f;   // 1.5 2^23: a sum with it is rounded to a whole number, whose last byte is the integer
+  uint32_t m[8];
+  float off = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)nearest127(v[i], top) & 0xffu) << (8 * (i % 4));
+  for (int i = 0; i < 8; ++i) {
+    const float s = fmaf(v[i], q.factor, kWhole);
+    m[i] = __float_as_uint(s);
+    off = fmaxf(off, fabsf(fmaf(v[i], q.factor, kWhole - s)));
+  }
+  if (q.always || !(off < 0.5f - kTie)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = (uint32_t)nearest127(v[i], q.top);
+  }
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {   // the last bytes of four words
+    const uint32_t lo = __builtin_amdgcn_perm(m[4 * h + 1], m[4 * h], 0x0c0c0400u), hi = __builtin_amdgcn_perm(m[4 * h + 3], m[4 * h + 2], 0x0c0c0400u);
+    w[h] = lo | hi << 16;
+  }
   return make_uint2(w[0], w[1]);
 }
 
@@ -143,7 +245,7 @@ struct RowsI8Args {
   int8_t *q;
   float *scale;
 };
-template <typename T, int TPR> __global__ void __launch_bounds__(Team<TPR>::THREADS) k_rows_i8(RowsI8Args a) {
+template <typename T, int TPR, int PER> __global__ void __launch_bounds__(Team<TPR>::THREADS) k_rows_i8(RowsI8Args a) {
   __shared__ uint32_t s_part[TPR > kWave ? TPR / kWave : 1];
   const int t = threadIdx.x % TPR;
   const int64_t ld = rows8_ld(a.dim);
@@ -151,29 +253,40 @@ template <typename T, int TPR> __global__ void __launch_bounds__(Team<TPR>::THRE
     const int64_t row = row0 + threadIdx.x / TPR;
     if (TPR <= kWave && row >= a.rows) continue;
     const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
+    Raw8<T> raw[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = 8 * (t + TPR * i);
+      raw[i].zero();
+      if (c < a.dim) raw[i].load(x + c);
+    }
     uint32_t top = 0u;
-    for (int c = 8 * t; c < a.dim; c += 8 * TPR) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
       float v[8];
-      load8(x + c, v);
+      raw[i].get(v);
       top = top_bits(v, top);
     }
     top = row_max<TPR>(top, s_part);
-    const float largest = top >= kInfinite ? 0.0f : __uint_as_float(top), scale = scale127(top);
-    for (int c = 8 * t; c < ld; c += 8 * TPR) {
-      uint2 q = make_uint2(0u, 0u);
-      if (c < a.dim) {
-        float v[8];
-        load8(x + c, v);
-        q = pack_i8(v, largest);
-      }
-      for (int j = 0; j < a.k; ++j) {
-        const int64_t p = a.place ? place_of(a.place, row * a.k + j, a.rows * a.k) : row;
-        if (p >= 0) *reinterpret_cast<uint2 *>(a.q + p * ld + c) = q;
-      }
+    const Quantise how = quantise_of(top);
+    const bool broken = top >= kInfinite;
+    uint2 q[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      float v[8];
+      raw[i].get(v);
+      q[i] = broken ? make_uint2(0u, 0u) : pack_i8(v, how);
     }
-    for (int j = t; j < a.k; j += TPR) {
+    const float scale = scale127(top);
+    for (int j = 0; j < a.k; ++j) {
       const int64_t p = a.place ? place_of(a.place, row * a.k + j, a.rows * a.k) : row;
-      if (p >= 0) a.scale[p] = scale;
+      if (p < 0) continue;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int c = 8 * (t + TPR * i);
+        if (c < ld) *reinterpret_cast<uint2 *>(a.q + p * ld + c) = q[i];
+      }
+      if (t == 0) a.scale[p] = scale;
     }
   }
 }
@@ -212,8 +325,8 @@ __global__ void __launch_bounds__(256) k_pack_i8(const S *__restrict__ w, int N,
     } else {
       float v[8];
       load8(w + at, v);
-      const float t = top[(int64_t)e * N + n];
-      half[h] = pack_i8(v, finite(t) ? t : 0.0f);
+      const uint32_t t = __float_as_uint(top[(int64_t)e * N + n]);
+      if (t < kInfinite) half[h] = pack_i8(v, quantise_of(t));
     }
   }
   packed[(int64_t)blockIdx.x * 256 + unit * 64 + lane] = make_uint4(half[0].x, half[0].y, half[1].x, half[1].y);
@@ -222,18 +335,30 @@ __global__ void __launch_bounds__(256) k_finish_scales(float *__restrict__ scale
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) scale[i] = scale127(__float_as_uint(scale[i]));
 }
 
-// call(TPR) with the threads that a row of `dim` values has
+// call(TPR, PER) with the threads that a row of `dim` values has, and their pieces: a wavefront up to 4096 columns, which needs no
+// barrier for its sum
 template <typename F> hipError_t by_dim(int64_t dim, F &&call) {
   using std::integral_constant;
   const int64_t pieces = (dim + 7) / 8;
-  if (pieces <= 16) return call(integral_constant<int, 16>{});
-  if (pieces <= 64) return call(integral_constant<int, 64>{});
-  return call(integral_constant<int, 256>{});
+  if (pieces <= 16) return call(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  if (pieces <= 32) return call(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+  if (pieces <= 64) return call(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (pieces <= 128) return call(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  if (pieces <= 192) return call(integral_constant<int, 64>{}, integral_constant<int, 3>{});
+  if (pieces <= 256) return call(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  if (pieces <= 384) return call(integral_constant<int, 64>{}, integral_constant<int, 6>{});
+  if (pieces <= 512) return call(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  if (pieces <= 1024) return call(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  if (pieces <= 2048) return call(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  if (pieces <= 4096) return call(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  return call(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
 }
 template <int TPR> unsigned blocks_of(int64_t rows) {
   const int64_t blocks = (rows + Team<TPR>::ROWS - 1) / Team<TPR>::ROWS;
   return (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
 }
+int64_t chunks_of(int64_t rows, int dim) { return (rows * (dim / 8) + kPieceThreads - 1) / kPieceThreads; }
+unsigned grid_of(int64_t chunks) { return (unsigned)(chunks < (1 << 22) ? chunks : (1 << 22)); }
 
 bool dtype_ok(int32_t dtype) { return dtype == GEAR_F32 || dtype == GEAR_BF16; }
 bool matrix_ok(const void *p, int64_t ld, int64_t dim) { return p && !((uintptr_t)p & 15) && ld >= dim && ld % 8 == 0 && ld < (1 << 20); }
@@ -255,16 +380,12 @@ extern "C" gear_status gear_expert_gather(const void *x, int32_t dtype, int64_t 
   if (!sizes_ok(rows, dim, k) || !dtype_ok(dtype)) return GEAR_ERR_INVALID;
   if (rows == 0) return GEAR_OK;
   if (!matrix_ok(x, ld_x, dim) || !matrix_ok(xs, ld_xs, dim) || !words_ok(place)) return GEAR_ERR_INVALID;
-  const GatherArgs a = {rows, ld_x, ld_xs, dim, k, x, place, xs};
-  const hipError_t err = by_dim(dim, [&](auto tpr) {
-    constexpr int TPR = decltype(tpr)::value;
-    if (dtype == GEAR_F32)
-      hipLaunchKernelGGL((k_gather<float, TPR>), dim3(blocks_of<TPR>(rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, a);
-    else
-      hipLaunchKernelGGL((k_gather<bf16_t, TPR>), dim3(blocks_of<TPR>(rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, a);
-    return hipGetLastError();
-  });
-  return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
+  const GatherArgs a = {rows, ld_x, ld_xs, dim, k, 8.0f / (float)dim, chunks_of(rows, dim), x, place, xs};
+  if (dtype == GEAR_F32)
+    hipLaunchKernelGGL(k_gather<float>, dim3(grid_of(a.chunks)), dim3(kPieceThreads), 0, (hipStream_t)stream, a);
+  else
+    hipLaunchKernelGGL(k_gather<bf16_t>, dim3(grid_of(a.chunks)), dim3(kPieceThreads), 0, (hipStream_t)stream, a);
+  return hipGetLastError() == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
 }
 
 extern "C" gear_status gear_expert_combine(const gear_expert_combine_args *a, void *stream) {
@@ -273,15 +394,12 @@ extern "C" gear_status gear_expert_combine(const gear_expert_combine_args *a, vo
   if (!matrix_ok(a->y, a->ld_y, a->dim) || !matrix_ok(a->out, a->ld_out, a->dim) || !words_ok(a->place) || ((uintptr_t)a->weight & 3))
     return GEAR_ERR_INVALID;
   if (a->residual && !matrix_ok(a->residual, a->ld_residual, a->dim)) return GEAR_ERR_INVALID;
-  const hipError_t err = by_dim(a->dim, [&](auto tpr) {
-    constexpr int TPR = decltype(tpr)::value;
-    if (a->dtype == GEAR_F32)
-      hipLaunchKernelGGL((k_combine<float, TPR>), dim3(blocks_of<TPR>(a->rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, *a);
-    else
-      hipLaunchKernelGGL((k_combine<bf16_t, TPR>), dim3(blocks_of<TPR>(a->rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, *a);
-    return hipGetLastError();
-  });
-  return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
+  const CombineArgs args = {*a, 8.0f / (float)a->dim, chunks_of(a->rows, a->dim)};
+  if (a->dtype == GEAR_F32)
+    hipLaunchKernelGGL(k_combine<float>, dim3(grid_of(args.chunks)), dim3(kPieceThreads), 0, (hipStream_t)stream, args);
+  else
+    hipLaunchKernelGGL(k_combine<bf16_t>, dim3(grid_of(args.chunks)), dim3(kPieceThreads), 0, (hipStream_t)stream, args);
+  return hipGetLastError() == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
 }
 
 extern "C" gear_status gear_expert_combine_backward(const gear_expert_combine_backward_args *a, void *stream) {
@@ -290,12 +408,12 @@ extern "C" gear_status gear_expert_combine_backward(const gear_expert_combine_ba
   if (!a->dy && !a->dweight) return GEAR_ERR_INVALID;
   if (!matrix_ok(a->dout, a->ld_dout, a->dim) || !words_ok(a->place) || !words_ok(a->weight) || ((uintptr_t)a->dweight & 3)) return GEAR_ERR_INVALID;
   if ((a->dweight && !matrix_ok(a->y, a->ld_y, a->dim)) || (a->dy && !matrix_ok(a->dy, a->ld_dy, a->dim))) return GEAR_ERR_INVALID;
-  const hipError_t err = by_dim(a->dim, [&](auto tpr) {
-    constexpr int TPR = decltype(tpr)::value;
+  const hipError_t err = by_dim(a->dim, [&](auto tpr, auto per) {
+    constexpr int TPR = decltype(tpr)::value, PER = decltype(per)::value;
     if (a->dtype == GEAR_F32)
-      hipLaunchKernelGGL((k_combine_back<float, TPR>), dim3(blocks_of<TPR>(a->rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, *a);
+      hipLaunchKernelGGL((k_combine_back<float, TPR, PER>), dim3(blocks_of<TPR>(a->rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, *a);
     else
-      hipLaunchKernelGGL((k_combine_back<bf16_t, TPR>), dim3(blocks_of<TPR>(a->rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, *a);
+      hipLaunchKernelGGL((k_combine_back<bf16_t, TPR, PER>), dim3(blocks_of<TPR>(a->rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, *a);
     return hipGetLastError();
   });
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
@@ -307,12 +425,12 @@ extern "C" gear_status gear_rows_i8(const void *x, int32_t dtype, int64_t ld_x, 
   if (rows == 0) return GEAR_OK;
   if (!matrix_ok(x, ld_x, dim) || ((uintptr_t)place & 3) || !q || ((uintptr_t)q & 15) || !words_ok(scale)) return GEAR_ERR_INVALID;
   const RowsI8Args a = {rows, ld_x, dim, k, x, place, q, scale};
-  const hipError_t err = by_dim(dim, [&](auto tpr) {
-    constexpr int TPR = decltype(tpr)::value;
+  const hipError_t err = by_dim(dim, [&](auto tpr, auto per) {
+    constexpr int TPR = decltype(tpr)::value, PER = decltype(per)::value;
     if (dtype == GEAR_F32)
-      hipLaunchKernelGGL((k_rows_i8<float, TPR>), dim3(blocks_of<TPR>(rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, a);
+      hipLaunchKernelGGL((k_rows_i8<float, TPR, PER>), dim3(blocks_of<TPR>(rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, a);
     else
-      hipLaunchKernelGGL((k_rows_i8<bf16_t, TPR>), dim3(blocks_of<TPR>(rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, a);
+      hipLaunchKernelGGL((k_rows_i8<bf16_t, TPR, PER>), dim3(blocks_of<TPR>(rows)), dim3(Team<TPR>::THREADS), 0, (hipStream_t)stream, a);
     return hipGetLastError();
   });
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
