@@ -103,7 +103,7 @@ template <typename T> __global__ void __launch_bounds__(kPieceThreads) k_combine
         for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[j], v[i], sum[i]);
       }
     }
-    store8(static_cast<T *>(a.out) + t.row * a.ld_out + t.c, sum);
+    stream8(static_cast<T *>(a.out) + t.row * a.ld_out + t.c, sum);
   }
 }
 
@@ -161,7 +161,7 @@ template <typename T, int TPR, int PER> __global__ void __launch_bounds__(Team<T
           if (a.dy && p[j] >= 0 && c < a.dim) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) dv[e] *= w[j];
-            store8(static_cast<T *>(a.dy) + p[j] * a.ld_dy + c, dv);
+            stream8(static_cast<T *>(a.dy) + p[j] * a.ld_dy + c, dv);
           }
         }
         if (a.dweight) {
