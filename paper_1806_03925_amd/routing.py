@@ -38,15 +38,15 @@ class Route:
         self.p_expert, self.p_weight, self.p_place, self.p_off = (t.data_ptr() for t in (expert, weight, place, off))
 
     @staticmethod
-    def _empty(rows: int, k: int, experts: int, gpu: int) -> "Route":
-        """One allocation for all four; the tensors are made when somebody asks for them."""
+    def _empty(rows: int, k: int, experts: int, gpu: int, more: int) -> "Route":
+        """One allocation for all four, and `more` bytes behind them on 256 bytes; the tensors are made when somebody asks for them."""
         r = object.__new__(Route)
         r.rows, r.k, r.experts, r.gpu = rows, k, experts, gpu
         r._expert = r._weight = r._place = r._off = None
-        r._room = torch.empty(3 * rows * k + experts + 1, dtype=torch.int32, device=gpu)
-        r.p_expert = r._room.data_ptr()
+        r._room = room = torch.empty((3 * rows * k + experts + 64 & -64) + more // 4, dtype=torch.int32, device=gpu)
+        r.p_expert = p = room.data_ptr()
         step = 4 * rows * k
-        r.p_weight, r.p_place, r.p_off = r.p_expert + step, r.p_expert + 2 * step, r.p_expert + 3 * step
+        r.p_weight, r.p_place, r.p_off = p + step, p + 2 * step, p + 3 * step
         return r
 
     def _part(self, i: int) -> torch.Tensor:
@@ -106,11 +106,10 @@ def gear_route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optio
     size = lib.gear_route_workspace_bytes(rows, experts, k, groups)
     if size == 0:
         _refuse(where, f"{k} of {experts} experts in {groups} groups for {rows} rows")
-    r = Route._empty(rows, k, experts, gpu)
-    ws = torch.empty(size, dtype=torch.uint8, device=gpu)
+    r = Route._empty(rows, k, experts, gpu, size)
     a = gear_route_args(rows, experts, k, _CODE[logits.dtype], code, groups, groups_kept, group_best, 1 if renormalise else 0, scale,
                         logits.data_ptr(), ld, bias, n, r.p_expert, r.p_weight, r.p_off, r.p_place)
-    status = lib.gear_route(C.byref(a), ws.data_ptr(), size, _raw_stream(gpu))
+    status = lib.gear_route(C.byref(a), r.p_off + 4 * experts + 259 & -256, size, _raw_stream(gpu))
     if status:
         _check(status, where)
     return r
@@ -145,17 +144,18 @@ def gear_route_backward(logits: torch.Tensor, route: Route, dweight: torch.Tenso
 
 
 def _of_route(t: torch.Tensor, route: Route, rows: int, where: str, name: str, dtype=None, dim: Optional[int] = None) -> int:
-    """Checks a matrix of `rows` rows on the route's GPU, the current one."""
-    ld = _matrix(t, _gpu(route.gpu, where, "the route"), where, name, dtype)
-    if t.shape[0] != rows or (dim is not None and t.shape[1] != dim):
-        _refuse(where, f"{name} has to be {(rows, dim if dim is not None else t.shape[1])}, not {tuple(t.shape)}")
-    return ld
+    """Checks a matrix of `rows` rows on the route's GPU, and returns the distance between its rows."""
+    size = t.shape
+    if len(size) == 2 and (size[0] != rows or (dim is not None and size[1] != dim)):
+        _refuse(where, f"{name} has to be {(rows, dim if dim is not None else size[1])}, not {tuple(size)}")
+    return _matrix(t, route.gpu, where, name, dtype)
 
 
 def gear_expert_gather(x: torch.Tensor, route: Route, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows x dim] copied to every place that the route gives its rows: [rows * k x dim] for gear_expert_matmul with route.off.  Rows
     from route.off[experts] on are not written.  Its gradient is gear_expert_combine(dxs, route, weighted=False)."""
     where = "gear_expert_gather"
+    _gpu(route.gpu, where, "the route")
     ld = _of_route(x, route, route.rows, where, "x")
     dim, places = x.shape[1], route.rows * route.k
     if out is None:
@@ -174,6 +174,7 @@ def gear_expert_combine(y: torch.Tensor, route: Route, weighted: bool = True, re
     """The way back: residual + the sum of the rows' places in y [rows * k x dim], each times its weight (weighted=False: 1).  out
     may be residual itself."""
     where = "gear_expert_combine"
+    _gpu(route.gpu, where, "the route")
     rows, places = route.rows, route.rows * route.k
     ld_y = _of_route(y, route, places, where, "y")
     dtype, dim = y.dtype, y.shape[1]
@@ -197,6 +198,7 @@ def gear_expert_combine_backward(dout: torch.Tensor, y: torch.Tensor, route: Rou
     """(dy, dweight) of gear_expert_combine with weights: dy [rows * k x dim], of which rows from route.off[experts] on are not
     written (dy may be y itself), and dweight [rows x k] (float32).  The residual's gradient is dout."""
     where = "gear_expert_combine_backward"
+    _gpu(route.gpu, where, "the route")
     rows, places = route.rows, route.rows * route.k
     ld_dout = _of_route(dout, route, rows, where, "dout")
     dtype, dim = dout.dtype, dout.shape[1]
@@ -278,6 +280,7 @@ def gear_rows_i8(x: torch.Tensor, out: Optional[RowsI8] = None) -> RowsI8:
 def gear_expert_gather_i8(x: torch.Tensor, route: Route, out: Optional[RowsI8] = None) -> RowsI8:
     """gear_expert_gather and gear_rows_i8 in one: rows from route.off[experts] on are not written."""
     where = "gear_expert_gather_i8"
+    _gpu(route.gpu, where, "the route")
     ld = _of_route(x, route, route.rows, where, "x")
     return _rows_i8(x, ld, route.rows, route.p_place, route.k, out, route.gpu, where)
 
