@@ -26,7 +26,7 @@ namespace gear {
 namespace {
 
 constexpr int kMaxRuns = 256;        // one for each CU
-constexpr int kRouteThreads = 1024, kGroupedThreads = 512;   // at most
+constexpr int threads_of(int v, bool grouped) { return grouped || v > 16 ? 512 : 1024; }   // of a workgroup, at most: what its registers allow
 constexpr int kMaxGroups = GEAR_MAX_GROUPS;
 
 struct RouteArgs {
@@ -47,16 +47,24 @@ __host__ __device__ constexpr int runs_ld(int runs) { return (runs + 7) / 8 * 8;
 __host__ __device__ constexpr bool narrow(int run) { return run <= 0xffff; }   // an expert is chosen once a row
 
 // ---- over a team: every lane gets the result, and every lane of the wavefront takes part -------------------------------
-template <int N> __device__ __forceinline__ int rotate(int v) { return __builtin_amdgcn_mov_dpp(v, 0x120 + N, 0xf, 0xf, true); }   // in 16 lanes
-template <int N> __device__ __forceinline__ float rotate(float v) { return __int_as_float(rotate<N>(__float_as_int(v))); }
-template <int LPR, typename V, typename F> __device__ __forceinline__ V team(V v, F &&f) {
-  v = f(v, rotate<8>(v));
-  v = f(v, rotate<4>(v));
-  v = f(v, rotate<2>(v));
-  v = f(v, rotate<1>(v));
-  if constexpr (LPR > 16) v = f(v, __shfl_xor(v, 16, kWave));
-  if constexpr (LPR > 32) v = f(v, __shfl_xor(v, 32, kWave));
-  return v;
+template <int CTRL> __device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
+// The other half of a group of 2 << STEP lanes, in some order: what it holds is the same in all of its lanes.
+template <int STEP> __device__ __forceinline__ int across(int v) {
+  if constexpr (STEP == 0) return moved<0xb1>(v);         // lanes 1 0 3 2
+  if constexpr (STEP == 1) return moved<0x4e>(v);         // lanes 2 3 0 1
+  if constexpr (STEP == 2) return moved<0x141>(v);        // eight lanes backwards
+  if constexpr (STEP == 3) return moved<0x140>(v);        // sixteen
+  return __shfl_xor(v, 1 << STEP, kWave);
+}
+template <int STEP> __device__ __forceinline__ float across(float v) { return __int_as_float(across<STEP>(__float_as_int(v))); }
+template <int STEP> __device__ __forceinline__ double across(double v) {
+  return __hiloint2double(across<STEP>(__double2hiint(v)), across<STEP>(__double2loint(v)));
+}
+template <int LPR, int STEP = 0, typename V, typename F> __device__ __forceinline__ V team(V v, F &&f) {
+  if constexpr ((1 << STEP) < LPR)
+    return team<LPR, STEP + 1>(f(v, across<STEP>(v)), f);
+  else
+    return v;
 }
 template <int LPR> __device__ __forceinline__ float team_max(float v) {
   return team<LPR>(v, [](float x, float y) { return fmaxf(x, y); });
@@ -77,13 +85,9 @@ template <int LPR> __device__ __forceinline__ uint64_t team_ballot(bool v) {   /
 }
 template <int LPR> __device__ __forceinline__ bool team_any(bool v) { return team_ballot<LPR>(v) != 0; }
 
-// over a wavefront, in fp64: within 16 lanes by rotations, then the four
-template <int N> __device__ __forceinline__ double rotate(double v) { return __hiloint2double(rotate<N>(__double2hiint(v)), rotate<N>(__double2loint(v))); }
+// over a wavefront, in fp64: within 16 lanes, then the four
 template <typename F> __device__ __forceinline__ double wave_of(double v, F &&f) {
-  v = f(v, rotate<8>(v));
-  v = f(v, rotate<4>(v));
-  v = f(v, rotate<2>(v));
-  v = f(v, rotate<1>(v));
+  v = team<16>(v, f);
   double r[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -144,16 +148,6 @@ __device__ __forceinline__ int number_of(float v, float bound, float steps, int 
   return (int)fmaxf(fmaf(v - bound, steps, 1.0f), 0.0f) << kTagBits | (kTag - expert);
 }
 
-template <int CTRL> __device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
-// the other half of a group of 2 << STEP lanes, in some order: what it holds is the same in all of its lanes
-template <int STEP> __device__ __forceinline__ int across(int v) {
-  if constexpr (STEP == 0) return moved<0xb1>(v);         // lanes 1 0 3 2
-  if constexpr (STEP == 1) return moved<0x4e>(v);         // lanes 2 3 0 1
-  if constexpr (STEP == 2) return moved<0x141>(v);        // eight lanes backwards
-  if constexpr (STEP == 3) return moved<0x140>(v);        // sixteen
-  return __shfl_xor(v, 1 << STEP, kWave);
-}
-
 // descending, by odd-even merges
 template <int V> struct Sorter {
   template <int I, int J> static __device__ __forceinline__ void exchange(int (&k)[V]) {
@@ -211,17 +205,37 @@ template <int STEP, int LPR> __device__ __forceinline__ void merge_lists(int (&m
 }
 
 // ---- order of the pairs -------------------------------------------------------------------------------------------
-// Places of the pairs of rows [first, last), those of run number `run`.  On entry s_wave[e] is the number of expert e's pairs in all
-// runs and s_base[e] that in the runs before this one.  s_base, s_wave: experts and rankers x experts words of LDS.
+// A wavefront's pairs, one behind the other, 64 at a time, four times 64 requested together; kept between counting and placing where these are all.
 __host__ __device__ constexpr int rankers_of(int experts) { return experts <= 512 ? 16 : 8; }   // wavefronts that rank: their counts fit in LDS
+__host__ __device__ constexpr int place_words(int experts) { return experts * (2 + rankers_of(experts)); }   // of LDS
+struct Slice {
+  static constexpr int AHEAD = 4, STEP = AHEAD * kWave;
+  int64_t begin, end;
+  int e[AHEAD];
+  __device__ __forceinline__ Slice(const RouteArgs &a, int64_t first, int64_t last) {
+    const int wave = threadIdx.x / kWave, waves = min((int)blockDim.x / kWave, rankers_of(a.experts));
+    const int64_t pairs = (last - first) * a.k, per = (pairs + waves - 1) / waves;
+    begin = first * a.k + min(wave * per, pairs);
+    end = wave < waves ? first * a.k + min((wave + 1) * per, pairs) : begin;
+  }
+  __device__ __forceinline__ void request(const RouteArgs &a, int64_t i0) {
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      const int64_t i = i0 + p * kWave + (threadIdx.x & 63);
+      e[p] = i < end ? a.expert[i] : -1;
+    }
+  }
+};
 
-__device__ __forceinline__ void places(const RouteArgs &a, int run, int64_t first, int64_t last, int32_t *s_base, int32_t *s_wave) {
+// Places of the pairs of rows [first, last), those of run number `run`; `slice`'s first pairs are requested.  On entry s_all[e] is the number of expert e's
+// pairs in all runs and s_base[e] that in the runs before this one; s_wave [rankers x experts] is zero.
+__device__ __forceinline__ void places(const RouteArgs &a, int run, Slice &slice, int32_t *s_base, int32_t *s_all, int32_t *s_wave) {
   const int threads = blockDim.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E = a.experts, waves = min(threads / kWave, rankers_of(E));
   __syncthreads();
   if (wave == 0) {   // where each expert begins
     int begin = 0;
     for (int e0 = 0; e0 < E; e0 += kWave) {
-      const int e = e0 + lane, mine = e < E ? s_wave[e] : 0;
+      const int e = e0 + lane, mine = e < E ? s_all[e] : 0;
       int upto = mine;
 #pragma unroll
       for (int o = 1; o < kWave; o <<= 1) {
@@ -236,28 +250,12 @@ __device__ __forceinline__ void places(const RouteArgs &a, int run, int64_t firs
     }
     if (run == 0 && lane == 0) a.off[E] = begin;
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < waves * E; i += threads) s_wave[i] = 0;
-  __syncthreads();
-  // a wavefront's pairs one behind the other, 64 at a time, four times 64 requested together: first it counts, then it places
-  constexpr int AHEAD = 4;
-  const int64_t pairs = (last - first) * a.k, per = (pairs + waves - 1) / waves;
-  const int64_t begin = first * a.k + min(wave * per, pairs);
-  const int64_t end = wave < waves ? first * a.k + min((wave + 1) * per, pairs) : begin;
   int32_t *mine = s_wave + min(wave, waves - 1) * E;
-  int e[AHEAD];
-  auto request = [&](int64_t i0) {
+  for (int64_t i0 = slice.begin; i0 < slice.end; i0 += Slice::STEP) {
+    if (i0 > slice.begin) slice.request(a, i0);
 #pragma unroll
-    for (int p = 0; p < AHEAD; ++p) {
-      const int64_t i = i0 + p * kWave + lane;
-      e[p] = i < end ? a.expert[i] : -1;
-    }
-  };
-  for (int64_t i0 = begin; i0 < end; i0 += AHEAD * kWave) {
-    request(i0);
-#pragma unroll
-    for (int p = 0; p < AHEAD; ++p)
-      if (e[p] >= 0) atomicAdd(mine + e[p], 1);
+    for (int p = 0; p < Slice::AHEAD; ++p)
+      if (slice.e[p] >= 0) atomicAdd(mine + slice.e[p], 1);
   }
   __syncthreads();
   for (int x = threadIdx.x; x < E; x += threads) {
@@ -274,23 +272,24 @@ __device__ __forceinline__ void places(const RouteArgs &a, int run, int64_t firs
   __syncthreads();
   int bits = 0;
   while ((1 << bits) < E) ++bits;
-  for (int64_t i0 = begin; i0 < end; i0 += AHEAD * kWave) {
-    if (end - begin > AHEAD * kWave) request(i0);   // else they are still there
+  for (int64_t i0 = slice.begin; i0 < slice.end; i0 += Slice::STEP) {
+    if (slice.end - slice.begin > Slice::STEP) slice.request(a, i0);
 #pragma unroll
-    for (int p = 0; p < AHEAD; ++p) {
+    for (int p = 0; p < Slice::AHEAD; ++p) {
       const int64_t i = i0 + p * kWave + lane;
-      if (i0 + p * kWave >= end) break;
-      uint64_t same = __ballot(e[p] >= 0);   // lanes of the same expert
+      if (i0 + p * kWave >= slice.end) break;
+      const int e = slice.e[p];
+      uint64_t same = __ballot(e >= 0);   // lanes of the same expert
       for (int b = 0; b < bits; ++b) {
-        const uint64_t set = __ballot((e[p] >> b) & 1);
-        same &= (e[p] >> b) & 1 ? set : ~set;
+        const uint64_t set = __ballot((e >> b) & 1);
+        same &= (e >> b) & 1 ? set : ~set;
       }
       const int rank = __popcll(same & ((1ull << lane) - 1));
       int at = -1;
-      if (e[p] >= 0) at = mine[e[p]] + rank;
+      if (e >= 0) at = mine[e] + rank;
       asm volatile("" ::: "memory");   // every lane has read before one adds
-      if (e[p] >= 0 && rank == 0) mine[e[p]] += __popcll(same);
-      if (i < end) a.place[i] = at;
+      if (e >= 0 && rank == 0) mine[e] += __popcll(same);
+      if (i < slice.end) a.place[i] = at;
     }
   }
 }
@@ -368,12 +367,12 @@ template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int ch
 }
 
 template <typename T, int LPR, int V, bool WIDE, bool GROUPED, bool FEW>   // FEW: k is at most kList
-__global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_route(RouteArgs a) {
+__global__ void __launch_bounds__(threads_of(V, GROUPED)) k_route(RouteArgs a) {
   constexpr int MAX_E = LPR * V, SLOTS = !FEW && LPR < GEAR_MAX_CHOSEN ? GEAR_MAX_CHOSEN / LPR : 1;   // of a lane
   static_assert(!WIDE || V % 4 == 0, "four neighbouring logits a load");
   static_assert(GEAR_MAX_EXPERTS <= 1024 && LPR >= kList, "a tag's bits; a lane for each of a list");
   extern __shared__ int32_t s_words[];                          // [experts] counts, then what places() needs
-  __shared__ float s_value[GROUPED ? kGroupedThreads * V : 1];
+  __shared__ float s_value[GROUPED ? threads_of(V, true) * V : 1];
   const int threads = blockDim.x, teams = threads / LPR;
   const int l = threadIdx.x % LPR, my_team = threadIdx.x / LPR, lane0_of_mine = threadIdx.x & 63 & ~(LPR - 1), E = a.experts;
   for (int e = threadIdx.x; e < E; e += threads) s_words[e] = 0;
@@ -510,16 +509,17 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
     float high = -INFINITY;
 #pragma unroll
     for (int v = 0; v < V; ++v) high = fmaxf(high, value[v]);
-    // Every lane's largest is at least the bound: LPR values are, 16 at least, more than the k + 1 that a list of eight is about.  Where a lane
-    // has none, or k is larger, nobody eligible lies below the bound.
+    // Every lane's largest is at least the bound: LPR values are.  Where these are no more than the k + 1 that matter, or a lane has none, nobody
+    // eligible lies below the bound.
+    constexpr bool ENOUGH = FEW && LPR > kList;
     float bound = team_min<LPR>(high);
     high = team_max<LPR>(high);
-    if (!FEW || __any(!(bound > -INFINITY))) {
+    if (!ENOUGH || __any(!(bound > -INFINITY))) {
       float low = INFINITY;
 #pragma unroll
       for (int v = 0; v < V; ++v) low = fminf(low, value[v] > -INFINITY ? value[v] : INFINITY);
       low = team_min<LPR>(low);
-      if (!FEW || !(bound > -INFINITY)) bound = low;
+      if (!ENOUGH || !(bound > -INFINITY)) bound = low;
     }
     const float range = high - bound, steps = fminf(kSteps / range, 0x1p127f);   // range 0: those below are still below 1
     int number[V];
@@ -628,7 +628,10 @@ __global__ void __launch_bounds__(GROUPED ? kGroupedThreads : kRouteThreads) k_r
     s_words[E + e] = s_words[e];
     s_words[e] = 0;
   }
-  places(a, 0, first, last, s_words, s_words + E);
+  for (int i = threadIdx.x; i < rankers_of(E) * E; i += threads) s_words[2 * E + i] = 0;
+  Slice slice(a, first, last);
+  slice.request(a, slice.begin);
+  places(a, 0, slice, s_words, s_words + E, s_words + 2 * E);
 }
 
 // Sixteen bytes of an expert's counts a lane: LANES lanes have those of all runs, a wavefront takes 64 / LANES experts at a time.  Every workgroup
@@ -640,6 +643,9 @@ template <typename T> __global__ void __launch_bounds__(kPlaceThreads) k_places(
   static_assert(LANES == 32 || LANES == 64, "a part of a wavefront, or all of it");
   const int64_t first = (int64_t)blockIdx.x * a.run, last = min(a.rows, first + a.run);
   const int E = a.experts, runs = gridDim.x, run = blockIdx.x, l = threadIdx.x % LANES;
+  Slice slice(a, first, last);
+  slice.request(a, slice.begin);
+  for (int i = threadIdx.x; i < rankers_of(E) * E; i += kPlaceThreads) s_words[2 * E + i] = 0;
   for (int e0 = 0; e0 < E; e0 += AT_ONCE * AHEAD) {
     uint4 c[AHEAD];
 #pragma unroll
@@ -666,7 +672,7 @@ template <typename T> __global__ void __launch_bounds__(kPlaceThreads) k_places(
       if (l == 0 && e < E) s_words[e] = before, s_words[E + e] = all;
     }
   }
-  places(a, run, first, last, s_words, s_words + E);
+  places(a, run, slice, s_words, s_words + E, s_words + 2 * E);
 }
 
 // ---- gradient -----------------------------------------------------------------------------------------------------
@@ -767,27 +773,39 @@ template <typename T, int LPR, int V, bool WIDE> __global__ void __launch_bounds
   }
 }
 
-// lanes of a row and logits of a lane: call(LPR, V) for `experts`
-template <typename F> hipError_t by_experts(int experts, F &&call) {
-  using std::integral_constant;
-  if (experts <= 64) return call(integral_constant<int, 16>{}, integral_constant<int, 4>{});
-  if (experts <= 128) return call(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-  if (experts <= 256) return call(integral_constant<int, 16>{}, integral_constant<int, 16>{});
-  if (experts <= 512) return call(integral_constant<int, 32>{}, integral_constant<int, 16>{});
-  return call(integral_constant<int, 64>{}, integral_constant<int, 16>{});
-}
-
-struct Runs {
-  int run, count, threads;
+// Lanes of a row and logits of a lane.  Half as many lanes for twice as many logits where there are rows for all of them: what is done once for every
+// four rows of a wavefront is then done for eight.  us with k = 8, eight lanes / sixteen: 65536 rows of 64 experts 19.5 / 23.9, of 160 with a bias 41 / 47,
+// of 256 37.0 / 39.9 and with a bias 44.5 / 50.0; not for 65 to 128 experts, whose registers spill (35.3 / 33.8), nor for fewer rows (16384 of 64 12.5 / 12.5).
+constexpr int kManyRows = 32768;
+struct Shape {
+  int lpr, v, threads, run, runs;
 };
-// Runs of rows: as many as there are CUs at most, of whole passes of a workgroup over its rows; a batch that fits in one has no more threads
-// than its rows need (one row of 64: 9.1 us by 1024 threads).
-Runs runs_of(int64_t rows, int experts, bool grouped) {
-  const int lpr = experts <= 256 ? 16 : experts <= 512 ? 32 : 64, most = grouped ? kGroupedThreads : kRouteThreads, teams = most / lpr;
-  const int64_t passes = (rows + teams - 1) / teams, each = (passes + kMaxRuns - 1) / kMaxRuns;
-  const int64_t run = (each > 0 ? each : 1) * teams;
-  const int threads = rows >= teams ? most : rows > 0 ? (int)((rows * lpr + kWave - 1) / kWave * kWave) : kWave;
-  return {(int)run, (int)(rows > 0 ? (rows + run - 1) / run : 1), threads};
+Shape shape_of(int64_t rows, int experts, int k, bool grouped) {
+  Shape s;
+  s.lpr = experts <= 256 ? 16 : experts <= 512 ? 32 : 64;
+  if (!grouped && k <= kList && rows >= kManyRows && (experts <= 64 || (experts > 128 && experts <= 256))) s.lpr = 8;
+  s.v = 4;
+  while (s.lpr * s.v < experts) s.v *= 2;
+  if (s.lpr > 16) s.v = 16;
+  // runs of rows: as many as there are CUs at most, of whole passes of a workgroup over its rows; a batch that fits in one has no more threads than
+  // its rows need (one row of 64 experts: 6.0 us by 64 threads, 9.1 by 1024)
+  s.threads = threads_of(s.v, grouped);
+  const int teams = s.threads / s.lpr;
+  const int64_t passes = (rows + teams - 1) / teams, each = (passes + kMaxRuns - 1) / kMaxRuns, run = (each > 0 ? each : 1) * teams;
+  s.run = (int)run;
+  s.runs = (int)(rows > 0 ? (rows + run - 1) / run : 1);
+  if (rows < teams) s.threads = rows > 0 ? (int)((rows * s.lpr + kWave - 1) / kWave * kWave) : kWave;
+  return s;
+}
+// call(LPR, V) for a shape
+template <typename F> hipError_t with_shape(const Shape &s, F &&call) {
+  using std::integral_constant;
+#define GEAR_SHAPE(L, W) \
+  if (s.lpr == L && s.v == W) return call(integral_constant<int, L>{}, integral_constant<int, W>{});
+  GEAR_SHAPE(8, 4) GEAR_SHAPE(8, 8) GEAR_SHAPE(8, 32)
+  GEAR_SHAPE(16, 4) GEAR_SHAPE(16, 8) GEAR_SHAPE(16, 16) GEAR_SHAPE(32, 16) GEAR_SHAPE(64, 16)
+#undef GEAR_SHAPE
+  return hipErrorInvalidValue;
 }
 
 bool sizes_ok(int64_t rows, int32_t experts, int32_t k) {
@@ -795,29 +813,38 @@ bool sizes_ok(int64_t rows, int32_t experts, int32_t k) {
          rows * k <= (1 << 30);
 }
 
-template <typename T, bool WIDE, bool GROUPED> hipError_t launch_route(const RouteArgs &a, const Runs &runs, hipStream_t s) {
-  return by_experts(a.experts, [&](auto lpr, auto v) {
-    const size_t lds = (size_t)a.experts * (1 + (runs.count == 1 ? rankers_of(a.experts) : 0)) * 4;
+template <typename T, bool WIDE, bool GROUPED> hipError_t launch_route(const RouteArgs &a, const Shape &shape, hipStream_t s) {
+  return with_shape(shape, [&](auto lpr, auto v) {
     constexpr int LPR = decltype(lpr)::value, V = decltype(v)::value;
-    if (a.k <= kList)
-      hipLaunchKernelGGL((k_route<T, LPR, V, WIDE, GROUPED, true>), dim3(runs.count), dim3(runs.threads), lds, s, a);
+    const size_t lds = (size_t)(shape.runs == 1 ? place_words(a.experts) : a.experts) * 4;
+    const dim3 grid(shape.runs), block(shape.threads);
+    if constexpr (LPR == 8 && GROUPED)
+      return hipErrorInvalidValue;     // shape_of gives no such shape
+    else if (a.k <= kList)
+      hipLaunchKernelGGL((k_route<T, LPR, V, WIDE, GROUPED, true>), grid, block, lds, s, a);
+    else if constexpr (LPR == 8)
+      return hipErrorInvalidValue;
     else
-      hipLaunchKernelGGL((k_route<T, LPR, V, WIDE, GROUPED, false>), dim3(runs.count), dim3(runs.threads), lds, s, a);
+      hipLaunchKernelGGL((k_route<T, LPR, V, WIDE, GROUPED, false>), grid, block, lds, s, a);
     return hipGetLastError();
   });
 }
 
-template <typename T> hipError_t launch_route_of(const RouteArgs &a, const Runs &runs, bool wide, hipStream_t s) {
-  if (a.groups > 1) return wide ? launch_route<T, true, true>(a, runs, s) : launch_route<T, false, true>(a, runs, s);
-  return wide ? launch_route<T, true, false>(a, runs, s) : launch_route<T, false, false>(a, runs, s);
+template <typename T> hipError_t launch_route_of(const RouteArgs &a, const Shape &shape, bool wide, hipStream_t s) {
+  if (a.groups > 1) return wide ? launch_route<T, true, true>(a, shape, s) : launch_route<T, false, true>(a, shape, s);
+  return wide ? launch_route<T, true, false>(a, shape, s) : launch_route<T, false, false>(a, shape, s);
 }
 
 template <typename T> hipError_t launch_back(const RouteBackArgs &a, hipStream_t s) {
-  return by_experts(a.experts, [&](auto lpr, auto v) {
+  return with_shape(shape_of(1, a.experts, a.k, false), [&](auto lpr, auto v) {
     constexpr int LPR = decltype(lpr)::value, TEAMS = 256 / LPR;
-    const int64_t blocks = (a.rows + TEAMS - 1) / TEAMS;
-    hipLaunchKernelGGL((k_route_back<T, LPR, decltype(v)::value, false>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, a);
-    return hipGetLastError();
+    if constexpr (LPR == 8) {
+      return hipErrorInvalidValue;     // not for one row
+    } else {
+      const int64_t blocks = (a.rows + TEAMS - 1) / TEAMS;
+      hipLaunchKernelGGL((k_route_back<T, LPR, decltype(v)::value, false>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, a);
+      return hipGetLastError();
+    }
   });
 }
 
@@ -828,8 +855,8 @@ using namespace gear;
 
 extern "C" size_t gear_route_workspace_bytes(int64_t rows, int32_t experts, int32_t k, int32_t groups) {
   if (!sizes_ok(rows, experts, k) || groups < 1) return 0;
-  const Runs r = runs_of(rows, experts, groups > 1);
-  return ((size_t)runs_ld(r.count) * experts * (narrow(r.run) ? 2 : 4) + 255) / 256 * 256;
+  const Shape s = shape_of(rows, experts, k, groups > 1);
+  return ((size_t)runs_ld(s.runs) * experts * (narrow(s.run) ? 2 : 4) + 255) / 256 * 256;
 }
 
 extern "C" gear_status gear_route(const gear_route_args *a, void *workspace, size_t workspace_bytes, void *stream) {
@@ -848,22 +875,22 @@ extern "C" gear_status gear_route(const gear_route_args *a, void *workspace, siz
                       a->ld_logits >= (1 << 20)))
     return GEAR_ERR_INVALID;
   if (a->rows == 0 && !a->off) return GEAR_OK;
-  const Runs r = runs_of(a->rows, a->experts, a->groups > 1);
+  const Shape shape = shape_of(a->rows, a->experts, a->k, a->groups > 1);
   if (a->off) {
     if (!workspace || ((uintptr_t)workspace & 255)) return GEAR_ERR_INVALID;
     if (workspace_bytes < gear_route_workspace_bytes(a->rows, a->experts, a->k, a->groups)) return GEAR_ERR_CAPACITY;
   }
   hipStream_t s = (hipStream_t)stream;
-  const RouteArgs p = {a->rows, a->ld_logits, r.run, a->experts, a->k, a->score == GEAR_SCORE_SOFTMAX, a->groups, a->groups_kept, a->group_best,
+  const RouteArgs p = {a->rows, a->ld_logits, shape.run, a->experts, a->k, a->score == GEAR_SCORE_SOFTMAX, a->groups, a->groups_kept, a->group_best,
                        a->renormalise != 0, a->scale, a->logits, a->bias, a->n, a->expert, a->weight, a->off, a->place, workspace};
   const bool wide = a->experts % 4 == 0 && a->ld_logits % 4 == 0 && ((uintptr_t)a->logits & (4 * size - 1)) == 0;
-  hipError_t err = a->dtype == GEAR_F32 ? launch_route_of<float>(p, r, wide, s) : launch_route_of<bf16_t>(p, r, wide, s);
-  if (err == hipSuccess && a->off && r.count > 1) {
-    const size_t lds = (size_t)a->experts * (1 + rankers_of(a->experts)) * 4;
-    if (narrow(r.run))
-      hipLaunchKernelGGL(k_places<uint16_t>, dim3(r.count), dim3(kPlaceThreads), lds, s, p);
+  hipError_t err = a->dtype == GEAR_F32 ? launch_route_of<float>(p, shape, wide, s) : launch_route_of<bf16_t>(p, shape, wide, s);
+  if (err == hipSuccess && a->off && shape.runs > 1) {
+    const size_t lds = (size_t)place_words(a->experts) * 4;
+    if (narrow(shape.run))
+      hipLaunchKernelGGL(k_places<uint16_t>, dim3(shape.runs), dim3(kPlaceThreads), lds, s, p);
     else
-      hipLaunchKernelGGL(k_places<int32_t>, dim3(r.count), dim3(kPlaceThreads), lds, s, p);
+      hipLaunchKernelGGL(k_places<int32_t>, dim3(shape.runs), dim3(kPlaceThreads), lds, s, p);
     err = hipGetLastError();
   }
   return err == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
