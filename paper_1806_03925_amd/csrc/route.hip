@@ -6,8 +6,8 @@
 // hundred thousand.  So the choice is made twice at most: from fp32, with a bound on its error, and again by the definition, in
 // fp64, by the wavefronts that have a row with two neighbours in its order closer than that.
 //
-// The choice from fp32.  A value becomes a whole number: how far it lies above a bound under the k-th, in 2^-21 of the way to the
-// largest, and behind that its expert's tag, so that one comparison moves both and equal ones come in the order of their experts.  The
+// The choice from fp32.  A value becomes a whole number: how far it lies above a bound under the k-th, in 2^-23 of the way to the
+// largest (2^-21 for 1024 experts), and behind that its expert's tag, so that one comparison moves both and equal ones come in the order of their experts.  The
 // conversion keeps the order, if not every difference, so only neighbours with the same or (where scores are added up) too
 // near numbers are in doubt.  A lane sorts its own by a network.  Where k is at most 8, teams then merge lists of 8 lane by lane,
 // log2(LPR) times, and keep the best of what falls off; else k + 1 times the largest of the team's first ones is taken and its lane moves
@@ -26,7 +26,8 @@ namespace gear {
 namespace {
 
 constexpr int kMaxRuns = 256;        // one for each CU
-constexpr int threads_of(int v, bool grouped) { return grouped || v > 16 ? 512 : 1024; }   // of a workgroup, at most: what its registers allow
+// threads of a workgroup, at most: what its registers and, with groups, its LDS allow
+constexpr int threads_of(int lpr, int v, bool grouped) { return grouped && lpr == kWave ? 256 : grouped || v > 16 ? 512 : 1024; }
 constexpr int kMaxGroups = GEAR_MAX_GROUPS;
 
 struct RouteArgs {
@@ -129,24 +130,19 @@ __device__ __forceinline__ float share(float l, bool softmax, float top, bool re
   return expf(l - shift) / (1.0f + expf(l));
 }
 
-// ---- whole numbers in the order of floats ------------------------------------------------------------------------------
-constexpr int kNobody = -2147483647 - 1;   // below every float's
-__device__ __forceinline__ int sortable(float f) {
-  const int b = __float_as_int(f + 0.0f);   // -0 is 0
-  return b ^ ((b >> 31) & 0x7fffffff);
-}
-__device__ __forceinline__ float unsorted(int s) { return __int_as_float(s ^ ((s >> 31) & 0x7fffffff)); }
-
 // ---- whole numbers that say whose they are ------------------------------------------------------------------------------
-constexpr int kTagBits = 10, kTag = (1 << kTagBits) - 1;      // the lower of equal values' experts has the larger tag
-static_assert(GEAR_MAX_EXPERTS <= kTag + 1, "an expert's number fits");
-constexpr float kSteps = 2097150.0f;                          // 2^21 - 2
-__device__ __forceinline__ bool is_somebody(int number) { return number > kTag; }
-__device__ __forceinline__ int expert_of(int number) { return kTag - (number & kTag); }
-// v, or -inf who may not be chosen; from `bound` (1) to the largest (2^21 - 1), 0 below
-__device__ __forceinline__ int number_of(float v, float bound, float steps, int expert) {
-  return (int)fmaxf(fmaf(v - bound, steps, 1.0f), 0.0f) << kTagBits | (kTag - expert);
-}
+// TAG last bits are the expert's number turned round, so that the lower one of equal values' experts has the larger number; the others
+// are 1 at the bound and STEPS + 1 at the largest value, 0 below the bound.
+template <int TAG> struct Numbers {
+  static constexpr int kLast = (1 << TAG) - 1, BITS = 31 - TAG < 23 ? 31 - TAG : 23;
+  static constexpr float STEPS = (float)((1 << BITS) - 4);
+  static __device__ __forceinline__ int of(float v, float bound, float steps, int expert) {   // v: -inf for who may not be chosen
+    return (int)fmaxf(fmaf(v - bound, steps, 1.0f), 0.0f) << TAG | (kLast - expert);
+  }
+  static __device__ __forceinline__ bool is_somebody(int number) { return number > kLast; }
+  static __device__ __forceinline__ int expert_of(int number) { return kLast - (number & kLast); }
+  static __device__ __forceinline__ int height_of(int number) { return number >> TAG; }
+};
 
 // descending, by odd-even merges
 template <int V> struct Sorter {
@@ -295,8 +291,9 @@ __device__ __forceinline__ void places(const RouteArgs &a, int run, Slice &slice
 }
 
 // The choice of one row by the definition, in fp64, by a whole wavefront: lane j gets the j-th expert, -1 where there is none.  The row is
-// read again: its values in fp64 are few for 64 lanes, and nobody keeps registers for them who does not need them.
-template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int choose_exactly(const RouteArgs &a, int64_t row, float top) {
+// read again: its values in fp64 are few for 64 lanes, and nobody keeps registers for them who does not need them.  scratch: MAX_E doubles of LDS
+// of this wavefront's, for groups.
+template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int choose_exactly(const RouteArgs &a, int64_t row, float top, double *scratch) {
   constexpr int V = MAX_E / kWave;
   const double kNone = -INFINITY;
   const int lane = threadIdx.x & 63, E = a.experts;
@@ -321,25 +318,23 @@ template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int ch
   }
   if constexpr (GROUPED) {
     const int per = E / a.groups;
-    double worth[1] = {kNone};    // lane q: group q's value
-    for (int q = 0; q < a.groups; ++q) {
-      double in[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int e = v * kWave + lane;
-        in[v] = e >= q * per && e < (q + 1) * per ? order[v] : kNone;
+    for (int v = 0; v < V; ++v) scratch[v * kWave + lane] = order[v];
+    asm volatile("" ::: "memory");   // LDS accesses of one wavefront come in order
+    __builtin_amdgcn_wave_barrier();
+    double worth[1] = {kNone};       // lane q: group q's value
+    if (lane < a.groups) {
+      double one = kNone, two = kNone;
+#pragma unroll 4
+      for (int c = 0; c < per; ++c) {
+        const double v = scratch[lane * per + c];
+        two = fmax(two, fmin(one, v));
+        one = fmax(one, v);
       }
-      const Best one = wave_best(in);
-      double sum_of_two = one.value;
-      if (a.best == 2) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (v * kWave + lane == one.index) in[v] = kNone;
-        const Best two = wave_best(in);
-        if (two.index >= 0) sum_of_two += two.value;
-      }
-      if (lane == q) worth[0] = sum_of_two;
+      worth[0] = a.best == 2 && two > kNone ? one + two : one;
     }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
     uint64_t keep = 0;
     for (int j = 0; j < a.kept; ++j) {
       const Best b = wave_best(worth);
@@ -367,12 +362,18 @@ template <typename T, int MAX_E, bool GROUPED> __device__ __forceinline__ int ch
 }
 
 template <typename T, int LPR, int V, bool WIDE, bool GROUPED, bool FEW>   // FEW: k is at most kList
-__global__ void __launch_bounds__(threads_of(V, GROUPED)) k_route(RouteArgs a) {
+__global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs a) {
   constexpr int MAX_E = LPR * V, SLOTS = !FEW && LPR < GEAR_MAX_CHOSEN ? GEAR_MAX_CHOSEN / LPR : 1;   // of a lane
   static_assert(!WIDE || V % 4 == 0, "four neighbouring logits a load");
   static_assert(GEAR_MAX_EXPERTS <= 1024 && LPR >= kList, "a tag's bits; a lane for each of a list");
+  constexpr int TAG = MAX_E <= 32 ? 5 : MAX_E <= 64 ? 6 : MAX_E <= 128 ? 7 : MAX_E <= 256 ? 8 : MAX_E <= 512 ? 9 : 10;
+  static_assert(MAX_E <= 1 << TAG, "an expert's number fits");
+  using Num = Numbers<TAG>;
   extern __shared__ int32_t s_words[];                          // [experts] counts, then what places() needs
-  __shared__ float s_value[GROUPED ? threads_of(V, true) * V : 1];
+  // a row's values for each team; a wavefront's are room for those of one row in 64 bits
+  constexpr int TEAM_VALUES = LPR == kWave ? 2 * MAX_E : MAX_E, WAVE_VALUES = kWave / LPR * TEAM_VALUES;
+  static_assert(WAVE_VALUES >= 2 * MAX_E, "doubles");
+  __shared__ __attribute__((aligned(16))) float s_value[GROUPED ? threads_of(LPR, V, true) / kWave * WAVE_VALUES : 4];
   const int threads = blockDim.x, teams = threads / LPR;
   const int l = threadIdx.x % LPR, my_team = threadIdx.x / LPR, lane0_of_mine = threadIdx.x & 63 & ~(LPR - 1), E = a.experts;
   for (int e = threadIdx.x; e < E; e += threads) s_words[e] = 0;
@@ -386,6 +387,10 @@ __global__ void __launch_bounds__(threads_of(V, GROUPED)) k_route(RouteArgs a) {
     bias[v] = a.bias && index(v) < E ? a.bias[index(v)] : 0.0f;
     if (!(bias[v] > -INFINITY)) bias[v] = -INFINITY;
   }
+  float most_bias = 0.0f;                     // of the finite ones' magnitudes
+#pragma unroll
+  for (int v = 0; v < V; ++v) most_bias = fmaxf(most_bias, fabsf(bias[v]) < INFINITY ? fabsf(bias[v]) : 0.0f);
+  most_bias = team_max<LPR>(most_bias);
   const bool scores = a.bias || GROUPED;      // the choice looks at them
 
   float lg[V];
@@ -444,24 +449,26 @@ __global__ void __launch_bounds__(threads_of(V, GROUPED)) k_route(RouteArgs a) {
 #pragma unroll
       for (int v = 0; v < V; ++v) value[v] = fmaf(value[v], inv, bias[v]);
     }
-    // How far apart two values have to be at least to be in their true order.  A softmax in fp32 is off by s (d + 13) 2^-23, d = top - l (argument, exponential, sum
-    // and quotient), which is largest at the row's largest score `inv`: 2^-19 of it.  A sigmoid is off by 2^-22.
-    const float apart = a.softmax ? inv * 0x1p-18f : 0x1p-20f;
+    // How far apart two values of which one is v have to be, to be in their true order.  A softmax in fp32 is off by s (d + 13) 2^-23, d = ln(largest / s) (argument,
+    // exponential, sum and quotient); s is at most |v| and the largest bias, s d at most 0.37 of the largest, `inv`.  A sigmoid is off by 2^-22.  And a sum is rounded.
+    auto apart = [&](float v) {
+      return a.softmax ? 0x1p-22f * (14.0f * (fabsf(v) + most_bias) + 0.4f * inv) : 0x1p-21f + 0x1p-22f * fabsf(v);
+    };
     bool unsure = false;
     uint64_t keep = ~0ull;
     if constexpr (GROUPED) {
       const int per = E / a.groups;
-      float *mine = s_value + my_team * MAX_E;
+      float *mine = s_value + my_team * TEAM_VALUES;
 #pragma unroll
       for (int v = 0; v < V; ++v)
         if (index(v) < E) mine[index(v)] = !empty && fminf(lg[v], bias[v]) > -INFINITY ? value[v] : -INFINITY;
       asm volatile("" ::: "memory");   // a team is part of one wavefront, whose LDS accesses come in order
       __builtin_amdgcn_wave_barrier();
-      int worth[kMaxGroups / LPR];
+      float worth[kMaxGroups / LPR];
 #pragma unroll
       for (int i = 0; i < kMaxGroups / LPR; ++i) {
         const int q = l + i * LPR;
-        worth[i] = kNobody;
+        worth[i] = -INFINITY;
         if (q < a.groups) {
           float one = -INFINITY, two = -INFINITY;
 #pragma unroll 4
@@ -470,29 +477,35 @@ __global__ void __launch_bounds__(threads_of(V, GROUPED)) k_route(RouteArgs a) {
             two = fmaxf(two, fminf(one, v));
             one = fmaxf(one, v);
           }
-          if (one > -INFINITY) worth[i] = (sortable(a.best == 2 && two > -INFINITY ? one + two : one) & ~(kMaxGroups - 1)) | (kMaxGroups - 1 - q);
+          worth[i] = a.best == 2 && two > -INFINITY ? one + two : one;
         }
       }
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
       keep = 0;
-      int before = kNobody;
+      float before = 0.0f;
       for (int j = 0; j <= a.kept; ++j) {
-        int best = worth[0];
+        float best = worth[0];
 #pragma unroll
-        for (int i = 1; i < kMaxGroups / LPR; ++i) best = max(best, worth[i]);
+        for (int i = 1; i < kMaxGroups / LPR; ++i) best = fmaxf(best, worth[i]);
+        const float mine_best = best;
         best = team_max<LPR>(best);
-        if (best == kNobody) continue;
-        if (j < a.kept) {
-          keep |= 1ull << (kMaxGroups - 1 - (best & (kMaxGroups - 1)));
-          before = best;
-        } else {   // only between the last that is kept and the first that is not does the order matter; six bits are the group's number
-          const float x = unsorted(before & ~(kMaxGroups - 1)), y = unsorted(best & ~(kMaxGroups - 1));
-          unsure = !(x - y > 0x1p-15f * fmaxf(fabsf(x), fabsf(y)) + 2.0f * apart);
+        if (!(best > -INFINITY)) continue;
+        if (j == a.kept) {   // only between the last that is kept and the first that is not does the order matter
+          unsure = !(before - best > apart(before) + apart(best) + 0x1p-22f * (fabsf(before) + fabsf(best)) + (a.best == 2 ? apart(before) + apart(best) : 0.0f));
+          continue;
         }
+        before = best;
+        // one of the groups of that value: the others' turn comes next
+        const bool is_mine = mine_best == best && (threadIdx.x & (LPR - 1)) == __builtin_ctzll(team_ballot<LPR>(mine_best == best) | 1ull << 63);
+        int taken = -1;
+#pragma unroll
+        for (int i = kMaxGroups / LPR - 1; i >= 0; --i)
+          if (is_mine && worth[i] == best) taken = l + i * LPR;
 #pragma unroll
         for (int i = 0; i < kMaxGroups / LPR; ++i)
-          if (worth[i] == best) worth[i] = kNobody;
+          if (l + i * LPR == taken) worth[i] = -INFINITY;
+        keep |= 1ull << team_max<LPR>(taken);
       }
     }
     // what decides, -inf where it may not be chosen
@@ -521,21 +534,19 @@ __global__ void __launch_bounds__(threads_of(V, GROUPED)) k_route(RouteArgs a) {
       low = team_min<LPR>(low);
       if (!ENOUGH || !(bound > -INFINITY)) bound = low;
     }
-    const float range = high - bound, steps = fminf(kSteps / range, 0x1p127f);   // range 0: those below are still below 1
+    const float range = high - bound, steps = fminf(Num::STEPS / range, 0x1p127f);   // range 0: those below are still below 1
     int number[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) number[v] = number_of(value[v], bound, steps, index(v));
+    for (int v = 0; v < V; ++v) number[v] = Num::of(value[v], bound, steps, index(v));
     Sorter<V>::sort(number);
-    // x before y in the order, y somebody: is that in doubt?  Sums of scores and biases: if they are `apart` or less, or their own rounding.
-    // Logits: if their numbers are the same but they may not be.  All are where the range is none; logits of 16 bits, which differ by 2^-8 of themselves,
-    // are unless they are next to nothing.
-    const int near = a.bias ? (int)fminf((apart + 0x1p-22f * fmaxf(fabsf(high), fabsf(bound))) * steps, 0x1p22f) + 2 : 0;
+    // x before y in the order, y somebody: is that in doubt?  Sums of scores and biases: if they are not `apart`, and three steps, which is what the
+    // way to a number costs.  Logits: if their numbers are the same but they may not be.  All are where the range is none; logits of 16 bits, which differ by
+    // 2^-8 of themselves, are unless they are next to nothing.
     auto doubt = [&](int x, int y) {
-      const int ahead = (x >> kTagBits) - (y >> kTagBits);
-      if (ahead > near) return false;
-      if (a.bias) return true;
-      if (sizeof(T) == 2 && fabsf(bound + (float)(x >> kTagBits) * (range * 0x1p-21f)) > range * 0x1p-10f) return false;
-      return range != 0.0f;
+      const int ahead = Num::height_of(x) - Num::height_of(y);
+      const float v = bound + (float)Num::height_of(x) * (range * (1.0f / Num::STEPS));
+      if (a.bias) return ahead <= (int)fminf(apart(v) * steps, 0x1p24f) + 3;
+      return ahead == 0 && range != 0.0f && !(sizeof(T) == 2 && fabsf(v) > range * 0x1p-10f);
     };
     unsure = !empty && (unsure || !(range < INFINITY));
     int chosen[SLOTS];
@@ -553,21 +564,21 @@ __global__ void __launch_bounds__(threads_of(V, GROUPED)) k_route(RouteArgs a) {
       static_assert(kList == 8, "three bits");
       const int mine = pick(list[0], list[1], list[2], list[3], list[4], list[5], list[6], list[7]);
       const int next = pick(list[1], list[2], list[3], list[4], list[5], list[6], list[7], rest);
-      const bool is = !empty && l < a.k && is_somebody(mine);
-      chosen[0] = is ? expert_of(mine) : -1;
-      if (is && is_somebody(next) && doubt(mine, next)) unsure = true;
+      const bool is = !empty && l < a.k && Num::is_somebody(mine);
+      chosen[0] = is ? Num::expert_of(mine) : -1;
+      if (is && Num::is_somebody(next) && doubt(mine, next)) unsure = true;
     } else {
 #pragma unroll
       for (int s = 0; s < SLOTS; ++s) chosen[s] = -1;
       int before = 0;
       for (int j = 0; j <= a.k; ++j) {        // one more, to see how far it is
         const int best = team_max<LPR>(number[0]);
-        const bool hit = number[0] == best, is = !empty && is_somebody(best);
+        const bool hit = number[0] == best, is = !empty && Num::is_somebody(best);
         if (is && j > 0 && doubt(before, best)) unsure = true;
         before = best;
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s)
-          if (is && j < a.k && j == l + s * LPR) chosen[s] = expert_of(best);
+          if (is && j < a.k && j == l + s * LPR) chosen[s] = Num::expert_of(best);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const int stay = number[v], next = v + 1 < V ? number[v + 1] : 0;   // values: a choice of elements would become an array in scratch
@@ -578,7 +589,8 @@ __global__ void __launch_bounds__(threads_of(V, GROUPED)) k_route(RouteArgs a) {
     for (uint64_t left = __ballot(unsure); left;) {   // by the definition, team by team
       const int lane0 = __builtin_ctzll(left) & ~(LPR - 1);
       left &= LPR == 64 ? 0 : ~(((1ull << (LPR & 63)) - 1) << lane0);
-      const int pick = choose_exactly<T, (MAX_E < kWave ? kWave : MAX_E), GROUPED>(a, row + lane0 / LPR - lane0_of_mine / LPR, __shfl(top, lane0, kWave));
+      const int pick = choose_exactly<T, (MAX_E < kWave ? kWave : MAX_E), GROUPED>(a, row + lane0 / LPR - lane0_of_mine / LPR, __shfl(top, lane0, kWave),
+                                                                                           reinterpret_cast<double *>(s_value + (GROUPED ? threadIdx.x / kWave * WAVE_VALUES : 0)));
 #pragma unroll
       for (int s = 0; s < SLOTS; ++s) {
         const int at = __shfl(pick, (l + s * LPR) & 63, kWave);
@@ -789,7 +801,7 @@ Shape shape_of(int64_t rows, int experts, int k, bool grouped) {
   if (s.lpr > 16) s.v = 16;
   // runs of rows: as many as there are CUs at most, of whole passes of a workgroup over its rows; a batch that fits in one has no more threads than
   // its rows need (one row of 64 experts: 6.0 us by 64 threads, 9.1 by 1024)
-  s.threads = threads_of(s.v, grouped);
+  s.threads = threads_of(s.lpr, s.v, grouped);
   const int teams = s.threads / s.lpr;
   const int64_t passes = (rows + teams - 1) / teams, each = (passes + kMaxRuns - 1) / kMaxRuns, run = (each > 0 ? each : 1) * teams;
   s.run = (int)run;
