@@ -57,7 +57,9 @@ template <int DT_, int WTM_, int WAVES_M_, int WAVES_N_> struct ProductTile {
   static constexpr bool HALVES = BM == 128 && BN == 256;
   static constexpr int STAGE_BYTES = BM * kKBlock, DMA = BM / 8 / WAVES;   // copies of a wavefront per stage, eight rows each
   static constexpr int PATCH_BYTES = WAVES * 32 * PATCH_LD * 2;
-  static constexpr int LDS_BYTES = kStages * STAGE_BYTES > PATCH_BYTES ? kStages * STAGE_BYTES : PATCH_BYTES;
+  static constexpr int TILE_BYTES = kStages * STAGE_BYTES > PATCH_BYTES ? kStages * STAGE_BYTES : PATCH_BYTES;
+  static constexpr int X_SCALES = DT == GEAR_I8 ? (BM + 63) / 64 * 64 : 0, W_SCALES = DT == GEAR_I8 ? BN : 0;   // floats behind the tile
+  static constexpr int LDS_BYTES = TILE_BYTES + 4 * (X_SCALES + W_SCALES);
   static_assert(DMA * 8 * WAVES == BM, "a copy is eight rows");
 };
 
@@ -256,6 +258,20 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
   const uint32_t x_rel = lds_base + (uint32_t)(wm * C::WTM * 32 + r) * 128u + (uint32_t)((g ^ (r >> 1 & 7)) << 4);
 
+  if constexpr (C::DT == GEAR_I8) {   // the factors of the results, on their way to LDS before anything else: nothing waits for them at the end
+    constexpr int ALL = (C::X_SCALES + C::W_SCALES) / kWave;
+    const auto xs_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.x_scale) + (int64_t)m0 * 4, 0, m_rows * 4, 0x00020000);
+    const auto ws_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.w_scale) + ((int64_t)t.e * a.N + n0) * 4, 0,
+                                                           min(a.N - n0, C::BN) * 4, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < (ALL + C::WAVES - 1) / C::WAVES; ++i) {   // the same number by every wavefront: the compiler counts what is on its way
+      const int p = min(i * C::WAVES + wave, ALL - 1), at = p * kWave + lane;
+      const bool is_x = p < C::X_SCALES / kWave;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_x ? xs_rsrc : ws_rsrc, (lds_ptr_t)(lds + C::TILE_BYTES + p * kWave * 4), 4,
+                                               (is_x ? at : at - C::X_SCALES) * 4, 0, 0, 0);
+    }
+    asm volatile("" ::: "memory");
+  }
   scales(0, 0);
   copy(0);
   load(b[0], 0, 0);
@@ -289,16 +305,16 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
                        a.N, lane);
   };
   if constexpr (C::DT == GEAR_I8) {
-    const float *x_of = reinterpret_cast<const float *>(a.x_scale) + m0, *w_of = reinterpret_cast<const float *>(a.w_scale) + (int64_t)t.e * a.N;
+    const float *x_of = reinterpret_cast<const float *>(lds + C::TILE_BYTES), *w_of = x_of + C::X_SCALES;
     float xr[C::WTM];
 #pragma unroll
-    for (int i = 0; i < C::WTM; ++i) xr[i] = x_of[min(wm * 32 * C::WTM + i * 32 + r, m_rows - 1)];
+    for (int i = 0; i < C::WTM; ++i) xr[i] = x_of[wm * 32 * C::WTM + i * 32 + r];
     f32x16_v v[C::WTM][TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const float4 wn4 = *reinterpret_cast<const float4 *>(w_of + min(n0 + wn * WN + j * 32 + 8 * q + 4 * g, a.N - 4));
+        const float4 wn4 = *reinterpret_cast<const float4 *>(w_of + wn * WN + j * 32 + 8 * q + 4 * g);
         const float wc[4] = {wn4.x, wn4.y, wn4.z, wn4.w};
 #pragma unroll
         for (int i = 0; i < C::WTM; ++i)
@@ -423,6 +439,16 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
         }
       }
   };
+  // the part of the tile that this wavefront adds up and stores, and its factors, on their way already
+  constexpr int PARTS = TM_ * TN_ * 4;
+  static_assert(DT != GEAR_I8 || PARTS == C::WAVES, "one part each");
+  float x_factor = 1.0f;
+  float4 w_factor = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+  if constexpr (DT == GEAR_I8) {
+    x_factor = reinterpret_cast<const float *>(a.x_scale)[m0 + min((wave >> 2) / TN_ * 32 + r, m_rows - 1)];
+    w_factor = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(a.w_scale) + (int64_t)t.e * a.N +
+                                                 min(n0 + (wave >> 2) % TN_ * 32 + 8 * (wave & 3) + 4 * g, a.N - 4));
+  }
   SplitBlock<C> b[C::AHEAD + 1];
 #pragma unroll
   for (int p = 0; p < C::AHEAD; ++p) load(b[p], wave + p * C::WAVES);
@@ -435,7 +461,6 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
   }
   // [wavefront][tile][element / 4][lane] of four values each: four consecutive columns of row lane % 32
   using Four = std::conditional_t<DT == GEAR_I8, int4, float4>;
-  constexpr int PARTS = TM_ * TN_ * 4;
 #pragma unroll
   for (int i = 0; i < TM_; ++i)
 #pragma unroll
@@ -457,9 +482,7 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
     if (m < m_rows && n < a.N) {
       float4 v = make_float4((float)sum.x, (float)sum.y, (float)sum.z, (float)sum.w);
       if constexpr (DT == GEAR_I8) {
-        const float xr = reinterpret_cast<const float *>(a.x_scale)[m0 + m];
-        const float4 wc = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(a.w_scale) + (int64_t)t.e * a.N + n);
-        v.x = v.x * xr * wc.x, v.y = v.y * xr * wc.y, v.z = v.z * xr * wc.z, v.w = v.w * xr * wc.w;
+        v.x = v.x * x_factor * w_factor.x, v.y = v.y * x_factor * w_factor.y, v.z = v.z * x_factor * w_factor.z, v.w = v.w * x_factor * w_factor.w;
       }
       if constexpr (F32)
         *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + (m0 + m) * a.ld_out + n) = v;
