@@ -639,7 +639,9 @@ template <int DT, int TM, int TN, int WAVES, int AHEAD> hipError_t launch_split(
 //     10.3; above, 512 x 1024 x 1152 bf16 11.9 / 7.8.  fp32, whose products are slow, up to 1024, against 64 x 128: 512 x 2048 53.5 /
 //     70.0, 1024 x 2048 98.8 / 74.6
 //   32 x 64 split over k by eight wavefronts where these are one for each CU at most and walk 48 k-blocks or more, against 32 x 128: 535 x
-//     816 x 5568 bf16 22.9 / 32.1, 512 x 800 x 8192 8 bits 18.1 / 25.1, but half as far, 512 x 800 x 4096 8 bits, 11.3 / 10.5
+//     816 x 5568 bf16 22.9 / 32.1, 512 x 800 x 8192 8 bits 18.1 / 25.1, but half as far, 512 x 800 x 4096 8 bits, 11.3 / 10.5; integers,
+//     whose blocks need no scales on the way, from 24 on: 512 x 800 x 2048 6.7 / 6.7, x 4096 9.4 / 10.6, 535 x 816 x 5568 12.5 / 17.5.  (At the other borders they are
+//     as 8 bits are.)
 //   32 x 128 up to 256 tiles, then 64 x 128 up to as many: 1024 x 1024 x 4096 bf16 25.2 / 27.1, 1024 x 2048 16.9 / 14.9, 256 x 8192
 //     54.4 / 50.3; where experts have few rows only above 512: 1000 x 1024 by 32 15.9 / 18.2
 //   64 x 256 above, against 32 x 128 and 64 x 128: 1500 x 2048 x 1024 bf16 12.0 / 13.6 / 14.2, 2000 x 2048 20.2 / 28.2 / 25.0, up to 512
@@ -657,7 +659,7 @@ template <int DT> hipError_t launch_product(const ProductArgs &a, bool f32, hipS
     if (empty > count / 3) return launch_split<DT, 1, 2, 4, 1>(a, f32, s);
     return launch_tile<DT, 1, 2, 2>(a, f32, s);
   } else {
-    if (tiles(32, 64) <= 256 && a.K * operand_bytes(DT) >= 48 * kKBlock) return launch_split<DT, 1, 2, 8, 1>(a, f32, s);
+    if (tiles(32, 64) <= 256 && a.K * operand_bytes(DT) >= (DT == GEAR_I8 ? 24 : 48) * kKBlock) return launch_split<DT, 1, 2, 8, 1>(a, f32, s);
     const int64_t narrow = tiles(32, 128);
     if (narrow <= 256 || (narrow <= 512 && a.rows < 256 * (int64_t)a.experts)) return launch_tile<DT, 1, 1, 2>(a, f32, s);
     if (narrow <= 512) return launch_tile<DT, 1, 2, 2>(a, f32, s);

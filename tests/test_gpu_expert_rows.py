@@ -230,7 +230,7 @@ def test_rows_of_zeros_infinities_and_denormals(g):
 
 
 PRODUCTS = [(1, 8, 8, 0), (1, 1024, 1152, 0), (5, 72, 136, 0), (33, 520, 576, 16), (300, 1024, 1152, 0), (535, 816, 6208, 0), (1024, 1024, 512, 0),
-            (700, 1024, 264, 9), (2000, 2048, 256, 0), (4097, 72, 320, 0), (9000, 264, 200, 4), (4096, 2048, 128, 7), (17408, 1024, 136, 8), (40, 24, 65536, 0)]
+            (700, 1024, 264, 9), (2000, 2048, 256, 0), (4097, 72, 320, 0), (9000, 264, 200, 4), (4096, 2048, 128, 7), (17408, 1024, 136, 8), (40, 24, 65536, 0), (300, 200, 3200, 0)]
 
 
 @pytest.mark.parametrize("rows,n,k,experts", PRODUCTS)
