@@ -119,7 +119,6 @@ template <int V> __device__ __forceinline__ Best wave_best(const double (&value)
 __device__ __forceinline__ double exact_score(float l, bool softmax, float top) {
   return softmax ? exp((double)l - (double)top) : 1.0 / (1.0 + exp(-(double)l));
 }
-// in fp32, off by (|v| + 2) 2^-23 of itself
 __device__ __forceinline__ float quick_exp(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504f); }
 // A chosen expert's share: its score up to a factor that is the same for all of its row where `relative`.  No sum of such scores
 // vanishes then, however small they are, when `top` is the largest chosen logit.
@@ -449,10 +448,13 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
 #pragma unroll
       for (int v = 0; v < V; ++v) value[v] = fmaf(value[v], inv, bias[v]);
     }
-    // How far apart two values of which one is v have to be, to be in their true order.  A softmax in fp32 is off by s (d + 13) 2^-23, d = ln(largest / s) (argument,
-    // exponential, sum and quotient); s is at most |v| and the largest bias, s d at most 0.37 of the largest, `inv`.  A sigmoid is off by 2^-22.  And a sum is rounded.
+    // How far apart two values of which one is v have to be, to be in their true order.  In units of 2^-23 of itself an exponential is off by 1.25 d + 1, d = top - l (its
+    // argument, the factor log2 e, the instruction), the sum by half a unit for each of V + 6 additions and by what its terms are off by on their average, at most 7 (the mean of d is
+    // below 4.5 whatever the scores of up to 1024 experts), the quotient and the value by 1 each: s (1.25 d + COEF), s at most |v| and the largest bias, s d at most 0.37 of
+    // the largest score, `inv`.  A sigmoid is off by 2.1 2^-23 (an exponential's error times s (1 - s), an addition, the reciprocal).  And a sum with a bias is rounded.
+    constexpr float COEF = 10.0f + 0.5f * (V + 6);
     auto apart = [&](float v) {
-      return a.softmax ? 0x1p-22f * (14.0f * (fabsf(v) + most_bias) + 0.4f * inv) : 0x1p-21f + 0x1p-22f * fabsf(v);
+      return a.softmax ? 0x1p-22f * (COEF * (fabsf(v) + most_bias) + 0.5f * inv) : 0x1.1p-21f + 0x1p-22f * fabsf(v);
     };
     bool unsure = false;
     uint64_t keep = ~0ull;

@@ -151,6 +151,11 @@ def _of_route(t: torch.Tensor, route: Route, rows: int, where: str, name: str, d
     return _matrix(t, route.gpu, where, name, dtype)
 
 
+def _not_itself(out: torch.Tensor, other: torch.Tensor, where: str, what: str) -> None:
+    if out.numel() and out.data_ptr() == other.data_ptr():
+        _refuse(where, f"{what}: rows would be read after others have been written in their place")
+
+
 def gear_expert_gather(x: torch.Tensor, route: Route, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows x dim] copied to every place that the route gives its rows: [rows * k x dim] for gear_expert_matmul with route.off.  Rows
     from route.off[experts] on are not written.  Its gradient is gear_expert_combine(dxs, route, weighted=False)."""
@@ -162,6 +167,7 @@ def gear_expert_gather(x: torch.Tensor, route: Route, out: Optional[torch.Tensor
         out, ld_out = torch.empty(places, dim, dtype=x.dtype, device=route.gpu), dim
     else:
         ld_out = _of_route(out, route, places, where, "out", x.dtype, dim)
+        _not_itself(out, x, where, "out may not be x")
     status = lib.gear_expert_gather(x.data_ptr(), _CODE[x.dtype], ld, route.rows, dim, route.p_place, route.k, out.data_ptr(), ld_out,
                                     _raw_stream(route.gpu))
     if status:
@@ -185,6 +191,7 @@ def gear_expert_combine(y: torch.Tensor, route: Route, weighted: bool = True, re
         out, ld_out = torch.empty(rows, dim, dtype=dtype, device=route.gpu), dim
     else:
         ld_out = _of_route(out, route, rows, where, "out", dtype, dim)
+        _not_itself(out, y, where, "out may not be y")
     a = gear_expert_combine_args(rows, dim, route.k, _CODE[dtype], y.data_ptr(), p_r, route.p_place, route.p_weight if weighted else None, out.data_ptr(),
                                  ld_y, ld_r, ld_out)
     status = lib.gear_expert_combine(C.byref(a), _raw_stream(route.gpu))
@@ -207,6 +214,7 @@ def gear_expert_combine_backward(dout: torch.Tensor, y: torch.Tensor, route: Rou
         dy, ld_dy = torch.empty(places, dim, dtype=dtype, device=route.gpu), dim
     else:
         ld_dy = _of_route(dy, route, places, where, "dy", dtype, dim)
+        _not_itself(dy, dout, where, "dy may not be dout")
     if dweight is None:
         dweight = torch.empty(rows, route.k, dtype=torch.float32, device=route.gpu)
     else:

@@ -155,6 +155,16 @@ def test_no_rows(g):
     assert g.gear_matmul_i8(g.gear_expert_gather_i8(x, route), w, route.off).shape == (0, 24)
 
 
+def test_results_in_the_place_of_rows_still_to_be_read_are_refused(g):
+    """With one expert a row the sizes would allow it."""
+    x = torch.randn(6, 64, device="cuda")
+    route = g.gear_route(torch.randn(6, 3, device="cuda"), 1)
+    for call in (lambda: g.gear_expert_gather(x, route, out=x), lambda: g.gear_expert_combine(x, route, out=x),
+                 lambda: g.gear_expert_combine_backward(x, x.clone(), route, dy=x)):
+        with pytest.raises(g.GearError):
+            call()
+
+
 # ---- 8-bit integers -------------------------------------------------------------------------------------------------
 def integers(v):
     """q and scale from the definition, 64 bits: floor, remainder and parity instead of a rounding."""

@@ -5,6 +5,7 @@ argument l - top of its exponential is off by |l - top| u, the exponential by 2 
 additions' u and what its terms are off by on their average (at most 8 u: terms that count have arguments of a few units), the division and the
 factor by 2 u: (|l - top| + 40) u of the weight.  Gradients of logits are sums of two such products, held to twice that of the sum of
 their magnitudes, and one rounding to the logits' type."""
+import ctypes
 import itertools
 import math
 
@@ -171,6 +172,44 @@ def test_padding(g, n):
     check(r, want)
     d = g.gear_route_backward(logits, r, torch.ones(100, 3, device="cuda"), renormalise=False)
     assert torch.equal(d[max(0, min(n, 100)):], torch.zeros_like(d[max(0, min(n, 100)):])) and torch.isfinite(d).all()
+
+
+@pytest.mark.parametrize("rows,groups", [(1, 1), (40, 1), (3000, 1), (40, 4), (3000, 4), (40_000, 1)])
+def test_the_choice_alone(g, rows, groups):
+    """From C, without an order of the pairs: no workspace is needed."""
+    from paper_1806_03925_amd import binding as b
+    logits = torch.randn(rows, 64, device="cuda", generator=gen(rows))
+    want = g.gear_route(logits, 5, groups=groups, groups_kept=max(1, groups // 2))
+    expert, weight = torch.empty_like(want.expert), torch.empty_like(want.weight)
+    a = b.gear_route_args(rows, 64, 5, b.GEAR_F32, b.GEAR_SCORE_SOFTMAX, groups, max(1, groups // 2), 1, 1, 1.0, logits.data_ptr(), 64, None, None,
+                          expert.data_ptr(), weight.data_ptr(), None, None)
+    assert b.lib.gear_route(ctypes.byref(a), None, 0, torch.cuda.current_stream().cuda_stream) == b.GEAR_OK
+    assert torch.equal(expert, want.expert) and torch.equal(weight, want.weight)
+
+
+@pytest.mark.parametrize("experts,k,dtype", [(24, 8, F32), (24, 3, BF16), (64, 8, F32), (63, 8, F32), (200, 8, F32), (256, 5, BF16), (130, 1, F32), (256, 8, F32)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_many_rows(g, experts, k, dtype, score):
+    """Long batches have kernels of their own: the same rows as in short ones, and some of them by the definition."""
+    rows = 33_001
+    r = gen(experts)
+    logits = (1.5 * torch.randn(rows, experts, device="cuda", generator=r)).to(dtype)
+    logits[5::7, experts // 3:] = -INF
+    logits[6::11] = 0.25
+    logits[12::13] = -INF
+    logits[100, 3], logits[200, 0] = math.nan, INF
+    bias = (0.2 / experts) * torch.randn(experts, device="cuda", generator=r)
+    for b in (None, bias):
+        for x in (logits, strided(logits, 1)):
+            long = g.gear_route(x, k, score, bias=b, renormalise=False, scale=2.5)
+            for first in (0, 1000, 20_000, rows - 700):
+                short = g.gear_route(x[first:first + 700], k, score, bias=b, renormalise=False, scale=2.5)
+                assert torch.equal(long.expert[first:first + 700], short.expert)
+                within(long.weight[first:first + 700], short.weight, 80 * U * short.weight.nan_to_num().abs())   # (d + 40) u of each; chosen logits are within 20 of the top here, masked rows too
+        part = slice(90, 210)
+        expert, weight, _, _, far = reference(logits[part], k, score, b, renormalise=False, scale=2.5)
+        assert torch.equal(long.expert[part].long(), expert)
+        within(long.weight[part], weight, (far + 40) * U * weight.nan_to_num().abs() + 2.0 ** -149)
 
 
 def test_no_rows(g):
