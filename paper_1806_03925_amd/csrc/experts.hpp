@@ -20,11 +20,17 @@ struct ExpertTile {
 // about 150 left, 16384 x 1152 x 1024 by 8 experts, 44.7 / 47.5.
 constexpr int kSlots = 512, kHalved = kSlots / 4;
 
-__device__ __forceinline__ int wave_add(int v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
+// sums of this and the lower lanes' v, by moves between lanes that need no LDS: within 16 lanes, then over the four
+template <int CTRL, int ROWS> __device__ __forceinline__ int add_moved(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int v) {
+  v = add_moved<0x111, 0xf>(v);   // one lane up, two, four, eight
+  v = add_moved<0x112, 0xf>(v);
+  v = add_moved<0x114, 0xf>(v);
+  v = add_moved<0x118, 0xf>(v);
+  v = add_moved<0x142, 0xa>(v);   // lane 15 to the second sixteen and 47 to the fourth
+  return add_moved<0x143, 0xc>(v);   // lane 31 to the upper half
 }
+__device__ __forceinline__ int wave_add(int v) { return __builtin_amdgcn_readlane(wave_scan(v), kWave - 1); }
 
 // whether off is a CSR index into `rows` rows; every lane of a wavefront gets the answer
 __device__ __forceinline__ bool offsets_ok(const int32_t *__restrict__ off, int experts, int rows, int lane) {
@@ -73,39 +79,38 @@ __device__ __forceinline__ ExpertTile expert_tile(const int32_t *__restrict__ of
     r.m0 = t.m * edge, r.m_end = rows, r.n_tile = t.n, r.have = true;
     return r;
   }
-  int total = 0;
+  // 64 experts at a time; the last 64's numbers (of 64 experts at most: all) stay for the search
+  int total = 0, a = 0, b = 0, mine = 0, upto = 0;
   bool bad = off[0] != 0;
-  for (int e0 = 0; e0 < experts; e0 += kWave) {
-    const int e = min(e0 + lane, experts - 1), a = off[e], b = off[e + 1];
+  auto read = [&](int e0) {
+    const int e = min(e0 + lane, experts - 1);
+    a = off[e], b = off[e + 1];
     const bool wrong = a < 0 || b < a || b > rows;
-    bad = bad || __any(wrong);
-    total += wave_add(wrong || e0 + lane >= experts ? 0 : (b - a + edge - 1) / edge);
+    mine = wrong || e0 + lane >= experts ? 0 : (b - a + edge - 1) / edge;
+    upto = wave_scan(mine);   // tiles of this and the lower lanes' experts
+    return wrong;
+  };
+  for (int e0 = 0; e0 < experts; e0 += kWave) {
+    bad = __any(read(e0)) || bad;
+    total += __builtin_amdgcn_readlane(upto, kWave - 1);
   }
   r.bad = bad;
-  total = __builtin_amdgcn_readfirstlane(total);   // the same in all lanes: what follows from it is scalar
   const int tile = tile_of(total * n_tiles);
   if (bad || tile >= total * n_tiles) return r;
   const TileAt t = tile_at(xcd_remap(tile, total * n_tiles), total, n_tiles);
   const int want = t.m;
   int before = 0;
   for (int e0 = 0; e0 < experts; e0 += kWave) {
-    const int e = min(e0 + lane, experts - 1), a = off[e], b = off[e + 1];
-    const int mine = e0 + lane >= experts ? 0 : (b - a + edge - 1) / edge;
-    int upto = mine;   // tiles of this and the lower lanes' experts
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int v = __shfl_up(upto, o, kWave);
-      if (lane >= o) upto += v;
-    }
+    if (experts > kWave) read(e0);
     const unsigned long long m = __ballot(before + upto > want);
     if (m) {
       const int at = __builtin_ctzll(m);
       r.e = e0 + at;
-      r.m0 = __shfl(a, at, kWave) + (want - before - __shfl(upto - mine, at, kWave)) * edge;
-      r.m_end = __shfl(b, at, kWave);
+      r.m0 = __builtin_amdgcn_readlane(a, at) + (want - before - __builtin_amdgcn_readlane(upto - mine, at)) * edge;
+      r.m_end = __builtin_amdgcn_readlane(b, at);
       break;
     }
-    before += __shfl(upto, kWave - 1, kWave);
+    before += __builtin_amdgcn_readlane(upto, kWave - 1);
   }
   r.e = __builtin_amdgcn_readfirstlane(r.e);
   r.m0 = __builtin_amdgcn_readfirstlane(r.m0);
