@@ -1,6 +1,7 @@
 // What the products grouped by expert share: where an expert's rows are, and which tile is a workgroup's (gfx950 only).
 #pragma once
 
+#include "lanes.hpp"
 #include "tn_tile.hpp"
 
 namespace gear {
@@ -19,18 +20,6 @@ struct ExpertTile {
 // 17408 x 1024 x 1152 bf16 (32 tiles left) 46.3 / 41.6, 20480 x 1024 x 1152 (128) 47.7 / 43.5, 9216 x 2048 x 4096 (64) 145 / 133; with
 // about 150 left, 16384 x 1152 x 1024 by 8 experts, 44.7 / 47.5.
 constexpr int kSlots = 512, kHalved = kSlots / 4;
-
-// sums of this and the lower lanes' v, by moves between lanes that need no LDS: within 16 lanes, then over the four
-template <int CTRL, int ROWS> __device__ __forceinline__ int add_moved(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
-__device__ __forceinline__ int wave_scan(int v) {
-  v = add_moved<0x111, 0xf>(v);   // one lane up, two, four, eight
-  v = add_moved<0x112, 0xf>(v);
-  v = add_moved<0x114, 0xf>(v);
-  v = add_moved<0x118, 0xf>(v);
-  v = add_moved<0x142, 0xa>(v);   // lane 15 to the second sixteen and 47 to the fourth
-  return add_moved<0x143, 0xc>(v);   // lane 31 to the upper half
-}
-__device__ __forceinline__ int wave_add(int v) { return __builtin_amdgcn_readlane(wave_scan(v), kWave - 1); }
 
 // whether off is a CSR index into `rows` rows; every lane of a wavefront gets the answer
 __device__ __forceinline__ bool offsets_ok(const int32_t *__restrict__ off, int experts, int rows, int lane) {

@@ -17,7 +17,7 @@
 // with the same runs finds from all counts where each run's pairs begin, ranks them (equal experts in a wavefront by ballots,
 // wavefronts in order) and writes their places.  Batches of one run are both in one launch.  No atomic decides an order: those on
 // counts in LDS only add.
-#include "gear_internal.hpp"
+#include "lanes.hpp"
 
 #include <cmath>
 #include <type_traits>
@@ -208,8 +208,8 @@ struct Slice {
   int64_t begin, end;
   int e[AHEAD];
   __device__ __forceinline__ Slice(const RouteArgs &a, int64_t first, int64_t last) {
-    const int wave = threadIdx.x / kWave, waves = min((int)blockDim.x / kWave, rankers_of(a.experts));
-    const int64_t pairs = (last - first) * a.k, per = (pairs + waves - 1) / waves;
+    const unsigned wave = threadIdx.x / kWave, waves = min((int)blockDim.x / kWave, rankers_of(a.experts));
+    const unsigned pairs = (unsigned)(last - first) * (unsigned)a.k, per = (pairs + waves - 1) / waves;   // at most 2^30 / 256 rows of 32
     begin = first * a.k + min(wave * per, pairs);
     end = wave < waves ? first * a.k + min((wave + 1) * per, pairs) : begin;
   }
@@ -231,17 +231,12 @@ __device__ __forceinline__ void places(const RouteArgs &a, int run, Slice &slice
     int begin = 0;
     for (int e0 = 0; e0 < E; e0 += kWave) {
       const int e = e0 + lane, mine = e < E ? s_all[e] : 0;
-      int upto = mine;
-#pragma unroll
-      for (int o = 1; o < kWave; o <<= 1) {
-        const int v = __shfl_up(upto, o, kWave);
-        if (lane >= o) upto += v;
-      }
+      const int upto = wave_scan(mine);
       if (e < E) {
         s_base[e] += begin + upto - mine;
         if (run == 0) a.off[e] = begin + upto - mine;
       }
-      begin += __shfl(upto, kWave - 1, kWave);
+      begin += __builtin_amdgcn_readlane(upto, kWave - 1);
     }
     if (run == 0 && lane == 0) a.off[E] = begin;
   }
