@@ -389,23 +389,29 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
 
   float lg[V];
   auto load = [&](int64_t row) {
+    const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+    auto four = [&](int v) {
+      if constexpr (sizeof(T) == 4) {
+        const float4 f = *reinterpret_cast<const float4 *>(x + index(v));
+        lg[v] = f.x, lg[v + 1] = f.y, lg[v + 2] = f.z, lg[v + 3] = f.w;
+      } else {
+        const uint2 f = *reinterpret_cast<const uint2 *>(x + index(v));
+        lg[v] = __uint_as_float(f.x << 16), lg[v + 1] = __uint_as_float(f.x & 0xffff0000u);
+        lg[v + 2] = __uint_as_float(f.y << 16), lg[v + 3] = __uint_as_float(f.y & 0xffff0000u);
+      }
+    };
+    if (WIDE && E == MAX_E && __all(row < used)) {   // the whole wavefront: nothing to fill in
+#pragma unroll
+      for (int v = 0; v < V; v += 4) four(v);
+      return;
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) lg[v] = -INFINITY;
     if (row >= used) return;
-    const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     if constexpr (WIDE) {
 #pragma unroll
       for (int v = 0; v < V; v += 4)
-        if (index(v) < E) {
-          if constexpr (sizeof(T) == 4) {
-            const float4 f = *reinterpret_cast<const float4 *>(x + index(v));
-            lg[v] = f.x, lg[v + 1] = f.y, lg[v + 2] = f.z, lg[v + 3] = f.w;
-          } else {
-            const uint2 f = *reinterpret_cast<const uint2 *>(x + index(v));
-            lg[v] = __uint_as_float(f.x << 16), lg[v + 1] = __uint_as_float(f.x & 0xffff0000u);
-            lg[v + 2] = __uint_as_float(f.y << 16), lg[v + 3] = __uint_as_float(f.y & 0xffff0000u);
-          }
-        }
+        if (index(v) < E) four(v);
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v)
@@ -516,20 +522,27 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
         if (!(keep >> (min(index(v), E - 1) / (E / a.groups)) & 1)) value[v] = -INFINITY;
     }
     if (row0 + teams < last) load(row + teams);     // on their way while these are sorted
-    float high = -INFINITY;
+    // The least of the largest values of all lanes, or of all lanes' halves, is reached by LPR values, or twice as many: more than the k + 1 that a list of eight is
+    // about.  Where there is no value in one of these, or k is larger, nobody eligible lies below the bound.
+    constexpr int PART = LPR > kList ? V : V / 2;
+    float high = -INFINITY, bound = INFINITY;
 #pragma unroll
-    for (int v = 0; v < V; ++v) high = fmaxf(high, value[v]);
-    // Every lane's largest is at least the bound: LPR values are.  Where these are no more than the k + 1 that matter, or a lane has none, nobody
-    // eligible lies below the bound.
-    constexpr bool ENOUGH = FEW && LPR > kList;
-    float bound = team_min<LPR>(high);
+    for (int p = 0; p < V; p += PART) {
+      float most = -INFINITY;
+#pragma unroll
+      for (int v = p; v < p + PART; ++v) most = fmaxf(most, value[v]);
+      high = fmaxf(high, most);
+      bound = fminf(bound, most);
+    }
+    bound = team_min<LPR>(bound);
     high = team_max<LPR>(high);
-    if (!ENOUGH || __any(!(bound > -INFINITY))) {
+    if (!FEW || __any(!(bound > -INFINITY))) {
+      asm volatile("" ::: "memory");   // a branch, not a choice of results
       float low = INFINITY;
 #pragma unroll
       for (int v = 0; v < V; ++v) low = fminf(low, value[v] > -INFINITY ? value[v] : INFINITY);
       low = team_min<LPR>(low);
-      if (!ENOUGH || !(bound > -INFINITY)) bound = low;
+      if (!FEW || !(bound > -INFINITY)) bound = low;
     }
     const float range = high - bound, steps = fminf(Num::STEPS / range, 0x1p127f);   // range 0: those below are still below 1
     int number[V];
