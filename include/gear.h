@@ -520,7 +520,7 @@ typedef struct {
 } gear_route_backward_args;
 gear_status gear_route_backward(const gear_route_backward_args *a, void *stream);
 
-/* Rows to their experts: xs[place[r, j]] = x[r], a copy for every slot that has a place.  xs [rows * k x dim] of x's type.  Rows of xs that
+/* Rows to their experts: xs[place[r, j]] = x[r], a copy for every slot that has a place.  xs [rows * k x dim] of x's type shares no memory with x.  Rows of xs that
  * are nobody's place (from off[experts] on) are left as they were.  Places outside [0, rows * k) are taken for none, here and below;
  * places other than gear_route's have to be distinct.  rows * k is at most 2^30. */
 gear_status gear_expert_gather(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t dim, const int32_t *place, int32_t k,
@@ -529,7 +529,7 @@ gear_status gear_expert_gather(const void *x, int32_t dtype, int64_t ld_x, int64
 /* Back again: out[r] = residual[r] + sum over j of weight[r, j] y[place[r, j]], added up in fp32 in the order of the slots.  residual may
  * be NULL (nothing), weight may be NULL (1 each: the gradient of gear_expert_gather, y being that of xs and residual what flows
  * into x itself).  A slot without a place counts as a row of zeros: a NaN weight makes the row NaN, other weights nothing.
- * out may be residual itself, but not y. */
+ * out may be residual itself, but shares no memory with y. */
 typedef struct {
   int64_t rows;
   int32_t dim, k, dtype;                  /* gear_dtype of y, residual and out */
@@ -541,8 +541,9 @@ typedef struct {
 } gear_expert_combine_args;
 gear_status gear_expert_combine(const gear_expert_combine_args *a, void *stream);
 
-/* Its gradients: dy[place[r, j]] = weight[r, j] dout[r] (rows that are nobody's place are left as they were; dy may be y itself, or NULL),
- * dweight[r, j] = dout[r] . y[place[r, j]] in fp32, 0 for a slot without a place (may be NULL).  The residual's gradient is dout. */
+/* Its gradients: dy[place[r, j]] = weight[r, j] dout[r] (rows that are nobody's place are left as they were; dy may be y itself, or NULL,
+ * and shares no memory with dout), dweight[r, j] = dout[r] . y[place[r, j]] in fp32, 0 for a slot without a place (may be NULL).
+ * The residual's gradient is dout. */
 typedef struct {
   int64_t rows;
   int32_t dim, k, dtype;                  /* gear_dtype of dout, y and dy */

@@ -439,13 +439,13 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
     float value[V];
     if (scores || (a.softmax && !a.renormalise)) {
       if (a.softmax) {
-        float sum = 0.0f;
+        float sum[2] = {0.0f, 0.0f};   // half as many additions one behind the other
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           value[v] = quick_exp(lg[v] - from);
-          sum += value[v];
+          sum[v & 1] += value[v];
         }
-        inv = empty ? 0.0f : 1.0f / team_add<LPR>(sum);
+        inv = empty ? 0.0f : 1.0f / team_add<LPR>(sum[0] + sum[1]);
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) value[v] = __builtin_amdgcn_rcpf(1.0f + quick_exp(-lg[v]));
@@ -454,10 +454,10 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
       for (int v = 0; v < V; ++v) value[v] = fmaf(value[v], inv, bias[v]);
     }
     // How far apart two values of which one is v have to be, to be in their true order.  In units of 2^-23 of itself an exponential is off by 1.25 d + 1, d = top - l (its
-    // argument, the factor log2 e, the instruction), the sum by half a unit for each of V + 6 additions and by what its terms are off by on their average, at most 7 (the mean of d is
+    // argument, the factor log2 e, the instruction), the sum by half a unit for each of V / 2 + 7 additions and by what its terms are off by on their average, at most 7 (the mean of d is
     // below 4.5 whatever the scores of up to 1024 experts), the quotient and the value by 1 each: s (1.25 d + COEF), s at most |v| and the largest bias, s d at most 0.37 of
     // the largest score, `inv`.  A sigmoid is off by 2.1 2^-23 (an exponential's error times s (1 - s), an addition, the reciprocal).  And a sum with a bias is rounded.
-    constexpr float COEF = 10.0f + 0.5f * (V + 6);
+    constexpr float COEF = 10.0f + 0.5f * (V / 2 + 7);
     auto apart = [&](float v) {
       return a.softmax ? 0x1p-22f * (COEF * (fabsf(v) + most_bias) + 0.5f * inv) : 0x1.1p-21f + 0x1p-22f * fabsf(v);
     };
@@ -498,8 +498,8 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
         const float mine_best = best;
         best = team_max<LPR>(best);
         if (!(best > -INFINITY)) continue;
-        if (j == a.kept) {   // only between the last that is kept and the first that is not does the order matter
-          unsure = !(before - best > apart(before) + apart(best) + 0x1p-22f * (fabsf(before) + fabsf(best)) + (a.best == 2 ? apart(before) + apart(best) : 0.0f));
+        if (j == a.kept) {   // only between the last that is kept and the first that is not does the order matter; two scores and two biases make a sum
+          unsure = !(before - best > (a.best == 2 ? 3.0f : 1.0f) * (apart(before) + apart(best)) + 0x1p-22f * (fabsf(before) + fabsf(best)));
           continue;
         }
         before = best;
