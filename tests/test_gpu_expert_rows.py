@@ -376,8 +376,9 @@ def test_a_layer_learns_by_its_gradients(g):
     p = [t.double().requires_grad_() for t in (x, wr, w)]
     want = layer64(*p, route.expert.long())
     grads = torch.autograd.grad(want, p, dout.double())
-    # two products of 72 terms one behind the other, each (k + 8) 2 u of its magnitudes, which are at most 72 times the largest terms: 1e-5 of the largest result holds
-    # 160 u 72 / 8 of slack beside the sums of three; weight gradients add up 150 rows the same way
+    # no bound of the worst case, which every term rounded one way would reach: a sum of n <= 150 terms of either sign errs by about sqrt(n) u = 7.3e-7 of its typical
+    # size, five of them stand in a row (logits, experts, sums, dots, gradients): 3.7e-6, and an error of logits of a typical size of 2.5 is a relative one of the
+    # weights: 9e-6.  Six deviations are 5.5e-5 of a typical value, and the largest is larger.  (Each operator by itself is held to its worst case above.)
     for got, ref in ((out, want.detach()), (dx, grads[0]), (dwr, grads[1]), (dw, grads[2])):
         within(got, ref, 1e-4 * ref.abs().max())
 
