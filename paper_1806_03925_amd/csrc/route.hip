@@ -738,7 +738,8 @@ template <typename T, int LPR, int V, bool WIDE> __global__ void __launch_bounds
     }
     int e[SLOTS];
     float f[SLOTS], p[SLOTS], inner = 0.0f;
-    bool broken = false, some = false;
+    bool broken = false;
+    int chosen = 0;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       const int j = l + s * LPR;
@@ -750,10 +751,10 @@ template <typename T, int LPR, int V, bool WIDE> __global__ void __launch_bounds
       f[s] = e[s] >= 0 ? a.scale * a.dweight[row * a.k + j] : 0.0f;
       p[s] = e[s] >= 0 ? w / a.scale : 0.0f;
       inner += p[s] * f[s];
-      some |= e[s] >= 0;
+      chosen += __popcll(team_ballot<LPR>(e[s] >= 0));
     }
     broken = team_any<LPR>(broken);
-    some = team_any<LPR>(some);      // else the row is padding, whatever its logits hold, or has no expert: zeros
+    const bool some = chosen > 0;    // else the row is padding, whatever its logits hold, or has no expert: zeros
     inner = team_add<LPR>(inner);
     __syncthreads();
 #pragma unroll
@@ -761,7 +762,7 @@ template <typename T, int LPR, int V, bool WIDE> __global__ void __launch_bounds
       if (e[s] < 0) continue;
       float d = f[s];
       if (!all) {
-        if (a.renormalise) d = p[s] * (f[s] - inner);
+        if (a.renormalise) d = p[s] * (f[s] - (chosen == 1 ? f[s] : inner));   // an only one's p is 1: zero, whatever its weight was rounded to
         if (!a.softmax) {
           const float v = to_f32(x[e[s]]), t = expf(-fabsf(v)), big = 1.0f / (1.0f + t), small = t / (1.0f + t);   // of |v|: s and 1 - s
           d *= a.renormalise ? (v > 0.0f ? small : big) : big * small;

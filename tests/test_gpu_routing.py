@@ -313,6 +313,17 @@ def test_gradient_against_differences(g, score, renormalise):
     within(got, want, 1e-8 + 2 * 48 * U * 1.5 * 2 * dw.abs().sum(1, keepdim=True))
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_gradient_of_an_only_expert(g, score):
+    """Divided by itself a weight is `scale` whatever its logit is: exactly zero, from one slot or from several of which one was filled."""
+    r = gen(8)
+    logits, dw = 4 * torch.randn(700, 24, device="cuda", generator=r), 100 * torch.randn(700, 20, device="cuda", generator=r)
+    for x, k in ((logits, 1), (torch.where(torch.arange(24, device="cuda") == 7, logits, -INF), 3), (torch.where(torch.arange(24, device="cuda") == 7, logits, -INF), 20)):
+        route = g.gear_route(x, k, score, scale=1.7)
+        assert int((route.expert >= 0).sum()) == 700
+        assert (g.gear_route_backward(x, route, dw[:, :k].contiguous(), score, True, 1.7) == 0).all()
+
+
 def test_gradient_of_broken_rows(g):
     logits = torch.randn(5, 20, device="cuda", generator=gen(6))
     logits[1, 3], logits[3, 0] = math.nan, INF
