@@ -4,14 +4,15 @@ current stream and do not synchronise, and results have no autograd history: gra
 from __future__ import annotations
 
 import ctypes as C
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from .binding import (GEAR_I8, GEAR_SCORE_SIGMOID, GEAR_SCORE_SOFTMAX, _check, gear_expert_combine_args,
+from .binding import (GEAR_BF16, GEAR_F32, GEAR_I8, GEAR_SCORE_SIGMOID, GEAR_SCORE_SOFTMAX, _check, gear_expert_combine_args,
                       gear_expert_combine_backward_args, gear_i8_args, gear_route_args, gear_route_backward_args, lib)
 from .experts import _CODE, _Packed, _gpu, _matrix, _raw_stream, _refuse, _vector, _weights, _word
 
+_SIZE = {GEAR_F32: 4, GEAR_BF16: 2}
 _SCORE = {"softmax": GEAR_SCORE_SOFTMAX, "sigmoid": GEAR_SCORE_SIGMOID}
 
 
@@ -83,6 +84,31 @@ def _logits(t: torch.Tensor, where: str, name: str, dtype=None, shape=None) -> i
     return _matrix(t, _gpu(t.get_device(), where, name), where, name, dtype, shape)
 
 
+class _Lines(NamedTuple):
+    """Where a matrix lies, in bytes: `rows` lines of `width`, `apart` from one to the next."""
+    at: int
+    rows: int
+    apart: int
+    width: int
+
+
+def _lines(t: torch.Tensor, ld: int) -> _Lines:
+    size = t.element_size()
+    return _Lines(t.data_ptr(), t.shape[0], ld * size, t.shape[1] * size)
+
+
+def _apart(out: _Lines, other: _Lines, where: str, what: str, itself: bool = False) -> None:
+    """Refuses memory for a result that holds what the call reads: workgroups come in any order.  Columns of one matrix beside each other
+    are apart; itself: out may be the other one."""
+    if not out.rows or not other.rows or (itself and out == other):
+        return
+    if out.at + (out.rows - 1) * out.apart + out.width <= other.at or other.at + (other.rows - 1) * other.apart + other.width <= out.at:
+        return
+    between = (other.at - out.at) % out.apart if out.apart else 0
+    if out.apart != other.apart or between < out.width or between + other.width > out.apart:
+        _refuse(where, what)
+
+
 def gear_route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optional[torch.Tensor] = None, groups: int = 1, groups_kept: int = 1,
                group_best: int = 1, renormalise: bool = True, scale: float = 1.0, n: Optional[torch.Tensor] = None) -> Route:
     """The k experts of every row of logits [rows x experts] (float32 or bfloat16), their weights, and the order of all pairs by
@@ -118,7 +144,7 @@ def gear_route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optio
 def gear_route_backward(logits: torch.Tensor, route: Route, dweight: torch.Tensor, score: str = "softmax", renormalise: bool = True,
                         scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The gradient [rows x experts] of the logits from that of the route's weights; score, renormalise and scale as gear_route had
-    them.  `out` may not be the logits themselves."""
+    them.  `out` shares no memory with what is read."""
     where = "gear_route_backward"
     ld = _logits(logits, where, "logits")
     gpu, dtype, shape = logits.get_device(), logits.dtype, logits.shape
@@ -133,8 +159,11 @@ def gear_route_backward(logits: torch.Tensor, route: Route, dweight: torch.Tenso
         out, ld_out = torch.empty(shape, dtype=dtype, device=gpu), experts
     else:
         ld_out = _matrix(out, gpu, where, "out", dtype, shape)
-        if rows and out.data_ptr() == logits.data_ptr():
-            _refuse(where, "out may not be the logits themselves")
+        lines = _lines(out, ld_out)
+        _apart(lines, _lines(logits, ld), where, "out may not share memory with the logits")
+        words = 4 * rows * route.k
+        for p in (dweight.data_ptr(), route.p_weight, route.p_expert):
+            _apart(lines, _Lines(p, 1, words, words), where, "out may not share memory with dweight or the route")
     a = gear_route_backward_args(rows, experts, route.k, _CODE[dtype], code, 1 if renormalise else 0, scale, logits.data_ptr(), ld, route.p_expert,
                                  route.p_weight, dweight.data_ptr(), out.data_ptr(), ld_out)
     status = lib.gear_route_backward(C.byref(a), _raw_stream(gpu))
@@ -151,25 +180,21 @@ def _of_route(t: torch.Tensor, route: Route, rows: int, where: str, name: str, d
     return _matrix(t, route.gpu, where, name, dtype)
 
 
-def _not_itself(out: torch.Tensor, other: torch.Tensor, where: str, what: str) -> None:
-    if out.numel() and out.data_ptr() == other.data_ptr():
-        _refuse(where, f"{what}: rows would be read after others have been written in their place")
-
-
 def gear_expert_gather(x: torch.Tensor, route: Route, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows x dim] copied to every place that the route gives its rows: [rows * k x dim] for gear_expert_matmul with route.off.  Rows
     from route.off[experts] on are not written.  Its gradient is gear_expert_combine(dxs, route, weighted=False)."""
     where = "gear_expert_gather"
     _gpu(route.gpu, where, "the route")
     ld = _of_route(x, route, route.rows, where, "x")
-    dim, places = x.shape[1], route.rows * route.k
+    dim, places, p_x, code = x.shape[1], route.rows * route.k, x.data_ptr(), _CODE[x.dtype]
     if out is None:
         out, ld_out = torch.empty(places, dim, dtype=x.dtype, device=route.gpu), dim
     else:
         ld_out = _of_route(out, route, places, where, "out", x.dtype, dim)
-        _not_itself(out, x, where, "out may not be x")
-    status = lib.gear_expert_gather(x.data_ptr(), _CODE[x.dtype], ld, route.rows, dim, route.p_place, route.k, out.data_ptr(), ld_out,
-                                    _raw_stream(route.gpu))
+        p_out, size = out.data_ptr(), _SIZE[code]
+        if p_out < p_x + route.rows * ld * size and p_x < p_out + places * ld_out * size:     # else they are far apart: these calls are short
+            _apart(_lines(out, ld_out), _lines(x, ld), where, "out may not share memory with x")
+    status = lib.gear_expert_gather(p_x, code, ld, route.rows, dim, route.p_place, route.k, out.data_ptr(), ld_out, _raw_stream(route.gpu))
     if status:
         _check(status, where)
     return out
@@ -191,7 +216,10 @@ def gear_expert_combine(y: torch.Tensor, route: Route, weighted: bool = True, re
         out, ld_out = torch.empty(rows, dim, dtype=dtype, device=route.gpu), dim
     else:
         ld_out = _of_route(out, route, rows, where, "out", dtype, dim)
-        _not_itself(out, y, where, "out may not be y")
+        lines = _lines(out, ld_out)
+        _apart(lines, _lines(y, ld_y), where, "out may not share memory with y")
+        if residual is not None:
+            _apart(lines, _lines(residual, ld_r), where, "out may be residual itself, but not share a part of its memory", True)
     a = gear_expert_combine_args(rows, dim, route.k, _CODE[dtype], y.data_ptr(), p_r, route.p_place, route.p_weight if weighted else None, out.data_ptr(),
                                  ld_y, ld_r, ld_out)
     status = lib.gear_expert_combine(C.byref(a), _raw_stream(route.gpu))
@@ -209,17 +237,26 @@ def gear_expert_combine_backward(dout: torch.Tensor, y: torch.Tensor, route: Rou
     rows, places = route.rows, route.rows * route.k
     ld_dout = _of_route(dout, route, rows, where, "dout")
     dtype, dim = dout.dtype, dout.shape[1]
+    code = _CODE[dtype]
     ld_y = _of_route(y, route, places, where, "y", dtype, dim)
     if dy is None:
         dy, ld_dy = torch.empty(places, dim, dtype=dtype, device=route.gpu), dim
     else:
         ld_dy = _of_route(dy, route, places, where, "dy", dtype, dim)
-        _not_itself(dy, dout, where, "dy may not be dout")
+        size = _SIZE[code]
+        p_dy, p_dout, p_y, n = dy.data_ptr(), dout.data_ptr(), y.data_ptr(), places * ld_dy * size
+        if p_dy < p_dout + rows * ld_dout * size and p_dout < p_dy + n:
+            _apart(_lines(dy, ld_dy), _lines(dout, ld_dout), where, "dy may not share memory with dout")
+        if p_dy < p_y + places * ld_y * size and p_y < p_dy + n:
+            _apart(_lines(dy, ld_dy), _lines(y, ld_y), where, "dy may be y itself, but not share a part of its memory", True)
     if dweight is None:
         dweight = torch.empty(rows, route.k, dtype=torch.float32, device=route.gpu)
     else:
         _vector(dweight, route.gpu, where, "dweight", torch.float32, places)
-    a = gear_expert_combine_backward_args(rows, dim, route.k, _CODE[dtype], dout.data_ptr(), y.data_ptr(), route.p_place, route.p_weight, dy.data_ptr(),
+        lines = _Lines(dweight.data_ptr(), 1 if places else 0, 4 * places, 4 * places)
+        for other in (_lines(dout, ld_dout), _lines(y, ld_y), _lines(dy, ld_dy), lines._replace(at=route.p_weight), lines._replace(at=route.p_place)):
+            _apart(lines, other, where, "dweight may not share memory with another matrix or the route")
+    a = gear_expert_combine_backward_args(rows, dim, route.k, code, dout.data_ptr(), y.data_ptr(), route.p_place, route.p_weight, dy.data_ptr(),
                                           dweight.data_ptr(), ld_dout, ld_y, ld_dy)
     status = lib.gear_expert_combine_backward(C.byref(a), _raw_stream(route.gpu))
     if status:
@@ -272,6 +309,10 @@ def _rows_i8(x: torch.Tensor, ld: int, rows: int, place: Optional[int], k: int, 
         out = RowsI8.empty(rows * k, dim, gpu)
     elif out.dim != dim or out.rows != rows * k or out.gpu != gpu:
         _refuse(where, "out has another shape than the rows or is on another GPU")
+    else:
+        lines = _lines(x, ld)
+        _apart(_Lines(out.p_q, out.rows, out.ld, out.ld), lines, where, "out may not share memory with x")
+        _apart(_Lines(out.p_scale, 1, 4 * out.rows, 4 * out.rows), lines, where, "out may not share memory with x")
     status = lib.gear_rows_i8(x.data_ptr(), _CODE[x.dtype], ld, rows, dim, place, k, out.p_q, out.p_scale, _raw_stream(gpu))
     if status:
         _check(status, where)

@@ -165,6 +165,34 @@ def test_results_in_the_place_of_rows_still_to_be_read_are_refused(g):
             call()
 
 
+def test_results_that_share_a_part_of_what_is_read_are_refused(g):
+    room = torch.randn(9, 64, device="cuda")
+    a, b, c = room[:6], room[1:7], room.view(-1)[16:16 + 6 * 64].view(6, 64)
+    logits = torch.randn(6, 3, device="cuda")
+    route = g.gear_route(logits, 1)
+    wide = torch.randn(6, 192, device="cuda")
+    dense = g.gear_route(logits, 3)
+    dw = torch.randn(6, 3, device="cuda")
+    for call in (lambda: g.gear_expert_gather(a, route, out=b), lambda: g.gear_expert_gather(a, route, out=c), lambda: g.gear_expert_combine(b, route, out=a),
+                 lambda: g.gear_expert_combine(a.clone(), route, residual=a, out=b), lambda: g.gear_expert_combine(a.clone(), route, residual=c, out=a),
+                 lambda: g.gear_expert_combine_backward(a, a.clone(), route, dy=b), lambda: g.gear_expert_combine_backward(a.clone(), a, route, dy=c),
+                 lambda: g.gear_expert_combine_backward(a, a.clone(), route, dweight=room.view(-1)[:6].view(6, 1)),
+                 lambda: g.gear_expert_combine_backward(a, a.clone(), route, dweight=route.weight),
+                 lambda: g.gear_expert_gather(wide[:, :64], route, out=wide[:, 32:96]),
+                 lambda: g.gear_route_backward(logits, dense, dw, out=dw), lambda: g.gear_route_backward(logits, dense, dw, out=dense.weight),
+                 lambda: g.gear_rows_i8(a, out=g.RowsI8(room.view(-1)[64:64 + 6 * 32].view(torch.int8).view(6, 128), torch.empty(6, device="cuda"), 64)),
+                 lambda: g.gear_rows_i8(a, out=g.RowsI8(torch.empty(6, 128, dtype=torch.int8, device="cuda"), room.view(-1)[:6], 64))):
+        with pytest.raises(g.GearError):
+            call()
+    # columns of one matrix, and parts of one allocation one behind the other
+    x = wide[:, :64].clone()
+    want = g.gear_expert_gather(x, route)
+    assert torch.equal(g.gear_expert_gather(wide[:, :64], route, out=wide[:, 64:128]), want)
+    assert torch.equal(g.gear_expert_combine(wide[:, 64:128], route, weighted=False, out=wide[:, 128:]), x)
+    both = torch.cat([x, x])
+    assert torch.equal(g.gear_expert_gather(both[:6], route, out=both[6:]), want)
+
+
 # ---- 8-bit integers -------------------------------------------------------------------------------------------------
 def integers(v):
     """q and scale from the definition, 64 bits: floor, remainder and parity instead of a rounding."""

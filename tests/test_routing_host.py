@@ -1,9 +1,11 @@
 """What rows that choose their experts, and products in 8-bit integers, check on the host: no GPU is needed to be refused."""
 import ctypes as C
+import itertools
 
 import pytest
 
 from paper_1806_03925_amd import binding as b
+from paper_1806_03925_amd import routing
 
 INVALID, CAPACITY, OK = b.GEAR_ERR_INVALID, b.GEAR_ERR_CAPACITY, b.GEAR_OK
 P = 1 << 20        # an address that is aligned and never used: every call below is refused before it could be
@@ -150,3 +152,25 @@ def test_the_other_products_do_not_take_integers():
     assert b.lib.gear_packed_weights_bytes(b.GEAR_I8, 1, 8, 8, 0) == 0
     a = b.gear_expert_args(dtype=b.GEAR_I8, out_dtype=1, rows=4, K=64, N=72, experts=1, x=P, packed=P, out=P, ld_x=128, ld_out=72)
     assert b.lib.gear_expert_product(C.byref(a), None) == INVALID
+
+
+def test_memory_of_results_is_apart_from_what_is_read():
+    """Every byte listed: nothing that shares one is let through, and of one distance between rows nothing that shares none is refused."""
+    def lines(at, rows, apart, width):
+        return routing._Lines(at, rows, apart, width), {at + r * apart + i for r in range(rows) for i in range(width)}
+
+    def refused(*a):
+        try:
+            routing._apart(*a)
+            return False
+        except b.GearError:
+            return True
+    some = [lines(at, rows, apart, width) for at, rows, (apart, width) in itertools.product(range(100, 131, 3), (0, 1, 3), ((0, 4), (4, 4), (9, 3), (9, 6)))]
+    for (out, mine), (other, its) in itertools.product(some, some):
+        shared = bool(mine & its)
+        assert refused(out, other, "", "") >= shared
+        if out.apart == other.apart > 0 and not shared:
+            # a row that wraps round the distance is refused though it may lie beyond the other's last one
+            between = (other.at - out.at) % out.apart
+            assert not refused(out, other, "", "") or between < out.width or between + other.width > out.apart
+        assert refused(out, other, "", "", True) == (refused(out, other, "", "") and out != other)
