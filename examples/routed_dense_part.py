@@ -54,8 +54,8 @@ class RoutedDensePart:
         f, _ = self.rows_of(ids, n)
         h = g.gear_rmsnorm(f, self.gain[0], EPS).y
         _, route = self.choose(h, n)
-        y = g.gear_matmul_i8(g.gear_expert_gather_i8(h, route), self.serve_A, route.off)
-        u = g.gear_expert_combine(y, route, residual=f)
+        y = g.gear_matmul_i8(g.gear_expert_gather_i8(h, route), self.serve_A, route.off, out_dtype=torch.float32)
+        u = g.gear_expert_combine(y, route, residual=f, out_dtype=f.dtype)       # one rounding, of the sum
         return g.gear_matmul_i8(g.gear_rows_i8(g.gear_rmsnorm(u, self.gain[1], EPS).y), self.serve_B, out_dtype=dtype)
 
     def gradients(self, ids: torch.Tensor, dfv_grads: torch.Tensor, n: torch.Tensor):

@@ -529,10 +529,12 @@ gear_status gear_expert_gather(const void *x, int32_t dtype, int64_t ld_x, int64
 /* Back again: out[r] = residual[r] + sum over j of weight[r, j] y[place[r, j]], added up in fp32 in the order of the slots.  residual may
  * be NULL (nothing), weight may be NULL (1 each: the gradient of gear_expert_gather, y being that of xs and residual what flows
  * into x itself).  A slot without a place counts as a row of zeros: a NaN weight makes the row NaN, other weights nothing.
- * out may be residual itself, but shares no memory with y. */
+ * out may be residual itself, but shares no memory with y.  y may be fp32 where residual and out are bf16: products that come in fp32 (the out_dtype of
+ * gear_expert_product and gear_product_i8) are then rounded once, as a part of the sum, and not each by itself before it. */
 typedef struct {
   int64_t rows;
-  int32_t dim, k, dtype;                  /* gear_dtype of y, residual and out */
+  int32_t dim, k, dtype;                  /* gear_dtype of residual and out, and of y unless y_f32 */
+  int32_t y_f32;                          /* y is fp32, whatever dtype is */
   const void *y, *residual;
   const int32_t *place;
   const float *weight;

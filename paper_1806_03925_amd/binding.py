@@ -112,8 +112,8 @@ class gear_route_backward_args(C.Structure):
 
 
 class gear_expert_combine_args(C.Structure):
-    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("y", C.c_void_p), ("residual", C.c_void_p),
-                ("place", C.c_void_p), ("weight", C.c_void_p), ("out", C.c_void_p), ("ld_y", C.c_int64), ("ld_residual", C.c_int64),
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("y_f32", C.c_int32), ("y", C.c_void_p),
+                ("residual", C.c_void_p), ("place", C.c_void_p), ("weight", C.c_void_p), ("out", C.c_void_p), ("ld_y", C.c_int64), ("ld_residual", C.c_int64),
                 ("ld_out", C.c_int64)]
 
 

@@ -73,7 +73,7 @@ struct CombineArgs {
   float one_over;
   int64_t chunks;
 };
-template <typename T> __global__ void __launch_bounds__(kPieceThreads) k_combine(CombineArgs args) {
+template <typename T, typename Y> __global__ void __launch_bounds__(kPieceThreads) k_combine(CombineArgs args) {   // Y: y's type
   const gear_expert_combine_args &a = args.a;
   for (int64_t chunk = blockIdx.x; chunk < args.chunks; chunk += gridDim.x) {
     const Piece t = piece_of(chunk, a.dim / 8, args.one_over);
@@ -85,7 +85,7 @@ template <typename T> __global__ void __launch_bounds__(kPieceThreads) k_combine
     for (int j0 = 0; j0 < a.k; j0 += 4) {   // four places on their way at a time
       int64_t p[4];
       float w[4];
-      Raw8<T> y[4];
+      Raw8<Y> y[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int64_t pair = t.row * a.k + j0 + j;
@@ -96,7 +96,7 @@ template <typename T> __global__ void __launch_bounds__(kPieceThreads) k_combine
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         y[j].zero();
-        if (p[j] >= 0) y[j].load(static_cast<const T *>(a.y) + p[j] * a.ld_y + t.c);
+        if (p[j] >= 0) y[j].load(static_cast<const Y *>(a.y) + p[j] * a.ld_y + t.c);
       }
       if (j0 == 0) res.get(sum);
 #pragma unroll
@@ -399,10 +399,13 @@ extern "C" gear_status gear_expert_combine(const gear_expert_combine_args *a, vo
     return GEAR_ERR_INVALID;
   if (a->residual && !matrix_ok(a->residual, a->ld_residual, a->dim)) return GEAR_ERR_INVALID;
   const CombineArgs args = {*a, 8.0f / (float)a->dim, chunks_of(a->rows, a->dim)};
+  const dim3 grid(grid_of(args.chunks)), block(kPieceThreads);
   if (a->dtype == GEAR_F32)
-    hipLaunchKernelGGL(k_combine<float>, dim3(grid_of(args.chunks)), dim3(kPieceThreads), 0, (hipStream_t)stream, args);
+    hipLaunchKernelGGL((k_combine<float, float>), grid, block, 0, (hipStream_t)stream, args);
+  else if (a->y_f32)
+    hipLaunchKernelGGL((k_combine<bf16_t, float>), grid, block, 0, (hipStream_t)stream, args);
   else
-    hipLaunchKernelGGL(k_combine<bf16_t>, dim3(grid_of(args.chunks)), dim3(kPieceThreads), 0, (hipStream_t)stream, args);
+    hipLaunchKernelGGL((k_combine<bf16_t, bf16_t>), grid, block, 0, (hipStream_t)stream, args);
   return hipGetLastError() == hipSuccess ? GEAR_OK : GEAR_ERR_HIP;
 }
 

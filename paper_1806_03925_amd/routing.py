@@ -201,14 +201,19 @@ def gear_expert_gather(x: torch.Tensor, route: Route, out: Optional[torch.Tensor
 
 
 def gear_expert_combine(y: torch.Tensor, route: Route, weighted: bool = True, residual: Optional[torch.Tensor] = None,
-                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+                        out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """The way back: residual + the sum of the rows' places in y [rows * k x dim], each times its weight (weighted=False: 1).  out
-    may be residual itself."""
+    may be residual itself.  Both are of y's type, or bfloat16 for y in float32 where out_dtype says so: products in float32 are then rounded
+    once, in the sum, and not each before it."""
     where = "gear_expert_combine"
     _gpu(route.gpu, where, "the route")
     rows, places = route.rows, route.rows * route.k
     ld_y = _of_route(y, route, places, where, "y")
-    dtype, dim = y.dtype, y.shape[1]
+    dim = y.shape[1]
+    dtype = out_dtype or y.dtype
+    y_f32 = dtype is not y.dtype
+    if y_f32 and (dtype is not torch.bfloat16 or y.dtype is not torch.float32):
+        _refuse(where, f"out_dtype has to be y's type, or bfloat16 for y in float32, not {dtype} for {y.dtype}")
     ld_r, p_r = 0, None
     if residual is not None:
         ld_r, p_r = _of_route(residual, route, rows, where, "residual", dtype, dim), residual.data_ptr()
@@ -220,8 +225,8 @@ def gear_expert_combine(y: torch.Tensor, route: Route, weighted: bool = True, re
         _apart(lines, _lines(y, ld_y), where, "out may not share memory with y")
         if residual is not None:
             _apart(lines, _lines(residual, ld_r), where, "out may be residual itself, but not share a part of its memory", True)
-    a = gear_expert_combine_args(rows, dim, route.k, _CODE[dtype], y.data_ptr(), p_r, route.p_place, route.p_weight if weighted else None, out.data_ptr(),
-                                 ld_y, ld_r, ld_out)
+    a = gear_expert_combine_args(rows, dim, route.k, _CODE[dtype], y_f32, y.data_ptr(), p_r, route.p_place, route.p_weight if weighted else None,
+                                 out.data_ptr(), ld_y, ld_r, ld_out)
     status = lib.gear_expert_combine(C.byref(a), _raw_stream(route.gpu))
     if status:
         _check(status, where)

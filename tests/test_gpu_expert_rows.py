@@ -449,3 +449,57 @@ def test_a_layer_serves_in_integers(g):
         # a product in bf16 (half a step and 5 u: the scales are fp32 themselves), the sum, and its rounding
         within(out, chosen.sum(1), HALF[BF16] * chosen.sum(1).abs() + (HALF[BF16] + (k + 8) * U) * 1.01 * chosen.abs().sum(1))
     assert int(g.gear_expert_status()) == g.GEAR_OK
+
+
+@pytest.mark.parametrize("rows,dim,k,experts", SHAPES)
+def test_combine_of_products_in_fp32(g, rows, dim, k, experts):
+    """Products that were not rounded on their way to a bf16 sum: one rounding in all, that of the result."""
+    r = gen(dim + k)
+    y = torch.randn(rows * k, dim, device="cuda", generator=r)
+    res = torch.randn(rows, dim, device="cuda", generator=r).to(BF16)
+    route = routed(g, rows, k, experts, rows)
+    there, row, place = pairs_of(route)
+    y[int(route.off[-1]):] = math.nan                        # nobody's
+    for weighted, residual in itertools.product((True, False), (None, res)):
+        w = route.weight.flatten()[there].double()[:, None] if weighted else 1.0
+        want = torch.zeros(rows, dim, dtype=torch.float64, device="cuda") if residual is None else residual.double()
+        size = want.abs().index_add_(0, row, (w * y[place].double()).abs())
+        want = want.index_add_(0, row, w * y[place].double())
+        got = g.gear_expert_combine(y, route, weighted=weighted, residual=residual, out_dtype=BF16)
+        assert got.dtype is BF16
+        within(got, want, (k + 2) * U * size + HALF[BF16] * want.abs())
+        out = strided(torch.zeros_like(res), 8) if residual is None else strided(residual, 24)
+        assert g.gear_expert_combine(strided(y, 16), route, weighted=weighted, residual=out if residual is not None else None, out=out, out_dtype=BF16) is out
+        assert torch.equal(out, got)
+    assert g.gear_expert_combine(y, route).dtype is F32          # said, not taken from the residual's type
+
+
+def test_combine_refuses_other_types(g):
+    x, y = torch.randn(4, 64, device="cuda"), torch.randn(8, 64, device="cuda")
+    route = g.gear_route(torch.randn(4, 6, device="cuda"), 2)
+    room = torch.zeros(12, 64, device="cuda")
+    for call in (lambda: g.gear_expert_combine(y.to(BF16), route, residual=x), lambda: g.gear_expert_combine(y.to(BF16), route, out=x),
+                 lambda: g.gear_expert_combine(y.to(BF16), route, out_dtype=F32), lambda: g.gear_expert_combine(y, route, residual=x.to(BF16), out=x),
+                 lambda: g.gear_expert_combine(y, route, residual=x.to(BF16)), lambda: g.gear_expert_combine(y, route, out=x.to(BF16)),
+                 lambda: g.gear_expert_combine(y, route, residual=x, out_dtype=BF16), lambda: g.gear_expert_combine(y, route, out=x, out_dtype=BF16),
+                 lambda: g.gear_expert_combine(y, route, residual=x.to(BF16), out_dtype=F32), lambda: g.gear_expert_combine(y, route, out_dtype=torch.float16),
+                 lambda: g.gear_expert_combine(room[:8], route, out=room[7:9].view(BF16).view(4, 64), out_dtype=BF16)):
+        with pytest.raises(g.GearError):
+            call()
+
+
+def test_a_layer_serves_with_one_rounding(g):
+    """Integers, their products and the sum in 32 bits: the result is off by its own rounding to bf16 and by what fp32 loses."""
+    rows, dim, out_dim, experts, k = 300, 136, 72, 16, 4
+    r = gen(13)
+    x, res = torch.randn(rows, dim, device="cuda", generator=r).to(BF16), torch.randn(rows, out_dim, device="cuda", generator=r).to(BF16)
+    w = torch.randn(experts, out_dim, dim, device="cuda", generator=r) * dim ** -0.5
+    route = g.gear_route(torch.randn(rows, experts, device="cuda", generator=r), k)
+    y = g.gear_matmul_i8(g.gear_expert_gather_i8(x, route), g.gear_weights_i8(w), route.off, out_dtype=F32)
+    out = g.gear_expert_combine(y, route, residual=res, out_dtype=BF16)
+    (xq, xs), (wq, ws) = integers(x), integers(w)
+    every = torch.stack([(xq * xs[:, None]) @ (wq[e] * ws[e][:, None]).t().contiguous() for e in range(experts)], 1)
+    chosen = every.gather(1, route.expert.long()[:, :, None].expand(-1, -1, out_dim)) * route.weight.double()[:, :, None]
+    want = res.double() + chosen.sum(1)
+    # 5 u of a product (its conversion, two factors, and the factors' own roundings), (k + 2) u of the sum
+    within(out, want, HALF[BF16] * want.abs() + 1.01 * (k + 7) * U * (res.double().abs() + chosen.abs().sum(1)))
