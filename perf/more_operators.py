@@ -354,8 +354,8 @@ def _called(s):
     if s.kind == "product_i8":
         return g.gear_matmul_i8(g.gear_rows_i8(s.x), s.weights, s.off)
     r = g.gear_route(s.logits, c["k"], n=s.n)
-    y = g.gear_matmul_i8(g.gear_expert_gather_i8(s.x, r), s.weights, r.off)
-    return r.expert, r.weight, g.gear_expert_combine(y, r, residual=s.residual)
+    y = g.gear_matmul_i8(g.gear_expert_gather_i8(s.x, r), s.weights, r.off, out_dtype=torch.float32)     # what is added up is not rounded before
+    return r.expert, r.weight, g.gear_expert_combine(y, r, residual=s.residual, out_dtype=s.residual.dtype)
 
 
 def run(s):
