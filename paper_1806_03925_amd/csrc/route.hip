@@ -554,13 +554,15 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
     for (int v = 0; v < V; ++v) number[v] = Num::of(value[v], bound, steps, index(v));
     Sorter<V>::sort(number);
     // x before y in the order, y somebody: is that in doubt?  Sums of scores and biases: if they are not `apart`, and three steps, which is what the
-    // way to a number costs.  Logits: if their numbers are the same but they may not be.  All are where the range is none; logits of 16 bits, which differ by
-    // 2^-8 of themselves, are unless they are next to nothing.
+    // way to a number costs.  Logits: if their numbers are the same but they may not be.  All are where the range is none.  Of 16 bits, ones whose numbers
+    // are the same are the same unless they are next to nothing, as they differ by 2^-8 of themselves, which is eight steps or more; but not where the range is so
+    // small that `steps` is cut and has fewer of them.
+    const bool uncut = range >= 0x1p-100f;
     auto doubt = [&](int x, int y) {
       const int ahead = Num::height_of(x) - Num::height_of(y);
       const float v = bound + (float)Num::height_of(x) * (range * (1.0f / Num::STEPS));
       if (a.bias) return ahead <= (int)fminf(apart(v) * steps, 0x1p24f) + 3;
-      return ahead == 0 && range != 0.0f && !(sizeof(T) == 2 && fabsf(v) > range * 0x1p-10f);
+      return ahead == 0 && range != 0.0f && !(sizeof(T) == 2 && uncut && fabsf(v) > range * 0x1p-10f);
     };
     unsure = !empty && (unsure || !(range < INFINITY));
     int chosen[SLOTS];

@@ -390,3 +390,54 @@ def test_two_streams_at_once(g):
     for w, rs in zip(want, got):
         for r in rs:
             assert torch.equal(r.expert, w.expert) and torch.equal(r.place, w.place) and torch.equal(r.off, w.off) and torch.equal(r.weight, w.weight)
+
+
+def reference_many(logits, k, score="softmax", bias=None, groups=1, groups_kept=1, group_best=1, renormalise=True, scale=1.0, n=None):
+    """What reference() gives, for long batches without NaN or +inf: sorts of whole columns in 64 bits."""
+    v = logits.double()
+    rows, experts = v.shape
+    there = torch.ones(rows, 1, dtype=torch.bool, device="cuda") if n is None else torch.arange(rows, device="cuda")[:, None] < n
+    top = torch.where(v.amax(1, keepdim=True) > -INF, v.amax(1, keepdim=True), 0.0)
+    s = torch.exp(v - top) if score == "softmax" else 1 / (1 + torch.exp(-v))
+    if score == "softmax":
+        s = s / s.sum(1, keepdim=True).clamp(min=1.0)
+    ok = (v > -INF) & there if bias is None else (v > -INF) & (bias > -INF) & there
+    value = torch.where(ok, s if bias is None else s + bias.double(), -INF)
+    order = torch.where(ok, v, -INF) if bias is None else value
+    if groups > 1:
+        best = torch.sort(value.view(rows, groups, -1), dim=2, descending=True).values[:, :, :group_best]
+        worth = torch.where((best > -INF).any(2), torch.where(best > -INF, best, 0.0).sum(2), -INF)
+        keep = torch.zeros(rows, groups, dtype=torch.bool, device="cuda")
+        keep.scatter_(1, torch.sort(worth, dim=1, descending=True, stable=True).indices[:, :groups_kept], True)
+        order = torch.where(keep.repeat_interleave(experts // groups, 1), order, -INF)
+    by = torch.sort(order, dim=1, descending=True, stable=True)
+    expert = torch.where(by.values[:, :k] > -INF, by.indices[:, :k], -1)
+    at = expert.clamp(min=0)
+    chosen = torch.where(expert >= 0, v.gather(1, at), -INF)
+    weight = torch.where(expert >= 0, s.gather(1, at), 0.0)
+    if renormalise:
+        if score == "softmax":
+            high = chosen.amax(1, keepdim=True)
+            weight = torch.where(expert >= 0, torch.exp(chosen - torch.where(high > -INF, high, 0.0)), 0.0)
+        total = weight.sum(1, keepdim=True)
+        weight = weight / torch.where(total > 0, total, 1.0)
+    far = torch.where(expert >= 0, (chosen - (top if score == "softmax" else 0.0)).abs(), 0.0)
+    line, pair = torch.sort(torch.where(expert >= 0, expert, experts).flatten(), stable=True)
+    place = torch.empty_like(pair).scatter_(0, pair, torch.arange(pair.numel(), device="cuda")).view(rows, k)
+    off = torch.searchsorted(line, torch.arange(experts + 1, device="cuda"))
+    return expert, scale * weight, torch.where(expert >= 0, place, -1), off, far
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("rows,experts,k,groups", [(40, 64, 8, 1), (40, 300, 5, 1), (40, 1000, 12, 1), (33_001, 64, 8, 1), (33_001, 256, 8, 1), (200, 160, 6, 8)])
+def test_logits_next_to_nothing(g, rows, experts, k, groups, score):
+    """bf16 logits down to the smallest denormal, one step of their type from each other: without a bias it is they that are compared, however close."""
+    r = gen(experts)
+    step = torch.arange(experts, device="cuda", dtype=torch.int16)
+    for low, high in ((0, 128), (0, 700), (128, 300), (0x300, 0x380), (0x600, 0x700), (0xb00, 0xc80), (0xd00, 0xe80)):
+        bits = torch.randint(low, high, (rows, experts), device="cuda", generator=r).to(torch.int16)
+        bits[::3] = (low + step % (high - low)).to(torch.int16)
+        bits[1::3] |= (torch.randint(0, 2, bits[1::3].shape, device="cuda", generator=r) * -32768).to(torch.int16)
+        for logits in (bits.view(BF16), bits.view(BF16).float()):
+            kw = dict(groups=groups, groups_kept=max(1, groups // 2), group_best=1)
+            check(g.gear_route(logits, k, score, **kw), reference_many(logits, k, score, **kw))
