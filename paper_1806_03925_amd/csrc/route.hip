@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
         if (index(v) < E) mine[index(v)] = !empty && fminf(lg[v], bias[v]) > -INFINITY ? value[v] : -INFINITY;
       asm volatile("" ::: "memory");   // a team is part of one wavefront, whose LDS accesses come in order
       __builtin_amdgcn_wave_barrier();
-      float worth[kMaxGroups / LPR];
+      float worth[kMaxGroups / LPR], cancelled = 0.0f;   // what vanishes where two values of a group have different signs: half of it
 #pragma unroll
       for (int i = 0; i < kMaxGroups / LPR; ++i) {
         const int q = l + i * LPR;
@@ -485,8 +485,10 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
             one = fmaxf(one, v);
           }
           worth[i] = a.best == 2 && two > -INFINITY ? one + two : one;
+          if (two > -INFINITY) cancelled = fmaxf(cancelled, fminf(one, -two));
         }
       }
+      if (a.best == 2) cancelled = team_max<LPR>(cancelled);
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
       keep = 0;
@@ -498,8 +500,10 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
         const float mine_best = best;
         best = team_max<LPR>(best);
         if (!(best > -INFINITY)) continue;
-        if (j == a.kept) {   // only between the last that is kept and the first that is not does the order matter; two scores and two biases make a sum
-          unsure = !(before - best > (a.best == 2 ? 3.0f : 1.0f) * (apart(before) + apart(best)) + 0x1p-22f * (fabsf(before) + fabsf(best)));
+        if (j == a.kept) {   // only between the last that is kept and the first that is not does the order matter; two scores and two biases make a sum,
+                             // and each of them is rounded by itself before
+          unsure = !(before - best > (a.best == 2 ? 3.0f * (apart(before) + apart(best)) + 0x1p-21f * cancelled : apart(before) + apart(best)) +
+                                         0x1p-22f * (fabsf(before) + fabsf(best)));
           continue;
         }
         before = best;

@@ -441,3 +441,18 @@ def test_logits_next_to_nothing(g, rows, experts, k, groups, score):
         for logits in (bits.view(BF16), bits.view(BF16).float()):
             kw = dict(groups=groups, groups_kept=max(1, groups // 2), group_best=1)
             check(g.gear_route(logits, k, score, **kw), reference_many(logits, k, score, **kw))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups", [(64, 8), (512, 16), (1024, 32)])
+@pytest.mark.parametrize("large", [64.0, 1e3, 2.0 ** 20])
+def test_groups_whose_largest_two_cancel(g, experts, groups, large, score):
+    """Two experts of each group are left, their biases large and opposite: what their sums in fp32 lose is a part of the biases, not of the sums."""
+    r = gen(experts)
+    per = experts // groups
+    logits = 2 * torch.randn(3000, experts, device="cuda", generator=r)
+    bias = torch.full((groups, per), -INF, device="cuda")
+    each = large * (1 + torch.arange(groups, device="cuda") / groups)       # apart, so that the choice within the groups kept is clear
+    bias[:, 1], bias[:, per - 1] = each, -each
+    kw = dict(bias=bias.flatten(), groups=groups, groups_kept=groups // 4, group_best=2)
+    check(g.gear_route(logits, 4, score, **kw), reference_many(logits, 4, score, **kw))
