@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
             two = fmaxf(two, fminf(one, v));
             one = fmaxf(one, v);
           }
-          worth[i] = a.best == 2 && two > -INFINITY ? one + two : one;
+          worth[i] = a.best == 2 && two > -INFINITY ? fmaxf(one + two, -0x1.fffffep127f) : one;   // below fp32's range is still eligible
           if (two > -INFINITY) cancelled = fmaxf(cancelled, fminf(one, -two));
         }
       }

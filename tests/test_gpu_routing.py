@@ -456,3 +456,20 @@ def test_groups_whose_largest_two_cancel(g, experts, groups, large, score):
     bias[:, 1], bias[:, per - 1] = each, -each
     kw = dict(bias=bias.flatten(), groups=groups, groups_kept=groups // 4, group_best=2)
     check(g.gear_route(logits, 4, score, **kw), reference_many(logits, 4, score, **kw))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups,kept,k", [(12, 3, 2, 6), (160, 8, 5, 16), (1024, 32, 12, 32)])
+def test_groups_parked_by_the_lowest_bias(g, experts, groups, kept, k, score):
+    """The type's lowest value for all of a group's experts: two of them are beyond fp32, but the group is still there to be chosen after the others."""
+    r = gen(experts)
+    logits = 2 * torch.randn(400, experts, device="cuda", generator=r)
+    logits[5::9, experts // 2:] = -INF
+    for value in (torch.finfo(F32).min, -2e38):
+        bias = 0.1 * torch.randn(groups, experts // groups, device="cuda", generator=r)
+        bias[::2] = value
+        bias[0, 1:] = 0.0 if groups > 3 else value
+        for best in (1, 2):
+            kw = dict(bias=bias.flatten(), groups=groups, groups_kept=kept, group_best=best)
+            check(g.gear_route(logits, k, score, **kw), reference_many(logits, k, score, **kw))
+            check(g.gear_route(logits[:9], k, score, **kw), reference(logits[:9], k, score, **kw))
