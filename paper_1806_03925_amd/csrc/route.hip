@@ -455,11 +455,11 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
     }
     // How far apart two values of which one is v have to be, to be in their true order.  In units of 2^-23 of itself an exponential is off by 1.25 d + 1, d = top - l (its
     // argument, the factor log2 e, the instruction), the sum by half a unit for each of V / 2 + 7 additions and by what its terms are off by on their average, at most 7 (the mean of d is
-    // below 4.5 whatever the scores of up to 1024 experts), the quotient and the value by 1 each: s (1.25 d + COEF), s at most |v| and the largest bias, s d at most 0.37 of
-    // the largest score, `inv`.  A sigmoid is off by 2.1 2^-23 (an exponential's error times s (1 - s), an addition, the reciprocal).  And a sum with a bias is rounded.
+    // below 4.5 whatever the scores of up to 1024 experts), the quotient and the product by 1 each: s (1.25 d + COEF), s at most |v| and the largest bias, and the
+    // largest score, `inv` (all that counts beside a bias far beyond the scores, which parks its expert: else every row would be in doubt), s d at most 0.37 of `inv`.  A sigmoid is off by 2.1 2^-23 (an exponential's error times s (1 - s), an addition, the reciprocal).  And a sum with a bias is rounded.
     constexpr float COEF = 10.0f + 0.5f * (V / 2 + 7);
     auto apart = [&](float v) {
-      return a.softmax ? 0x1p-22f * (COEF * (fabsf(v) + most_bias) + 0.5f * inv) : 0x1.1p-21f + 0x1p-22f * fabsf(v);
+      return a.softmax ? 0x1p-22f * (COEF * fminf(inv, fabsf(v) + most_bias) + 0.5f * (inv + fabsf(v))) : 0x1.1p-21f + 0x1p-22f * fabsf(v);
     };
     bool unsure = false;
     uint64_t keep = ~0ull;

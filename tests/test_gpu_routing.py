@@ -473,3 +473,21 @@ def test_groups_parked_by_the_lowest_bias(g, experts, groups, kept, k, score):
             kw = dict(bias=bias.flatten(), groups=groups, groups_kept=kept, group_best=best)
             check(g.gear_route(logits, k, score, **kw), reference_many(logits, k, score, **kw))
             check(g.gear_route(logits[:9], k, score, **kw), reference(logits[:9], k, score, **kw))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,k,groups", [(64, 8, 1), (256, 8, 1), (160, 6, 8), (700, 12, 1)])
+def test_experts_parked_by_large_biases(g, experts, k, groups, score):
+    """A bias far beyond all scores, as a finite mask, changes nothing for the others: neither their order, also where fp32 cannot tell their sums apart, nor their weights."""
+    r = gen(experts)
+    logits = 1.5 * torch.randn(4000, experts, device="cuda", generator=r)
+    row = torch.randn(experts, device="cuda", generator=r)
+    s = torch.softmax(row.double(), 0) if score == "softmax" else torch.sigmoid(row.double())
+    for close, park in itertools.product((False, True), (-1e4, -100.0, 1e4, -3e38)):
+        bias = (0.75 - s).float() if close else 0.1 / experts * torch.randn(experts, device="cuda", generator=r)
+        logits[::50] = row
+        bias[experts // 2] = park
+        if park < 0:
+            bias[experts // 2 + 1] = park
+        kw = dict(bias=bias, groups=groups, groups_kept=max(1, groups // 2), group_best=min(2, groups))
+        check(g.gear_route(logits, k, score, **kw), reference_many(logits, k, score, **kw))
