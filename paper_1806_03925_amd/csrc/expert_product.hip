@@ -68,6 +68,16 @@ __device__ __forceinline__ i32x16_v mfma_i8(i32x16_v acc, const u32x4_v &x, cons
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_v, w), __builtin_bit_cast(i32x4_v, x), acc, 0, 0, 0);
 }
 
+// A row's factor in two: sums are below 2^31, and one times a factor of 2^97 or more could be infinite though the output's factor brings the result back.  Such a
+// factor is taken 2^-32 times, and the result 2^32 times; what lies between is then below fp32's normal numbers never, and beyond them only if the result is.  (A sum times a smaller factor
+// loses nothing, however small it is: a whole number of the factor's own units.)
+struct RowFactor {
+  float factor, after;
+  __device__ __forceinline__ explicit RowFactor(float x) : factor(x), after(1.0f) {
+    if (fabsf(x) >= 0x1p96f) factor = x * 0x1p-32f, after = 0x1p32f;
+  }
+};
+
 // One unit pair (half a k-block): rows from LDS, weights b[unit][column tile] from registers.
 template <typename C, int WHICH>
 __device__ __forceinline__ void mma_half(AccOf<C::DT> (&acc)[C::WTM][TN], uint32_t addr, const u32x4_v (&b)[2][TN],
@@ -306,9 +316,14 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
   };
   if constexpr (C::DT == GEAR_I8) {
     const float *x_of = reinterpret_cast<const float *>(lds + C::TILE_BYTES), *w_of = x_of + C::X_SCALES;
-    float xr[C::WTM];
+    float xr[C::WTM], after[C::WTM];
+    bool large = false;
 #pragma unroll
-    for (int i = 0; i < C::WTM; ++i) xr[i] = x_of[wm * 32 * C::WTM + i * 32 + r];
+    for (int i = 0; i < C::WTM; ++i) {
+      const RowFactor f(x_of[wm * 32 * C::WTM + i * 32 + r]);
+      xr[i] = f.factor, after[i] = f.after;
+      large = large || f.after != 1.0f;
+    }
     f32x16_v v[C::WTM][TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j)
@@ -321,6 +336,12 @@ template <typename C, bool F32> __device__ __forceinline__ void product_tile(con
 #pragma unroll
           for (int h = 0; h < 4; ++h) v[i][j][4 * q + h] = (float)acc[i][j][4 * q + h] * xr[i] * wc[h];
       }
+    if (__any(large)) {
+#pragma unroll
+      for (int i = 0; i < C::WTM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) v[i][j] *= after[i];
+    }
     store(v);
   } else {
     store(acc);
@@ -482,7 +503,9 @@ template <typename C, bool F32> __device__ __forceinline__ void split_tile(const
     if (m < m_rows && n < a.N) {
       float4 v = make_float4((float)sum.x, (float)sum.y, (float)sum.z, (float)sum.w);
       if constexpr (DT == GEAR_I8) {
-        v.x = v.x * x_factor * w_factor.x, v.y = v.y * x_factor * w_factor.y, v.z = v.z * x_factor * w_factor.z, v.w = v.w * x_factor * w_factor.w;
+        const RowFactor f(x_factor);
+        v.x = v.x * f.factor * w_factor.x * f.after, v.y = v.y * f.factor * w_factor.y * f.after;
+        v.z = v.z * f.factor * w_factor.z * f.after, v.w = v.w * f.factor * w_factor.w * f.after;
       }
       if constexpr (F32)
         *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + (m0 + m) * a.ld_out + n) = v;

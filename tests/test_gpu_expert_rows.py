@@ -503,3 +503,29 @@ def test_a_layer_serves_with_one_rounding(g):
     want = res.double() + chosen.sum(1)
     # 5 u of a product (its conversion, two factors, and the factors' own roundings), (k + 2) u of the sum
     within(out, want, HALF[BF16] * want.abs() + 1.01 * (k + 7) * U * (res.double().abs() + chosen.abs().sum(1)))
+
+
+@pytest.mark.parametrize("rows,n,k,experts", [(1, 72, 136, 0), (5, 1024, 4096, 0), (33, 520, 576, 16), (300, 1024, 1152, 0), (1500, 1024, 3200, 3), (4096, 2048, 128, 7)])
+@pytest.mark.parametrize("x_power,w_power", [(122, -100), (122, -140), (-140, 110), (-148, 120), (-60, -60), (100, 20), (0, -149)])
+def test_products_of_extreme_scales(g, rows, n, k, experts, x_power, w_power):
+    """Scales that take sums times one of them out of fp32's range, while the result is an ordinary number (or one beyond the range, or next to nothing)."""
+    r = gen(rows + n + k)
+    e = max(1, experts)
+    q = torch.randint(-127, 128, (rows, (k + 127) // 128 * 128), device="cuda", generator=r).to(torch.int8)
+    q[:, k:] = 0
+    w = torch.randint(-127, 128, (e, n, k), device="cuda", generator=r).to(torch.int8)
+    power = lambda p, *shape: (torch.exp2(torch.rand(*shape, device="cuda", dtype=torch.float64, generator=r)) * 2.0 ** p).float()
+    x_scale, w_scale = power(x_power, rows), power(w_power, e, n)
+    x_scale[rows // 2], w_scale[0, n // 2] = 0.75, 0.75       # ordinary ones among them
+    bounds = [0] + sorted(torch.randint(0, rows + 1, (e - 1,), generator=torch.Generator().manual_seed(rows)).tolist()) + [rows]
+    off = torch.tensor(bounds, dtype=torch.int32, device="cuda") if experts else None
+    rows8, weights = g.RowsI8(q, x_scale, k), g.gear_weights_i8(w, w_scale)
+    for dtype in (F32, BF16):
+        out = g.gear_matmul_i8(rows8, weights, off, out_dtype=dtype)
+        want = torch.cat([(q[a:b, :k].double() @ w[i].double().t().contiguous()) * (x_scale[a:b, None].double() * w_scale[i].double())
+                          for i, (a, b) in enumerate(zip(bounds, bounds[1:]))])
+        half, least = (HALF[BF16], 2.0 ** -133) if dtype is BF16 else (0.0, 2.0 ** -149)
+        most = torch.finfo(dtype).max
+        edge = (want.abs() > most * (1 - 2.0 ** -6))          # may round to infinity or not
+        assert torch.where(edge & (want.abs() > most * (1 + 2.0 ** -6)), out.double() == want.sign() * math.inf, True).all()
+        within(torch.where(edge, 0.0, out), torch.where(edge, 0.0, want), torch.where(edge, 0.0, (3.01 * U + half) * want.abs() + least))
