@@ -92,6 +92,7 @@ template <typename T, typename Y> __global__ void __launch_bounds__(kPieceThread
         const bool in = j0 + j < a.k;
         p[j] = in ? place_of(a.place, pair, a.rows * a.k) : -1;
         w[j] = !in ? 0.0f : a.weight ? a.weight[pair] : 1.0f;
+        if (p[j] < 0 && w[j] == w[j]) w[j] = 0.0f;          // not an infinity times the zeros of no place; a NaN stays
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {

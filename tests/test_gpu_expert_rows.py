@@ -529,3 +529,18 @@ def test_products_of_extreme_scales(g, rows, n, k, experts, x_power, w_power):
         edge = (want.abs() > most * (1 - 2.0 ** -6))          # may round to infinity or not
         assert torch.where(edge & (want.abs() > most * (1 + 2.0 ** -6)), out.double() == want.sign() * math.inf, True).all()
         within(torch.where(edge, 0.0, out), torch.where(edge, 0.0, want), torch.where(edge, 0.0, (3.01 * U + half) * want.abs() + least))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_infinite_weights_without_a_place_are_nothing(g, dtype):
+    """Only a program's own weights can be infinite; at a slot without a place they add no more than any other number."""
+    x = torch.randn(5, 64, device="cuda", generator=gen(2)).to(dtype)
+    place = torch.tensor([[0, -1], [-1, 1], [10, 2], [-1, -1], [3, -1]], dtype=torch.int32, device="cuda")
+    weight = torch.tensor([[1.0, math.inf], [-math.inf, 2.0], [math.inf, 1.0], [math.inf, -math.inf], [1.0, math.nan]], device="cuda")
+    route = g.Route(place.clamp(max=0), weight, place, torch.tensor([0, 4], dtype=torch.int32, device="cuda"))
+    y = torch.randn(10, 64, device="cuda", generator=gen(3)).to(dtype)
+    out = g.gear_expert_combine(y, route, residual=x)
+    factor = torch.tensor([1.0, 2.0, 1.0, 0.0], dtype=torch.float64, device="cuda")[:, None]
+    want = x[:4].double() + factor * y[[0, 1, 2, 0]].double()
+    within(out[:4], want, 4 * U * (x[:4].double().abs() + (factor * y[[0, 1, 2, 0]].double()).abs()) + HALF[dtype] * want.abs())
+    assert torch.equal(out[3], x[3]) and out[4].isnan().all()
