@@ -520,7 +520,7 @@ typedef struct {
 } gear_route_backward_args;
 gear_status gear_route_backward(const gear_route_backward_args *a, void *stream);
 
-/* Rows to their experts: xs[place[r, j]] = x[r], a copy for every slot that has a place.  xs [rows * k x dim] of x's type shares no memory with x.  Rows of xs that
+/* Rows to their experts: xs[place[r, j]] = x[r], a copy for every slot that has a place.  xs [rows * k x dim] of x's type shares no memory with x or place.  Rows of xs that
  * are nobody's place (from off[experts] on) are left as they were.  Places outside [0, rows * k) are taken for none, here and below;
  * places other than gear_route's have to be distinct.  rows * k is at most 2^30. */
 gear_status gear_expert_gather(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t dim, const int32_t *place, int32_t k,
@@ -529,7 +529,7 @@ gear_status gear_expert_gather(const void *x, int32_t dtype, int64_t ld_x, int64
 /* Back again: out[r] = residual[r] + sum over j of weight[r, j] y[place[r, j]], added up in fp32 in the order of the slots.  residual may
  * be NULL (nothing), weight may be NULL (1 each: the gradient of gear_expert_gather, y being that of xs and residual what flows
  * into x itself).  A slot without a place counts as a row of zeros: a NaN weight makes the row NaN, other weights nothing.
- * out may be residual itself, but shares no memory with y.  y may be fp32 where residual and out are bf16: products that come in fp32 (the out_dtype of
+ * out may be residual itself, but shares no memory with y, place or weight.  y may be fp32 where residual and out are bf16: products that come in fp32 (the out_dtype of
  * gear_expert_product and gear_product_i8) are then rounded once, as a part of the sum, and not each by itself before it. */
 typedef struct {
   int64_t rows;
@@ -544,7 +544,7 @@ typedef struct {
 gear_status gear_expert_combine(const gear_expert_combine_args *a, void *stream);
 
 /* Its gradients: dy[place[r, j]] = weight[r, j] dout[r] (rows that are nobody's place are left as they were; dy may be y itself, or NULL,
- * and shares no memory with dout), dweight[r, j] = dout[r] . y[place[r, j]] in fp32, 0 for a slot without a place (may be NULL).
+ * and shares no memory with dout, place, weight or dweight), dweight[r, j] = dout[r] . y[place[r, j]] in fp32, 0 for a slot without a place (may be NULL).
  * The residual's gradient is dout. */
 typedef struct {
   int64_t rows;
@@ -566,7 +566,7 @@ gear_status gear_expert_combine_backward(const gear_expert_combine_backward_args
  * their end. */
 
 /* x [rows x dim] in 8-bit integers.  place NULL (k then 1): row r of q and scale is x[r].  Otherwise x[r] goes to row place[r, j] for every
- * slot that has a place, as gear_expert_gather does it; q and scale have rows * k rows then. */
+ * slot that has a place, as gear_expert_gather does it; q and scale have rows * k rows then.  They share no memory with x, place or each other. */
 gear_status gear_rows_i8(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t dim, const int32_t *place, int32_t k, int8_t *q,
                          float *scale, void *stream);
 
@@ -578,7 +578,7 @@ size_t gear_packed_i8_bytes(int32_t experts, int32_t N, int32_t K);
 gear_status gear_pack_weights_i8(const void *w, int32_t src_dtype, int32_t experts, int32_t N, int32_t K, int8_t *packed, float *scale, void *stream);
 
 /* out[r, n] = x_scale[r] w_scale[e, n] sum over k of x[r, k] w_e[n, k] for the rows of every expert: off, status, keep_status and out as for
- * gear_expert_product; x rows of ld_x bytes, at least gear_rows8_ld(K) and a multiple of 16. */
+ * gear_expert_product; x rows of ld_x bytes, at least gear_rows8_ld(K) and a multiple of 16.  out shares no memory with what is read. */
 typedef struct {
   int32_t out_dtype;
   int64_t rows;

@@ -90,7 +90,7 @@ __device__ __forceinline__ ExpertTile expert_tile(const int32_t *__restrict__ of
   const int want = t.m;
   int before = 0;
   for (int e0 = 0; e0 < experts; e0 += kWave) {
-    if (experts > kWave) read(e0);
+    if (experts > kWave && __any(read(e0))) return r;   // changed since they were found right: nothing is written by them
     const unsigned long long m = __ballot(before + upto > want);
     if (m) {
       const int at = __builtin_ctzll(m);

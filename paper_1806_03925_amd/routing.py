@@ -109,6 +109,14 @@ def _apart(out: _Lines, other: _Lines, where: str, what: str, itself: bool = Fal
         _refuse(where, what)
 
 
+def _clear_of(out: _Lines, where: str, what: str, *words: Tuple[Optional[int], int]) -> None:
+    """Refuses memory for a result that holds any of `words`, (address, bytes) each; an address of None or 0 is nothing."""
+    end = out.at + out.rows * out.apart
+    for at, size in words:
+        if at and at < end and out.at < at + size:     # else they are far apart: these calls are short
+            _apart(out, _Lines(at, 1, size, size), where, what)
+
+
 def gear_route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optional[torch.Tensor] = None, groups: int = 1, groups_kept: int = 1,
                group_best: int = 1, renormalise: bool = True, scale: float = 1.0, n: Optional[torch.Tensor] = None) -> Route:
     """The k experts of every row of logits [rows x experts] (float32 or bfloat16), their weights, and the order of all pairs by
@@ -194,6 +202,8 @@ def gear_expert_gather(x: torch.Tensor, route: Route, out: Optional[torch.Tensor
         p_out, size = out.data_ptr(), _SIZE[code]
         if p_out < p_x + route.rows * ld * size and p_x < p_out + places * ld_out * size:     # else they are far apart: these calls are short
             _apart(_lines(out, ld_out), _lines(x, ld), where, "out may not share memory with x")
+        if p_out < route.p_place + 4 * places and route.p_place < p_out + places * ld_out * size:
+            _clear_of(_lines(out, ld_out), where, "out may not share memory with the route", (route.p_place, 4 * places))
     status = lib.gear_expert_gather(p_x, code, ld, route.rows, dim, route.p_place, route.k, out.data_ptr(), ld_out, _raw_stream(route.gpu))
     if status:
         _check(status, where)
@@ -225,6 +235,7 @@ def gear_expert_combine(y: torch.Tensor, route: Route, weighted: bool = True, re
         _apart(lines, _lines(y, ld_y), where, "out may not share memory with y")
         if residual is not None:
             _apart(lines, _lines(residual, ld_r), where, "out may be residual itself, but not share a part of its memory", True)
+        _clear_of(lines, where, "out may not share memory with the route", (route.p_place, 4 * places), (route.p_weight if weighted else None, 4 * places))
     a = gear_expert_combine_args(rows, dim, route.k, _CODE[dtype], y_f32, y.data_ptr(), p_r, route.p_place, route.p_weight if weighted else None,
                                  out.data_ptr(), ld_y, ld_r, ld_out)
     status = lib.gear_expert_combine(C.byref(a), _raw_stream(route.gpu))
@@ -254,6 +265,9 @@ def gear_expert_combine_backward(dout: torch.Tensor, y: torch.Tensor, route: Rou
             _apart(_lines(dy, ld_dy), _lines(dout, ld_dout), where, "dy may not share memory with dout")
         if p_dy < p_y + places * ld_y * size and p_y < p_dy + n:
             _apart(_lines(dy, ld_dy), _lines(y, ld_y), where, "dy may be y itself, but not share a part of its memory", True)
+        for p in (route.p_place, route.p_weight):
+            if p_dy < p + 4 * places and p < p_dy + n:
+                _clear_of(_lines(dy, ld_dy), where, "dy may not share memory with the route", (p, 4 * places))
     if dweight is None:
         dweight = torch.empty(rows, route.k, dtype=torch.float32, device=route.gpu)
     else:
@@ -281,6 +295,7 @@ class RowsI8:
         if q.dtype is not torch.int8 or dim < 1 or q.shape != (rows, (dim + 127) // 128 * 128) or not q.is_contiguous():
             _refuse(where, "q has to be [rows x gear_rows8_ld(dim)] contiguous int8")
         _vector(scale, self.gpu, where, "scale", torch.float32, rows)
+        _apart(_Lines(q.data_ptr(), 1, q.numel(), q.numel()), _Lines(scale.data_ptr(), 1, 4 * rows, 4 * rows), where, "scale may not share memory with q")
         self.rows, self.dim, self.ld = rows, dim, q.shape[1]
         self._q, self._scale, self._room, self.p_q, self.p_scale = q, scale, None, q.data_ptr(), scale.data_ptr()
 
@@ -316,8 +331,9 @@ def _rows_i8(x: torch.Tensor, ld: int, rows: int, place: Optional[int], k: int, 
         _refuse(where, "out has another shape than the rows or is on another GPU")
     else:
         lines = _lines(x, ld)
-        _apart(_Lines(out.p_q, out.rows, out.ld, out.ld), lines, where, "out may not share memory with x")
-        _apart(_Lines(out.p_scale, 1, 4 * out.rows, 4 * out.rows), lines, where, "out may not share memory with x")
+        for mine in (_Lines(out.p_q, out.rows, out.ld, out.ld), _Lines(out.p_scale, 1, 4 * out.rows, 4 * out.rows)):
+            _apart(mine, lines, where, "out may not share memory with x")
+            _clear_of(mine, where, "out may not share memory with the route", (place, 4 * rows * k))
     status = lib.gear_rows_i8(x.data_ptr(), _CODE[x.dtype], ld, rows, dim, place, k, out.p_q, out.p_scale, _raw_stream(gpu))
     if status:
         _check(status, where)
@@ -396,6 +412,8 @@ def gear_matmul_i8(rows: RowsI8, weights: WeightsI8, off: Optional[torch.Tensor]
         out, ld_out = torch.empty(rows.rows, n, dtype=out_dtype, device=gpu), n
     else:
         ld_out = _matrix(out, gpu, where, "out", None, (rows.rows, n))
+        _clear_of(_lines(out, ld_out), where, "out may not share memory with what is read", (rows.p_q, rows.rows * rows.ld), (rows.p_scale, 4 * rows.rows),
+                  (weights.address, weights.packed.numel()), (weights.p_scale, 4 * experts * n), (off, 4 * (experts + 1)), (status, 4))
     a = gear_i8_args(_CODE[out.dtype], rows.rows, weights.K, n, experts, rows.p_q, rows.p_scale, weights.address, weights.p_scale, off,
                      out.data_ptr(), rows.ld, ld_out, status, keep)
     code = lib.gear_product_i8(C.byref(a), _raw_stream(gpu))

@@ -544,3 +544,54 @@ def test_infinite_weights_without_a_place_are_nothing(g, dtype):
     want = x[:4].double() + factor * y[[0, 1, 2, 0]].double()
     within(out[:4], want, 4 * U * (x[:4].double().abs() + (factor * y[[0, 1, 2, 0]].double()).abs()) + HALF[dtype] * want.abs())
     assert torch.equal(out[3], x[3]) and out[4].isnan().all()
+
+
+def test_results_in_the_memory_of_a_route_or_of_a_products_operands_are_refused(g):
+    """Every workgroup reads places, weights and offsets, and none may find a result there."""
+    def parts(room, *sizes):       # int32 words, one behind the other, each on 64 bytes
+        out, at = [], 0
+        for n in sizes:
+            out.append(room.view(-1)[at:at + n])
+            at += (n + 15) // 16 * 16
+        return out
+    rows, dim = 8, 64
+    source = g.gear_route(torch.randn(rows, 3, device="cuda"), 2)
+    x, y = torch.randn(rows, dim, device="cuda"), torch.randn(2 * rows, dim, device="cuda")
+
+    def route_in(room):
+        expert, weight, place, off = parts(room, 16, 16, 16, 4)
+        for t, v in ((expert, source.expert), (weight, source.weight.view(torch.int32)), (place, source.place), (off, source.off)):
+            t.copy_(v.flatten())
+        return g.Route(expert.view(rows, 2), weight.view(torch.float32).view(rows, 2), place.view(rows, 2), off)
+    few, many = (torch.zeros(n, dim, dtype=torch.int32, device="cuda") for n in (rows, 2 * rows))
+    in_few, in_many = route_in(few), route_in(many)
+    f32 = lambda t: t.view(torch.float32)
+    q = g.gear_rows_i8(torch.randn(8, 64, device="cuda"))
+    w = g.gear_weights_i8(torch.randn(3, 256, 64, device="cuda"))
+    o = torch.empty(8 * 256, device="cuda")
+    off = o[:4].view(torch.int32)
+    off.copy_(torch.tensor([0, 2, 5, 8], dtype=torch.int32))
+    ordinary, scale = off.clone(), o[16:24].fill_(1.0)
+    few8 = g.gear_weights_i8(torch.randn(3, 8, 64, device="cuda"))
+    few8.scale, few8.p_scale = o.view(-1)[:24].view(3, 8), o.data_ptr()
+    wide = torch.zeros(8 * 256 * 4, dtype=torch.int8, device="cuda")
+    for call in (lambda: g.gear_expert_gather(x, in_many, out=f32(many)), lambda: g.gear_expert_combine(y, in_few, out=f32(few)),
+                 lambda: g.gear_expert_combine(y, in_few, weighted=False, residual=f32(few), out=f32(few)),
+                 lambda: g.gear_expert_combine_backward(x, y, in_many, dy=f32(many)),
+                 lambda: g.gear_expert_gather_i8(x, in_many, out=g.RowsI8(many.view(-1)[:512].view(torch.int8).view(16, 128), torch.empty(16, device="cuda"), dim)),
+                 lambda: g.gear_expert_gather_i8(x, in_many, out=g.RowsI8(torch.empty(16, 128, dtype=torch.int8, device="cuda"), f32(in_many.place.flatten()), dim)),
+                 lambda: g.RowsI8(wide[:1024].view(8, 128), wide[512:544].view(torch.float32), 64),
+                 lambda: g.gear_matmul_i8(q, w, off, out=o.view(8, 256)),
+                 lambda: g.gear_matmul_i8(g.RowsI8(q.q, scale, 64), w, ordinary, out=o.view(8, 256)),
+                 lambda: g.gear_matmul_i8(g.RowsI8(wide[:1024].view(8, 128), q.scale, 64), w, ordinary, out=wide.view(torch.float32).view(8, 256)),
+                 lambda: g.gear_matmul_i8(q, w, ordinary, out=o.view(8, 256), status=o[40:41].view(torch.int32)),
+                 lambda: g.gear_matmul_i8(q, w, ordinary, out=w.packed.view(torch.float32)[:8 * 256].view(8, 256)),
+                 lambda: g.gear_matmul_i8(q, few8, ordinary, out=o[16:80].view(8, 8))):
+        with pytest.raises(g.GearError):
+            call()
+    # beside each other they are fine
+    room = torch.zeros(8, 512, device="cuda")
+    assert torch.equal(g.gear_matmul_i8(q, w, ordinary, out=room[:, 256:]), g.gear_matmul_i8(q, w, ordinary, out_dtype=F32))
+    out = torch.zeros(2 * rows + 2, dim, dtype=torch.int32, device="cuda")
+    beside = route_in(out[2 * rows:])
+    assert torch.equal(g.gear_expert_gather(x, beside, out=f32(out[:2 * rows])), g.gear_expert_gather(x, source))
