@@ -724,13 +724,13 @@ struct RouteBackArgs {
   void *dlogits;
 };
 
-template <typename T, int LPR, int V, bool WIDE> __global__ void __launch_bounds__(256) k_route_back(RouteBackArgs a) {
+template <typename T, int LPR, int V> __global__ void __launch_bounds__(256) k_route_back(RouteBackArgs a) {
   constexpr int TEAMS = 256 / LPR, MAX_E = LPR * V, SLOTS = LPR < GEAR_MAX_CHOSEN ? GEAR_MAX_CHOSEN / LPR : 1;
   __shared__ float s_flow[TEAMS * MAX_E];
   const int l = threadIdx.x % LPR, team = threadIdx.x / LPR, E = a.experts;
   float *flow = s_flow + team * MAX_E;
   const bool all = a.softmax && !a.renormalise;
-  auto index = [&](int v) { return WIDE ? (v / 4) * (LPR * 4) + l * 4 + v % 4 : v * LPR + l; };
+  auto index = [&](int v) { return v * LPR + l; };
   for (int64_t row0 = (int64_t)blockIdx.x * TEAMS; row0 < a.rows; row0 += (int64_t)gridDim.x * TEAMS) {
     const int64_t row = row0 + team;
     const bool have = row < a.rows;
@@ -875,7 +875,7 @@ template <typename T> hipError_t launch_back(const RouteBackArgs &a, hipStream_t
       return hipErrorInvalidValue;     // not for one row
     } else {
       const int64_t blocks = (a.rows + TEAMS - 1) / TEAMS;
-      hipLaunchKernelGGL((k_route_back<T, LPR, decltype(v)::value, false>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, a);
+      hipLaunchKernelGGL((k_route_back<T, LPR, decltype(v)::value>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, a);
       return hipGetLastError();
     }
   });
