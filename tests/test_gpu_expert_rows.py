@@ -595,3 +595,23 @@ def test_results_in_the_memory_of_a_route_or_of_a_products_operands_are_refused(
     out = torch.zeros(2 * rows + 2, dim, dtype=torch.int32, device="cuda")
     beside = route_in(out[2 * rows:])
     assert torch.equal(g.gear_expert_gather(x, beside, out=f32(out[:2 * rows])), g.gear_expert_gather(x, source))
+
+
+@pytest.mark.parametrize("experts,n,k", [(1, 8, 8), (1, 264, 4104), (3, 72, 136), (16, 520, 576)])
+def test_weights_in_bf16(g, experts, n, k):
+    """Weights of that type are the integers nearest to them, and nothing is rounded twice."""
+    r = gen(n + k)
+    w = (torch.randn(experts, n, k, device="cuda", generator=r) * torch.exp(torch.randn(experts, n, 1, device="cuda", generator=r))).to(BF16)
+    w[0, 1], w[-1, 2, k // 2], w[-1, 3, 0] = 0.0, math.inf, math.nan
+    x = torch.randn(70, k, device="cuda", generator=r)
+    b = [round(70 * i / experts) for i in range(experts + 1)]
+    q, weights = g.gear_rows_i8(x), g.gear_weights_i8(w)
+    wq, ws = integers(w)
+    within(weights.scale, ws, U * ws.nan_to_num())
+    same = g.gear_weights_i8(w.float())
+    assert torch.equal(same.scale.nan_to_num(), weights.scale.nan_to_num())
+    off = torch.tensor(b, dtype=torch.int32, device="cuda")
+    out = g.gear_matmul_i8(q, weights, off, out_dtype=F32)
+    want = torch.cat([q.q[b[i]:b[i + 1], :k].double() @ wq[i].t().contiguous() * weights.scale[i].double() for i in range(experts)]) * q.scale[:, None].double()
+    within(out, want, 3.01 * U * want.nan_to_num().abs())
+    assert torch.equal(out.nan_to_num(), g.gear_matmul_i8(q, same, off, out_dtype=F32).nan_to_num())

@@ -491,3 +491,49 @@ def test_experts_parked_by_large_biases(g, experts, k, groups, score):
             bias[experts // 2 + 1] = park
         kw = dict(bias=bias, groups=groups, groups_kept=max(1, groups // 2), group_best=min(2, groups))
         check(g.gear_route(logits, k, score, **kw), reference_many(logits, k, score, **kw))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("rows", [1, 3, 16])
+@pytest.mark.parametrize("experts,groups,kept,best,k", GROUPS)
+def test_groups_in_one_workgroup(g, experts, groups, kept, best, k, rows, score):
+    """Choice and order in one launch, which takes the most LDS of all."""
+    r = gen(experts + rows)
+    logits = torch.randn(rows, experts, device="cuda", generator=r)
+    logits[rows // 2, ::3] = -INF
+    bias = 0.2 * torch.randn(experts, device="cuda", generator=r)
+    for b in (None, bias):
+        for x in (logits, logits.to(BF16), strided(logits, 3)):
+            kw = dict(bias=b, groups=groups, groups_kept=kept, group_best=best)
+            check(g.gear_route(x, k, score, **kw), reference(x, k, score, **kw))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("rows,experts,groups,kept,best,k", [(10_001, 160, 8, 3, 2, 6), (9_000, 12, 3, 2, 2, 4), (33_001, 64, 16, 4, 1, 8), (5_000, 512, 16, 4, 2, 20), (3_000, 1024, 4, 3, 2, 32)])
+def test_groups_of_long_batches(g, rows, experts, groups, kept, best, k, score, dtype):
+    """Workgroups that take several passes over rows, the next one's logits on their way while LDS holds this one's."""
+    r = gen(rows)
+    logits = (1.5 * torch.randn(rows, experts, device="cuda", generator=r)).to(dtype)
+    logits[5::11, experts // 3:] = -INF
+    logits[6::97] = 0.25
+    logits[12::101] = -INF
+    bias = 0.05 * torch.randn(experts, device="cuda", generator=r)
+    bias[1::7] = -INF
+    n = torch.tensor([rows - rows // 20], dtype=torch.int32, device="cuda")
+    for b in (None, bias):
+        kw = dict(bias=b, groups=groups, groups_kept=kept, group_best=best, scale=2.5, n=n)
+        check(g.gear_route(logits, k, score, **kw), reference_many(logits, k, score, **kw))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,k,dtype", [(24, 3, BF16), (64, 8, F32), (63, 8, BF16), (160, 8, F32), (256, 8, BF16), (256, 16, F32), (300, 4, F32), (1024, 8, BF16)])
+def test_divided_weights_of_long_batches(g, experts, k, dtype, score):
+    rows = 33_001
+    r = gen(experts)
+    logits = (1.5 * torch.randn(rows, experts, device="cuda", generator=r)).to(dtype)
+    logits[5::7, experts // 3:] = -INF
+    logits[12::13] = -INF
+    bias = (0.2 / experts) * torch.randn(experts, device="cuda", generator=r)
+    for b in (None, bias):
+        check(g.gear_route(logits, k, score, bias=b, scale=2.5), reference_many(logits, k, score, b, scale=2.5))
