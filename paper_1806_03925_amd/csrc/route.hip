@@ -633,13 +633,14 @@ __global__ void __launch_bounds__(threads_of(LPR, V, GROUPED)) k_route(RouteArgs
       w[s] = chosen[s] >= 0 ? share(logit[s], a.softmax, highest, a.renormalise) : 0.0f;
       total += w[s];
     }
-    const float factor = a.renormalise ? a.scale / team_add<LPR>(total) : a.scale * inv;
+    total = a.renormalise ? team_add<LPR>(total) : 1.0f;
+    const float factor = a.renormalise ? a.scale : a.scale * inv;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       const int j = l + s * LPR;
       if (row < last && j < a.k) {
         a.expert[row * a.k + j] = chosen[s];
-        a.weight[row * a.k + j] = broken ? NAN : chosen[s] >= 0 ? w[s] * factor : 0.0f;
+        a.weight[row * a.k + j] = broken ? NAN : chosen[s] >= 0 ? w[s] / total * factor : 0.0f;   // not scale / total, which may be infinite
         if (chosen[s] >= 0) atomicAdd(&s_words[chosen[s]], 1);
       }
     }
@@ -708,7 +709,7 @@ template <typename T> __global__ void __launch_bounds__(kPlaceThreads) k_places(
 }
 
 // ---- gradient -----------------------------------------------------------------------------------------------------
-// With f_j = scale dw_j at the chosen experts and zero elsewhere, and p = weight / scale where weights are divided by their sum:
+// With f_j = dw_j at the chosen experts and zero elsewhere, and p = weight / scale where weights are divided by their sum, scale times
 //   softmax             dl_i = s_i (f_i - sum_j s_j f_j)            every logit
 //   softmax, divided    dl_j = p_j (f_j - sum_i p_i f_i)            the chosen ones' (the sum of the others cancels)
 //   sigmoid             dl_j = s_j (1 - s_j) f_j
@@ -754,7 +755,7 @@ template <typename T, int LPR, int V> __global__ void __launch_bounds__(256) k_r
       const float w = in ? a.weight[row * a.k + j] : 0.0f;
       broken |= w != w;
       if (e[s] >= E) e[s] = -1;
-      f[s] = e[s] >= 0 ? a.scale * a.dweight[row * a.k + j] : 0.0f;
+      f[s] = e[s] >= 0 ? a.dweight[row * a.k + j] : 0.0f;
       p[s] = e[s] >= 0 ? w / a.scale : 0.0f;
       inner += p[s] * f[s];
       chosen += __popcll(team_ballot<LPR>(e[s] >= 0));
@@ -773,6 +774,7 @@ template <typename T, int LPR, int V> __global__ void __launch_bounds__(256) k_r
           const float v = to_f32(x[e[s]]), t = expf(-fabsf(v)), big = 1.0f / (1.0f + t), small = t / (1.0f + t);   // of |v|: s and 1 - s
           d *= a.renormalise ? (v > 0.0f ? small : big) : big * small;
         }
+        d *= a.scale;
       }
       flow[e[s]] = d;
     }
@@ -794,9 +796,9 @@ template <typename T, int LPR, int V> __global__ void __launch_bounds__(256) k_r
       }
       sum = team_add<LPR>(sum);
       dot = team_add<LPR>(dot);
-      const float inv = none ? 0.0f : 1.0f / sum;
+      const float inv = none ? 0.0f : 1.0f / sum, scaled = inv * a.scale;
 #pragma unroll
-      for (int v = 0; v < V; ++v) d[v] = lg[v] * inv * (d[v] - dot * inv);
+      for (int v = 0; v < V; ++v) d[v] = lg[v] * scaled * (d[v] - dot * inv);
     }
     T *out = static_cast<T *>(a.dlogits) + row * a.ld_d;
 #pragma unroll

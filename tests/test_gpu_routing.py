@@ -537,3 +537,26 @@ def test_divided_weights_of_long_batches(g, experts, k, dtype, score):
     bias = (0.2 / experts) * torch.randn(experts, device="cuda", generator=r)
     for b in (None, bias):
         check(g.gear_route(logits, k, score, bias=b, scale=2.5), reference_many(logits, k, score, b, scale=2.5))
+
+
+@pytest.mark.parametrize("renormalise", [True, False])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("scale", [3.3e38, 1e-30])
+def test_scales_at_the_ends_of_fp32(g, scale, score, renormalise):
+    """Nothing on the way to a weight or to its gradient is larger than these are themselves."""
+    r = gen(21)
+    scale = float(np.float32(scale))
+    logits, dw = torch.randn(300, 40, device="cuda", generator=r) - 1, torch.rand(300, 6, device="cuda", generator=r) * 2 - 1
+    route = g.gear_route(logits, 6, score, renormalise=renormalise, scale=scale)
+    check(route, reference(logits, 6, score, renormalise=renormalise, scale=scale))
+    v = logits.double().requires_grad_()
+    w = weights64(v, route.expert, score, renormalise, scale)
+    want = torch.autograd.grad(w, v, dw.double())[0]
+    # as in test_gradient: twice what the two products' factors are off by, of the sum of their magnitudes; 24 bits of a scale's and a weight's quotient are among the 40
+    p = w.detach() / scale
+    inner = (p * dw.abs().double()).sum(1, keepdim=True)
+    size = torch.zeros_like(want).scatter_add_(1, route.expert.long(), p * (dw.abs().double() + inner))
+    if score == "softmax" and not renormalise:
+        size += torch.softmax(v, 1).detach() * inner
+    far = (logits.double() - (logits.double().amax(1, keepdim=True) if score == "softmax" else 0)).abs()
+    within(g.gear_route_backward(logits, route, dw, score, renormalise, scale), want, scale * (2 * (far + 40) * U * size + 2.0 ** -43 * inner))
