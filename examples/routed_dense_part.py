@@ -4,7 +4,7 @@ DFV(image) for an image with features f, its k experts e of `experts` and their 
 
     h = norm(f),    u = f + sum_e w_e A_e h,    DFV = B norm(u)
 
-Inference for the cache multiplies in 8-bit integers.  Back-propagation of a step's averaged gradients (Section 3, step 6) runs in
+Inference for the cache multiplies in 8-bit integers and adds up in fp32.  Back-propagation of a step's averaged gradients (Section 3, step 6) runs in
 bf16 with fp32 weights: gradients of all layers and of the router through the weights, clipped together, one SGD step.  No loss
 balances the experts: a bias that only the choice sees rises for those with fewer rows than their share and falls for the others.
 """

@@ -548,7 +548,7 @@ gear_status gear_expert_combine(const gear_expert_combine_args *a, void *stream)
  * The residual's gradient is dout. */
 typedef struct {
   int64_t rows;
-  int32_t dim, k, dtype;                  /* gear_dtype of dout, y and dy */
+  int32_t dim, k, dtype;                  /* gear_dtype of dout, y and dy, also where the sum took y in fp32 */
   const void *dout, *y;
   const int32_t *place;
   const float *weight;

@@ -6,6 +6,7 @@
 // Every one is a walk over the rows r, not over the places: what a row's k places share is read once, and what they add up to
 // stays in registers.  Bound by memory; us and TB/s of what they have to move, bf16, 16384 x 1152 with k = 2 / 65536 x 2048 with k = 4 (a large copy: 4.75):
 //   gather 21.0, 5.4 / 226, 5.9;  combine 28.4, 5.3 / 306, 5.3;  its gradients 32.2, 5.9 / 470, 5.1
+//   combine of y in fp32 33.0, 6.9 and 491, 5.5 (y is half in the caches where it is small);
 //   rows to integers 65536 x 4096 134, 6.0;  to four experts each 16384 x 1152 22.5, 5.0
 // Sums and gradients leave past the L2, which then keeps more of what is read (us past it / through it: combine 26.9 / 29.7 and 280 / 328, its
 // gradients 31.5 / 35.9 and 470 / 461); copies do not (250 / 228), and the next product reads them.

@@ -14,7 +14,7 @@
 // on.  Bound by these instructions: 65536 rows of 256 fp32 logits with a bias, k = 8, take 31.8 us, 1400 vector instructions for eight rows, which keep the
 // vector pipes busy for three quarters of a wavefront's life; its 74 MB would take 15.7.  (k times the largest of all in fp64: 114 us; one by one from sorted
 // numbers: 48.)  A row in doubt costs its wavefront 3 to 7 us, one in a thousand to ten thousand of random ones; with groups one such row is a
-// quarter of a launch over 10001 rows (24.9 us; 20 without).
+// quarter of a launch over 10001 rows (25.0 us; 20 without).
 //
 // The order of the pairs is a counting sort by expert.  A workgroup takes a run of rows and counts its experts; a second launch
 // with the same runs finds from all counts where each run's pairs begin, ranks them (equal experts in a wavefront by ballots,

@@ -247,7 +247,8 @@ def gear_expert_combine(y: torch.Tensor, route: Route, weighted: bool = True, re
 def gear_expert_combine_backward(dout: torch.Tensor, y: torch.Tensor, route: Route, dy: Optional[torch.Tensor] = None,
                                  dweight: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dy, dweight) of gear_expert_combine with weights: dy [rows * k x dim], of which rows from route.off[experts] on are not
-    written (dy may be y itself), and dweight [rows x k] (float32).  The residual's gradient is dout."""
+    written (dy may be y itself), and dweight [rows x k] (float32).  y is of dout's type, also where the sum took it in float32.  The residual's
+    gradient is dout."""
     where = "gear_expert_combine_backward"
     _gpu(route.gpu, where, "the route")
     rows, places = route.rows, route.rows * route.k
@@ -387,8 +388,9 @@ def gear_weights_i8(w: torch.Tensor, scale: Optional[torch.Tensor] = None) -> We
 
 def gear_matmul_i8(rows: RowsI8, weights: WeightsI8, off: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                    out_dtype: torch.dtype = torch.bfloat16, status: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """rows times the transposed weights of each row's expert, [rows x N]: integers added up exactly, then scaled.  off, status and rows from
-    off[experts] on as for gear_matmul8."""
+    """rows times the transposed weights of each row's expert, [rows x N]: integers added up exactly, then scaled, then rounded to out_dtype;
+    float32 is for what gear_expert_combine adds up.  off, status and rows from off[experts] on as for gear_matmul8.  `out` shares no memory
+    with what is read."""
     where = "gear_matmul_i8"
     gpu, n, experts = _gpu(rows.gpu, where, "rows"), weights.N, weights.experts
     if rows.dim != weights.K:

@@ -1,7 +1,7 @@
 """Rows on their way to their experts and back, and products in 8-bit integers, against evaluations in 64 bits.
 
 Tolerances.  u = 2^-24.  A weighted sum of k rows in fp32: (k + 2) u of the sum of its terms' magnitudes, and one rounding of the result.  A dot product of
-dim terms, added up by at least 16 threads (64 above 128 columns, 256 above 512) and then in a tree: at most (dim / 16 + 16) u of its magnitudes.
+dim terms, added up by at least 16 threads (32 above 128 columns, 64 above 256, 256 above 4096) and then in a tree: at most (dim / 16 + 16) u of its magnitudes.
 Integers and copies are equal.  A product in integers is exact up to its conversion and two factors: 3 u, and one rounding to bf16."""
 import itertools
 import math
